@@ -110,6 +110,11 @@ def _ids(g, t, vocab, masked):
     return ids
 
 
+def _pow2(e):
+    """2^e for whole numbers e in [-126, 127], from the bits of an fp32 number."""
+    return (e.int() + 127 << 23).view(torch.float32)
+
+
 def _quantize(x):
     """(q, e): the checkpoint of x in its public layout: int8 [tokens, blocks * 128] and int8 [tokens, blocks]."""
     t, d = x.shape
@@ -119,13 +124,14 @@ def _quantize(x):
     v = v.view(t, nb, BLOCK)
     m, k = torch.frexp(v.abs().amax(2))
     e = torch.where(m <= 127 / 128, k - 7, k - 6).clamp_(min=-126)
-    q = torch.round(v * torch.exp2(-e.float())[:, :, None]).to(torch.int8)
+    e = torch.where(m == 0, -126, e)
+    q = torch.round(v * _pow2(-e)[:, :, None]).to(torch.int8)
     return q.view(t, nb * BLOCK), e.to(torch.int8)
 
 
 def _values(q, e, d, dtype=torch.float32):
     t, nb = e.shape
-    v = q.view(t, nb, BLOCK).to(dtype) * torch.exp2(e.to(dtype))[:, :, None]
+    v = q.view(t, nb, BLOCK).to(dtype) * _pow2(e).to(dtype)[:, :, None]
     return v.reshape(t, nb * BLOCK)[:, :d]
 
 
