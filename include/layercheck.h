@@ -630,6 +630,123 @@ lc_status lc_measure_noalloc(int device, void* cuda_stream, const lc_segment* se
 lc_status lc_measure_noalloc_debug(int device, void* cuda_stream, const lc_segment* segs, int32_t nseg,
                                    int32_t nlayers, double* sums_out, int32_t debug_flags);
 
+/* --- operators of the training step around the optimizer ---------------- *
+ * What a training step computes next to the arrays above: the embedding
+ * lookup, layer and root-mean-square norms, activations kept for the
+ * backward pass in 8 bits, and the gradients that lc_adamw_step_measure
+ * reads.  Like lc_measure_noalloc they need no context and allocate nothing:
+ * each call enqueues its work on `cuda_stream` of `device` and returns.
+ *   - Every array is device memory of `device` (managed memory is refused),
+ *     aligned to its element size; vector loads, bulk tensor copies and their
+ *     fallbacks are chosen from the addresses and strides given.
+ *   - Outputs must not overlap inputs or one another (interleaved columns of
+ *     one buffer, with the same row stride, do not).
+ *   - A `workspace` is scratch of the size that the call's *_workspace
+ *     function returns (0: none needed, NULL allowed), 256-byte aligned.  It
+ *     holds nothing between calls.  Calls that may overlap on the GPU need
+ *     one each.
+ *   - Sums are taken in fp32 in an order that the sizes fix, without floating
+ *     point atomics: the same inputs give the same bits.
+ *   - 0 tokens are allowed: outputs per token are untouched, gradients are 0
+ *     (or stay as they are with `accumulate`).
+ * Errors of each: INVALID_ARG (sizes, types, strides, pointers, overlap),
+ * CAPACITY (workspace too small), CUDA. */
+
+/* Rows of `dim` elements of type dtype (lc_dtype); row r starts `stride`
+ * elements behind row r-1.  Inputs may repeat a row (stride 0), outputs need
+ * stride >= dim. */
+typedef struct {
+    void* data;
+    int64_t stride;
+    int32_t dtype;
+    int32_t reserved;
+} lc_rows;
+
+/* Types of token ids. */
+#define LC_I32 2
+#define LC_I64 3
+
+/* y[t] = scale * table[ids[t]] for ntok tokens, computed in fp32 and rounded
+ * to y's type, which is the table's.  A negative id marks a position without
+ * a token: its row is zero.  An id >= vocab is an error of the caller's data:
+ * its row is NaN.  ids: device array of ntok LC_I32 or LC_I64. */
+lc_status lc_embed(int device, void* cuda_stream, const lc_rows* table, int64_t vocab, int64_t dim,
+                   const void* ids, int32_t id_type, int64_t ntok, float scale, const lc_rows* y);
+
+/* grad[v] = scale * sum of dy[t] over the tokens with ids[t] == v, in
+ * ascending t, rounded once to grad's type; every other row is 0.  With
+ * accumulate != 0 the sums are added to grad instead and the other rows stay
+ * as they are (a tied output projection's gradient, micro-batches).  Ids
+ * outside [0, vocab) and the id skip_id (-1: none) contribute nothing.
+ * dy and grad may have different types. */
+lc_status lc_embed_grad(int device, void* cuda_stream, const lc_rows* dy, const void* ids, int32_t id_type,
+                        int64_t ntok, float scale, int64_t skip_id, const lc_rows* grad, int64_t vocab,
+                        int64_t dim, int32_t accumulate, void* workspace, uint64_t workspace_bytes);
+uint64_t lc_embed_grad_workspace(int64_t ntok, int64_t vocab, int64_t dim);
+
+/* An activation kept in 8 bits: ntok rows of dim values in blocks of 128.
+ * Value c of row t is q[t * q_stride + c] * 2^e[t * e_stride + c / 128], with q
+ * in [-127, 127] and e in [-126, 121]: each is exactly a bf16 (and fp32)
+ * number, so everything that reads the checkpoint sees the same values.
+ * e = 127 marks a block that held a NaN or an infinity: all of it reads as
+ * NaN.  A row has ceil(dim / 128) blocks; q is 16-byte aligned, q_stride a
+ * multiple of 16 and >= 128 * blocks, e_stride >= blocks. */
+#define LC_ACT_BLOCK 128
+typedef struct {
+    int8_t* q;
+    int64_t q_stride;   /* bytes */
+    int8_t* e;
+    int64_t e_stride;   /* bytes */
+} lc_act;
+
+/* Keeps x in 8 bits: per block the smallest e >= -126 with 127 * 2^e >= the
+ * largest magnitude, q = x * 2^-e rounded to nearest even.  Magnitudes above
+ * 127 * 2^121 (the last 1 % of the types' range) are kept as that number.
+ * The values of the last block beyond dim are stored as 0. */
+lc_status lc_act_save(int device, void* cuda_stream, const lc_rows* x, int64_t ntok, int64_t dim,
+                      const lc_act* act);
+
+/* y = the values of the checkpoint (exact in either type). */
+lc_status lc_act_load(int device, void* cuda_stream, const lc_act* act, int64_t ntok, int64_t dim,
+                      const lc_rows* y);
+
+#define LC_NORM_LAYER 0   /* y = (x - mean) * rstd * weight + bias, rstd = 1 / sqrt(var + eps)        */
+#define LC_NORM_RMS 1     /* y = x * rstd * weight (+ bias), rstd = 1 / sqrt(mean of x^2 + eps)       */
+#define LC_NORM_MAX_DIM 16384
+
+/* The norm of every row of x over its dim elements, dim <= LC_NORM_MAX_DIM.
+ * weight: dim elements of w_dtype; bias: the same, or NULL.  mean (LC_NORM_LAYER; NULL for
+ * LC_NORM_RMS) and rstd receive ntok fp32 each, for the backward.  y has x's
+ * type.  keep (nullable): x is also kept in 8 bits, as by lc_act_save, on the
+ * same pass.  Statistics are fp32, the variance taken about the mean. */
+lc_status lc_norm(int device, void* cuda_stream, int32_t kind, const lc_rows* x, int64_t ntok, int64_t dim,
+                  const void* weight, const void* bias, int32_t w_dtype, double eps, const lc_rows* y,
+                  float* mean, float* rstd, const lc_act* keep);
+
+/* Gradients of lc_norm from dy, the input (x, or its checkpoint `kept`;
+ * exactly one of them) and the forward's mean and rstd: with h = (x - mean) *
+ * rstd and a = dy * weight,
+ *   dx = rstd * (a - mean(a) - h * mean(a * h))     (LC_NORM_RMS: without mean(a))
+ *   dweight = sum over t of dy * h,  dbias = sum over t of dy.
+ * dx has dy's type (NULL: not wanted).  dweight and dbias: dim elements of
+ * g_dtype, each may be NULL; accumulate != 0 adds to them. */
+lc_status lc_norm_grad(int device, void* cuda_stream, int32_t kind, const lc_rows* dy, const lc_rows* x,
+                       const lc_act* kept, int64_t ntok, int64_t dim, const void* weight, int32_t w_dtype,
+                       const float* mean, const float* rstd, const lc_rows* dx, void* dweight, void* dbias,
+                       int32_t g_dtype, int32_t accumulate, void* workspace, uint64_t workspace_bytes);
+uint64_t lc_norm_grad_workspace(int64_t ntok, int64_t dim);
+
+/* The gradient of a linear layer's weight (y = x W^T) with the layer's input
+ * kept in 8 bits: dw[n][k] = sum over t of dy[t][n] * x[t][k], `rows` by dim,
+ * added to dw with accumulate != 0.  Products and sums are fp32 (tensor cores
+ * on bf16 operands, which the checkpoint's values are exactly; a 32-bit dy is
+ * split into three bf16 parts that add up to it).  dy and dw may have
+ * different types. */
+lc_status lc_weight_grad(int device, void* cuda_stream, const lc_rows* dy, const lc_act* x, int64_t ntok,
+                         int64_t rows, int64_t dim, const lc_rows* dw, int32_t accumulate, void* workspace,
+                         uint64_t workspace_bytes);
+uint64_t lc_weight_grad_workspace(int64_t ntok, int64_t rows, int64_t dim, int32_t dy_dtype);
+
 #ifdef __cplusplus
 }
 #endif

@@ -25,6 +25,10 @@ LC_DRIFT_SNAPSHOT, LC_DRIFT_ACCUMULATE = 0, 1
 LC_COPY_BULK, LC_COPY_THREADS = 0, 1
 LC_DEBUG_BULK_STALL = 1
 LC_DEBUG_MEASURE_STALL = 2
+LC_I32, LC_I64 = 2, 3
+LC_NORM_LAYER, LC_NORM_RMS = 0, 1
+LC_NORM_MAX_DIM = 16384
+LC_ACT_BLOCK = 128
 LC_SPAN_GATHER, LC_SPAN_D2H, LC_SPAN_H2D, LC_SPAN_SCATTER = 0, 1, 2, 3
 SPAN_NAMES = {0: "gather", 1: "d2h", 2: "h2d", 3: "scatter"}
 
@@ -88,6 +92,14 @@ class lc_copy_span(C.Structure):
                 ("bytes", C.c_uint64), ("start_ms", C.c_double), ("end_ms", C.c_double)]
 
 
+class lc_rows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("stride", C.c_int64), ("dtype", C.c_int32), ("reserved", C.c_int32)]
+
+
+class lc_act(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("q_stride", C.c_int64), ("e", C.c_void_p), ("e_stride", C.c_int64)]
+
+
 ctx_p = C.c_void_p
 store_p = C.c_void_p
 P = C.POINTER
@@ -139,6 +151,23 @@ SIGNATURES = {
     "lc_store_load_dir": (C.c_int, [ctx_p, C.c_char_p, C.c_int64, P(store_p), C.c_void_p]),
     "lc_manifest_read": (C.c_int, [C.c_char_p, C.c_int32, P(lc_manifest_record), C.c_int64,
                                    P(C.c_int64), P(C.c_int32), P(C.c_uint32), P(C.c_int32)]),
+    "lc_embed": (C.c_int, [C.c_int, C.c_void_p, P(lc_rows), C.c_int64, C.c_int64, C.c_void_p, C.c_int32,
+                           C.c_int64, C.c_float, P(lc_rows)]),
+    "lc_embed_grad": (C.c_int, [C.c_int, C.c_void_p, P(lc_rows), C.c_void_p, C.c_int32, C.c_int64, C.c_float,
+                                C.c_int64, P(lc_rows), C.c_int64, C.c_int64, C.c_int32, C.c_void_p,
+                                C.c_uint64]),
+    "lc_embed_grad_workspace": (C.c_uint64, [C.c_int64, C.c_int64, C.c_int64]),
+    "lc_act_save": (C.c_int, [C.c_int, C.c_void_p, P(lc_rows), C.c_int64, C.c_int64, P(lc_act)]),
+    "lc_act_load": (C.c_int, [C.c_int, C.c_void_p, P(lc_act), C.c_int64, C.c_int64, P(lc_rows)]),
+    "lc_norm": (C.c_int, [C.c_int, C.c_void_p, C.c_int32, P(lc_rows), C.c_int64, C.c_int64, C.c_void_p,
+                          C.c_void_p, C.c_int32, C.c_double, P(lc_rows), C.c_void_p, C.c_void_p, P(lc_act)]),
+    "lc_norm_grad": (C.c_int, [C.c_int, C.c_void_p, C.c_int32, P(lc_rows), P(lc_rows), P(lc_act), C.c_int64,
+                               C.c_int64, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, P(lc_rows),
+                               C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_uint64]),
+    "lc_norm_grad_workspace": (C.c_uint64, [C.c_int64, C.c_int64]),
+    "lc_weight_grad": (C.c_int, [C.c_int, C.c_void_p, P(lc_rows), P(lc_act), C.c_int64, C.c_int64, C.c_int64,
+                                 P(lc_rows), C.c_int32, C.c_void_p, C.c_uint64]),
+    "lc_weight_grad_workspace": (C.c_uint64, [C.c_int64, C.c_int64, C.c_int64, C.c_int32]),
 }
 
 # limits of lc_measure_noalloc (include/layercheck.h)
