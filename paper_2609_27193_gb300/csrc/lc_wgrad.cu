@@ -3,17 +3,26 @@
 //
 // A matrix product over the tokens on the 5th-generation tensor cores.  A value of
 // the checkpoint is exactly a bf16 number, so it is an operand without a rounding;
-// it is made on the way, never stored: bulk tensor copies bring 8-bit tiles of the
-// checkpoint and bf16 tiles of dy into shared memory, converter warps turn the
-// 8-bit tile into bf16 and write it to tensor memory, one operand of the product;
-// the other is dy's tile in shared memory as it came (its rows are tokens, so both
-// operands are read along the output dimensions).  The accumulator is fp32 in
-// tensor memory.
+// it is made on the way and never leaves the multiprocessor.  Two CTAs of a
+// cluster share a tile of 256 features x 256 columns of dy: each holds 128 of
+// either, so a byte of dy that comes from L2 serves 256 features.  In each CTA
 //
-//   warp 0    one thread issues the copies of a stage (64 tokens)
-//   warp 1    one thread issues the products of a stage
-//   warps 4-11 convert a stage each (a lane is a feature, a warp 32 tokens of 32
-//             features), and write the outputs at the end
+//   warp 0    one thread issues the bulk tensor copies of a stage (64 tokens): an
+//             8-bit tile of the checkpoint, a bf16 tile of dy
+//   warp 1    one thread of the first CTA issues the products for both
+//   warps 2-3 bring the tokens' exponents, kChunk stages ahead at a time
+//   warps 4-11 turn the 8-bit tile into the bf16 operand in shared memory, four
+//             warps a stage; tokens are rows there as in memory, and the product
+//             takes both operands that way, so nothing is transposed
+//   warps 12-19 add up the results
+//
+// The tensor cores add in fp32, but a chain of many products loses more than a sum
+// in registers does (8192 tokens in one chain: 2.5e-6 off; in pieces of 512:
+// 1.2e-7).  So a chain is kChunk stages long; two accumulators in tensor memory
+// take turns, and the last eight warps add the finished one to their registers
+// while the other is being filled.  The CTAs are persistent and the stages of one
+// tile follow those of the last, so the outputs are written while the next tile's
+// products run.
 //
 // A 32-bit dy is split into three bf16 parts that add up to it exactly (8 + 8 + 8
 // bits of significand, cut off, not rounded, so nothing overflows), and a bf16 dy
@@ -21,7 +30,7 @@
 // kernel of their own.  Few output tiles are split over the tokens; the parts are
 // added in order by another kernel.
 //
-// Waits are bounded: one that runs out leaves NaN in the tile's outputs.
+// Waits are bounded: one that runs out leaves NaN in the outputs.
 #include <cuda.h>
 
 #include "lc_bulk.cuh"
@@ -30,26 +39,32 @@
 namespace lc {
 namespace {
 
-constexpr int kTileK = 128;      // features of a tile: the lanes of tensor memory, and one exponent a token
-constexpr int kTileN = 256;      // columns of dy of a tile
+constexpr int kHalf = 128;       // features and columns of dy that a CTA of the pair holds
+constexpr int kTile = 2 * kHalf; // of the pair's tile
 constexpr int kTok = 64;         // tokens of a stage
-constexpr int kStages = 5;
-constexpr int kXBytes = kTok * kTileK;             // 8-bit tile
-constexpr int kBox = 64;                           // columns of one dy copy: 128 bytes, the swizzle's span
+constexpr int kStages = 7;       // stages of copies in flight
+constexpr int kOps = 3;          // converted operands
+constexpr int kChunk = 8;        // stages that one accumulator adds up
+constexpr int kXBytes = kTok * kHalf;              // 8-bit tile
+constexpr int kBox = 64;                           // columns of a copy or operand box: 128 bytes, the swizzle's span
 constexpr int kBoxBytes = kTok * kBox * 2;
-constexpr int kYBytes = kTileN / kBox * kBoxBytes;
-constexpr int kStageBytes = kXBytes + kYBytes;
+constexpr int kOpBytes = kHalf / kBox * kBoxBytes; // a bf16 tile
+constexpr int kStageBytes = kOpBytes + kXBytes;    // dy, 8-bit tile
 constexpr int kConvWarp = 4, kConvWarps = 8;       // first converter warp (a multiple of 4), their number
-constexpr int kThreads = (kConvWarp + kConvWarps) * 32;
-constexpr int kTmemCols = 512;
-constexpr int kAcol = kTileN;                      // tensor memory: accumulator, then a stage's operand each
-constexpr int kAcols = kTok / 2;
-static_assert(kAcol + kStages * kAcols <= kTmemCols, "tensor memory");
-constexpr int kSmem = kStages * kStageBytes + 1024;   // and room to align the tiles to 1024 bytes
+constexpr int kSumWarp = kConvWarp + kConvWarps, kSumWarps = 8;
+constexpr int kThreads = (kSumWarp + kSumWarps) * 32;
+// Registers of a thread once the roles part: 4 * 32 * 40 + 8 * 32 * 56 + 8 * 32 * 160 = 60416, within the 640 * 96 =
+// 61440 of the launch.
+constexpr int kLaunchRegs = 96, kRoleRegs = 40, kConvRegs = 56, kSumRegs = 160;
+static_assert(kConvWarp * 32 * kRoleRegs + kConvWarps * 32 * kConvRegs + kSumWarps * 32 * kSumRegs <= kThreads * kLaunchRegs &&
+                  kThreads * kLaunchRegs <= 65536, "registers");
+constexpr int kTmemCols = 512;                     // two accumulators of 256 columns
+constexpr int kSmem = kStages * kStageBytes + kOps * kOpBytes + 1024;   // and room to align the tiles to 1024 bytes
+constexpr int kAcc = kTile / 2;                    // columns that a thread adds up
 
-// Instruction descriptor: fp32 accumulator, bf16 operands, the first from tensor
-// memory, the second with its rows along the reduction; 128 x 256.
-constexpr uint32_t kIdesc = 1u << 4 | 1u << 7 | 1u << 10 | 1u << 16 | uint32_t(kTileN / 8) << 17 | uint32_t(kTileK / 16) << 24;
+// Instruction descriptor: fp32 accumulator, bf16 operands, both with their rows
+// along the reduction; 256 x 256.
+constexpr uint32_t kIdesc = 1u << 4 | 1u << 7 | 1u << 10 | 1u << 15 | 1u << 16 | uint32_t(kTile / 8) << 17 | uint32_t(kTile / 16) << 24;
 
 struct WgradParams {
     const int8_t* e;
@@ -57,7 +72,8 @@ struct WgradParams {
     float* part;           // [splits][rows][dim] (splits > 1)
     int64_t e_pitch, dw_pitch;
     int32_t ntok, rows, dim;
-    int32_t ntiles_n, stages, stages_part, parts, splits, per_split;   // stages of a dy part, of all parts, of a split
+    int32_t items;         // tiles * splits
+    int32_t ntiles_n, stages, stages_part, splits, per_split;   // stages in all, of a part of dy, of a split
     int32_t tok_part;      // rows of dy between the parts
     int32_t accumulate, dw_bf16;
 };
@@ -69,32 +85,28 @@ __device__ __forceinline__ void tma_2d(uint32_t dst, const CUtensorMap* map, int
         : "memory");
 }
 
+// Once the products issued so far are done: an arrival at the barrier in both CTAs.
 __device__ __forceinline__ void tc_commit(uint32_t bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+    asm volatile(
+        "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
+        "h"(uint16_t(3))
+        : "memory");
 }
 
-// d += a * b: a in tensor memory, b in shared memory.
-__device__ __forceinline__ void tc_mma(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t add) {
+// d += a * b over both CTAs' halves; both operands in shared memory.
+__device__ __forceinline__ void tc_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t add) {
     asm volatile(
         "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
-        "r"(a), "l"(b), "r"(idesc), "r"(add)
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(add)
         : "memory");
 }
 
-// Shared-memory descriptor of a dy tile: 64-column boxes of 128-byte swizzled
+// Shared-memory descriptor of a bf16 tile: 64-column boxes of 128-byte swizzled
 // rows, 8 tokens 1024 bytes apart, the next 64 columns a box further.
-__device__ __forceinline__ uint64_t y_desc(uint32_t addr) {
+__device__ __forceinline__ uint64_t op_desc(uint32_t addr) {
     return uint64_t((addr & 0x3ffffu) >> 4) | uint64_t(kBoxBytes >> 4) << 16 | uint64_t(1024 >> 4) << 32 |
            uint64_t(1) << 46 | uint64_t(2) << 61;
-}
-
-__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t (&r)[16]) {
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(addr),
-        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
-        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
-        : "memory");
 }
 
 __device__ __forceinline__ void tmem_ld16(uint32_t addr, uint32_t (&r)[16]) {
@@ -107,9 +119,28 @@ __device__ __forceinline__ void tmem_ld16(uint32_t addr, uint32_t (&r)[16]) {
         : "memory");
 }
 
-// Two values of the checkpoint (bytes 0 and 2 of `q`) as bf16, times their tokens'
-// scales.  A byte's low seven bits go into the fraction of 128; 128, or 256 for a
-// negative one, comes off again: exact, as is the product with a power of two.
+// The barrier at this address in the pair's first CTA.
+__device__ __forceinline__ uint32_t in_first(uint32_t bar) {
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(bar));
+    return r;
+}
+// An arrival at a barrier of either CTA.  What it announces is read where it was
+// written (the tensor core of each multiprocessor reads its own shared memory, after
+// a proxy fence there), so no memory has to become visible to the other CTA: a
+// release for the whole cluster costs a full memory barrier a stage, which took most
+// of the converters' time (the kernel 1.36 ms instead of 0.82 at 8192 tokens, 14336 ->
+// 4096).
+__device__ __forceinline__ void arrive_cluster(uint32_t bar) {
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void cluster_barrier() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+// Two values of the checkpoint (bytes 0 and 2 of `q`) as bf16, times their scale.
+// A byte's low seven bits go into the fraction of 128; 128, or 256 for a negative
+// one, comes off again: exact, as is the product with a power of two.
 __device__ __forceinline__ uint32_t act_pair(uint32_t q, uint32_t scale) {
     const uint32_t v = (q & 0x007f007fu) | 0x43004300u, c = (q & 0x00800080u) | 0x43004300u;
     __nv_bfloat162 d = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&v), *reinterpret_cast<const __nv_bfloat162*>(&c));
@@ -117,141 +148,273 @@ __device__ __forceinline__ uint32_t act_pair(uint32_t q, uint32_t scale) {
     return *reinterpret_cast<const uint32_t*>(&d);
 }
 
-__global__ void __launch_bounds__(kThreads, 1)
+// One piece of work: a tile, or a split of one.
+struct Item {
+    int n0, k0, split, s0, stages;
+};
+__device__ __forceinline__ Item item_of(const WgradParams& p, int i) {
+    Item w;
+    const int tile = i / p.splits;
+    w.split = i - tile * p.splits;
+    w.n0 = tile % p.ntiles_n * kTile;
+    w.k0 = tile / p.ntiles_n * kTile;
+    w.s0 = w.split * p.per_split;
+    w.stages = (w.s0 + p.per_split < p.stages ? w.s0 + p.per_split : p.stages) - w.s0;
+    return w;
+}
+
+template <int N>
+__device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N>
+__device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+
+// A place in a ring of N and the parity of its round.
+template <int N>
+struct Ring {
+    int at = 0;
+    uint32_t round = 0;   // parity
+    __device__ __forceinline__ void next() {
+        if (++at == N) {
+            at = 0;
+            round ^= 1;
+        }
+    }
+};
+
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     wgrad_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CUtensorMap ymap, WgradParams p) {
     extern __shared__ uint8_t raw[];
-    __shared__ __align__(8) uint64_t bars[3 * kStages + 1];   // full, converted, empty; all products done
+    // full and empty: a stage's copies have landed / its products are done (each CTA's own).  converted: both CTAs'
+    // operands are in place (the first CTA's); op_free: their products are done.  summed: an accumulator is complete;
+    // taken: both CTAs have read it (the first CTA's).  scaled and used: a chunk's scales are there / no longer needed.
+    __shared__ __align__(8) uint64_t bars[2 * kStages + 2 * kOps + 8];
+    __shared__ __align__(16) uint16_t scales[2][kChunk * kTok];   // 2^e as bf16
     __shared__ uint32_t tmem_base;
     __shared__ volatile uint32_t failed;
-    __shared__ __align__(16) uint16_t scales[kConvWarps][2][32];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = blockIdx.x & 1, pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
     const uint32_t tiles = (smem_addr(raw) + 1023) & ~1023u;
-    const uint32_t full = smem_addr(bars), conv = full + 8 * kStages, empty = conv + 8 * kStages, done = empty + 8 * kStages;
-    const int tile = blockIdx.x / p.splits, split = blockIdx.x % p.splits;
-    const int n0 = tile % p.ntiles_n * kTileN, k0 = tile / p.ntiles_n * kTileK;
-    const int s0 = split * p.per_split, s1 = s0 + p.per_split < p.stages ? s0 + p.per_split : p.stages;
+    const uint32_t ops = tiles + kStages * kStageBytes;
+    const uint32_t full = smem_addr(bars), empty = full + 8 * kStages, converted = empty + 8 * kStages, op_free = converted + 8 * kOps;
+    const uint32_t summed = op_free + 8 * kOps, taken = summed + 16, scaled = taken + 16, used = scaled + 16;
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; ++i) {
             mbar_init(full + 8 * i, 1);
-            mbar_init(conv + 8 * i, kConvWarps);
             mbar_init(empty + 8 * i, 1);
         }
-        mbar_init(done, 1);
+        for (int i = 0; i < kOps; ++i) {
+            mbar_init(converted + 8 * i, kConvWarps);   // half of each CTA's
+            mbar_init(op_free + 8 * i, 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(summed + 8 * i, 1);
+            mbar_init(taken + 8 * i, 2 * kSumWarps);
+            mbar_init(scaled + 8 * i, 2);
+            mbar_init(used + 8 * i, kConvWarps);
+        }
         failed = 0;
         mbar_init_fence();
     }
     if (warp == 1) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem_base)), "r"(kTmemCols) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem_base)), "r"(kTmemCols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
+    cluster_barrier();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = tmem_base;
     dependency_wait();
 
-    if (warp == 0) {
-        if (lane == 0) {
-            int s = s0;
-            for (; s < s1; ++s) {
-                const int i = s - s0, b = i % kStages;
-                if (i >= kStages && !mbar_wait_bounded(empty + 8 * b, (i / kStages - 1) & 1, kWaitNs)) {
-                    failed = 1;
-                    break;
+    if (warp < kConvWarp) {
+        fewer_registers<kRoleRegs>();
+        bool ok = true;
+        if (warp == 0 && lane == 0) {
+            Ring<kStages> st;
+            int it = 0;
+            for (int i = pair; i < p.items && ok; i += pairs) {
+                const Item w = item_of(p, i);
+                int part = w.s0 / p.stages_part, t = (w.s0 - part * p.stages_part) * kTok;
+                for (int s = 0; s < w.stages; ++s, ++it, st.next()) {
+                    ok = it < kStages || mbar_wait_bounded(empty + 8 * st.at, st.round ^ 1, kWaitNs);
+                    if (!ok) break;
+                    const uint32_t at = tiles + st.at * kStageBytes, bar = full + 8 * st.at;
+                    mbar_expect_tx(bar, kStageBytes);
+                    tma_2d(at + kOpBytes, &xmap, w.k0 + rank * kHalf, t, bar);
+                    for (int j = 0; j < kHalf / kBox; ++j)
+                        tma_2d(at + j * kBoxBytes, &ymap, w.n0 + rank * kHalf + j * kBox, part * p.tok_part + t, bar);
+                    t += kTok;
+                    if (t >= p.stages_part * kTok) {
+                        t = 0;
+                        ++part;
+                    }
                 }
-                const int part = s / p.stages_part, t = (s - part * p.stages_part) * kTok;
-                const uint32_t at = tiles + b * kStageBytes;
-                mbar_expect_tx(full + 8 * b, kStageBytes);
-                tma_2d(at + kYBytes, &xmap, k0, t, full + 8 * b);
-                for (int j = 0; j < kTileN / kBox; ++j)
-                    tma_2d(at + j * kBoxBytes, &ymap, n0 + j * kBox, part * p.tok_part + t, full + 8 * b);
             }
             // every copy lands before the CTA's memory is given back
-            for (int i = s - s0 > kStages ? s - s0 - kStages : 0; i < s - s0; ++i)
-                if (!mbar_wait_bounded(full + 8 * (i % kStages), (i / kStages) & 1, kWaitNs)) failed = 1;
-        }
-    } else if (warp == 1) {
-        if (lane == 0) {
-            bool ok = true;
-            for (int s = s0; s < s1 && ok; ++s) {
-                const int i = s - s0, b = i % kStages;
-                ok = mbar_wait_bounded(full + 8 * b, (i / kStages) & 1, kWaitNs) &&
-                     mbar_wait_bounded(conv + 8 * b, (i / kStages) & 1, kWaitNs);
-                if (!ok) break;
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const uint32_t y = tiles + b * kStageBytes, a = tmem + kAcol + b * kAcols;
+            for (int i = it > kStages ? it - kStages : 0; i < it; ++i)
+                if (!mbar_wait_bounded(full + 8 * (i % kStages), (i / kStages) & 1, kWaitNs)) ok = false;
+        } else if (warp == 1 && lane == 0 && rank == 0) {
+            Ring<kStages> st;
+            Ring<kOps> op;
+            Ring<2> acc;
+            int chunk = 0;
+            for (int i = pair; i < p.items && ok; i += pairs) {
+                const Item w = item_of(p, i);
+                for (int s = 0; s < w.stages; ++s, st.next(), op.next()) {
+                    const bool first = s % kChunk == 0;
+                    if (first && chunk >= 2) ok = mbar_wait_bounded(taken + 8 * acc.at, acc.round ^ 1, kWaitNs);
+                    ok = ok && mbar_wait_bounded(converted + 8 * op.at, op.round, kWaitNs);
+                    if (!ok) break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    const uint64_t x = op_desc(ops + op.at * kOpBytes), y = op_desc(tiles + st.at * kStageBytes);
+                    // 16 tokens are 2048 bytes further
 #pragma unroll
-                for (int k = 0; k < kTok / 16; ++k) tc_mma(tmem, a + k * 8, y_desc(y + k * 2048), kIdesc, i > 0 || k > 0);
-                tc_commit(empty + 8 * b);
-            }
-            if (!ok) failed = 1;
-            tc_commit(done);
-            if (!ok) mbar_wait_bounded(done, 0, kDrainNs);   // what was issued ends before the memory is given back
-        }
-    } else if (warp >= kConvWarp) {
-        const int w = warp - kConvWarp, quad = warp & 3, half = w >> 2;
-        const int t_in = half * 32;
-        const int8_t* ep = p.e + k0 / LC_ACT_BLOCK;
-        auto exponent = [&](int s) -> int {
-            const int t = s % p.stages_part * kTok + t_in + lane;
-            return s < s1 && t < p.ntok ? int(__ldg(ep + int64_t(t) * p.e_pitch)) : 0;
-        };
-        bool ok = true;
-        int e_next = exponent(s0);
-        for (int s = s0; s < s1; ++s) {
-            const int i = s - s0, b = i % kStages;
-            const int e = e_next;
-            e_next = exponent(s + 1);
-            // 2^e as bf16 (the upper half of the fp32 number), NaN for 127
-            scales[w][i & 1][lane] = e == 127 ? uint16_t(0x7fff) : uint16_t((e + 127) << 7);
-            __syncwarp();
-            if (!mbar_wait_warp(full + 8 * b, (i / kStages) & 1)) {
-                ok = false;
-                break;
-            }
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const uint8_t* x = raw + (tiles - smem_addr(raw)) + b * kStageBytes + kYBytes + t_in * kTileK + quad * 32 + lane;
-            uint32_t a[16];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const uint4 sc = *reinterpret_cast<const uint4*>(&scales[w][i & 1][8 * k]);
-                const uint32_t s2[4] = {sc.x, sc.y, sc.z, sc.w};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int t = 8 * k + 2 * j;
-                    a[4 * k + j] = act_pair(__byte_perm(x[t * kTileK], x[(t + 1) * kTileK], 0x5410), s2[j]);
+                    for (int k = 0; k < kTok / 16; ++k)
+                        tc_mma(tmem + acc.at * kTile, x + k * (2048 >> 4), y + k * (2048 >> 4), kIdesc, !first || k > 0);
+                    tc_commit(op_free + 8 * op.at);
+                    tc_commit(empty + 8 * st.at);
+                    if (s % kChunk == kChunk - 1 || s == w.stages - 1) {
+                        tc_commit(summed + 8 * acc.at);
+                        acc.next();
+                        ++chunk;
+                    }
                 }
             }
-            tmem_st16(tmem + (uint32_t(quad * 32) << 16) + kAcol + b * kAcols + t_in / 2, a);
-            asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
-            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-            mbar_arrive_warp(conv + 8 * b, lane);
-        }
-        if (ok) ok = mbar_wait_warp(done, 0);
-        if (!ok) failed = 1;
-        __syncwarp();
-        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        const bool bad = failed != 0;
-        const int k = k0 + quad * 32 + lane;
-        for (int c = 0; c < kTileN / 2; c += 16) {
-            const int nc = half * (kTileN / 2) + c;
-            if (n0 + nc >= p.rows) break;
-            uint32_t r[16];
-            __syncwarp();
-            tmem_ld16(tmem + (uint32_t(quad * 32) << 16) + nc, r);
+        } else if (warp >= 2) {
+            int chunk = 0;
+            for (int i = pair; i < p.items && ok; i += pairs) {
+                const Item w = item_of(p, i);
+                const int f = w.k0 + rank * kHalf;
+                const int8_t* ep = p.e + f / LC_ACT_BLOCK;
+                for (int s = 0; s < w.stages; s += kChunk, ++chunk) {
+                    const int buf = chunk & 1, t_in = (warp - 2) * 32 + lane;
+                    int e[kChunk];
 #pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                const int n = n0 + nc + j;
-                if (n >= p.rows || k >= p.dim) continue;
-                float v = bad ? __uint_as_float(0x7fffffffu) : __uint_as_float(r[j]);
-                if (p.splits > 1) {
-                    p.part[(int64_t(split) * p.rows + n) * p.dim + k] = v;
-                } else if (p.dw_bf16) {
-                    __nv_bfloat16* o = reinterpret_cast<__nv_bfloat16*>(p.dw + n * p.dw_pitch) + k;
-                    *o = __float2bfloat16_rn(p.accumulate ? __bfloat162float(*o) + v : v);
-                } else {
-                    float* o = reinterpret_cast<float*>(p.dw + n * p.dw_pitch) + k;
-                    *o = p.accumulate ? *o + v : v;
+                    for (int j = 0; j < kChunk; ++j) {
+                        const int t = (w.s0 + s + j) % p.stages_part * kTok + t_in;
+                        e[j] = s + j < w.stages && t < p.ntok && f < p.dim ? int(__ldg(ep + int64_t(t) * p.e_pitch)) : 0;
+                    }
+                    ok = chunk < 2 || mbar_wait_warp(used + 8 * buf, (chunk / 2 - 1) & 1);
+                    if (!ok) break;
+                    // the upper half of the fp32 number 2^e, NaN for 127
+#pragma unroll
+                    for (int j = 0; j < kChunk; ++j)
+                        scales[buf][j * kTok + t_in] = e[j] == 127 ? uint16_t(0x7fff) : uint16_t((e[j] + 127) << 7);
+                    mbar_arrive_warp(scaled + 8 * buf, lane);
+                }
+            }
+        }
+        if (!ok) failed = 1;
+    } else if (warp < kSumWarp) {
+        fewer_registers<kConvRegs>();
+        const int group = (warp - kConvWarp) >> 2, w4 = warp & 3;
+        // 16 features, the c-th of the 8-bit row's eight pieces, of tokens t0 + 4 r, r = 0..3
+        const int c = lane & 7, t0 = w4 * 16 + (lane >> 3);
+        // 16-byte pieces 2c and 2c + 1 of the operand's row; lanes of its second box store them in the other order, so
+        // that the eight lanes of a row meet in no bank.  Tokens 4 apart: the swizzle (token mod 8) flips its upper bit.
+        const int first = (c & 3) * 2 + (c >> 2), second = first ^ 1;
+        const bool swap = c >= 4;
+        const uint32_t x_off = kOpBytes + t0 * kHalf + c * 16;
+        const uint32_t o_off = (c >> 2) * kBoxBytes + t0 * 128;
+        const uint32_t sw = uint32_t(t0 & 7) << 4;
+        const uint32_t first_converted = in_first(converted);
+        const uint32_t align = tiles - smem_addr(raw);
+        Ring<kStages> st;
+        Ring<kOps> op;
+        bool ok = true;
+        int it = 0, chunk = 0;
+        for (int i = pair; i < p.items && ok; i += pairs) {
+            const int stages = item_of(p, i).stages;
+            for (int s = 0; s < stages; ++s, ++it, st.next(), op.next()) {
+                const int sb = chunk & 1;
+                if (s % kChunk == 0) ok = mbar_wait_warp(scaled + 8 * sb, (chunk >> 1) & 1);
+                if ((it & 1) == group && ok) {
+                    ok = mbar_wait_warp(full + 8 * st.at, st.round);
+                    const uint8_t* x = raw + align + st.at * kStageBytes + x_off;
+                    uint4 q[4];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) q[r] = *reinterpret_cast<const uint4*>(x + r * 4 * kHalf);
+                    if (ok && it >= kOps) ok = mbar_wait_warp(op_free + 8 * op.at, op.round ^ 1);
+                    uint8_t* o = raw + align + kStages * kStageBytes + op.at * kOpBytes + o_off;
+                    const uint16_t* sc = &scales[sb][s % kChunk * kTok + t0];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const uint32_t s2 = sc[4 * r] * 0x10001u;
+                        const uint32_t qw[4] = {q[r].x, q[r].y, q[r].z, q[r].w};
+                        uint32_t v[8];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            v[2 * j] = act_pair(__byte_perm(qw[j], 0, 0x4140), s2);
+                            v[2 * j + 1] = act_pair(__byte_perm(qw[j], 0, 0x4342), s2);
+                        }
+                        const uint4 lo = make_uint4(v[0], v[1], v[2], v[3]), hi = make_uint4(v[4], v[5], v[6], v[7]);
+                        const uint32_t z = sw ^ ((r & 1) << 6);
+                        *reinterpret_cast<uint4*>(o + r * 512 + ((first << 4) ^ z)) = swap ? hi : lo;
+                        *reinterpret_cast<uint4*>(o + r * 512 + ((second << 4) ^ z)) = swap ? lo : hi;
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) arrive_cluster(first_converted + 8 * op.at);
+                }
+                if (!ok) break;
+                if (s % kChunk == kChunk - 1 || s == stages - 1) {
+                    mbar_arrive_warp(used + 8 * sb, lane);
+                    ++chunk;
+                }
+            }
+        }
+        if (!ok) failed = 1;
+    } else {
+        more_registers<kSumRegs>();
+        const int quad = warp & 3, half = (warp - kSumWarp) >> 2;
+        const uint32_t first_taken = in_first(taken);
+        const uint32_t from = tmem + (uint32_t(quad * 32) << 16) + half * kAcc;
+        Ring<2> a;
+        bool ok = true;
+        for (int i = pair; i < p.items; i += pairs) {
+            const Item w = item_of(p, i);
+            float acc[kAcc];
+#pragma unroll
+            for (int j = 0; j < kAcc; ++j) acc[j] = 0.0f;
+            for (int s = 0; s < w.stages && ok; s += kChunk, a.next()) {
+                ok = mbar_wait_warp(summed + 8 * a.at, a.round);
+                if (!ok) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll
+                for (int j = 0; j < kAcc; j += 16) {
+                    uint32_t r[16];
+                    tmem_ld16(from + a.at * kTile + j, r);
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) acc[j + k] += __uint_as_float(r[k]);
+                }
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) arrive_cluster(first_taken + 8 * a.at);
+            }
+            if (!ok) failed = 1;
+            const float off = failed ? __uint_as_float(0x7fffffffu) : 0.0f;   // NaN after a wait that ran out
+            const int k = w.k0 + rank * kHalf + quad * 32 + lane;
+            const int n0 = w.n0 + half * kAcc;
+            const int cnt = k < p.dim ? p.rows - n0 : 0;
+            if (p.splits == 1 && p.dw_bf16) {
+                __nv_bfloat16* o = reinterpret_cast<__nv_bfloat16*>(p.dw + int64_t(n0) * p.dw_pitch) + k;
+                const int64_t pitch = p.dw_pitch / 2;
+#pragma unroll
+                for (int j = 0; j < kAcc; ++j) {
+                    if (j < cnt) *o = __float2bfloat16_rn(p.accumulate ? __bfloat162float(*o) + acc[j] + off : acc[j] + off);
+                    o += pitch;
+                    asm volatile("" : "+l"(o)::"memory");   // one pointer that moves on, not kAcc of them
+                }
+            } else {
+                const bool add = p.accumulate && p.splits == 1;
+                float* o = p.splits > 1 ? p.part + (int64_t(w.split) * p.rows + n0) * p.dim + k
+                                        : reinterpret_cast<float*>(p.dw + int64_t(n0) * p.dw_pitch) + k;
+                const int64_t pitch = p.splits > 1 ? p.dim : p.dw_pitch / 4;
+#pragma unroll
+                for (int j = 0; j < kAcc; ++j) {
+                    if (j < cnt) *o = add ? *o + acc[j] + off : acc[j] + off;
+                    o += pitch;
+                    asm volatile("" : "+l"(o)::"memory");
                 }
             }
         }
@@ -259,9 +422,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     __syncwarp();
     __syncthreads();
+    // the other CTA's barriers and operands are used until here
+    cluster_barrier();
     if (warp == 1) {
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
     }
 }
 
@@ -359,18 +524,18 @@ constexpr int64_t al(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
 
 // How a product is cut: output tiles, parts of dy, and splits of the tokens where
 // the tiles alone leave multiprocessors idle (each split at least 4 stages long).
-constexpr int kSms = 152;
+constexpr int kPairs = 76;
 struct Shape {
     int64_t tiles_n, tiles_k, stages_part, stages, splits, per_split;
 };
 Shape shape_of(int64_t ntok, int64_t rows, int64_t dim, int32_t dy_dtype) {
     Shape s;
-    s.tiles_n = (rows + kTileN - 1) / kTileN;
-    s.tiles_k = (dim + kTileK - 1) / kTileK;
+    s.tiles_n = (rows + kTile - 1) / kTile;
+    s.tiles_k = (dim + kTile - 1) / kTile;
     s.stages_part = (ntok + kTok - 1) / kTok;
     s.stages = s.stages_part * (dy_dtype == LC_F32 ? 3 : 1);
     const int64_t tiles = s.tiles_n * s.tiles_k;
-    s.splits = tiles >= kSms ? 1 : kSms / tiles;
+    s.splits = tiles >= kPairs ? 1 : kPairs / tiles;
     if (s.splits > (s.stages + 3) / 4) s.splits = (s.stages + 3) / 4;
     if (s.splits < 1) s.splits = 1;
     s.per_split = (s.stages + s.splits - 1) / s.splits;
@@ -379,6 +544,30 @@ Shape shape_of(int64_t ntok, int64_t rows, int64_t dim, int32_t dy_dtype) {
 }
 int64_t staged_bytes(int64_t ntok, int64_t rows, int32_t dy_dtype) {
     return al(al(ntok, kTok) * al(rows, 64) * 2 * (dy_dtype == LC_F32 ? 3 : 1), 256);
+}
+// Pairs of CTAs that the device holds at once.
+cudaError_t resident_pairs(int device, int* pairs) {
+    static int held[kOpsMaxDevices];
+    if (!held[device]) {
+        cudaError_t e = cudaFuncSetAttribute(wgrad_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+        if (e != cudaSuccess) return e;
+        cudaLaunchAttribute attr{};
+        attr.id = cudaLaunchAttributeClusterDimension;
+        attr.val.clusterDim.x = 2;
+        attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+        cudaLaunchConfig_t c{};
+        c.gridDim = dim3(2 * kPairs);
+        c.blockDim = dim3(kThreads);
+        c.dynamicSmemBytes = kSmem;
+        c.attrs = &attr;
+        c.numAttrs = 1;
+        int n = 0;
+        e = cudaOccupancyMaxActiveClusters(&n, wgrad_kernel, &c);
+        if (e != cudaSuccess) return e;
+        held[device] = n < 1 ? 1 : n;
+    }
+    *pairs = held[device];
+    return cudaSuccess;
 }
 constexpr int64_t kMost = (int64_t(1) << 31) - 1024;
 
@@ -462,7 +651,7 @@ extern "C" lc_status lc_weight_grad(int device, void* cuda_stream, const lc_rows
         yrows = q.tok_pad * (f32 ? 3 : 1);
     }
     CUtensorMap xmap, ymap;
-    if (!encode(&xmap, CU_TENSOR_MAP_DATA_TYPE_UINT8, x->q, blocks * LC_ACT_BLOCK, ntok, x->q_stride, kTileK, CU_TENSOR_MAP_SWIZZLE_NONE) ||
+    if (!encode(&xmap, CU_TENSOR_MAP_DATA_TYPE_UINT8, x->q, blocks * LC_ACT_BLOCK, ntok, x->q_stride, kHalf, CU_TENSOR_MAP_SWIZZLE_NONE) ||
         !encode(&ymap, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, ydata, ycols, yrows, ypitch, kBox, CU_TENSOR_MAP_SWIZZLE_128B))
         return fail_status(LC_ERR_CUDA, "%s: no tensor map", call);
     WgradParams p{};
@@ -474,6 +663,7 @@ extern "C" lc_status lc_weight_grad(int device, void* cuda_stream, const lc_rows
     p.ntok = int32_t(ntok);
     p.rows = int32_t(rows);
     p.dim = int32_t(dim);
+    p.items = int32_t(tiles * sh.splits);
     p.ntiles_n = int32_t(sh.tiles_n);
     p.stages = int32_t(sh.stages);
     p.stages_part = int32_t(sh.stages_part);
@@ -482,13 +672,10 @@ extern "C" lc_status lc_weight_grad(int device, void* cuda_stream, const lc_rows
     p.tok_part = int32_t(tok_part);
     p.accumulate = accumulate != 0;
     p.dw_bf16 = dw->dtype == LC_BF16;
-    static bool ready[kOpsMaxDevices];
-    if (!ready[device]) {
-        e = cudaFuncSetAttribute(wgrad_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
-        if (e != cudaSuccess) return ops_launched(call, e);
-        ready[device] = true;
-    }
-    e = launch_dependent(wgrad_kernel, int(tiles * sh.splits), kThreads, kSmem, s, xmap, ymap, p);
+    int pairs = 0;
+    e = resident_pairs(device, &pairs);
+    if (e != cudaSuccess) return ops_launched(call, e);
+    e = launch_dependent(wgrad_kernel, 2 * (p.items < pairs ? p.items : pairs), kThreads, kSmem, s, xmap, ymap, p);
     if (e == cudaSuccess && sh.splits > 1) {
         JoinParams j{p.part, p.dw, dw_pitch, rows, dim, p.splits, p.accumulate, p.dw_bf16};
         const int64_t want = (rows * dim + 1023) / 1024, most = int64_t(ops_sm_count(device)) * 32;
