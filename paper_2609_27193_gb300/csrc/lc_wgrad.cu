@@ -42,14 +42,14 @@ namespace {
 constexpr int kHalf = 128;       // features and columns of dy that a CTA of the pair holds
 constexpr int kTile = 2 * kHalf; // of the pair's tile
 constexpr int kTok = 64;         // tokens of a stage
-constexpr int kStages = 7;       // stages of copies in flight
-constexpr int kOps = 3;          // converted operands
+constexpr int kStages = 5;       // stages in flight
 constexpr int kChunk = 8;        // stages that one accumulator adds up
 constexpr int kXBytes = kTok * kHalf;              // 8-bit tile
 constexpr int kBox = 64;                           // columns of a copy or operand box: 128 bytes, the swizzle's span
 constexpr int kBoxBytes = kTok * kBox * 2;
 constexpr int kOpBytes = kHalf / kBox * kBoxBytes; // a bf16 tile
-constexpr int kStageBytes = kOpBytes + kXBytes;    // dy, 8-bit tile
+constexpr int kLoadBytes = kOpBytes + kXBytes;     // what the copies of a stage bring: dy, 8-bit tile
+constexpr int kStageBytes = kLoadBytes + kOpBytes; // and the operand
 constexpr int kConvWarp = 4, kConvWarps = 8;       // first converter warp (a multiple of 4), their number
 constexpr int kSumWarp = kConvWarp + kConvWarps, kSumWarps = 8;
 constexpr int kThreads = (kSumWarp + kSumWarps) * 32;
@@ -59,7 +59,7 @@ constexpr int kLaunchRegs = 96, kRoleRegs = 40, kConvRegs = 56, kSumRegs = 160;
 static_assert(kConvWarp * 32 * kRoleRegs + kConvWarps * 32 * kConvRegs + kSumWarps * 32 * kSumRegs <= kThreads * kLaunchRegs &&
                   kThreads * kLaunchRegs <= 65536, "registers");
 constexpr int kTmemCols = 512;                     // two accumulators of 256 columns
-constexpr int kSmem = kStages * kStageBytes + kOps * kOpBytes + 1024;   // and room to align the tiles to 1024 bytes
+constexpr int kSmem = kStages * kStageBytes + 1024;   // and room to align the tiles to 1024 bytes
 constexpr int kAcc = kTile / 2;                    // columns that a thread adds up
 
 // Instruction descriptor: fp32 accumulator, bf16 operands, both with their rows
@@ -138,15 +138,20 @@ __device__ __forceinline__ void cluster_barrier() {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-// Two values of the checkpoint (bytes 0 and 2 of `q`) as bf16, times their scale.
-// A byte's low seven bits go into the fraction of 128; 128, or 256 for a negative
-// one, comes off again: exact, as is the product with a power of two.
+// Two values of the checkpoint (bytes 0 and 2 of `q`; the others are ignored) as
+// bf16, times their scale.  A byte's low seven bits go into the fraction of 128;
+// 128, or 256 for a negative one, comes off again: exact, as is the product with a
+// power of two.
 __device__ __forceinline__ uint32_t act_pair(uint32_t q, uint32_t scale) {
     const uint32_t v = (q & 0x007f007fu) | 0x43004300u, c = (q & 0x00800080u) | 0x43004300u;
     __nv_bfloat162 d = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&v), *reinterpret_cast<const __nv_bfloat162*>(&c));
     d = __hmul2(d, *reinterpret_cast<const __nv_bfloat162*>(&scale));
     return *reinterpret_cast<const uint32_t*>(&d);
 }
+// Bytes 0 and 2 of a word make one pair and bytes 1 and 3 the other, which spares
+// the permutations that neighbours would need: of every four features of the
+// operand the middle two have changed places.
+__device__ __forceinline__ int feature_of(int row) { return (row & ~3) | (row & 1) << 1 | (row >> 1 & 1); }
 
 // One piece of work: a tile, or a split of one.
 struct Item {
@@ -185,26 +190,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     wgrad_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CUtensorMap ymap, WgradParams p) {
     extern __shared__ uint8_t raw[];
     // full and empty: a stage's copies have landed / its products are done (each CTA's own).  converted: both CTAs'
-    // operands are in place (the first CTA's); op_free: their products are done.  summed: an accumulator is complete;
-    // taken: both CTAs have read it (the first CTA's).  scaled and used: a chunk's scales are there / no longer needed.
-    __shared__ __align__(8) uint64_t bars[2 * kStages + 2 * kOps + 8];
+    // operands are in place (the first CTA's).  summed: an accumulator is complete; taken: both CTAs have read it (the
+    // first CTA's).  scaled and used: a chunk's scales are there / no longer needed.
+    __shared__ __align__(8) uint64_t bars[3 * kStages + 8];
     __shared__ __align__(16) uint16_t scales[2][kChunk * kTok];   // 2^e as bf16
     __shared__ uint32_t tmem_base;
     __shared__ volatile uint32_t failed;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = blockIdx.x & 1, pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
     const uint32_t tiles = (smem_addr(raw) + 1023) & ~1023u;
-    const uint32_t ops = tiles + kStages * kStageBytes;
-    const uint32_t full = smem_addr(bars), empty = full + 8 * kStages, converted = empty + 8 * kStages, op_free = converted + 8 * kOps;
-    const uint32_t summed = op_free + 8 * kOps, taken = summed + 16, scaled = taken + 16, used = scaled + 16;
+    const uint32_t full = smem_addr(bars), empty = full + 8 * kStages, converted = empty + 8 * kStages;
+    const uint32_t summed = converted + 8 * kStages, taken = summed + 16, scaled = taken + 16, used = scaled + 16;
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; ++i) {
             mbar_init(full + 8 * i, 1);
             mbar_init(empty + 8 * i, 1);
-        }
-        for (int i = 0; i < kOps; ++i) {
             mbar_init(converted + 8 * i, kConvWarps);   // half of each CTA's
-            mbar_init(op_free + 8 * i, 1);
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(summed + 8 * i, 1);
@@ -239,7 +240,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                     ok = it < kStages || mbar_wait_bounded(empty + 8 * st.at, st.round ^ 1, kWaitNs);
                     if (!ok) break;
                     const uint32_t at = tiles + st.at * kStageBytes, bar = full + 8 * st.at;
-                    mbar_expect_tx(bar, kStageBytes);
+                    mbar_expect_tx(bar, kLoadBytes);
                     tma_2d(at + kOpBytes, &xmap, w.k0 + rank * kHalf, t, bar);
                     for (int j = 0; j < kHalf / kBox; ++j)
                         tma_2d(at + j * kBoxBytes, &ymap, w.n0 + rank * kHalf + j * kBox, part * p.tok_part + t, bar);
@@ -255,23 +256,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                 if (!mbar_wait_bounded(full + 8 * (i % kStages), (i / kStages) & 1, kWaitNs)) ok = false;
         } else if (warp == 1 && lane == 0 && rank == 0) {
             Ring<kStages> st;
-            Ring<kOps> op;
             Ring<2> acc;
             int chunk = 0;
             for (int i = pair; i < p.items && ok; i += pairs) {
                 const Item w = item_of(p, i);
-                for (int s = 0; s < w.stages; ++s, st.next(), op.next()) {
+                for (int s = 0; s < w.stages; ++s, st.next()) {
                     const bool first = s % kChunk == 0;
                     if (first && chunk >= 2) ok = mbar_wait_bounded(taken + 8 * acc.at, acc.round ^ 1, kWaitNs);
-                    ok = ok && mbar_wait_bounded(converted + 8 * op.at, op.round, kWaitNs);
+                    ok = ok && mbar_wait_bounded(converted + 8 * st.at, st.round, kWaitNs);
                     if (!ok) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const uint64_t x = op_desc(ops + op.at * kOpBytes), y = op_desc(tiles + st.at * kStageBytes);
+                    const uint64_t y = op_desc(tiles + st.at * kStageBytes), x = y + (kLoadBytes >> 4);
                     // 16 tokens are 2048 bytes further
 #pragma unroll
                     for (int k = 0; k < kTok / 16; ++k)
                         tc_mma(tmem + acc.at * kTile, x + k * (2048 >> 4), y + k * (2048 >> 4), kIdesc, !first || k > 0);
-                    tc_commit(op_free + 8 * op.at);
                     tc_commit(empty + 8 * st.at);
                     if (s % kChunk == kChunk - 1 || s == w.stages - 1) {
                         tc_commit(summed + 8 * acc.at);
@@ -308,24 +307,20 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     } else if (warp < kSumWarp) {
         fewer_registers<kConvRegs>();
         const int group = (warp - kConvWarp) >> 2, w4 = warp & 3;
-        // 16 features, the c-th of the 8-bit row's eight pieces, of tokens t0 + 4 r, r = 0..3
-        const int c = lane & 7, t0 = w4 * 16 + (lane >> 3);
-        // 16-byte pieces 2c and 2c + 1 of the operand's row; lanes of its second box store them in the other order, so
-        // that the eight lanes of a row meet in no bank.  Tokens 4 apart: the swizzle (token mod 8) flips its upper bit.
-        const int first = (c & 3) * 2 + (c >> 2), second = first ^ 1;
-        const bool swap = c >= 4;
+        // 16 features, the c-th of the 8-bit row's eight pieces, of tokens t0 + 4 r, r = 0..3.  They are pieces 2 (c mod 4)
+        // and the next of the operand's row in box c / 4; piece i of token t lies at i xor (t mod 8).  Lanes of the second
+        // box have the neighbour of the others' token, so eight lanes meet in no bank, neither here nor there.
+        const int c = lane & 7, t0 = w4 * 16 + ((lane >> 3) ^ (c >> 2));
         const uint32_t x_off = kOpBytes + t0 * kHalf + c * 16;
-        const uint32_t o_off = (c >> 2) * kBoxBytes + t0 * 128;
-        const uint32_t sw = uint32_t(t0 & 7) << 4;
+        const uint32_t row_off = kLoadBytes + (c >> 2) * kBoxBytes + t0 * 128, piece = uint32_t((c & 3) * 2 ^ (t0 & 7)) << 4;
         const uint32_t first_converted = in_first(converted);
         const uint32_t align = tiles - smem_addr(raw);
         Ring<kStages> st;
-        Ring<kOps> op;
         bool ok = true;
         int it = 0, chunk = 0;
         for (int i = pair; i < p.items && ok; i += pairs) {
             const int stages = item_of(p, i).stages;
-            for (int s = 0; s < stages; ++s, ++it, st.next(), op.next()) {
+            for (int s = 0; s < stages; ++s, ++it, st.next()) {
                 const int sb = chunk & 1;
                 if (s % kChunk == 0) ok = mbar_wait_warp(scaled + 8 * sb, (chunk >> 1) & 1);
                 if ((it & 1) == group && ok) {
@@ -334,8 +329,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                     uint4 q[4];
 #pragma unroll
                     for (int r = 0; r < 4; ++r) q[r] = *reinterpret_cast<const uint4*>(x + r * 4 * kHalf);
-                    if (ok && it >= kOps) ok = mbar_wait_warp(op_free + 8 * op.at, op.round ^ 1);
-                    uint8_t* o = raw + align + kStages * kStageBytes + op.at * kOpBytes + o_off;
+                    // the stage's copies were issued after its last products: the operand's place is free
+                    uint8_t* o = raw + align + st.at * kStageBytes + row_off;
                     const uint16_t* sc = &scales[sb][s % kChunk * kTok + t0];
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
@@ -344,17 +339,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                         uint32_t v[8];
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
-                            v[2 * j] = act_pair(__byte_perm(qw[j], 0, 0x4140), s2);
-                            v[2 * j + 1] = act_pair(__byte_perm(qw[j], 0, 0x4342), s2);
+                            v[2 * j] = act_pair(qw[j], s2);
+                            v[2 * j + 1] = act_pair(qw[j] >> 8, s2);
                         }
-                        const uint4 lo = make_uint4(v[0], v[1], v[2], v[3]), hi = make_uint4(v[4], v[5], v[6], v[7]);
-                        const uint32_t z = sw ^ ((r & 1) << 6);
-                        *reinterpret_cast<uint4*>(o + r * 512 + ((first << 4) ^ z)) = swap ? hi : lo;
-                        *reinterpret_cast<uint4*>(o + r * 512 + ((second << 4) ^ z)) = swap ? lo : hi;
+                        const uint32_t at = piece ^ (r & 1) << 6;
+                        *reinterpret_cast<uint4*>(o + r * 512 + at) = make_uint4(v[0], v[1], v[2], v[3]);
+                        *reinterpret_cast<uint4*>(o + r * 512 + (at ^ 16)) = make_uint4(v[4], v[5], v[6], v[7]);
                     }
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();
-                    if (lane == 0) arrive_cluster(first_converted + 8 * op.at);
+                    if (lane == 0) arrive_cluster(first_converted + 8 * st.at);
                 }
                 if (!ok) break;
                 if (s % kChunk == kChunk - 1 || s == stages - 1) {
@@ -393,7 +387,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             }
             if (!ok) failed = 1;
             const float off = failed ? __uint_as_float(0x7fffffffu) : 0.0f;   // NaN after a wait that ran out
-            const int k = w.k0 + rank * kHalf + quad * 32 + lane;
+            const int k = w.k0 + rank * kHalf + feature_of(quad * 32 + lane);
             const int n0 = w.n0 + half * kAcc;
             const int cnt = k < p.dim ? p.rows - n0 : 0;
             if (p.splits == 1 && p.dw_bf16) {
