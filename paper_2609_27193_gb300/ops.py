@@ -38,9 +38,10 @@ class Act:
 
     def __init__(self, q, e, dim):
         blocks = -(-int(dim) // LC_ACT_BLOCK)
-        if (q.dtype != torch.int8 or e.dtype != torch.int8 or q.dim() != 2 or e.dim() != 2 or dim <= 0
-                or q.shape[1] < blocks * LC_ACT_BLOCK or e.shape[1] < blocks or q.shape[0] != e.shape[0]
-                or q.stride(1) != 1 or e.stride(1) != 1):
+        qs, es, qt, et = q.shape, e.shape, q.stride(), e.stride()
+        if (q.dtype != torch.int8 or e.dtype != torch.int8 or len(qs) != 2 or len(es) != 2 or dim <= 0
+                or qs[1] < blocks * LC_ACT_BLOCK or es[1] < blocks or qs[0] != es[0]
+                or qt[1] != 1 or (et[1] != 1 and es[1] > 1)):
             raise ValueError("a checkpoint of width %d has int8 rows of %d values and %d exponents"
                              % (dim, blocks * LC_ACT_BLOCK, blocks))
         if q.device != e.device:
@@ -50,8 +51,11 @@ class Act:
     @classmethod
     def empty(cls, rows, dim, device):
         blocks = -(-int(dim) // LC_ACT_BLOCK)
-        return cls(torch.empty(rows, blocks * LC_ACT_BLOCK, dtype=torch.int8, device=device),
-                   torch.empty(rows, blocks, dtype=torch.int8, device=device), dim)
+        act = cls.__new__(cls)
+        act.q = torch.empty((rows, blocks * LC_ACT_BLOCK), dtype=torch.int8, device=device)
+        act.e = torch.empty((rows, blocks), dtype=torch.int8, device=device)
+        act.dim = int(dim)
+        return act
 
     @property
     def rows(self):
@@ -69,9 +73,10 @@ def _rows(t, name):
     code = _CODE.get(t.dtype)
     if code is None:
         raise TypeError("%s must be bfloat16 or float32, got %s" % (name, t.dtype))
-    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+    stride = t.stride()
+    if len(stride) != 2 or (stride[1] != 1 and t.shape[1] > 1):
         raise ValueError("%s must be 2-D with contiguous rows" % name)
-    return lc_rows(t.data_ptr(), t.stride(0), code, 0)
+    return lc_rows(t.data_ptr(), stride[0], code, 0)
 
 
 def _on(device, *tensors):
@@ -83,8 +88,8 @@ def _on(device, *tensors):
     return device.index
 
 
-def _stream(index):
-    return torch.cuda.current_stream(index).cuda_stream
+# the handle of torch's current stream, without a Stream object around it (1 us a call)
+_stream = torch._C._cuda_getCurrentRawStream
 
 
 def _workspace(device, stream, nbytes):
@@ -113,7 +118,7 @@ def _ids(ids):
 
 
 def _shaped(t, rows, dim, name):
-    if t.shape[0] != rows or t.shape[1] != dim:
+    if t.shape != (rows, dim):
         raise ValueError("%s must have shape [%d, %d]" % (name, rows, dim))
 
 
@@ -125,9 +130,10 @@ def embed(table, ids, scale=1.0, out=None):
     rt, it = _rows(table, "table"), _ids(ids)
     n, (vocab, dim) = ids.numel(), table.shape
     if out is None:
-        out = torch.empty(n, dim, dtype=table.dtype, device=device)
+        out = torch.empty((n, dim), dtype=table.dtype, device=device)
+    else:
+        _shaped(out, n, dim, "out")
     ro = _rows(out, "out")
-    _shaped(out, n, dim, "out")
     check(_abi.load().lc_embed(index, _stream(index), rt, vocab, dim, ids.data_ptr(), it, n, scale, ro))
     return out
 
@@ -147,10 +153,11 @@ def embed_grad(dy, ids, vocab=None, scale=1.0, grad=None, dtype=None, skip_id=-1
             raise ValueError("accumulate needs grad")
         if vocab is None:
             raise ValueError("vocab or grad is needed")
-        grad = torch.empty(vocab, dim, dtype=dtype or dy.dtype, device=device)
+        grad = torch.empty((vocab, dim), dtype=dtype or dy.dtype, device=device)
+    else:
+        vocab = grad.shape[0]
+        _shaped(grad, vocab, dim, "grad")
     rg = _rows(grad, "grad")
-    vocab = grad.shape[0]
-    _shaped(grad, vocab, dim, "grad")
     lib, stream = _abi.load(), _stream(index)
     need = lib.lc_embed_grad_workspace(n, vocab, dim)
     check(lib.lc_embed_grad(index, stream, rd, ids.data_ptr(), it, n, scale, skip_id, rg, vocab, dim,
@@ -176,11 +183,13 @@ def act_load(act, out=None, dtype=torch.bfloat16):
     """The values of a checkpoint, exact in bfloat16 and in float32."""
     device = act.q.device
     index = _on(device, out)
+    n, dim = act.q.shape[0], act.dim
     if out is None:
-        out = torch.empty(act.rows, act.dim, dtype=dtype, device=device)
+        out = torch.empty((n, dim), dtype=dtype, device=device)
+    else:
+        _shaped(out, n, dim, "out")
     ro = _rows(out, "out")
-    _shaped(out, act.rows, act.dim, "out")
-    check(_abi.load().lc_act_load(index, _stream(index), act._c(), act.rows, act.dim, ro))
+    check(_abi.load().lc_act_load(index, _stream(index), act._c(), n, dim, ro))
     return out
 
 
@@ -203,13 +212,13 @@ def norm(x, weight, bias=None, eps=1e-5, kind="layer", out=None, keep=None):
     if keep is not None and (keep.rows != n or keep.dim != dim):
         raise ValueError("the checkpoint must have %d rows of %d" % (n, dim))
     if out is None:
-        out = torch.empty(n, dim, dtype=x.dtype, device=device)
+        out = torch.empty((n, dim), dtype=x.dtype, device=device)
+    else:
+        _shaped(out, n, dim, "out")
     ro = _rows(out, "out")
-    _shaped(out, n, dim, "out")
     layer = _KIND[kind] == LC_NORM_LAYER
-    stats = torch.empty(2 if layer else 1, n, dtype=torch.float32, device=device)
-    rstd = stats[0]
-    mean = stats[1] if layer else None
+    rstd = torch.empty(n, dtype=torch.float32, device=device)
+    mean = torch.empty(n, dtype=torch.float32, device=device) if layer else None
     check(_abi.load().lc_norm(index, _stream(index), _KIND[kind], rx, n, dim, w, b, _CODE[weight.dtype], eps, ro,
                               mean.data_ptr() if layer else None, rstd.data_ptr(),
                               None if keep is None else keep._c()))
@@ -236,13 +245,14 @@ def norm_grad(dy, x, weight, mean, rstd, bias=False, dx=None, dweight=None, dbia
     if accumulate and (dweight is None or (bias and dbias is None)):
         raise ValueError("accumulate needs the gradients to add to")
     if dx is None:
-        dx = torch.empty(n, dim, dtype=dy.dtype, device=device)
+        dx = torch.empty((n, dim), dtype=dy.dtype, device=device)
+    else:
+        _shaped(dx, n, dim, "dx")
     if dweight is None:
         dweight = torch.empty(dim, dtype=dbias.dtype if dbias is not None else dtype, device=device)
     if dbias is None and bias:
         dbias = torch.empty(dim, dtype=dweight.dtype, device=device)
     rdx = _rows(dx, "dx")
-    _shaped(dx, n, dim, "dx")
     pw = _param(dweight, dim, "dweight")
     pb = None if dbias is None else _param(dbias, dim, "dbias")
     if dbias is not None and dbias.dtype != dweight.dtype:
@@ -268,9 +278,10 @@ def weight_grad(dy, act, grad=None, dtype=torch.float32, accumulate=False):
     if grad is None:
         if accumulate:
             raise ValueError("accumulate needs grad")
-        grad = torch.empty(rows, act.dim, dtype=dtype, device=device)
+        grad = torch.empty((rows, act.dim), dtype=dtype, device=device)
+    else:
+        _shaped(grad, rows, act.dim, "grad")
     rg = _rows(grad, "grad")
-    _shaped(grad, rows, act.dim, "grad")
     lib, stream = _abi.load(), _stream(index)
     need = lib.lc_weight_grad_workspace(n, rows, act.dim, rd.dtype)
     check(lib.lc_weight_grad(index, stream, rd, act._c(), n, rows, act.dim, rg, 1 if accumulate else 0,
