@@ -20,78 +20,151 @@ struct ActParams {
     int8_t* q;
     int8_t* e;
     int64_t ntok, dim, blocks, x_pitch, q_pitch, e_pitch;
-    int64_t items, segs;  // items = ntok * segs
+    int64_t items, segs;  // items = ntok * segs (segments of a row)
 };
 
-// A warp keeps one block, four values a lane.  VEC: 4 consecutive values (8- or
-// 16-byte loads); otherwise every 32nd, element by element.
+constexpr int kUnroll = 4;   // vectors that a lane has in flight
+
+// A warp keeps a segment of a row.  VEC: kUnroll vectors of 16 bytes a lane, a
+// block in 128 / V neighbouring lanes; otherwise kUnroll blocks, a lane every 32nd
+// value of each.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(kActThreads) act_save_kernel(ActParams p) {
+    constexpr int V = VEC ? kVec<T> : 4, L = VEC ? LC_ACT_BLOCK / V : 32;
     const int lane = threadIdx.x & 31;
-    const int64_t step = int64_t(gridDim.x) * (kActThreads / 32);
-    for (int64_t item = int64_t(blockIdx.x) * (kActThreads / 32) + (threadIdx.x >> 5); item < p.items; item += step) {
-        const int64_t t = item / p.blocks, b = item - t * p.blocks;
-        const T* x = reinterpret_cast<const T*>(p.x + t * p.x_pitch);
-        const int64_t c0 = b * LC_ACT_BLOCK;
-        float f[4];
+    const int64_t item = int64_t(blockIdx.x) * (kActThreads / 32) + (threadIdx.x >> 5);
+    if (item >= p.items) return;
+    int64_t t, seg;
+    split_item(item, p.segs, t, seg);
+    const T* x = reinterpret_cast<const T*>(p.x + t * p.x_pitch);
+    int8_t* q = p.q + t * p.q_pitch;
+    const int64_t c0 = seg * (32 * V * kUnroll), padded = p.blocks * LC_ACT_BLOCK;
+    float f[kUnroll][V];
+    if constexpr (VEC) {
+        uint4 v[kUnroll];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int64_t c = c0 + (VEC ? lane * 4 + i : i * 32 + lane);
-            f[i] = c < p.dim ? to_f32(x[c]) : 0.0f;
+        for (int u = 0; u < kUnroll; ++u) {
+            const int64_t c = c0 + (u * 32 + lane) * V;
+            if (c + V <= p.dim) v[u] = ld_stream(x + c);
         }
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            const int64_t c = c0 + (u * 32 + lane) * V;
+            unpack(v[u], f[u]);
+            if (c + V > p.dim) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) f[u][i] = c + i < p.dim ? to_f32(x[c + i]) : 0.0f;
+            }
+        }
+    } else {
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u)
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const int64_t c = c0 + u * LC_ACT_BLOCK + i * 32 + lane;
+                f[u][i] = c < p.dim ? to_f32(x[c]) : 0.0f;
+            }
+    }
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
         float amax = 0.0f;
-        bool bad = false;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            amax = fmaxf(amax, fabsf(f[i]));
-            bad |= !(fabsf(f[i]) <= 3.402823466e38f);
-        }
+        for (int i = 0; i < V; ++i) amax = max_nan(amax, f[u][i]);
+        const int code = act_code(block_amax<L>(amax));
+        uint32_t w[V / 4];
+        act_bytes<V>(f[u], code, w);
+        const int64_t c = c0 + (VEC ? (u * 32 + lane) * V : u * LC_ACT_BLOCK);
+        if (c >= padded) break;
+        if constexpr (!VEC) {
 #pragma unroll
-        for (int o = 16; o; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-        bad = __any_sync(0xffffffffu, bad);
-        const int e = bad ? 127 : act_exponent(amax);
-        const float inv = bad ? 0.0f : act_inverse(e);
-        int8_t* q = p.q + t * p.q_pitch + c0;
-        int v[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = bad ? 0 : act_steps(f[i], inv);
-        if constexpr (VEC) {
-            *reinterpret_cast<uint32_t*>(q + lane * 4) =
-                uint32_t(v[0] & 255) | uint32_t(v[1] & 255) << 8 | uint32_t(v[2] & 255) << 16 | uint32_t(v[3]) << 24;
+            for (int i = 0; i < 4; ++i) q[c + i * 32 + lane] = int8_t(w[0] >> (8 * i));
+        } else if constexpr (V == 8) {
+            *reinterpret_cast<uint2*>(q + c) = make_uint2(w[0], w[1]);
         } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) q[i * 32 + lane] = int8_t(v[i]);
+            *reinterpret_cast<uint32_t*>(q + c) = w[0];
         }
-        if (lane == 0) p.e[t * p.e_pitch + b] = int8_t(e);
+        if (lane % L == 0) p.e[t * p.e_pitch + c / LC_ACT_BLOCK] = int8_t(code);
     }
 }
 
-// A thread gives 4 values.
+// A warp gives a segment of a row: kUnroll times 8 values a lane (VEC), or
+// kUnroll blocks, every 32nd value.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(kActThreads) act_load_kernel(ActParams p) {
+    constexpr int V = VEC ? 8 : 4;
     const int lane = threadIdx.x & 31;
-    const int64_t step = int64_t(gridDim.x) * (kActThreads / 32);
-    for (int64_t item = int64_t(blockIdx.x) * (kActThreads / 32) + (threadIdx.x >> 5); item < p.items; item += step) {
-        const int64_t t = item / p.blocks, b = item - t * p.blocks;
-        T* x = reinterpret_cast<T*>(const_cast<uint8_t*>(p.x) + t * p.x_pitch);
-        const int64_t c0 = b * LC_ACT_BLOCK;
-        const float s = act_scale(p.e[t * p.e_pitch + b]);
-        const int8_t* q = p.q + t * p.q_pitch + c0;
+    const int64_t item = int64_t(blockIdx.x) * (kActThreads / 32) + (threadIdx.x >> 5);
+    if (item >= p.items) return;
+    int64_t t, seg;
+    split_item(item, p.segs, t, seg);
+    T* x = reinterpret_cast<T*>(const_cast<uint8_t*>(p.x) + t * p.x_pitch);
+    const int8_t* q = p.q + t * p.q_pitch;
+    const int8_t* e = p.e + t * p.e_pitch;
+    const int64_t c0 = seg * (32 * V * kUnroll);
+    if constexpr (VEC) {
+        uint2 w[kUnroll];
+        int code[kUnroll];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int k = VEC ? lane * 4 + i : i * 32 + lane;
-            if (c0 + k < p.dim) x[c0 + k] = from_f32<T>(float(q[k]) * s);
+        for (int u = 0; u < kUnroll; ++u) {
+            const int64_t c = c0 + (u * 32 + lane) * V;
+            if (c >= p.dim) break;
+            w[u] = __ldcs(reinterpret_cast<const uint2*>(q + c));   // a row ends with a whole block
+            code[u] = e[c / LC_ACT_BLOCK];
+        }
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            const int64_t c = c0 + (u * 32 + lane) * V;
+            if (c >= p.dim) break;
+            const uint32_t s = act_scale2(code[u]);
+            const uint2 a = act_values(w[u].x, s), b = act_values(w[u].y, s);
+            const uint4 v = make_uint4(a.x, a.y, b.x, b.y);
+            if (c + V <= p.dim) {
+                if constexpr (sizeof(T) == 2) {
+                    st_stream(x + c, v);
+                } else {
+                    float f[8];
+                    unpack(v, f);
+                    st_stream(x + c, make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])));
+                    st_stream(x + c + 4, make_uint4(__float_as_uint(f[4]), __float_as_uint(f[5]), __float_as_uint(f[6]), __float_as_uint(f[7])));
+                }
+            } else {
+                float f[8];
+                unpack(v, f);
+#pragma unroll
+                for (int i = 0; i < V; ++i)
+                    if (c + i < p.dim) x[c + i] = from_f32<T>(f[i]);
+            }
+        }
+    } else {
+        int v[kUnroll][V], code[kUnroll];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            const int64_t c = c0 + u * LC_ACT_BLOCK;
+            if (c >= p.dim) break;
+            code[u] = e[c / LC_ACT_BLOCK];
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[u][i] = q[c + i * 32 + lane];
+        }
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            const int64_t c = c0 + u * LC_ACT_BLOCK + lane;
+            const float s = act_scale(code[u]);
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                if (c + i * 32 < p.dim) x[c + i * 32] = from_f32<T>(float(v[u][i]) * s);
         }
     }
 }
 
+// `per`: values of a segment.
 template <typename K>
-cudaError_t launch_act(K kernel, ActParams p, int sms, cudaStream_t s) {
-    p.items = p.ntok * p.blocks;
-    const int64_t want = (p.items + kActThreads / 32 - 1) / (kActThreads / 32);
-    const int64_t most = int64_t(sms) * 256;
+cudaError_t launch_act(K kernel, ActParams p, int64_t per, cudaStream_t s) {
+    p.segs = (p.dim + per - 1) / per;
+    p.items = p.ntok * p.segs;
+    const int64_t grid = (p.items + kActThreads / 32 - 1) / (kActThreads / 32);
+    if (grid > 0x7fffffff) return cudaErrorInvalidValue;
     cudaGetLastError();
-    kernel<<<unsigned(want < most ? want : most), kActThreads, 0, s>>>(p);
+    kernel<<<unsigned(grid), kActThreads, 0, s>>>(p);
     return cudaGetLastError();
 }
 
@@ -125,13 +198,15 @@ lc_status check(const char* call, int device, const lc_rows* x, const char* name
 
 }  // namespace
 
-cudaError_t act_save_rows(const lc_rows* x, const lc_act* a, int64_t ntok, int64_t dim, int sms, cudaStream_t s) {
+cudaError_t act_save_rows(const lc_rows* x, const lc_act* a, int64_t ntok, int64_t dim, cudaStream_t s) {
     const ActParams p = act_params(x, a, ntok, dim);
     const bool vec = aligned16(x->data) && p.x_pitch % 16 == 0;
+    using B = __nv_bfloat16;
     if (x->dtype == LC_BF16)
-        return vec ? launch_act(act_save_kernel<__nv_bfloat16, true>, p, sms, s)
-                   : launch_act(act_save_kernel<__nv_bfloat16, false>, p, sms, s);
-    return vec ? launch_act(act_save_kernel<float, true>, p, sms, s) : launch_act(act_save_kernel<float, false>, p, sms, s);
+        return vec ? launch_act(act_save_kernel<B, true>, p, 32 * 8 * kUnroll, s)
+                   : launch_act(act_save_kernel<B, false>, p, 32 * 4 * kUnroll, s);
+    return vec ? launch_act(act_save_kernel<float, true>, p, 32 * 4 * kUnroll, s)
+               : launch_act(act_save_kernel<float, false>, p, 32 * 4 * kUnroll, s);
 }
 
 }  // namespace lc
@@ -145,8 +220,7 @@ extern "C" lc_status lc_act_save(int device, void* cuda_stream, const lc_rows* x
     const lc_status st = check("lc_act_save", device, x, "x", act, ntok, dim, true);
     if (st != LC_OK || ntok == 0) return st;
     if (!cur.ok) return fail_status(LC_ERR_CUDA, "lc_act_save: cannot make device %d current", device);
-    return ops_launched("lc_act_save",
-                        act_save_rows(x, act, ntok, dim, ops_sm_count(device), static_cast<cudaStream_t>(cuda_stream)));
+    return ops_launched("lc_act_save", act_save_rows(x, act, ntok, dim, static_cast<cudaStream_t>(cuda_stream)));
 }
 
 extern "C" lc_status lc_act_load(int device, void* cuda_stream, const lc_act* act, int64_t ntok, int64_t dim,
@@ -157,14 +231,15 @@ extern "C" lc_status lc_act_load(int device, void* cuda_stream, const lc_act* ac
     if (st != LC_OK || ntok == 0) return st;
     if (!cur.ok) return fail_status(LC_ERR_CUDA, "lc_act_load: cannot make device %d current", device);
     const ActParams p = act_params(y, act, ntok, dim);
-    const int sms = ops_sm_count(device);
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     const bool vec = aligned16(y->data) && p.x_pitch % 16 == 0;
+    using B = __nv_bfloat16;
     cudaError_t e;
     if (y->dtype == LC_BF16)
-        e = vec ? launch_act(act_load_kernel<__nv_bfloat16, true>, p, sms, s)
-                : launch_act(act_load_kernel<__nv_bfloat16, false>, p, sms, s);
+        e = vec ? launch_act(act_load_kernel<B, true>, p, 32 * 8 * kUnroll, s)
+                : launch_act(act_load_kernel<B, false>, p, 32 * 4 * kUnroll, s);
     else
-        e = vec ? launch_act(act_load_kernel<float, true>, p, sms, s) : launch_act(act_load_kernel<float, false>, p, sms, s);
+        e = vec ? launch_act(act_load_kernel<float, true>, p, 32 * 8 * kUnroll, s)
+                : launch_act(act_load_kernel<float, false>, p, 32 * 4 * kUnroll, s);
     return ops_launched("lc_act_load", e);
 }

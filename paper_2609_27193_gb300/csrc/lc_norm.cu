@@ -170,33 +170,17 @@ __global__ void __launch_bounds__(cta_threads(G)) norm_kernel(NormParams p) {
 #pragma unroll
                 for (int i = 0; i < VPT; ++i) {
                     float amax = 0.0f;
-                    bool bad = false;
 #pragma unroll
-                    for (int j = 0; j < V; ++j) {
-                        amax = fmaxf(amax, fabsf(f[i][j]));
-                        bad |= !(fabsf(f[i][j]) <= 3.402823466e38f);
-                    }
-                    float key = bad ? __uint_as_float(0x7f800000u) : amax;
-#pragma unroll
-                    for (int o = L / 2; o; o >>= 1) key = fmaxf(key, __shfl_xor_sync(0xffffffffu, key, o));
-                    bad = key > 3.402823466e38f;
-                    const int e = bad ? 127 : act_exponent(key);
-                    const float inv = bad ? 0.0f : act_inverse(e);
+                    for (int j = 0; j < V; ++j) amax = max_nan(amax, f[i][j]);
+                    const int code = act_code(block_amax<L>(amax));
                     const int c = column<V, G, VPT, VEC>(t, i, 0);
                     if (c < (p.dim + LC_ACT_BLOCK - 1) / LC_ACT_BLOCK * LC_ACT_BLOCK) {
                         uint32_t w[V / 4];
-#pragma unroll
-                        for (int j = 0; j < V; j += 4) {
-                            uint32_t v = 0;
-#pragma unroll
-                            for (int k = 0; k < 4; ++k)
-                                v |= uint32_t((bad ? 0 : act_steps(f[i][j + k], inv)) & 255) << (8 * k);
-                            w[j / 4] = v;
-                        }
+                        act_bytes<V>(f[i], code, w);
                         int8_t* q = p.q + r * p.q_pitch + c;
                         if constexpr (V == 8) *reinterpret_cast<uint2*>(q) = make_uint2(w[0], w[1]);
                         else *reinterpret_cast<uint32_t*>(q) = w[0];
-                        if (c % LC_ACT_BLOCK == 0) p.e[r * p.e_pitch + c / LC_ACT_BLOCK] = int8_t(e);
+                        if (c % LC_ACT_BLOCK == 0) p.e[r * p.e_pitch + c / LC_ACT_BLOCK] = int8_t(code);
                     }
                 }
             }
@@ -542,7 +526,7 @@ extern "C" lc_status lc_norm(int device, void* cuda_stream, int32_t kind, const 
         p.e_pitch = keep->e_stride;
     } else if (keep) {
         // rows off 16 bytes: a lane's columns are not one block's, so the checkpoint has a pass of its own
-        const cudaError_t err = act_save_rows(x, keep, ntok, dim, sms, s);
+        const cudaError_t err = act_save_rows(x, keep, ntok, dim, s);
         if (err != cudaSuccess) return ops_launched(call, err);
     }
     cudaError_t err;

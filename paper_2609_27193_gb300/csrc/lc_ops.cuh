@@ -58,7 +58,7 @@ lc_status ops_check_act(const char* call, const lc_act* a, int64_t rows, int64_t
 lc_status ops_launched(const char* call, cudaError_t e);
 
 // Keeps rows in 8 bits (the norm uses it where it cannot do so on its own pass).
-cudaError_t act_save_rows(const lc_rows* x, const lc_act* a, int64_t ntok, int64_t dim, int sms, cudaStream_t s);
+cudaError_t act_save_rows(const lc_rows* x, const lc_act* a, int64_t ntok, int64_t dim, cudaStream_t s);
 
 inline Span2 span_of(const char* name, const lc_rows* r, int64_t rows, int64_t dim, bool out) {
     const int e = elem_size(r->dtype);
@@ -134,14 +134,69 @@ __device__ __forceinline__ int act_exponent(float amax) {
     const int e = int(b >> 23) - 127 - 6 + ((b & 0x7fffffu) > 0x7e0000u ? 1 : 0);
     return e < -126 ? -126 : e > 121 ? 121 : e;
 }
-// A value in steps of its block (inv = 2^-e), to nearest even; 128 only where e
-// stopped at 121.
-__device__ __forceinline__ int act_steps(float x, float inv) {
-    const int q = __float2int_rn(x * inv);
-    return q > 127 ? 127 : q < -127 ? -127 : q;
-}
 // 2^-e for e in [-126, 121].
 __device__ __forceinline__ float act_inverse(int e) { return __uint_as_float(uint32_t(127 - e) << 23); }
+// The larger magnitude, NaN if either is.
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(fabsf(b)));
+    return r;
+}
+// Largest magnitude of a block that N neighbouring lanes hold, for all of them.
+template <int N>
+__device__ __forceinline__ float block_amax(float amax) {
+#pragma unroll
+    for (int o = N / 2; o; o >>= 1) amax = max_nan(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+    return amax;
+}
+// Exponent that is stored for a block whose largest magnitude is amax: 127 if that is not finite.
+__device__ __forceinline__ int act_code(float amax) { return amax <= 3.402823466e38f ? act_exponent(amax) : 127; }
+// V values in steps of 2^e, to nearest even, as bytes.  x * 2^-e + 1.5 * 2^23 is
+// rounded to a whole number by the addition (the product is exact), whose low byte
+// is the step in two's complement.  128 steps occur only where e stopped at 121.
+template <int V>
+__device__ __forceinline__ void act_bytes(const float (&f)[V], int code, uint32_t (&w)[V / 4]) {
+    const float inv = act_inverse(code == 127 ? 0 : code);
+#pragma unroll
+    for (int i = 0; i < V; i += 4) {
+        uint32_t q[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            float x = f[i + k];
+            if (code == 121) x = fminf(fmaxf(x, -127.0f * 0x1p121f), 127.0f * 0x1p121f);
+            q[k] = __float_as_uint(fmaf(x, inv, 12582912.0f));
+        }
+        w[i / 4] = code == 127 ? 0u : __byte_perm(__byte_perm(q[0], q[1], 0x0040), __byte_perm(q[2], q[3], 0x0040), 0x5410);
+    }
+}
+// A block's scale as bf16 in both halves: the upper half of the fp32 number.
+__device__ __forceinline__ uint32_t act_scale2(int code) { return (code == 127 ? 0x7fffu : uint32_t(code + 127) << 7) * 0x10001u; }
+// Two values of the checkpoint (bytes 0 and 2 of `q`; the others are ignored) as
+// bf16, times their scale.  A byte's low seven bits go into the fraction of 128;
+// 128, or 256 for a negative one, comes off again: exact, as is the product with a
+// power of two.
+__device__ __forceinline__ uint32_t act_pair(uint32_t q, uint32_t scale) {
+    const uint32_t v = (q & 0x007f007fu) | 0x43004300u, c = (q & 0x00800080u) | 0x43004300u;
+    __nv_bfloat162 d = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&v), *reinterpret_cast<const __nv_bfloat162*>(&c));
+    d = __hmul2(d, *reinterpret_cast<const __nv_bfloat162*>(&scale));
+    return *reinterpret_cast<const uint32_t*>(&d);
+}
+// The four values of a word, in order.
+__device__ __forceinline__ uint2 act_values(uint32_t q, uint32_t scale) {
+    return make_uint2(act_pair(__byte_perm(q, 0, 0x4140), scale), act_pair(__byte_perm(q, 0, 0x4342), scale));
+}
+// item / parts and the rest; 32 bits wide where that is enough (a 64-bit division
+// is a few times the length).
+__device__ __forceinline__ void split_item(int64_t item, int64_t parts, int64_t& row, int64_t& part) {
+    if (((item | parts) >> 32) == 0) {
+        const uint32_t r = uint32_t(item) / uint32_t(parts);
+        row = r;
+        part = uint32_t(item) - r * uint32_t(parts);
+    } else {
+        row = item / parts;
+        part = item - row * parts;
+    }
+}
 #endif
 
 }  // namespace lc

@@ -138,16 +138,6 @@ __device__ __forceinline__ void cluster_barrier() {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-// Two values of the checkpoint (bytes 0 and 2 of `q`; the others are ignored) as
-// bf16, times their scale.  A byte's low seven bits go into the fraction of 128;
-// 128, or 256 for a negative one, comes off again: exact, as is the product with a
-// power of two.
-__device__ __forceinline__ uint32_t act_pair(uint32_t q, uint32_t scale) {
-    const uint32_t v = (q & 0x007f007fu) | 0x43004300u, c = (q & 0x00800080u) | 0x43004300u;
-    __nv_bfloat162 d = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&v), *reinterpret_cast<const __nv_bfloat162*>(&c));
-    d = __hmul2(d, *reinterpret_cast<const __nv_bfloat162*>(&scale));
-    return *reinterpret_cast<const uint32_t*>(&d);
-}
 // Bytes 0 and 2 of a word make one pair and bytes 1 and 3 the other, which spares
 // the permutations that neighbours would need: of every four features of the
 // operand the middle two have changed places.
