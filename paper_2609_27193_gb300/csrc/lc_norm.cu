@@ -9,6 +9,13 @@
 // same columns, so the gradients of weight and bias stay in its registers over all
 // its rows.  Each CTA leaves one fp32 row of sums of them, and a second kernel adds
 // those rows in order: two levels, no atomics, the same bits every time.
+//
+// Rows whose addresses and length are multiples of 16 bytes (and enough of them)
+// stream through shared memory: every group of threads has a ring of rows there, the
+// next ones on their way by bulk copies while it works on one.  In registers as many
+// bytes in flight would leave no room for the work: 16384 rows of 4096 bf16 through
+// a root-mean-square norm 79 us that way, 45 so, their backward from the checkpoint 109 us and 73.
+#include "lc_bulk.cuh"
 #include "lc_ops.cuh"
 
 namespace lc {
@@ -52,15 +59,22 @@ __device__ __forceinline__ int column(int t, int i, int j) {
     return VEC ? (i * G + t) * V + j : (i * V + j) * G + t;
 }
 
+// The thread's part of a row.  All vectors are asked for before the first is
+// unpacked: in one loop each would be waited for in turn.
 template <typename T, int G, int VPT, bool VEC>
 __device__ __forceinline__ void load_row(const uint8_t* row, int t, int dim, float (&f)[VPT][kVec<T>]) {
     constexpr int V = kVec<T>;
     const T* r = reinterpret_cast<const T*>(row);
+    uint4 raw[VPT];
+    if constexpr (VEC) {
+#pragma unroll
+        for (int i = 0; i < VPT; ++i)
+            if (column<V, G, VPT, VEC>(t, i, 0) + V <= dim) raw[i] = ld_stream(r + column<V, G, VPT, VEC>(t, i, 0));
+    }
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
-        if (VEC && column<V, G, VPT, VEC>(t, i, 0) + V <= dim) {
-            unpack(ld_stream(r + column<V, G, VPT, VEC>(t, i, 0)), f[i]);
-        } else {
+        if constexpr (VEC) unpack(raw[i], f[i]);
+        if (!VEC || column<V, G, VPT, VEC>(t, i, 0) + V > dim) {
 #pragma unroll
             for (int j = 0; j < V; ++j) {
                 const int c = column<V, G, VPT, VEC>(t, i, j);
@@ -70,20 +84,18 @@ __device__ __forceinline__ void load_row(const uint8_t* row, int t, int dim, flo
     }
 }
 
+// The i-th of the thread's vectors of a row.
 template <typename T, int G, int VPT, bool VEC>
-__device__ __forceinline__ void store_row(uint8_t* row, int t, int dim, const float (&f)[VPT][kVec<T>]) {
+__device__ __forceinline__ void store_vec(uint8_t* row, int t, int i, int dim, const float (&f)[kVec<T>]) {
     constexpr int V = kVec<T>;
     T* r = reinterpret_cast<T*>(row);
+    if (VEC && column<V, G, VPT, VEC>(t, i, 0) + V <= dim) {
+        st_stream(r + column<V, G, VPT, VEC>(t, i, 0), pack(f));
+    } else {
 #pragma unroll
-    for (int i = 0; i < VPT; ++i) {
-        if (VEC && column<V, G, VPT, VEC>(t, i, 0) + V <= dim) {
-            st_stream(r + column<V, G, VPT, VEC>(t, i, 0), pack(f[i]));
-        } else {
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                const int c = column<V, G, VPT, VEC>(t, i, j);
-                if (c < dim) r[c] = from_f32<T>(f[i][j]);
-            }
+        for (int j = 0; j < V; ++j) {
+            const int c = column<V, G, VPT, VEC>(t, i, j);
+            if (c < dim) r[c] = from_f32<T>(f[j]);
         }
     }
 }
@@ -124,9 +136,18 @@ __device__ __forceinline__ void load_param(const uint8_t* p, bool bf16, int t, i
     }
 }
 
+// The threads of a group meet.  NT: threads of its CTA; several groups have a
+// barrier each, besides the CTA's own (0) where the sixteen that there are suffice.
+template <int G, int NT>
+__device__ __forceinline__ void group_barrier() {
+    if constexpr (G == 32) __syncwarp();
+    else if constexpr (NT == G) __syncthreads();
+    else asm volatile("bar.sync %0, %1;" ::"r"(int(threadIdx.x) / G + (NT / G < 16 ? 1 : 0)), "n"(G) : "memory");
+}
+
 // Sum over the group's G threads; every thread gets it.  `slot` alternates, so one
 // barrier a sum is enough.
-template <int G, int N>
+template <int G, int NT, int N>
 __device__ __forceinline__ void group_sum(float (&v)[N], float (*shared)[32][N], int& slot) {
 #pragma unroll
     for (int k = 0; k < N; ++k)
@@ -138,12 +159,13 @@ __device__ __forceinline__ void group_sum(float (&v)[N], float (*shared)[32][N],
 #pragma unroll
             for (int k = 0; k < N; ++k) shared[slot][warp][k] = v[k];
         }
-        __syncthreads();
+        group_barrier<G, NT>();
+        const int w0 = NT == G ? 0 : int(threadIdx.x) / G * (G / 32);
 #pragma unroll
         for (int k = 0; k < N; ++k) {
             float s = 0.0f;
 #pragma unroll
-            for (int w = 0; w < G / 32; ++w) s += shared[slot][w][k];
+            for (int w = 0; w < G / 32; ++w) s += shared[slot][w0 + w][k];
             v[k] = s;
         }
         slot ^= 1;
@@ -192,28 +214,41 @@ __global__ void __launch_bounds__(cta_threads(G)) norm_kernel(NormParams p) {
             for (int i = 0; i < VPT; ++i)
 #pragma unroll
                 for (int j = 0; j < V; ++j) s[0] += f[i][j];
-            group_sum<G>(s, shared, slot);
+            group_sum<G, cta_threads(G)>(s, shared, slot);
             mean = s[0] * p.inv_dim;
             s[0] = 0.0f;
         }
 #pragma unroll
-        for (int i = 0; i < VPT; ++i)
+        for (int i = 0; i < VPT; ++i) {
+            if (!VEC || column<V, G, VPT, VEC>(t, i, 0) + V > p.dim) {
+                // what lies beyond the row is at the mean
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+                    if (column<V, G, VPT, VEC>(t, i, j) >= p.dim) f[i][j] = mean;
+            }
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                const float d = f[i][j] - mean;
-                if (column<V, G, VPT, VEC>(t, i, j) < p.dim) s[0] += d * d;
+                f[i][j] -= mean;
+                s[0] = fmaf(f[i][j], f[i][j], s[0]);
             }
-        group_sum<G>(s, shared, slot);
+        }
+        group_sum<G, cta_threads(G)>(s, shared, slot);
         const float rstd = rsqrtf(s[0] * p.inv_dim + p.eps);
+        uint8_t* y = p.y + r * p.y_pitch;
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
-            float w[V], b[V];
+            if (VEC && column<V, G, VPT, VEC>(t, i, 0) >= p.dim) break;
+            float w[V];
             load_param<V, G, VPT, VEC>(p.w, p.w_bf16, t, i, p.dim, w);
-            if (p.b) load_param<V, G, VPT, VEC>(p.b, p.w_bf16, t, i, p.dim, b);
 #pragma unroll
-            for (int j = 0; j < V; ++j) f[i][j] = (f[i][j] - mean) * rstd * w[j] + (p.b ? b[j] : 0.0f);
+            for (int j = 0; j < V; ++j) f[i][j] *= rstd * w[j];
+            if (p.b) {
+                load_param<V, G, VPT, VEC>(p.b, p.w_bf16, t, i, p.dim, w);
+#pragma unroll
+                for (int j = 0; j < V; ++j) f[i][j] += w[j];
+            }
+            store_vec<T, G, VPT, VEC>(y, t, i, p.dim, f[i]);
         }
-        store_row<T, G, VPT, VEC>(p.y + r * p.y_pitch, t, p.dim, f);
         if (t == 0) {
             if (!p.rms) p.mean[r] = mean;
             p.rstd[r] = rstd;
@@ -249,22 +284,37 @@ __global__ void __launch_bounds__(cta_threads(G)) norm_grad_kernel(NormGradParam
         if constexpr (KEPT) {
             const int8_t* q = p.q + r * p.q_pitch;
             const int8_t* ex = p.e + r * p.e_pitch;
+            uint32_t w[VPT][V / 4];
+            int code[VPT];
+            if constexpr (VEC) {
+                // V values of one block; a row ends with a whole block
+#pragma unroll
+                for (int i = 0; i < VPT; ++i) {
+                    const int c = column<V, G, VPT, VEC>(t, i, 0);
+                    w[i][0] = code[i] = 0;
+                    if (c >= p.dim) continue;
+                    if constexpr (V == 8) {
+                        const uint2 v = __ldcs(reinterpret_cast<const uint2*>(q + c));
+                        w[i][0] = v.x;
+                        w[i][1] = v.y;
+                    } else {
+                        w[i][0] = __ldcs(reinterpret_cast<const uint32_t*>(q + c));
+                    }
+                    code[i] = ex[c / LC_ACT_BLOCK];
+                }
+            }
 #pragma unroll
             for (int i = 0; i < VPT; ++i) {
-                const int c0 = column<V, G, VPT, VEC>(t, i, 0);
-                if (VEC && c0 + V <= p.dim) {
-                    // V values of one block
-                    const float s = act_scale(ex[c0 / LC_ACT_BLOCK]);
-                    uint32_t w[V / 4];
-                    if constexpr (V == 8) {
-                        const uint2 v = __ldg(reinterpret_cast<const uint2*>(q + c0));
-                        w[0] = v.x;
-                        w[1] = v.y;
-                    } else {
-                        w[0] = __ldg(reinterpret_cast<const uint32_t*>(q + c0));
-                    }
+                if constexpr (VEC) {
+                    const uint32_t s2 = act_scale2(code[i]);
 #pragma unroll
-                    for (int j = 0; j < V; ++j) h[i][j] = float(int8_t(w[j / 4] >> (8 * (j % 4)))) * s;
+                    for (int j = 0; j < V; j += 4) {
+                        const uint2 v = act_values(w[i][j / 4], s2);
+                        h[i][j] = __uint_as_float(v.x << 16);
+                        h[i][j + 1] = __uint_as_float(v.x & 0xffff0000u);
+                        h[i][j + 2] = __uint_as_float(v.y << 16);
+                        h[i][j + 3] = __uint_as_float(v.y & 0xffff0000u);
+                    }
                 } else {
 #pragma unroll
                     for (int j = 0; j < V; ++j) {
@@ -297,14 +347,15 @@ __global__ void __launch_bounds__(cta_threads(G)) norm_grad_kernel(NormGradParam
                 s[1] += g[i][j] * h[i][j];
             }
         }
-        group_sum<G>(s, shared, slot);
+        group_sum<G, cta_threads(G)>(s, shared, slot);
         if (p.dx) {
             const float m1 = p.rms ? 0.0f : s[0] * p.inv_dim, m2 = s[1] * p.inv_dim;
 #pragma unroll
             for (int i = 0; i < VPT; ++i)
 #pragma unroll
                 for (int j = 0; j < V; ++j) g[i][j] = rstd * (g[i][j] - m1 - h[i][j] * m2);
-            store_row<T, G, VPT, VEC>(p.dx + r * p.dx_pitch, t, p.dim, g);
+#pragma unroll
+            for (int i = 0; i < VPT; ++i) store_vec<T, G, VPT, VEC>(p.dx + r * p.dx_pitch, t, i, p.dim, g[i]);
         }
     }
     dependents_may_start();
@@ -347,6 +398,359 @@ __global__ void __launch_bounds__(cta_threads(G)) norm_grad_kernel(NormGradParam
         }
 }
 
+// --- rows through shared memory ---------------------------------------------------
+
+constexpr int kRingMax = 8;               // rows that a group has in flight at most
+constexpr size_t kRingSmem = 224 * 1024;  // of a CTA, with the barriers and sums that are not dynamic
+
+// A group's ring: `depth` rows of `bytes`, filled by the group's first thread.
+struct RowRing {
+    uint32_t data, bar;      // shared-memory addresses of this group's part
+    uint32_t bytes;
+    int depth, at = 0;
+    uint32_t round = 0;
+    __device__ __forceinline__ uint32_t row() const { return data + at * bytes; }
+    __device__ __forceinline__ uint32_t full() const { return bar + at * 8; }
+    __device__ __forceinline__ void next() {
+        if (++at == depth) {
+            at = 0;
+            round ^= 1;
+        }
+    }
+};
+
+__device__ __forceinline__ uint4 lds128(uint32_t addr) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+
+// The group's wait for its row.  After a wait that ran out nothing is waited for any
+// more: every row that follows becomes NaN, and the groups still meet at their
+// barriers.
+__device__ __forceinline__ bool ring_wait(const RowRing& ring, volatile uint32_t* failed) {
+    if (*failed) return false;
+    if (mbar_wait_warp(ring.full(), ring.round)) return true;
+    *failed = 1;
+    return false;
+}
+
+// After a wait that ran out: what is still on its way lands before the memory is given back.
+__device__ __forceinline__ void ring_drain(const RowRing& ring, uint32_t failed, int t) {
+    if (!failed || t) return;
+    for (int i = 0; i < ring.depth; ++i) mbar_wait_bounded(ring.bar + 8 * i, i < ring.at ? ring.round ^ 1 : ring.round, kDrainNs);
+}
+
+// Weight or bias as fp32 in the order in which the threads of a group take them:
+// [VPT * V / 4][G] of four.
+template <int V, int G, int VPT>
+__device__ __forceinline__ void stage_param(float4* out, const uint8_t* p, bool bf16, int dim, int threads) {
+    for (int k = threadIdx.x; k < VPT * V / 4 * G; k += threads) {
+        const int c = (k / G / (V / 4) * G + k % G) * V + k / G % (V / 4) * 4;
+        float w[4];
+#pragma unroll
+        for (int m = 0; m < 4; ++m)
+            w[m] = c + m >= dim ? 0.0f
+                   : bf16       ? to_f32(reinterpret_cast<const __nv_bfloat16*>(p)[c + m])
+                                : reinterpret_cast<const float*>(p)[c + m];
+        out[k] = make_float4(w[0], w[1], w[2], w[3]);
+    }
+}
+
+constexpr int fwd_threads(int G) { return 1024; }
+
+template <typename T, int G, int VPT>
+__global__ void __launch_bounds__(fwd_threads(G), 1) norm_ring_kernel(NormParams p, int depth) {
+    constexpr int V = kVec<T>, NT = fwd_threads(G), R = NT / G;
+    extern __shared__ __align__(128) uint8_t smem[];
+    __shared__ float shared[2][32][1];
+    __shared__ __align__(8) uint64_t bars[R * kRingMax];
+    __shared__ volatile uint32_t failed;
+    int slot = 0;
+    const int t = threadIdx.x % G, group = threadIdx.x / G;
+    float4* params = reinterpret_cast<float4*>(smem);
+    constexpr int kParam = VPT * V / 4 * G;
+    RowRing ring;
+    ring.bytes = uint32_t(p.dim) * uint32_t(sizeof(T));
+    ring.depth = depth;
+    ring.data = smem_addr(smem) + kParam * 16 * (p.b ? 2 : 1) + group * depth * ring.bytes;
+    ring.bar = smem_addr(bars) + group * kRingMax * 8;
+    if (threadIdx.x < R * kRingMax) {
+        mbar_init(smem_addr(bars) + 8 * threadIdx.x, 1);
+        mbar_init_fence();
+    }
+    if (threadIdx.x == 0) failed = 0;
+    __syncthreads();
+    // rows of the group: consecutive ones go to different CTAs
+    const int64_t step = int64_t(gridDim.x) * R;
+    int64_t r = int64_t(group) * gridDim.x + blockIdx.x;
+    int64_t ahead = r;           // first row not asked for
+    if (t == 0)
+        for (int i = 0; i < depth && ahead < p.ntok; ++i, ahead += step) {
+            mbar_expect_tx(ring.bar + 8 * i, ring.bytes);
+            bulk_g2s(ring.data + i * ring.bytes, p.x + ahead * p.x_pitch, ring.bytes, ring.bar + 8 * i);
+        }
+    stage_param<V, G, VPT>(params, p.w, p.w_bf16, p.dim, NT);
+    if (p.b) stage_param<V, G, VPT>(params + kParam, p.b, p.w_bf16, p.dim, NT);
+    __syncthreads();
+    for (; r < p.ntok; r += step) {
+        const bool ok = ring_wait(ring, &failed);
+        float f[VPT][V];
+#pragma unroll
+        for (int i = 0; i < VPT; ++i) {
+            const int c = (i * G + t) * V;
+            if (c < p.dim) {
+                unpack(lds128(ring.row() + c * int(sizeof(T))), f[i]);
+                if (!ok) f[i][0] = __uint_as_float(0x7fffffffu);
+            } else {
+#pragma unroll
+                for (int j = 0; j < V; ++j) f[i][j] = 0.0f;
+            }
+        }
+        // the row has been read by all once they met in a sum
+        auto refill = [&]() {
+            if (t == 0 && ahead < p.ntok && !failed) {
+                mbar_expect_tx(ring.full(), ring.bytes);
+                bulk_g2s(ring.row(), p.x + ahead * p.x_pitch, ring.bytes, ring.full());
+            }
+            ahead += step;
+            ring.next();
+        };
+        if (p.q) {
+            constexpr int L = LC_ACT_BLOCK / V;
+#pragma unroll
+            for (int i = 0; i < VPT; ++i) {
+                float amax = 0.0f;
+#pragma unroll
+                for (int j = 0; j < V; ++j) amax = max_nan(amax, f[i][j]);
+                const int code = act_code(block_amax<L>(amax));
+                const int c = (i * G + t) * V;
+                if (c < (p.dim + LC_ACT_BLOCK - 1) / LC_ACT_BLOCK * LC_ACT_BLOCK) {
+                    uint32_t w[V / 4];
+                    act_bytes<V>(f[i], code, w);
+                    int8_t* q = p.q + r * p.q_pitch + c;
+                    if constexpr (V == 8) *reinterpret_cast<uint2*>(q) = make_uint2(w[0], w[1]);
+                    else *reinterpret_cast<uint32_t*>(q) = w[0];
+                    if (c % LC_ACT_BLOCK == 0) p.e[r * p.e_pitch + c / LC_ACT_BLOCK] = int8_t(code);
+                }
+            }
+        }
+        float s[1] = {0.0f};
+        float mean = 0.0f;
+        float part[4] = {};          // short chains
+        if (!p.rms) {
+#pragma unroll
+            for (int i = 0; i < VPT; ++i)
+#pragma unroll
+                for (int j = 0; j < V; ++j) part[j & 3] += f[i][j];
+            s[0] = (part[0] + part[1]) + (part[2] + part[3]);
+            group_sum<G, NT>(s, shared, slot);
+            refill();
+            mean = s[0] * p.inv_dim;
+            part[0] = part[1] = part[2] = part[3] = 0.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < VPT; ++i) {
+            if ((i * G + t) * V >= p.dim) break;
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                f[i][j] -= mean;
+                part[j & 3] = fmaf(f[i][j], f[i][j], part[j & 3]);
+            }
+        }
+        s[0] = (part[0] + part[1]) + (part[2] + part[3]);
+        group_sum<G, NT>(s, shared, slot);
+        if (p.rms) refill();
+        const float rstd = rsqrtf(s[0] * p.inv_dim + p.eps);
+        T* y = reinterpret_cast<T*>(p.y + r * p.y_pitch);
+#pragma unroll
+        for (int i = 0; i < VPT; ++i) {
+            const int c = (i * G + t) * V;
+            if (c >= p.dim) break;
+#pragma unroll
+            for (int j = 0; j < V; j += 4) {
+                const float4 w = params[(i * (V / 4) + j / 4) * G + t];
+                float4 b = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                if (p.b) b = params[kParam + (i * (V / 4) + j / 4) * G + t];
+                f[i][j] = fmaf(f[i][j], rstd * w.x, b.x);
+                f[i][j + 1] = fmaf(f[i][j + 1], rstd * w.y, b.y);
+                f[i][j + 2] = fmaf(f[i][j + 2], rstd * w.z, b.z);
+                f[i][j + 3] = fmaf(f[i][j + 3], rstd * w.w, b.w);
+            }
+            st_stream(y + c, pack(f[i]));
+        }
+        if (t == 0) {
+            if (!p.rms) p.mean[r] = mean;
+            p.rstd[r] = rstd;
+        }
+    }
+    ring_drain(ring, failed, t);
+}
+
+constexpr int bwd_threads(int G) { return 512; }
+
+// The backward.  A slot holds the rows of dy and of x (or its 8-bit values; their
+// exponents are asked for a row ahead into registers).
+template <typename T, int G, int VPT, bool KEPT>
+__global__ void __launch_bounds__(bwd_threads(G), 1) norm_grad_ring_kernel(NormGradParams p, int depth) {
+    constexpr int V = kVec<T>, NT = bwd_threads(G), R = NT / G;
+    extern __shared__ __align__(128) uint8_t smem[];
+    __shared__ float shared[2][32][2];
+    __shared__ __align__(8) uint64_t bars[R * kRingMax];
+    __shared__ volatile uint32_t failed;
+    dependents_may_start();
+    int slot = 0;
+    const int t = threadIdx.x % G, group = threadIdx.x / G;
+    float4* params = reinterpret_cast<float4*>(smem);
+    constexpr int kParam = VPT * V / 4 * G;
+    const uint32_t dy_bytes = uint32_t(p.dim) * uint32_t(sizeof(T));
+    const uint32_t x_bytes = KEPT ? uint32_t(p.dim + LC_ACT_BLOCK - 1) / LC_ACT_BLOCK * LC_ACT_BLOCK : dy_bytes;
+    RowRing ring;
+    ring.bytes = dy_bytes + x_bytes;
+    ring.depth = depth;
+    ring.data = smem_addr(smem) + kParam * 16 + group * depth * ring.bytes;
+    ring.bar = smem_addr(bars) + group * kRingMax * 8;
+    if (threadIdx.x < R * kRingMax) {
+        mbar_init(smem_addr(bars) + 8 * threadIdx.x, 1);
+        mbar_init_fence();
+    }
+    if (threadIdx.x == 0) failed = 0;
+    __syncthreads();
+    const int64_t step = int64_t(gridDim.x) * R;
+    int64_t r = int64_t(group) * gridDim.x + blockIdx.x;
+    int64_t ahead = r;
+    auto fetch = [&](int at) {
+        const uint32_t to = ring.data + at * ring.bytes, bar = ring.bar + 8 * at;
+        mbar_expect_tx(bar, ring.bytes);
+        bulk_g2s(to, p.dy + ahead * p.dy_pitch, dy_bytes, bar);
+        bulk_g2s(to + dy_bytes, KEPT ? reinterpret_cast<const uint8_t*>(p.q) + ahead * p.q_pitch : p.x + ahead * p.x_pitch, x_bytes, bar);
+    };
+    if (t == 0)
+        for (int i = 0; i < depth && ahead < p.ntok; ++i, ahead += step) fetch(i);
+    stage_param<V, G, VPT>(params, p.w, p.w_bf16, p.dim, NT);
+    __syncthreads();
+    float dw[VPT][V], db[VPT][V];
+#pragma unroll
+    for (int i = 0; i < VPT; ++i)
+#pragma unroll
+        for (int j = 0; j < V; ++j) dw[i][j] = db[i][j] = 0.0f;
+    int code[VPT];
+    float mean = 0.0f, rstd = 0.0f;
+    auto row_values = [&](int64_t at) {   // what a row has beside its vectors
+        if (at >= p.ntok) return;
+        if (!p.rms) mean = __ldg(p.mean + at);
+        rstd = __ldg(p.rstd + at);
+        if constexpr (KEPT) {
+#pragma unroll
+            for (int i = 0; i < VPT; ++i) {
+                const int c = (i * G + t) * V;
+                if (c < p.dim) code[i] = __ldg(p.e + at * p.e_pitch + c / LC_ACT_BLOCK);
+            }
+        }
+    };
+    row_values(r);
+    for (; r < p.ntok; r += step) {
+        const bool ok = ring_wait(ring, &failed);
+        float a[VPT][V], h[VPT][V];   // dy, then dy w; x, then its normalised value
+        const float mu = mean, rs = ok ? rstd : __uint_as_float(0x7fffffffu);
+#pragma unroll
+        for (int i = 0; i < VPT; ++i) {
+            const int c = (i * G + t) * V;
+            if (c >= p.dim) break;
+            unpack(lds128(ring.row() + c * int(sizeof(T))), a[i]);
+            if constexpr (KEPT) {
+                const uint32_t at = ring.row() + dy_bytes + c;
+                uint32_t q[V / 4];
+                if constexpr (V == 8) asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(q[0]), "=r"(q[1]) : "r"(at) : "memory");
+                else asm volatile("ld.shared.u32 %0, [%1];" : "=r"(q[0]) : "r"(at) : "memory");
+                // a byte + 128 in the fraction of 2^23 gives its value; the product with the scale is exact
+                const float sc = act_scale(code[i]);
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    const float u = __uint_as_float(__byte_perm(q[j / 4] ^ 0x80808080u, 0x4b000000u, 0x7650 | (j & 3)));
+                    h[i][j] = fmaf(u - 8388736.0f, sc, -mu) * rs;
+                }
+            } else {
+                unpack(lds128(ring.row() + dy_bytes + c * int(sizeof(T))), h[i]);
+#pragma unroll
+                for (int j = 0; j < V; ++j) h[i][j] = (h[i][j] - mu) * rs;
+            }
+        }
+        row_values(r + step);
+        float s[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int i = 0; i < VPT; ++i) {
+            if ((i * G + t) * V >= p.dim) break;
+            float s0[4] = {}, s1[4] = {};   // short chains
+#pragma unroll
+            for (int j = 0; j < V; j += 4) {
+                const float4 w4 = params[(i * (V / 4) + j / 4) * G + t];
+                const float w[4] = {w4.x, w4.y, w4.z, w4.w};
+#pragma unroll
+                for (int m = 0; m < 4; ++m) {
+                    dw[i][j + m] = fmaf(a[i][j + m], h[i][j + m], dw[i][j + m]);
+                    db[i][j + m] += a[i][j + m];
+                    a[i][j + m] *= w[m];
+                    s0[m] += a[i][j + m];
+                    s1[m] = fmaf(a[i][j + m], h[i][j + m], s1[m]);
+                }
+            }
+            s[0] += (s0[0] + s0[1]) + (s0[2] + s0[3]);
+            s[1] += (s1[0] + s1[1]) + (s1[2] + s1[3]);
+        }
+        group_sum<G, NT>(s, shared, slot);
+        if constexpr (G == 32) __syncwarp();
+        if (t == 0 && ahead < p.ntok && !failed) fetch(ring.at);
+        ahead += step;
+        ring.next();
+        if (p.dx) {
+            const float m1 = p.rms ? 0.0f : s[0] * p.inv_dim * rs, m2 = s[1] * p.inv_dim * rs;
+            T* dx = reinterpret_cast<T*>(p.dx + r * p.dx_pitch);
+#pragma unroll
+            for (int i = 0; i < VPT; ++i) {
+                const int c = (i * G + t) * V;
+                if (c >= p.dim) break;
+#pragma unroll
+                for (int j = 0; j < V; ++j) a[i][j] = fmaf(a[i][j], rs, -m1) - h[i][j] * m2;
+                st_stream(dx + c, pack(a[i]));
+            }
+        }
+    }
+    ring_drain(ring, failed, t);
+    if (!p.want_params) return;
+    // one row of sums for the CTA: its groups add theirs in turn, over the memory of the rings (all rows were read)
+    __syncthreads();
+    float2* sums = reinterpret_cast<float2*>(smem);
+    for (int k = 0; k < R; ++k) {
+        if (group == k) {
+#pragma unroll
+            for (int i = 0; i < VPT; ++i)
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    float2& a = sums[(i * V + j) * G + t];
+                    if (k) {
+                        dw[i][j] += a.x;
+                        db[i][j] += a.y;
+                    }
+                    if (k < R - 1) a = make_float2(dw[i][j], db[i][j]);
+                }
+        }
+        if (R > 1) __syncthreads();
+    }
+    if (group != R - 1) return;
+    float* out = p.part + int64_t(blockIdx.x) * 2 * p.dim;
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+        const int c = (i * G + t) * V;
+        if (c >= p.dim) break;
+#pragma unroll
+        for (int j = 0; j < V; j += 4) {
+            *reinterpret_cast<float4*>(out + c + j) = make_float4(dw[i][j], dw[i][j + 1], dw[i][j + 2], dw[i][j + 3]);
+            *reinterpret_cast<float4*>(out + p.dim + c + j) = make_float4(db[i][j], db[i][j + 1], db[i][j + 2], db[i][j + 3]);
+        }
+    }
+}
+
 struct FoldParams {
     const float* part;
     uint8_t* dw;
@@ -354,24 +758,26 @@ struct FoldParams {
     int32_t rows, dim, g_bf16, accumulate;
 };
 
-// Adds the CTAs' rows of sums: 32 columns a CTA, 8 threads a column, each taking
-// every 8th row, their sums added in order.
-__global__ void __launch_bounds__(256) norm_fold_kernel(FoldParams p) {
-    __shared__ float sums[8][32];
+// Adds the CTAs' rows of sums: 32 columns a CTA, a warp every 32nd row, the warps'
+// sums added in order.
+__global__ void __launch_bounds__(1024) norm_fold_kernel(FoldParams p) {
+    __shared__ float sums[32][33];
     dependency_wait();
-    const int c = blockIdx.x * 32 + (threadIdx.x & 31), k = threadIdx.x >> 5;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int c = blockIdx.x * 32 + lane;
     uint8_t* out = blockIdx.y ? p.db : p.dw;
     if (!out) return;
     const float* part = p.part + (blockIdx.y ? p.dim : 0);
     float s = 0.0f;
     if (c < p.dim) {
-#pragma unroll 8
-        for (int r = k; r < p.rows; r += 8) s += part[int64_t(r) * 2 * p.dim + c];
+#pragma unroll 4
+        for (int r = warp; r < p.rows; r += 32) s += part[int64_t(r) * 2 * p.dim + c];
     }
-    sums[k][threadIdx.x & 31] = s;
+    sums[warp][lane] = s;
     __syncthreads();
-    if (k || c >= p.dim) return;
-    for (int i = 1; i < 8; ++i) s += sums[i][threadIdx.x];
+    if (warp || c >= p.dim) return;
+#pragma unroll
+    for (int i = 1; i < 32; ++i) s += sums[i][lane];
     if (p.g_bf16) {
         __nv_bfloat16* o = reinterpret_cast<__nv_bfloat16*>(out) + c;
         *o = __float2bfloat16_rn(p.accumulate ? __bfloat162float(*o) + s : s);
@@ -381,18 +787,103 @@ __global__ void __launch_bounds__(256) norm_fold_kernel(FoldParams p) {
     }
 }
 
+// Shared memory above 48 KB has to be asked for, once for a kernel and device.
+template <typename K>
+cudaError_t allow_smem(K kernel, bool (&ready)[kOpsMaxDevices]) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess && !ready[dev]) {
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kRingSmem));
+        ready[dev] = e == cudaSuccess;
+    }
+    return e;
+}
+
+// Rows of a group's ring in what the parameters leave of shared memory (0: none fits).
+int ring_depth(size_t params, int groups, size_t row) {
+    if (params + groups * row > kRingSmem) return 0;
+    const size_t n = (kRingSmem - params) / (groups * row);
+    return n < kRingMax ? int(n) : kRingMax;
+}
+
+template <typename T, int G, int VPT>
+cudaError_t launch_norm_ring(const NormParams& p, int sms, cudaStream_t s, bool* done) {
+    constexpr int V = kVec<T>, NT = fwd_threads(G), R = NT / G;
+    static bool ready[kOpsMaxDevices];
+    const size_t params = size_t(VPT) * V * G * 4 * (p.b ? 2 : 1), row = size_t(p.dim) * sizeof(T);
+    const int depth = ring_depth(params, R, row);
+    *done = depth > 0;
+    if (!depth) return cudaSuccess;
+    const cudaError_t e = allow_smem(norm_ring_kernel<T, G, VPT>, ready);
+    if (e != cudaSuccess) return e;
+    const int64_t grid = p.ntok < sms ? p.ntok : sms;
+    cudaGetLastError();
+    norm_ring_kernel<T, G, VPT><<<unsigned(grid), NT, params + R * depth * row, s>>>(p, depth);
+    return cudaGetLastError();
+}
+
+template <typename T>
+cudaError_t dispatch_norm_ring(const NormParams& p, int sms, cudaStream_t s, bool* done) {
+    constexpr int M = 8 / kVec<T>;          // 16 values a thread, from a warp a row on
+    const int nv = p.dim / kVec<T> / M;
+    if (nv <= 32) return launch_norm_ring<T, 32, M>(p, sms, s, done);
+    if (nv <= 64) return launch_norm_ring<T, 32, 2 * M>(p, sms, s, done);
+    if (nv <= 96) return launch_norm_ring<T, 32, 3 * M>(p, sms, s, done);
+    if (nv <= 128) return launch_norm_ring<T, 64, 2 * M>(p, sms, s, done);
+    if (nv <= 256) return launch_norm_ring<T, 128, 2 * M>(p, sms, s, done);
+    if (nv <= 512) return launch_norm_ring<T, 256, 2 * M>(p, sms, s, done);
+    if (nv <= 1024) return launch_norm_ring<T, 512, 2 * M>(p, sms, s, done);
+    return launch_norm_ring<T, 1024, 2 * M>(p, sms, s, done);
+}
+
+template <typename T, int G, int VPT, bool KEPT>
+cudaError_t launch_grad_ring(const NormGradParams& p, int sms, cudaStream_t s, int* ctas) {
+    constexpr int V = kVec<T>, NT = bwd_threads(G), R = NT / G;
+    static bool ready[kOpsMaxDevices];
+    const size_t params = size_t(VPT) * V * G * 4;
+    const size_t row = size_t(p.dim) * sizeof(T) + (KEPT ? (size_t(p.dim) + LC_ACT_BLOCK - 1) / LC_ACT_BLOCK * LC_ACT_BLOCK
+                                                         : size_t(p.dim) * sizeof(T));
+    const int depth = ring_depth(params, R, row);
+    *ctas = 0;
+    if (!depth) return cudaSuccess;
+    const cudaError_t e = allow_smem(norm_grad_ring_kernel<T, G, VPT, KEPT>, ready);
+    if (e != cudaSuccess) return e;
+    int64_t grid = p.ntok < sms ? p.ntok : sms;
+    grid = grid < kGradCtas ? grid : kGradCtas;
+    *ctas = int(grid);
+    size_t smem = params + R * depth * row;
+    if (R > 1 && smem < 2 * params) smem = 2 * params;   // the groups' sums
+    cudaGetLastError();
+    norm_grad_ring_kernel<T, G, VPT, KEPT><<<unsigned(grid), NT, smem, s>>>(p, depth);
+    return cudaGetLastError();
+}
+
+template <typename T, bool KEPT>
+cudaError_t dispatch_grad_ring(const NormGradParams& p, int sms, cudaStream_t s, int* ctas) {
+    constexpr int M = 8 / kVec<T>;
+    const int nv = p.dim / kVec<T> / M;
+    if (nv <= 32) return launch_grad_ring<T, 32, M, KEPT>(p, sms, s, ctas);
+    if (nv <= 64) return launch_grad_ring<T, 32, 2 * M, KEPT>(p, sms, s, ctas);
+    if (nv <= 96) return launch_grad_ring<T, 32, 3 * M, KEPT>(p, sms, s, ctas);
+    if (nv <= 128) return launch_grad_ring<T, 64, 2 * M, KEPT>(p, sms, s, ctas);
+    if (nv <= 256) return launch_grad_ring<T, 128, 2 * M, KEPT>(p, sms, s, ctas);
+    if (nv <= 512) return launch_grad_ring<T, 256, 2 * M, KEPT>(p, sms, s, ctas);
+    if (nv <= 1024) return launch_grad_ring<T, 512, 2 * M, KEPT>(p, sms, s, ctas);
+    return launch_grad_ring<T, 512, 4 * M, KEPT>(p, sms, s, ctas);
+}
+
 template <typename T, int G, int VPT, bool VEC>
 cudaError_t launch_norm(const NormParams& p, int sms, cudaStream_t s) {
     constexpr int R = cta_threads(G) / G;
     const int64_t want = (p.ntok + R - 1) / R;
-    const int64_t most = int64_t(sms) * 64;
+    const int64_t most = int64_t(sms) * 1024;
     cudaGetLastError();
     norm_kernel<T, G, VPT, VEC><<<unsigned(want < most ? want : most), cta_threads(G), 0, s>>>(p);
     return cudaGetLastError();
 }
 
 // Threads of a row and vectors of a thread: a warp up to 4 vectors a lane, then
-// groups of warps with 2 a thread.
+// groups of warps.
 template <typename T, bool VEC>
 cudaError_t dispatch_norm(const NormParams& p, int sms, cudaStream_t s) {
     const int nv = (p.dim + kVec<T> - 1) / kVec<T>;
@@ -400,11 +891,11 @@ cudaError_t dispatch_norm(const NormParams& p, int sms, cudaStream_t s) {
     if (nv <= 64) return launch_norm<T, 32, 2, VEC>(p, sms, s);
     if (nv <= 128) return launch_norm<T, 32, 4, VEC>(p, sms, s);
     if (nv <= 256) return launch_norm<T, 128, 2, VEC>(p, sms, s);
-    if (nv <= 512) return launch_norm<T, 256, 2, VEC>(p, sms, s);
-    if (nv <= 1024) return launch_norm<T, 512, 2, VEC>(p, sms, s);
+    if (nv <= 512) return launch_norm<T, 128, 4, VEC>(p, sms, s);
+    if (nv <= 1024) return launch_norm<T, 256, 4, VEC>(p, sms, s);
     if constexpr (kVec<T> == 4)
         if (nv > 2048) return launch_norm<T, 1024, 4, VEC>(p, sms, s);
-    return launch_norm<T, 1024, 2, VEC>(p, sms, s);
+    return launch_norm<T, 512, 4, VEC>(p, sms, s);
 }
 
 template <typename T, int G, int VPT, bool VEC, bool KEPT, bool SMEM>
@@ -447,6 +938,7 @@ cudaError_t dispatch_grad(const NormGradParams& p, int sms, cudaStream_t s, int*
     return launch_grad<T, 1024, 2, VEC, KEPT, true>(p, sms, s, ctas);
 }
 
+constexpr int64_t kRingRows = 4;   // rows a multiprocessor from which the rings are taken
 constexpr int64_t kMaxRows = int64_t(1) << 40;
 
 bool plain_params(const void* w, int64_t dim, int32_t dtype) {
@@ -529,7 +1021,12 @@ extern "C" lc_status lc_norm(int device, void* cuda_stream, int32_t kind, const 
         const cudaError_t err = act_save_rows(x, keep, ntok, dim, s);
         if (err != cudaSuccess) return ops_launched(call, err);
     }
-    cudaError_t err;
+    cudaError_t err = cudaSuccess;
+    // few rows: a ring's set-up costs more than it hides
+    bool done = false;
+    if (vec && dim * e % 16 == 0 && ntok >= kRingRows * sms)
+        err = x->dtype == LC_BF16 ? dispatch_norm_ring<__nv_bfloat16>(p, sms, s, &done) : dispatch_norm_ring<float>(p, sms, s, &done);
+    if (done || err != cudaSuccess) return ops_launched(call, err);
     if (x->dtype == LC_BF16)
         err = vec ? dispatch_norm<__nv_bfloat16, true>(p, sms, s) : dispatch_norm<__nv_bfloat16, false>(p, sms, s);
     else
@@ -639,7 +1136,13 @@ extern "C" lc_status lc_norm_grad(int device, void* cuda_stream, int32_t kind, c
     const int sms = ops_sm_count(device);
     using B = __nv_bfloat16;
     int ctas = 0;
-    if (dy->dtype == LC_BF16)
+    if (vec && dim * e % 16 == 0 && ntok >= kRingRows * sms) {
+        if (dy->dtype == LC_BF16) err = x ? dispatch_grad_ring<B, false>(p, sms, s, &ctas) : dispatch_grad_ring<B, true>(p, sms, s, &ctas);
+        else err = x ? dispatch_grad_ring<float, false>(p, sms, s, &ctas) : dispatch_grad_ring<float, true>(p, sms, s, &ctas);
+    }
+    if (ctas || err != cudaSuccess) {
+        // through the rings
+    } else if (dy->dtype == LC_BF16)
         err = x ? (vec ? dispatch_grad<B, true, false>(p, sms, s, &ctas) : dispatch_grad<B, false, false>(p, sms, s, &ctas))
                 : (vec ? dispatch_grad<B, true, true>(p, sms, s, &ctas) : dispatch_grad<B, false, true>(p, sms, s, &ctas));
     else
@@ -653,7 +1156,7 @@ extern "C" lc_status lc_norm_grad(int device, void* cuda_stream, int32_t kind, c
         attr.val.programmaticStreamSerializationAllowed = 1;
         cudaLaunchConfig_t c{};
         c.gridDim = dim3(unsigned((dim + 31) / 32), dbias ? 2 : 1);
-        c.blockDim = dim3(256);
+        c.blockDim = dim3(1024);
         c.stream = s;
         c.attrs = &attr;
         c.numAttrs = 1;

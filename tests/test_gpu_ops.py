@@ -411,6 +411,59 @@ def test_norm_grad_long(ops):
     within(db, rdb, broom, "dbias")
 
 
+MANY = [(617, 40, BF, BF), (5000, 64, F32, F32), (613, 256, F32, F32), (640, 520, BF, F32), (3001, 768, BF, BF),
+        (611, 1024, BF, BF), (1300, 2048, BF, BF), (620, 4096, BF, F32), (609, 4096, F32, BF), (612, 6000, BF, BF),
+        (610, 8192, F32, F32), (625, 12296, BF, BF), (610, 16384, BF, BF), (615, 16384, F32, F32)]
+
+
+@pytest.mark.parametrize("kind", ["layer", "rms"])
+@pytest.mark.parametrize("t,d,dt,wt", MANY)
+def test_norm_of_many_rows(ops, kind, t, d, dt, wt):
+    """Enough rows to stream through shared memory; rows of a wider buffer too; a NaN stays in its row."""
+    g = gen(t * d)
+    shift = 2.0 if kind == "layer" else 0.0
+    src = (randn(g, t, d) + shift).to(dt)
+    src[t // 2, d // 3] = math.nan
+    w = 1 + randn(g, d, dtype=wt, spread=0.2)
+    b = randn(g, d, dtype=wt) if kind == "layer" else None
+    dsrc = randn(g, t, d, dtype=dt)
+    for extra in (0, 16):
+        x, _ = strided(src, 0, extra)
+        dy, _ = strided(dsrc, 8, extra)
+        y, mean, rstd, keep = ops.norm(x, w, b, kind=kind, keep=True)
+        ref, rmean, rrstd, xhat = norm_ref(x, w, b, kind, 1e-5)
+        a = x.double().abs().mean(1)
+        if mean is not None:
+            within(mean, rmean, SUMS * U * a, "mean")
+        within(rstd, rrstd, (SUMS + 4) * U * rrstd, "rstd")
+        room = ((SUMS + 8) * U * xhat.abs() + (SUMS + 8) * U * (a * rrstd)[:, None]) * w.double().abs()
+        within(y, ref, room + (4 * U * b.double().abs() if b is not None else 0), "y")
+        q, e, _ = quantize(x)
+        assert torch.equal(keep.q, q) and torch.equal(keep.e, e)
+        assert torch.equal(ops.norm(x, w, b, kind=kind)[0].isnan().any(1), x.isnan().any(1))
+        # gradients: from the rows without the NaN, whole
+        ok = ~x.isnan().any(1)
+        stat = rstd.clone()
+        stat[~ok] = 1.0
+        mu = None if mean is None else torch.where(ok, mean, 0.0)
+        for kept in (False, True):
+            seen = values(keep.q, keep.e)[:, :d] if kept else x
+            dx, dw, db = ops.norm_grad(dy, keep if kept else x, w, mu, stat, bias=True)
+            assert torch.isnan(dx[t // 2]).any() and torch.isfinite(dx[ok]).all()
+            rdx, room, rdw, wroom, rdb, broom = norm_grad_ref(dy[ok], seen[ok], w, None if mu is None else mu[ok], stat[ok])
+            within(dx[ok], rdx, room, "dx")
+            within(db, dsrc.double().sum(0), (t + 16) * U * dsrc.double().abs().sum(0), "dbias")
+            bad = torch.isnan(dw)
+            assert bad[d // 3] and int(bad.sum()) <= (128 if kept else 1)
+            src2 = torch.where(seen.isnan(), 0.0, seen.double())
+            h = (src2 if mu is None else torch.where(seen.isnan(), 0.0, src2 - mu.double()[:, None])) * stat.double()[:, None]
+            full = (dsrc.double() * h).sum(0)
+            within(dw[~bad], full[~bad], ((t + 16) * U * (dsrc.double() * h).abs().sum(0) + 6 * U * (
+                dsrc.double().abs() * (src2.abs() + shift + 1) * stat.double()[:, None]).sum(0))[~bad], "dweight")
+            again = ops.norm_grad(dy, keep if kept else x, w, mu, stat, bias=True)
+            assert torch.equal(again[0][ok], dx[ok]) and torch.equal(again[1][~bad], dw[~bad]) and torch.equal(again[2], db)
+
+
 @pytest.mark.parametrize("kind", ["layer", "rms"])
 def test_norm_grad_is_the_derivative(ops, kind):
     """Central differences of sum(dy * norm) in 64 bits."""
