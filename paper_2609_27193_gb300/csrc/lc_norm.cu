@@ -145,28 +145,52 @@ __device__ __forceinline__ void group_barrier() {
     else asm volatile("bar.sync %0, %1;" ::"r"(int(threadIdx.x) / G + (NT / G < 16 ? 1 : 0)), "n"(G) : "memory");
 }
 
-// Sum over the group's G threads; every thread gets it.  `slot` alternates, so one
-// barrier a sum is enough.
+// Sums of N values (1 or 2) over the group's G threads; every thread gets them.
+// Two values share the steps of a warp: after the first, one half of it works on
+// either.  `slot` alternates, so one barrier a sum is enough.
 template <int G, int NT, int N>
-__device__ __forceinline__ void group_sum(float (&v)[N], float (*shared)[32][N], int& slot) {
+__device__ __forceinline__ void group_sum(float (&v)[N], float (*shared)[N][32], int& slot) {
+    const int lane = threadIdx.x & 31;
+    float x = v[0];
+    if constexpr (N == 2) {
+        const bool up = lane & 16;
+        x = (up ? v[1] : v[0]) + __shfl_xor_sync(0xffffffffu, up ? v[0] : v[1], 16);
+    } else {
+        x += __shfl_xor_sync(0xffffffffu, x, 16);
+    }
 #pragma unroll
-    for (int k = 0; k < N; ++k)
-#pragma unroll
-        for (int o = 16; o; o >>= 1) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
-    if constexpr (G > 32) {
+    for (int o = 8; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    if constexpr (G == 32) {
+        v[0] = N == 2 ? __shfl_sync(0xffffffffu, x, 0) : x;
+        if constexpr (N == 2) v[1] = __shfl_sync(0xffffffffu, x, 16);
+    } else {
         const int warp = threadIdx.x >> 5;
-        if ((threadIdx.x & 31) == 0) {
-#pragma unroll
-            for (int k = 0; k < N; ++k) shared[slot][warp][k] = v[k];
-        }
+        if (lane == 0) shared[slot][0][warp] = x;
+        if (N == 2 && lane == 16) shared[slot][N - 1][warp] = x;
         group_barrier<G, NT>();
         const int w0 = NT == G ? 0 : int(threadIdx.x) / G * (G / 32);
 #pragma unroll
         for (int k = 0; k < N; ++k) {
-            float s = 0.0f;
+            const float* from = &shared[slot][k][w0];
+            if constexpr (G > 256) {
+                // more warps than a thread should add up: a lane each
+                float s = lane < G / 32 ? from[lane] : 0.0f;
 #pragma unroll
-            for (int w = 0; w < G / 32; ++w) s += shared[slot][w0 + w][k];
-            v[k] = s;
+                for (int o = 16; o; o >>= 1)
+                    if (o < G / 32) s += __shfl_xor_sync(0xffffffffu, s, o);
+                v[k] = __shfl_sync(0xffffffffu, s, 0);
+            } else if constexpr (G == 64) {
+                const float2 s = *reinterpret_cast<const float2*>(from);
+                v[k] = s.x + s.y;
+            } else {
+                float s = 0.0f;
+#pragma unroll
+                for (int w = 0; w < G / 32; w += 4) {
+                    const float4 q = *reinterpret_cast<const float4*>(from + w);
+                    s += (q.x + q.y) + (q.z + q.w);
+                }
+                v[k] = s;
+            }
         }
         slot ^= 1;
     }
@@ -178,7 +202,7 @@ template <typename T, int G, int VPT, bool VEC>
 __global__ void __launch_bounds__(cta_threads(G)) norm_kernel(NormParams p) {
     constexpr int V = kVec<T>;
     constexpr int R = cta_threads(G) / G;   // rows of a CTA at a time
-    __shared__ float shared[2][32][1];
+    __shared__ __align__(16) float shared[2][1][32];
     int slot = 0;
     const int t = threadIdx.x % G;
     const int64_t step = int64_t(gridDim.x) * R;
@@ -264,7 +288,7 @@ __global__ void __launch_bounds__(cta_threads(G)) norm_grad_kernel(NormGradParam
     constexpr int V = kVec<T>;
     constexpr int R = cta_threads(G) / G;
     extern __shared__ float2 sums[];
-    __shared__ float shared[2][32][2];
+    __shared__ __align__(16) float shared[2][2][32];
     int slot = 0;
     const int t = threadIdx.x % G;
     float dw[SMEM ? 1 : VPT][V], db[SMEM ? 1 : VPT][V];
@@ -463,7 +487,7 @@ template <typename T, int G, int VPT>
 __global__ void __launch_bounds__(fwd_threads(G), 1) norm_ring_kernel(NormParams p, int depth) {
     constexpr int V = kVec<T>, NT = fwd_threads(G), R = NT / G;
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ float shared[2][32][1];
+    __shared__ __align__(16) float shared[2][1][32];
     __shared__ __align__(8) uint64_t bars[R * kRingMax];
     __shared__ volatile uint32_t failed;
     int slot = 0;
@@ -595,7 +619,7 @@ template <typename T, int G, int VPT, bool KEPT>
 __global__ void __launch_bounds__(bwd_threads(G), 1) norm_grad_ring_kernel(NormGradParams p, int depth) {
     constexpr int V = kVec<T>, NT = bwd_threads(G), R = NT / G;
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ float shared[2][32][2];
+    __shared__ __align__(16) float shared[2][2][32];
     __shared__ __align__(8) uint64_t bars[R * kRingMax];
     __shared__ volatile uint32_t failed;
     dependents_may_start();
@@ -718,35 +742,47 @@ __global__ void __launch_bounds__(bwd_threads(G), 1) norm_grad_ring_kernel(NormG
     }
     ring_drain(ring, failed, t);
     if (!p.want_params) return;
-    // one row of sums for the CTA: its groups add theirs in turn, over the memory of the rings (all rows were read)
-    __syncthreads();
-    float2* sums = reinterpret_cast<float2*>(smem);
-    for (int k = 0; k < R; ++k) {
-        if (group == k) {
-#pragma unroll
-            for (int i = 0; i < VPT; ++i)
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    float2& a = sums[(i * V + j) * G + t];
-                    if (k) {
-                        dw[i][j] += a.x;
-                        db[i][j] += a.y;
-                    }
-                    if (k < R - 1) a = make_float2(dw[i][j], db[i][j]);
-                }
-        }
-        if (R > 1) __syncthreads();
-    }
-    if (group != R - 1) return;
+    // one row of sums for the CTA: every group leaves its own in the rings' memory (all rows were read), and each
+    // column is added over the groups in order
     float* out = p.part + int64_t(blockIdx.x) * 2 * p.dim;
+    if constexpr (R == 1) {
 #pragma unroll
-    for (int i = 0; i < VPT; ++i) {
-        const int c = (i * G + t) * V;
-        if (c >= p.dim) break;
+        for (int i = 0; i < VPT; ++i) {
+            const int c = (i * G + t) * V;
+            if (c >= p.dim) break;
 #pragma unroll
-        for (int j = 0; j < V; j += 4) {
-            *reinterpret_cast<float4*>(out + c + j) = make_float4(dw[i][j], dw[i][j + 1], dw[i][j + 2], dw[i][j + 3]);
-            *reinterpret_cast<float4*>(out + p.dim + c + j) = make_float4(db[i][j], db[i][j + 1], db[i][j + 2], db[i][j + 3]);
+            for (int j = 0; j < V; j += 4) {
+                *reinterpret_cast<float4*>(out + c + j) = make_float4(dw[i][j], dw[i][j + 1], dw[i][j + 2], dw[i][j + 3]);
+                *reinterpret_cast<float4*>(out + p.dim + c + j) = make_float4(db[i][j], db[i][j + 1], db[i][j + 2], db[i][j + 3]);
+            }
+        }
+    } else {
+        __syncthreads();
+        constexpr int kCols = VPT * V * G;
+        float4* sums = reinterpret_cast<float4*>(smem);   // [groups][dw, db][VPT * V / 4][G]
+#pragma unroll
+        for (int i = 0; i < VPT; ++i)
+#pragma unroll
+            for (int j = 0; j < V; j += 4) {
+                float4* at = sums + group * (kCols / 2) + (i * (V / 4) + j / 4) * G + t;
+                at[0] = make_float4(dw[i][j], dw[i][j + 1], dw[i][j + 2], dw[i][j + 3]);
+                at[kCols / 4] = make_float4(db[i][j], db[i][j + 1], db[i][j + 2], db[i][j + 3]);
+            }
+        __syncthreads();
+        for (int k = threadIdx.x; k < kCols / 2; k += NT) {
+            const int q = k % (kCols / 4);
+            const int c = (q / G / (V / 4) * G + q % G) * V + q / G % (V / 4) * 4;
+            if (c >= p.dim) continue;
+            float4 v = sums[k];
+#pragma unroll 4
+            for (int g = 1; g < R; ++g) {
+                const float4 x = sums[g * (kCols / 2) + k];
+                v.x += x.x;
+                v.y += x.y;
+                v.z += x.z;
+                v.w += x.w;
+            }
+            *reinterpret_cast<float4*>(out + (k < kCols / 4 ? 0 : p.dim) + c) = v;
         }
     }
 }
@@ -852,7 +888,7 @@ cudaError_t launch_grad_ring(const NormGradParams& p, int sms, cudaStream_t s, i
     grid = grid < kGradCtas ? grid : kGradCtas;
     *ctas = int(grid);
     size_t smem = params + R * depth * row;
-    if (R > 1 && smem < 2 * params) smem = 2 * params;   // the groups' sums
+    if (R > 1 && smem < 2 * R * params) smem = 2 * R * params;   // the groups' sums
     cudaGetLastError();
     norm_grad_ring_kernel<T, G, VPT, KEPT><<<unsigned(grid), NT, smem, s>>>(p, depth);
     return cudaGetLastError();
