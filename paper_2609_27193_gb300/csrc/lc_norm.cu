@@ -615,11 +615,13 @@ constexpr int bwd_threads(int G) { return 512; }
 
 // The backward.  A slot holds the rows of dy and of x (or its 8-bit values; their
 // exponents are asked for a row ahead into registers).
-template <typename T, int G, int VPT, bool KEPT>
+// LEAN: no means (root-mean-square norm) and no gradient of a bias.
+template <typename T, int G, int VPT, bool KEPT, bool LEAN>
 __global__ void __launch_bounds__(bwd_threads(G), 1) norm_grad_ring_kernel(NormGradParams p, int depth) {
     constexpr int V = kVec<T>, NT = bwd_threads(G), R = NT / G;
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ __align__(16) float shared[2][2][32];
+    float(*shared1)[1][32] = reinterpret_cast<float(*)[1][32]>(shared);
     __shared__ __align__(8) uint64_t bars[R * kRingMax];
     __shared__ volatile uint32_t failed;
     dependents_may_start();
@@ -653,16 +655,16 @@ __global__ void __launch_bounds__(bwd_threads(G), 1) norm_grad_ring_kernel(NormG
         for (int i = 0; i < depth && ahead < p.ntok; ++i, ahead += step) fetch(i);
     stage_param<V, G, VPT>(params, p.w, p.w_bf16, p.dim, NT);
     __syncthreads();
-    float dw[VPT][V], db[VPT][V];
+    float2 dw[VPT][V / 2], db[LEAN ? 1 : VPT][V / 2];
 #pragma unroll
     for (int i = 0; i < VPT; ++i)
 #pragma unroll
-        for (int j = 0; j < V; ++j) dw[i][j] = db[i][j] = 0.0f;
+        for (int j = 0; j < V / 2; ++j) dw[i][j] = db[LEAN ? 0 : i][j] = both(0.0f);
     int code[VPT];
     float mean = 0.0f, rstd = 0.0f;
     auto row_values = [&](int64_t at) {   // what a row has beside its vectors
         if (at >= p.ntok) return;
-        if (!p.rms) mean = __ldg(p.mean + at);
+        if (!LEAN && !p.rms) mean = __ldg(p.mean + at);
         rstd = __ldg(p.rstd + at);
         if constexpr (KEPT) {
 #pragma unroll
@@ -675,7 +677,7 @@ __global__ void __launch_bounds__(bwd_threads(G), 1) norm_grad_ring_kernel(NormG
     row_values(r);
     for (; r < p.ntok; r += step) {
         const bool ok = ring_wait(ring, &failed);
-        float a[VPT][V], h[VPT][V];   // dy, then dy w; x, then its normalised value
+        float2 a[VPT][V / 2], h[VPT][V / 2];   // dy, then dy w; x, then its normalised value
         const float mu = mean, rs = ok ? rstd : __uint_as_float(0x7fffffffu);
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
@@ -690,52 +692,71 @@ __global__ void __launch_bounds__(bwd_threads(G), 1) norm_grad_ring_kernel(NormG
                 // a byte + 128 in the fraction of 2^23 gives its value; the product with the scale is exact
                 const float sc = act_scale(code[i]);
 #pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    const float u = __uint_as_float(__byte_perm(q[j / 4] ^ 0x80808080u, 0x4b000000u, 0x7650 | (j & 3)));
-                    h[i][j] = fmaf(u - 8388736.0f, sc, -mu) * rs;
+                for (int j = 0; j < V / 2; ++j) {
+                    const uint32_t w = q[j / 2] ^ 0x80808080u;
+                    const int b = j & 1 ? 2 : 0;
+                    const float2 u = make_float2(__uint_as_float(__byte_perm(w, 0x4b000000u, 0x7650 | b)),
+                                                 __uint_as_float(__byte_perm(w, 0x4b000000u, 0x7651 | b)));
+                    const float2 v = add2(u, both(-8388736.0f));
+                    if constexpr (LEAN) h[i][j] = mul2(v, both(sc * rs));
+                    else h[i][j] = mul2(fma2(v, both(sc), both(-mu)), both(rs));
                 }
             } else {
                 unpack(lds128(ring.row() + dy_bytes + c * int(sizeof(T))), h[i]);
 #pragma unroll
-                for (int j = 0; j < V; ++j) h[i][j] = (h[i][j] - mu) * rs;
+                for (int j = 0; j < V / 2; ++j) {
+                    if constexpr (!LEAN) h[i][j] = add2(h[i][j], both(-mu));
+                    h[i][j] = mul2(h[i][j], both(rs));
+                }
             }
         }
         row_values(r + step);
         float s[2] = {0.0f, 0.0f};
+        float2 s0[2] = {both(0.0f), both(0.0f)}, s1[2] = {both(0.0f), both(0.0f)};   // short chains
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
             if ((i * G + t) * V >= p.dim) break;
-            float s0[4] = {}, s1[4] = {};   // short chains
 #pragma unroll
-            for (int j = 0; j < V; j += 4) {
-                const float4 w4 = params[(i * (V / 4) + j / 4) * G + t];
-                const float w[4] = {w4.x, w4.y, w4.z, w4.w};
+            for (int j = 0; j < V / 2; j += 2) {
+                const float4 w4 = params[(i * (V / 4) + j / 2) * G + t];
+                const float2 w[2] = {make_float2(w4.x, w4.y), make_float2(w4.z, w4.w)};
 #pragma unroll
-                for (int m = 0; m < 4; ++m) {
-                    dw[i][j + m] = fmaf(a[i][j + m], h[i][j + m], dw[i][j + m]);
-                    db[i][j + m] += a[i][j + m];
-                    a[i][j + m] *= w[m];
-                    s0[m] += a[i][j + m];
-                    s1[m] = fmaf(a[i][j + m], h[i][j + m], s1[m]);
+                for (int m = 0; m < 2; ++m) {
+                    dw[i][j + m] = fma2(a[i][j + m], h[i][j + m], dw[i][j + m]);
+                    if constexpr (!LEAN) db[i][j + m] = add2(db[i][j + m], a[i][j + m]);
+                    a[i][j + m] = mul2(a[i][j + m], w[m]);
+                    if constexpr (!LEAN) s0[m] = add2(s0[m], a[i][j + m]);
+                    s1[m] = fma2(a[i][j + m], h[i][j + m], s1[m]);
                 }
             }
-            s[0] += (s0[0] + s0[1]) + (s0[2] + s0[3]);
-            s[1] += (s1[0] + s1[1]) + (s1[2] + s1[3]);
         }
-        group_sum<G, NT>(s, shared, slot);
+        s0[0] = add2(s0[0], s0[1]);
+        s1[0] = add2(s1[0], s1[1]);
+        s[0] = s0[0].x + s0[0].y;
+        s[1] = s1[0].x + s1[0].y;
+        if constexpr (LEAN) {
+            float one[1] = {s[1]};
+            group_sum<G, NT>(one, shared1, slot);
+            s[1] = one[0];
+        } else {
+            group_sum<G, NT>(s, shared, slot);
+        }
         if constexpr (G == 32) __syncwarp();
         if (t == 0 && ahead < p.ntok && !failed) fetch(ring.at);
         ahead += step;
         ring.next();
         if (p.dx) {
-            const float m1 = p.rms ? 0.0f : s[0] * p.inv_dim * rs, m2 = s[1] * p.inv_dim * rs;
+            const float m1 = LEAN || p.rms ? 0.0f : s[0] * p.inv_dim * rs, m2 = s[1] * p.inv_dim * rs;
             T* dx = reinterpret_cast<T*>(p.dx + r * p.dx_pitch);
 #pragma unroll
             for (int i = 0; i < VPT; ++i) {
                 const int c = (i * G + t) * V;
                 if (c >= p.dim) break;
 #pragma unroll
-                for (int j = 0; j < V; ++j) a[i][j] = fmaf(a[i][j], rs, -m1) - h[i][j] * m2;
+                for (int j = 0; j < V / 2; ++j) {
+                    const float2 v = LEAN ? mul2(a[i][j], both(rs)) : fma2(a[i][j], both(rs), both(-m1));
+                    a[i][j] = fma2(h[i][j], both(-m2), v);
+                }
                 st_stream(dx + c, pack(a[i]));
             }
         }
@@ -745,15 +766,16 @@ __global__ void __launch_bounds__(bwd_threads(G), 1) norm_grad_ring_kernel(NormG
     // one row of sums for the CTA: every group leaves its own in the rings' memory (all rows were read), and each
     // column is added over the groups in order
     float* out = p.part + int64_t(blockIdx.x) * 2 * p.dim;
+    auto quad = [](const float2& x, const float2& y) { return make_float4(x.x, x.y, y.x, y.y); };
     if constexpr (R == 1) {
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
             const int c = (i * G + t) * V;
             if (c >= p.dim) break;
 #pragma unroll
-            for (int j = 0; j < V; j += 4) {
-                *reinterpret_cast<float4*>(out + c + j) = make_float4(dw[i][j], dw[i][j + 1], dw[i][j + 2], dw[i][j + 3]);
-                *reinterpret_cast<float4*>(out + p.dim + c + j) = make_float4(db[i][j], db[i][j + 1], db[i][j + 2], db[i][j + 3]);
+            for (int j = 0; j < V / 2; j += 2) {
+                *reinterpret_cast<float4*>(out + c + 2 * j) = quad(dw[i][j], dw[i][j + 1]);
+                if constexpr (!LEAN) *reinterpret_cast<float4*>(out + p.dim + c + 2 * j) = quad(db[i][j], db[i][j + 1]);
             }
         }
     } else {
@@ -763,13 +785,13 @@ __global__ void __launch_bounds__(bwd_threads(G), 1) norm_grad_ring_kernel(NormG
 #pragma unroll
         for (int i = 0; i < VPT; ++i)
 #pragma unroll
-            for (int j = 0; j < V; j += 4) {
-                float4* at = sums + group * (kCols / 2) + (i * (V / 4) + j / 4) * G + t;
-                at[0] = make_float4(dw[i][j], dw[i][j + 1], dw[i][j + 2], dw[i][j + 3]);
-                at[kCols / 4] = make_float4(db[i][j], db[i][j + 1], db[i][j + 2], db[i][j + 3]);
+            for (int j = 0; j < V / 2; j += 2) {
+                float4* at = sums + group * (kCols / 2) + (i * (V / 4) + j / 2) * G + t;
+                at[0] = quad(dw[i][j], dw[i][j + 1]);
+                if constexpr (!LEAN) at[kCols / 4] = quad(db[i][j], db[i][j + 1]);
             }
         __syncthreads();
-        for (int k = threadIdx.x; k < kCols / 2; k += NT) {
+        for (int k = threadIdx.x; k < kCols / (LEAN ? 4 : 2); k += NT) {
             const int q = k % (kCols / 4);
             const int c = (q / G / (V / 4) * G + q % G) * V + q / G % (V / 4) * 4;
             if (c >= p.dim) continue;
@@ -872,7 +894,7 @@ cudaError_t dispatch_norm_ring(const NormParams& p, int sms, cudaStream_t s, boo
     return launch_norm_ring<T, 1024, 2 * M>(p, sms, s, done);
 }
 
-template <typename T, int G, int VPT, bool KEPT>
+template <typename T, int G, int VPT, bool KEPT, bool LEAN>
 cudaError_t launch_grad_ring(const NormGradParams& p, int sms, cudaStream_t s, int* ctas) {
     constexpr int V = kVec<T>, NT = bwd_threads(G), R = NT / G;
     static bool ready[kOpsMaxDevices];
@@ -882,7 +904,7 @@ cudaError_t launch_grad_ring(const NormGradParams& p, int sms, cudaStream_t s, i
     const int depth = ring_depth(params, R, row);
     *ctas = 0;
     if (!depth) return cudaSuccess;
-    const cudaError_t e = allow_smem(norm_grad_ring_kernel<T, G, VPT, KEPT>, ready);
+    const cudaError_t e = allow_smem(norm_grad_ring_kernel<T, G, VPT, KEPT, LEAN>, ready);
     if (e != cudaSuccess) return e;
     int64_t grid = p.ntok < sms ? p.ntok : sms;
     grid = grid < kGradCtas ? grid : kGradCtas;
@@ -890,22 +912,22 @@ cudaError_t launch_grad_ring(const NormGradParams& p, int sms, cudaStream_t s, i
     size_t smem = params + R * depth * row;
     if (R > 1 && smem < 2 * R * params) smem = 2 * R * params;   // the groups' sums
     cudaGetLastError();
-    norm_grad_ring_kernel<T, G, VPT, KEPT><<<unsigned(grid), NT, smem, s>>>(p, depth);
+    norm_grad_ring_kernel<T, G, VPT, KEPT, LEAN><<<unsigned(grid), NT, smem, s>>>(p, depth);
     return cudaGetLastError();
 }
 
-template <typename T, bool KEPT>
+template <typename T, bool KEPT, bool LEAN>
 cudaError_t dispatch_grad_ring(const NormGradParams& p, int sms, cudaStream_t s, int* ctas) {
     constexpr int M = 8 / kVec<T>;
     const int nv = p.dim / kVec<T> / M;
-    if (nv <= 32) return launch_grad_ring<T, 32, M, KEPT>(p, sms, s, ctas);
-    if (nv <= 64) return launch_grad_ring<T, 32, 2 * M, KEPT>(p, sms, s, ctas);
-    if (nv <= 96) return launch_grad_ring<T, 32, 3 * M, KEPT>(p, sms, s, ctas);
-    if (nv <= 128) return launch_grad_ring<T, 64, 2 * M, KEPT>(p, sms, s, ctas);
-    if (nv <= 256) return launch_grad_ring<T, 128, 2 * M, KEPT>(p, sms, s, ctas);
-    if (nv <= 512) return launch_grad_ring<T, 256, 2 * M, KEPT>(p, sms, s, ctas);
-    if (nv <= 1024) return launch_grad_ring<T, 512, 2 * M, KEPT>(p, sms, s, ctas);
-    return launch_grad_ring<T, 512, 4 * M, KEPT>(p, sms, s, ctas);
+    if (nv <= 32) return launch_grad_ring<T, 32, M, KEPT, LEAN>(p, sms, s, ctas);
+    if (nv <= 64) return launch_grad_ring<T, 32, 2 * M, KEPT, LEAN>(p, sms, s, ctas);
+    if (nv <= 96) return launch_grad_ring<T, 32, 3 * M, KEPT, LEAN>(p, sms, s, ctas);
+    if (nv <= 128) return launch_grad_ring<T, 64, 2 * M, KEPT, LEAN>(p, sms, s, ctas);
+    if (nv <= 256) return launch_grad_ring<T, 128, 2 * M, KEPT, LEAN>(p, sms, s, ctas);
+    if (nv <= 512) return launch_grad_ring<T, 256, 2 * M, KEPT, LEAN>(p, sms, s, ctas);
+    if (nv <= 1024) return launch_grad_ring<T, 512, 2 * M, KEPT, LEAN>(p, sms, s, ctas);
+    return launch_grad_ring<T, 512, 4 * M, KEPT, LEAN>(p, sms, s, ctas);
 }
 
 template <typename T, int G, int VPT, bool VEC>
@@ -1173,8 +1195,12 @@ extern "C" lc_status lc_norm_grad(int device, void* cuda_stream, int32_t kind, c
     using B = __nv_bfloat16;
     int ctas = 0;
     if (vec && dim * e % 16 == 0 && ntok >= kRingRows * sms) {
-        if (dy->dtype == LC_BF16) err = x ? dispatch_grad_ring<B, false>(p, sms, s, &ctas) : dispatch_grad_ring<B, true>(p, sms, s, &ctas);
-        else err = x ? dispatch_grad_ring<float, false>(p, sms, s, &ctas) : dispatch_grad_ring<float, true>(p, sms, s, &ctas);
+        const bool lean = kind == LC_NORM_RMS && !dbias, bf = dy->dtype == LC_BF16;
+        auto go = [&](auto f) { err = f(p, sms, s, &ctas); };
+        if (bf && x) go(lean ? dispatch_grad_ring<B, false, true> : dispatch_grad_ring<B, false, false>);
+        else if (bf) go(lean ? dispatch_grad_ring<B, true, true> : dispatch_grad_ring<B, true, false>);
+        else if (x) go(lean ? dispatch_grad_ring<float, false, true> : dispatch_grad_ring<float, false, false>);
+        else go(lean ? dispatch_grad_ring<float, true, true> : dispatch_grad_ring<float, true, false>);
     }
     if (ctas || err != cudaSuccess) {
         // through the rings
