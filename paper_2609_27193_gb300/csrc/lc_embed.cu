@@ -143,43 +143,61 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(SortParams p) 
         for (int64_t i = int64_t(rank) * kSortThreads + threadIdx.x; i < words; i += int64_t(nc) * kSortThreads)
             p.present[i] = 0;
     }
+    constexpr int U = 4;                       // items of a lane that are asked for at once
+    const bool once = hi - lo <= 32 * U;       // all of the warp's items: they stay in registers
     for (int pass = 0; pass < p.passes; ++pass) {
         const int shift = pass * p.digit;
         const uint32_t* ksrc = p.key[(pass & 1) ^ 1];
         const uint32_t* psrc = p.pos[(pass & 1) ^ 1];
-        auto key_at = [&](int64_t i) -> uint32_t {
-            if (pass) return __ldcg(ksrc + i);
-            const int64_t id = int64_t(static_cast<const I*>(p.ids)[i]);
-            return uint32_t(id >= 0 && id < p.vocab && id != p.skip ? id : p.vocab);
+        uint32_t key[U], pos[U];
+        auto load = [&](int64_t at) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int64_t i = at + u * 32 + lane;
+                key[u] = 0;
+                if (i >= hi) continue;
+                if (pass) {
+                    key[u] = __ldcg(ksrc + i);
+                    pos[u] = __ldcg(psrc + i);
+                } else {
+                    const int64_t id = int64_t(static_cast<const I*>(p.ids)[i]);
+                    key[u] = uint32_t(id >= 0 && id < p.vocab && id != p.skip ? id : p.vocab);
+                    pos[u] = uint32_t(i);
+                }
+            }
         };
         for (int b = lane; b < bins; b += 32) cnt[b] = 0;
         __syncwarp();
-        for (int64_t i = lo; i < hi; i += 32) {
-            const bool in = i + lane < hi;
-            const uint32_t d = in ? (key_at(i + lane) >> shift) & uint32_t(bins - 1) : ~0u;
-            const uint32_t same = __match_any_sync(0xffffffffu, d);
-            if (in && lane == __ffs(same) - 1) cnt[d] += __popc(same);
-            __syncwarp();
+        for (int64_t at = lo; at < hi; at += 32 * U) {
+            load(at);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (at + u * 32 + lane < hi) atomicAdd(cnt + ((key[u] >> shift) & uint32_t(bins - 1)), 1u);
         }
         __syncthreads();
-        for (int b = threadIdx.x; b < bins; b += kSortThreads) {
-            uint32_t s = 0;
-            for (int w = 0; w < kSortWarps; ++w) {
-                const uint32_t c = sm[w * bins + b];
-                sm[w * bins + b] = s;
-                s += c;
-            }
-            tot[b] = s;
+        // a thread a digit value (bins <= kSortThreads): its counts over the warps
+        const bool mine = int(threadIdx.x) < bins;
+        uint32_t c[kSortWarps];
+        uint32_t sum = 0;
+        if (mine) {
+#pragma unroll
+            for (int w = 0; w < kSortWarps; ++w) c[w] = sm[w * bins + threadIdx.x];
+#pragma unroll
+            for (int w = 0; w < kSortWarps; ++w) sum += c[w];
+            tot[threadIdx.x] = sum;
         }
         cluster.sync();
-        // bins <= kSortThreads: a thread a digit value
         uint32_t before = 0, all = 0;
-        if (int(threadIdx.x) < bins)
-            for (int r = 0; r < nc; ++r) {
-                const uint32_t t = cluster.map_shared_rank(tot, r)[threadIdx.x];
-                if (r < rank) before += t;
-                all += t;
+        if (mine) {
+            uint32_t other[kSortCluster];
+#pragma unroll
+            for (int r = 0; r < kSortCluster; ++r) other[r] = r < nc ? cluster.map_shared_rank(tot, r)[threadIdx.x] : 0;
+#pragma unroll
+            for (int r = 0; r < kSortCluster; ++r) {
+                if (r < rank) before += other[r];
+                all += other[r];
             }
+        }
         uint32_t scan = all;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -188,26 +206,37 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(SortParams p) 
         }
         if (lane == 31) warp_sum[warp] = scan;
         __syncthreads();
-        uint32_t base = before + scan - all;
-        for (int w = 0; w < warp; ++w) base += warp_sum[w];
-        if (int(threadIdx.x) < bins)
-            for (int w = 0; w < kSortWarps; ++w) sm[w * bins + threadIdx.x] += base;
+        uint32_t lower = lane < warp ? warp_sum[lane] : 0;       // the warps with smaller digit values
+#pragma unroll
+        for (int o = 16; o; o >>= 1) lower += __shfl_xor_sync(0xffffffffu, lower, o);
+        if (mine) {
+            uint32_t base = before + scan - all + lower;
+#pragma unroll
+            for (int w = 0; w < kSortWarps; ++w) {
+                sm[w * bins + threadIdx.x] = base;
+                base += c[w];
+            }
+        }
         __syncthreads();
         uint32_t* kdst = p.key[pass & 1];
         uint32_t* pdst = p.pos[pass & 1];
-        for (int64_t i = lo; i < hi; i += 32) {
-            const bool in = i + lane < hi;
-            const uint32_t key = in ? key_at(i + lane) : 0u;
-            const uint32_t d = in ? (key >> shift) & uint32_t(bins - 1) : ~0u;
-            const uint32_t same = __match_any_sync(0xffffffffu, d);
-            uint32_t at = 0;
-            if (in) at = cnt[d] + __popc(same & ((1u << lane) - 1));
-            __syncwarp();
-            if (in && lane == __ffs(same) - 1) cnt[d] += __popc(same);
-            __syncwarp();
-            if (in) {
-                kdst[at] = key;
-                pdst[at] = pass ? __ldcg(psrc + i + lane) : uint32_t(i + lane);
+        for (int64_t at = lo; at < hi; at += 32 * U) {
+            if (!once) load(at);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (at + u * 32 >= hi) break;
+                const bool in = at + u * 32 + lane < hi;
+                const uint32_t d = in ? (key[u] >> shift) & uint32_t(bins - 1) : ~0u;
+                const uint32_t same = __match_any_sync(0xffffffffu, d);
+                const int first = __ffs(same) - 1;
+                uint32_t to = 0;
+                if (in && lane == first) to = atomicAdd(cnt + d, uint32_t(__popc(same)));
+                __syncwarp();   // the next items' atomics come after these
+                to = __shfl_sync(0xffffffffu, to, first) + __popc(same & ((1u << lane) - 1));
+                if (in) {
+                    kdst[to] = key[u];
+                    pdst[to] = pos[u];
+                }
             }
         }
         cluster.sync();
@@ -227,34 +256,56 @@ struct SumParams {
     const uint32_t* present;
     const uint8_t* dy;
     uint8_t* grad;
-    float* part;          // [chunks][2][slabs][kSumThreads][E]: a chunk's open rows at its start and end
+    float* part;          // [chunks][2][slabs][G][E]: a chunk's open rows at its start and end
     int64_t n, vocab, dim, dy_pitch, grad_pitch;
-    int64_t chunk, chunks, slabs, sum_ctas, zero_rows;
+    int64_t chunk, chunks, slabs, items, sum_ctas, zero_rows;   // items = chunks * slabs
     float scale;
     int32_t accumulate;
 };
 
-// The columns of a thread: E consecutive ones (16-byte loads of dy), or E that lie
-// kSumThreads apart (single elements).
-template <typename TD, bool VEC>
+// The columns of a thread of a group of G: E consecutive ones (16-byte loads of dy),
+// or E that lie G apart (single elements).
+template <typename TD, bool VEC, int G>
 struct Columns {
     static constexpr int E = VEC ? kVec<TD> : 4;
     int64_t c0;
     int64_t dim;
-    __device__ Columns(int64_t slab, int64_t d)
-        : c0(slab * kSumThreads * E + (VEC ? int(threadIdx.x) * E : int(threadIdx.x))), dim(d) {}
-    __device__ int64_t col(int e) const { return VEC ? c0 + e : c0 + int64_t(e) * kSumThreads; }
+    __device__ Columns(int64_t slab, int64_t d) : c0(slab * G * E + int(threadIdx.x) % G * (VEC ? E : 1)), dim(d) {}
+    __device__ int64_t col(int e) const { return VEC ? c0 + e : c0 + int64_t(e) * G; }
     __device__ bool whole() const { return VEC && c0 + E <= dim; }
-    __device__ void load(const uint8_t* row, float (&f)[E]) const {
+    // A row's part as it lies in memory, and its values: all rows of a batch are asked for before one is unpacked.
+    struct Raw {
+        uint4 v;
+        TD e[VEC ? 1 : E];
+    };
+    __device__ __forceinline__ void load(const uint8_t* row, Raw& raw) const {
         const TD* r = reinterpret_cast<const TD*>(row);
         if constexpr (VEC) {
-            if (whole()) {
-                unpack(ld_stream(r + c0), f);
-                return;
-            }
-        }
+            if (whole()) raw.v = ld_stream(r + c0);
+        } else {
 #pragma unroll
-        for (int e = 0; e < E; ++e) f[e] = col(e) < dim ? to_f32(r[col(e)]) : 0.0f;
+            for (int e = 0; e < E; ++e)
+                if (col(e) < dim) raw.e[e] = r[col(e)];
+        }
+    }
+    __device__ __forceinline__ void add(const uint8_t* row, const Raw& raw, float (&acc)[E]) const {
+        if constexpr (VEC) {
+            if (whole()) {
+                float f[E];
+                unpack(raw.v, f);
+#pragma unroll
+                for (int e = 0; e < E; ++e) acc[e] += f[e];
+            } else {
+                const TD* r = reinterpret_cast<const TD*>(row);
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (col(e) < dim) acc[e] += to_f32(r[col(e)]);
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (col(e) < dim) acc[e] += to_f32(raw.e[e]);
+        }
     }
     // grad = f (+ grad)
     template <typename TG>
@@ -302,37 +353,56 @@ struct Columns {
     }
 };
 
-__device__ __forceinline__ int64_t part_at(const SumParams& p, int64_t chunk, int which, int64_t slab, int E) {
-    return (((chunk * 2 + which) * p.slabs + slab) * kSumThreads + threadIdx.x) * E;
+template <int G, int E>
+__device__ __forceinline__ int64_t part_at(const SumParams& p, int64_t chunk, int which, int64_t slab) {
+    return (((chunk * 2 + which) * p.slabs + slab) * G + int(threadIdx.x) % G) * E;
 }
 
-template <typename TD, typename TG, bool VEC>
+// A group of G threads sums one chunk of the sorted list in G * E columns.
+template <typename TD, typename TG, bool VEC, int G>
 __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(SumParams p) {
-    using Cols = Columns<TD, VEC>;
+    using Cols = Columns<TD, VEC, G>;
     constexpr int E = Cols::E;
     constexpr int U = 8;   // rows in flight
     dependency_wait();
     dependents_may_start();
+    const int lane = threadIdx.x & 31;
     if (int64_t(blockIdx.x) >= p.sum_ctas) {
-        // rows without a token
+        // rows without a token: a warp at a time asks for the bits of up to 32 rows and clears what it finds
         const int64_t r0 = (int64_t(blockIdx.x) - p.sum_ctas) * p.zero_rows;
         const int64_t r1 = r0 + p.zero_rows < p.vocab ? r0 + p.zero_rows : p.vocab;
         const int64_t bytes = p.dim * int64_t(sizeof(TG));
-        for (int64_t r = r0; r < r1; ++r) {
-            if (p.present[r / 32] >> (r & 31) & 1) continue;
-            uint8_t* row = p.grad + r * p.grad_pitch;
-            int64_t done = 0;
-            if constexpr (VEC) {
+        const int warp = threadIdx.x >> 5;
+        constexpr int W = kSumThreads / 32;
+        for (int64_t first = r0; first < r1; first += 32) {
+            const int64_t mine = first + lane;
+            uint32_t empty = __ballot_sync(0xffffffffu, mine < r1 && !(p.present[(mine < r1 ? mine : first) / 32] >> (mine & 31) & 1));
+            const bool whole = VEC && bytes % 16 == 0;
+            if (whole) {
+                // the warp's share of all the rows' vectors
                 const int64_t nv = bytes / 16;
-                for (int64_t i = threadIdx.x; i < nv; i += kSumThreads) st_stream(row + i * 16, make_uint4(0, 0, 0, 0));
-                done = nv * 16;
+                while (empty) {
+                    const int64_t r = first + __ffs(empty) - 1;
+                    empty &= empty - 1;
+                    uint8_t* row = p.grad + r * p.grad_pitch;
+                    for (int64_t i = threadIdx.x; i < nv; i += kSumThreads) st_stream(row + i * 16, make_uint4(0, 0, 0, 0));
+                }
+                continue;
             }
-            for (int64_t i = done / int64_t(sizeof(TG)) + threadIdx.x; i < p.dim; i += kSumThreads)
-                reinterpret_cast<TG*>(row)[i] = from_f32<TG>(0.0f);
+            for (int k = 0; empty; ++k) {
+                const int64_t r = first + __ffs(empty) - 1;
+                empty &= empty - 1;
+                if (k % W != warp) continue;
+                TG* row = reinterpret_cast<TG*>(p.grad + r * p.grad_pitch);
+                for (int64_t i = lane; i < p.dim; i += 32) row[i] = from_f32<TG>(0.0f);
+            }
         }
         return;
     }
-    const int64_t chunk = blockIdx.x / p.slabs, slab = blockIdx.x % p.slabs;
+    const int64_t item = int64_t(blockIdx.x) * (kSumThreads / G) + int(threadIdx.x) / G;
+    if (item >= p.items) return;
+    int64_t chunk, slab;
+    split_item(item, p.slabs, chunk, slab);
     const Cols cols(slab, p.dim);
     const int64_t s0 = chunk * p.chunk;
     const int64_t s1 = s0 + p.chunk < p.n ? s0 + p.chunk : p.n;
@@ -340,80 +410,125 @@ __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(SumParams p) {
     float acc[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) acc[e] = 0.0f;
-    uint32_t key = p.key[s0];
-    bool open = s0 > 0 && p.key[s0 - 1] == key;   // the row began in an earlier chunk
-    for (int64_t s = s0; s < s1; s += U) {
-        uint32_t k[U + 1];
-        float f[U][E];
+    // 32 entries of the list at a time, one a lane; the next ones are asked for early
+    auto entry = [&](int64_t s, uint32_t& key, uint32_t& pos) {
+        key = s < p.n && s <= s1 ? p.key[s] : none;
+        pos = s < s1 ? p.pos[s] : 0;
+    };
+    uint32_t key_next, pos_next;
+    entry(s0 + lane, key_next, pos_next);
+    const uint32_t before = s0 > 0 ? p.key[s0 - 1] : none;
+    bool open = __shfl_sync(0xffffffffu, key_next, 0) == before;   // the row began in an earlier chunk
+    for (int64_t base = s0; base < s1; base += 32) {
+        const uint32_t key32 = key_next, pos32 = pos_next;
+        if (__shfl_sync(0xffffffffu, key32, 0) == none) break;     // sorted last: nothing more contributes
+        entry(base + 32 + lane, key_next, pos_next);
+        const uint32_t after = __shfl_sync(0xffffffffu, key_next, 0);
+#pragma unroll 1
+        for (int part = 0; part < 32; part += U) {
+            if (base + part >= s1) break;
+            typename Cols::Raw raw[U];
+            uint32_t k[U + 1], at[U];
 #pragma unroll
-        for (int u = 0; u <= U; ++u) k[u] = s + u < p.n && s + u <= s1 ? p.key[s + u] : none;
-        if (k[0] == none) break;   // sorted last: nothing more contributes
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (s + u < s1 && k[u] != none) cols.load(p.dy + int64_t(p.pos[s + u]) * p.dy_pitch, f[u]);
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (s + u >= s1 || k[u] == none) break;
-#pragma unroll
-            for (int e = 0; e < E; ++e) acc[e] += f[u][e];
-            const bool last = s + u + 1 >= s1;
-            const uint32_t next = k[u + 1];
-            if (next == k[u] && !last) continue;
-            if (open || (last && next == k[u])) {
-                float* out = p.part + part_at(p, chunk, open ? 0 : 1, slab, E);
-#pragma unroll
-                for (int e = 0; e < E; ++e) out[e] = acc[e];
-            } else {
-#pragma unroll
-                for (int e = 0; e < E; ++e) acc[e] *= p.scale;
-                cols.template store<TG>(p.grad + int64_t(k[u]) * p.grad_pitch, acc, p.accumulate != 0);
+            for (int u = 0; u < U; ++u) {
+                k[u] = __shfl_sync(0xffffffffu, key32, part + u);
+                at[u] = __shfl_sync(0xffffffffu, pos32, part + u);
+                if (base + part + u < s1 && k[u] != none) cols.load(p.dy + int64_t(at[u]) * p.dy_pitch, raw[u]);
             }
-            open = false;
+            k[U] = part + U < 32 ? __shfl_sync(0xffffffffu, key32, (part + U) & 31) : after;
 #pragma unroll
-            for (int e = 0; e < E; ++e) acc[e] = 0.0f;
+            for (int u = 0; u < U; ++u) {
+                if (base + part + u >= s1 || k[u] == none) break;
+                cols.add(p.dy + int64_t(at[u]) * p.dy_pitch, raw[u], acc);
+                const bool last = base + part + u + 1 >= s1;
+                const uint32_t next = k[u + 1];
+                if (next == k[u] && !last) continue;
+                if (open || next == k[u]) {
+                    float* out = p.part + part_at<G, E>(p, chunk, open ? 0 : 1, slab);
+#pragma unroll
+                    for (int e = 0; e < E; e += 4) *reinterpret_cast<float4*>(out + e) = make_float4(acc[e], acc[e + 1], acc[e + 2], acc[e + 3]);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < E; ++e) acc[e] *= p.scale;
+                    cols.template store<TG>(p.grad + int64_t(k[u]) * p.grad_pitch, acc, p.accumulate != 0);
+                }
+                open = false;
+#pragma unroll
+                for (int e = 0; e < E; ++e) acc[e] = 0.0f;
+            }
         }
     }
 }
 
-// Rows that cross chunks: the CTA of the chunk in which the row begins adds its
-// parts in order.
-template <typename TD, typename TG, bool VEC>
-__global__ void __launch_bounds__(kSumThreads) embed_join_kernel(SumParams p) {
-    using Cols = Columns<TD, VEC>;
-    constexpr int E = Cols::E;
-    constexpr int U = 8;
+// Rows that cross chunks.  The CTA of the chunk in which such a row begins adds its
+// parts: its groups take equal runs of them, and the groups' sums are added in order.
+constexpr int kJoinThreads = 512;
+template <typename TD, typename TG, bool VEC, int G>
+__global__ void __launch_bounds__(kJoinThreads) embed_join_kernel(SumParams p) {
+    using Cols = Columns<TD, VEC, G>;
+    constexpr int E = Cols::E, R = kJoinThreads / G;
+    constexpr int U = 4;
+    __shared__ float4 sums[kJoinThreads][E / 4];
     dependency_wait();
-    const int64_t chunk = blockIdx.x / p.slabs, slab = blockIdx.x % p.slabs;
+    int64_t chunk, slab;
+    split_item(blockIdx.x, p.slabs, chunk, slab);
     const int64_t s0 = chunk * p.chunk, s1 = s0 + p.chunk;
     if (s1 >= p.n) return;
-    const uint32_t key = p.key[s1];
-    if (key == uint32_t(p.vocab) || p.key[s1 - 1] != key) return;              // no row crosses this chunk's end
-    if (s0 > 0 && p.key[s0 - 1] == key) return;                                // it began in an earlier chunk
-    // chunks c in (chunk, last] begin with this row: the largest one, by bisection
-    int64_t lo = chunk + 1, hi = p.chunks - 1;
-    while (lo < hi) {
-        const int64_t mid = (lo + hi + 1) / 2;
-        if (p.key[mid * p.chunk] == key) lo = mid;
-        else hi = mid - 1;
+    const uint32_t key = p.key[s1], last = p.key[s1 - 1], before = s0 > 0 ? p.key[s0 - 1] : uint32_t(p.vocab);
+    if (key == uint32_t(p.vocab) || last != key) return;   // no row crosses this chunk's end
+    if (s0 > 0 && before == key) return;                   // it began in an earlier chunk
+    // chunks c in (chunk, lo] begin with this row: the largest one, by a search that looks at 32 places at a time
+    const int lane = threadIdx.x & 31;
+    int64_t lo = chunk + 1, hi = p.chunks;                 // key[lo * chunk] == key, hi: beyond
+    while (hi - lo > 1) {
+        const int64_t gap = (hi - lo + 31) / 32, c = lo + gap * (lane + 1);
+        const uint32_t same = __ballot_sync(0xffffffffu, c < hi && p.key[c * p.chunk] == key);
+        const int64_t n = __popc(same);                    // sorted: the first n of them
+        const int64_t top = lo + gap * (n + 1);
+        lo += gap * n;
+        hi = top < hi ? top : hi;
     }
-    const int64_t stride = p.slabs * 2 * kSumThreads * E;
-    const float* first = p.part + part_at(p, chunk, 1, slab, E);
-    const float* rest = p.part + part_at(p, chunk + 1, 0, slab, E);
-    const int64_t m = lo - chunk;
+    const int64_t stride = p.slabs * 2 * G * E;
+    const int group = threadIdx.x / G;
+    const int64_t m = lo - chunk + 1;                      // parts: the chunk's last row, then the others' first
+    const int64_t per = (m + R - 1) / R;
+    const int64_t i0 = group * per < m ? group * per : m, i1 = i0 + per < m ? i0 + per : m;
+    const float* first = p.part + part_at<G, E>(p, chunk, 1, slab);
+    const float* rest = p.part + part_at<G, E>(p, chunk, 0, slab);
     float acc[E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) acc[e] = first[e];
-    for (int64_t i = 0; i < m; i += U) {
-        float f[U][E];
+    for (int e = 0; e < E; ++e) acc[e] = 0.0f;
+    for (int64_t i = i0; i < i1; i += U) {
+        float4 f[U][E / 4];
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int e = 0; e < E; ++e) f[u][e] = i + u < m ? rest[(i + u) * stride + e] : 0.0f;
+            for (int e = 0; e < E / 4; ++e)
+                f[u][e] = i + u < i1 ? reinterpret_cast<const float4*>(i + u ? rest + (i + u) * stride : first)[e]
+                                     : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int e = 0; e < E; ++e) acc[e] += f[u][e];
+            for (int e = 0; e < E / 4; ++e) {
+                acc[4 * e] += f[u][e].x;
+                acc[4 * e + 1] += f[u][e].y;
+                acc[4 * e + 2] += f[u][e].z;
+                acc[4 * e + 3] += f[u][e].w;
+            }
     }
+#pragma unroll
+    for (int e = 0; e < E / 4; ++e) sums[threadIdx.x][e] = make_float4(acc[4 * e], acc[4 * e + 1], acc[4 * e + 2], acc[4 * e + 3]);
+    __syncthreads();
+    if (group) return;
+    for (int g = 1; g < R && g * per < m; ++g)
+#pragma unroll
+        for (int e = 0; e < E / 4; ++e) {
+            const float4 f = sums[g * G + threadIdx.x][e];
+            acc[4 * e] += f.x;
+            acc[4 * e + 1] += f.y;
+            acc[4 * e + 2] += f.z;
+            acc[4 * e + 3] += f.w;
+        }
 #pragma unroll
     for (int e = 0; e < E; ++e) acc[e] *= p.scale;
     const Cols cols(slab, p.dim);
@@ -422,11 +537,11 @@ __global__ void __launch_bounds__(kSumThreads) embed_join_kernel(SumParams p) {
 
 constexpr size_t al256(size_t x) { return (x + 255) & ~size_t(255); }
 
-// Chunks of the sorted list: long enough to fill the device a few times over, at
-// most 1024 of them beyond that, so that a row which all tokens share is joined
-// from no more parts.
+// Chunks of the sorted list: whole batches of 8 rows, long enough to fill the device
+// a few times over, and no more than 1024 of them beyond that, so that a row which
+// all tokens share is joined from no more parts.
 int64_t chunk_of(int64_t n, int64_t slabs) {
-    int64_t c = n * slabs / 2432;
+    int64_t c = n * slabs / 4864;
     if (c < n / 1024) c = n / 1024;
     c = (c + 7) / 8 * 8;
     return c < 8 ? 8 : c;
@@ -452,16 +567,35 @@ GradLayout grad_layout(int64_t n, int64_t vocab, int64_t part_floats) {
     return l;
 }
 
+// The group of threads that takes a chunk: as many as a row's columns need, up to
+// kSumThreads; wider rows are cut into slabs.
 struct SumShape {
-    int64_t slabs, chunk, chunks, part_floats;
+    int64_t group, slabs, chunk, chunks, part_floats;
 };
 SumShape sum_shape(int64_t n, int64_t dim, int E) {
     SumShape s;
-    s.slabs = (dim + kSumThreads * E - 1) / (kSumThreads * E);
+    s.group = dim <= 32 * E ? 32 : dim <= 64 * E ? 64 : kSumThreads;
+    s.slabs = (dim + s.group * E - 1) / (s.group * E);
     s.chunk = chunk_of(n, s.slabs);
     s.chunks = (n + s.chunk - 1) / s.chunk;
-    s.part_floats = s.chunks * 2 * s.slabs * kSumThreads * E;
+    s.part_floats = s.chunks * 2 * s.slabs * s.group * E;
     return s;
+}
+
+template <typename TD, typename TG, bool VEC, int G>
+cudaError_t launch_group(SumParams p, cudaStream_t s) {
+    p.sum_ctas = (p.items + kSumThreads / G - 1) / (kSumThreads / G);
+    int64_t zero = 0;
+    if (!p.accumulate) {
+        // 16 KB a CTA, whole words of the bitmap where rows are that short
+        p.zero_rows = 16384 / (p.dim * int64_t(sizeof(TG)));
+        p.zero_rows = p.zero_rows < 1 ? 1 : p.zero_rows > 32 ? p.zero_rows / 32 * 32 : p.zero_rows;
+        zero = (p.vocab + p.zero_rows - 1) / p.zero_rows;
+    }
+    cudaError_t e = launch_dependent(embed_sum_kernel<TD, TG, VEC, G>, int(p.sum_ctas + zero), kSumThreads, 0, s, p);
+    if (e == cudaSuccess && p.chunks > 1)
+        e = launch_dependent(embed_join_kernel<TD, TG, VEC, G>, int(p.items), kJoinThreads, 0, s, p);
+    return e;
 }
 
 template <typename TD, typename TG, bool VEC>
@@ -469,17 +603,10 @@ cudaError_t launch_sum(SumParams p, const SumShape& sh, cudaStream_t s) {
     p.slabs = sh.slabs;
     p.chunk = sh.chunk;
     p.chunks = sh.chunks;
-    p.sum_ctas = sh.chunks * sh.slabs;
-    int64_t zero = 0;
-    if (!p.accumulate) {
-        p.zero_rows = 65536 / (p.dim * int64_t(sizeof(TG)));
-        p.zero_rows = p.zero_rows < 1 ? 1 : p.zero_rows > 256 ? 256 : p.zero_rows;
-        zero = (p.vocab + p.zero_rows - 1) / p.zero_rows;
-    }
-    cudaError_t e = launch_dependent(embed_sum_kernel<TD, TG, VEC>, int(p.sum_ctas + zero), kSumThreads, 0, s, p);
-    if (e == cudaSuccess && p.chunks > 1)
-        e = launch_dependent(embed_join_kernel<TD, TG, VEC>, int(p.sum_ctas), kSumThreads, 0, s, p);
-    return e;
+    p.items = sh.chunks * sh.slabs;
+    if (sh.group == 32) return launch_group<TD, TG, VEC, 32>(p, s);
+    if (sh.group == 64) return launch_group<TD, TG, VEC, 64>(p, s);
+    return launch_group<TD, TG, VEC, kSumThreads>(p, s);
 }
 
 template <typename I>
