@@ -26,7 +26,8 @@ constexpr int kSortThreads = 1024;
 constexpr int kSortWarps = kSortThreads / 32;
 constexpr int kSortCluster = 8;
 constexpr int kSortBits = 9;                 // digits of at most 9 bits
-constexpr int64_t kSortAlone = 2048;         // up to this many tokens one CTA sorts
+constexpr int64_t kSortPer = 2048;           // tokens of a CTA before the cluster grows
+constexpr int64_t kSortShared = 65536;       // up to this many tokens the list stays in shared memory
 constexpr int kSumThreads = 128;
 constexpr int64_t kMaxTokens = int64_t(1) << 31;
 
@@ -110,32 +111,42 @@ cudaError_t launch_embed(EmbedParams p, int sms, cudaStream_t s) {
 struct SortParams {
     const void* ids;
     int64_t n, vocab, skip;
-    uint32_t* key[2];
+    uint32_t* key[2];      // [1]: the sorted list; [0]: between passes (lists that do not stay in shared memory)
     uint32_t* pos[2];
     uint32_t* present;     // bitmap of the rows that have a token (null: not wanted)
     int32_t digit, passes; // bits of a digit, digits
+    int64_t cap;           // places of a CTA in the list, a multiple of 1024 (SHARED: 1 << cap_log2)
+    int32_t cap_log2;
 };
 
 // Sorts the tokens by id: least significant digit first, each pass a stable
 // counting sort.  One cluster does it all: every warp owns a contiguous range of
-// the list, counts its digits (lanes with the same digit find one another by
-// match), the counts become offsets by sums over the warps, the cluster's CTAs
-// (distributed shared memory) and the digits, and the warp hands its items out in
-// order.  Tokens that contribute nothing get the key `vocab` and end up last.
-template <typename I>
+// the list, counts its digits, the counts become offsets by sums over the warps, the
+// cluster's CTAs (distributed shared memory) and the digits, and the warp hands its
+// items out in order (lanes with the same digit find one another by match).  Tokens
+// that contribute nothing get the key `vocab` and end up last.
+//   SHARED: between passes an item goes straight to its next place in the shared
+// memory of the CTA that has it there; a list in global memory costs a trip there
+// and a fence of the whole cluster a pass (16381 tokens: 18 us that way, @@ so).
+template <typename I, bool SHARED>
 __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(SortParams p) {
-    extern __shared__ uint32_t sm[];
+    extern __shared__ uint32_t sm[];           // counts [warps][digit values], then (SHARED) keys [2][cap], positions [2][cap]
     __shared__ uint32_t tot[1 << kSortBits];
     __shared__ uint32_t warp_sum[kSortWarps];
     dependents_may_start();
     cg::cluster_group cluster = cg::this_cluster();
     const int rank = int(cluster.block_rank()), nc = int(cluster.num_blocks());
+    auto meet = [&]() {
+        if (nc == 1) __syncthreads();
+        else cluster.sync();
+    };
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int bins = 1 << p.digit;
     uint32_t* cnt = sm + warp * bins;
-    int64_t per = (p.n + int64_t(nc) * kSortWarps - 1) / (int64_t(nc) * kSortWarps);
-    per = (per + 31) & ~int64_t(31);
-    int64_t lo = (int64_t(rank) * kSortWarps + warp) * per;
+    const int64_t cap = p.cap;
+    uint32_t* list = sm + kSortWarps * bins;
+    const int64_t c0 = rank * cap, per = cap / kSortWarps;
+    int64_t lo = c0 + warp * per;
     lo = lo < p.n ? lo : p.n;
     const int64_t hi = lo + per < p.n ? lo + per : p.n;
     if (p.present) {
@@ -147,22 +158,29 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(SortParams p) 
     const bool once = hi - lo <= 32 * U;       // all of the warp's items: they stay in registers
     for (int pass = 0; pass < p.passes; ++pass) {
         const int shift = pass * p.digit;
-        const uint32_t* ksrc = p.key[(pass & 1) ^ 1];
-        const uint32_t* psrc = p.pos[(pass & 1) ^ 1];
+        const bool last = pass == p.passes - 1;
+        // the list that this pass reads; the one it writes is the other, the last one's always [1]
+        const int to_list = (p.passes - pass) & 1, from = to_list ^ 1;
+        // (an index into the parameters' arrays would put them on the stack)
+        const uint32_t *key_from = from ? p.key[1] : p.key[0], *pos_from = from ? p.pos[1] : p.pos[0];
+        uint32_t *key_to = from ? p.key[0] : p.key[1], *pos_to = from ? p.pos[0] : p.pos[1];
         uint32_t key[U], pos[U];
         auto load = [&](int64_t at) {
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int64_t i = at + u * 32 + lane;
-                key[u] = 0;
+                key[u] = pos[u] = 0;
                 if (i >= hi) continue;
-                if (pass) {
-                    key[u] = __ldcg(ksrc + i);
-                    pos[u] = __ldcg(psrc + i);
-                } else {
+                if (pass == 0) {
                     const int64_t id = int64_t(static_cast<const I*>(p.ids)[i]);
                     key[u] = uint32_t(id >= 0 && id < p.vocab && id != p.skip ? id : p.vocab);
                     pos[u] = uint32_t(i);
+                } else if constexpr (SHARED) {
+                    key[u] = list[from * cap + (i - c0)];
+                    pos[u] = list[(2 + from) * cap + (i - c0)];
+                } else {
+                    key[u] = __ldcg(key_from + i);
+                    pos[u] = __ldcg(pos_from + i);
                 }
             }
         };
@@ -177,16 +195,13 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(SortParams p) 
         __syncthreads();
         // a thread a digit value (bins <= kSortThreads): its counts over the warps
         const bool mine = int(threadIdx.x) < bins;
-        uint32_t c[kSortWarps];
-        uint32_t sum = 0;
         if (mine) {
-#pragma unroll
-            for (int w = 0; w < kSortWarps; ++w) c[w] = sm[w * bins + threadIdx.x];
-#pragma unroll
-            for (int w = 0; w < kSortWarps; ++w) sum += c[w];
+            uint32_t sum = 0;
+#pragma unroll 8
+            for (int w = 0; w < kSortWarps; ++w) sum += sm[w * bins + threadIdx.x];
             tot[threadIdx.x] = sum;
         }
-        cluster.sync();
+        meet();
         uint32_t before = 0, all = 0;
         if (mine) {
             uint32_t other[kSortCluster];
@@ -211,15 +226,20 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(SortParams p) 
         for (int o = 16; o; o >>= 1) lower += __shfl_xor_sync(0xffffffffu, lower, o);
         if (mine) {
             uint32_t base = before + scan - all + lower;
+            // 8 at a time: more would not stay in registers, and local memory is far away here
+#pragma unroll 1
+            for (int w = 0; w < kSortWarps; w += 8) {
+                uint32_t c[8];
 #pragma unroll
-            for (int w = 0; w < kSortWarps; ++w) {
-                sm[w * bins + threadIdx.x] = base;
-                base += c[w];
+                for (int k = 0; k < 8; ++k) c[k] = sm[(w + k) * bins + threadIdx.x];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    sm[(w + k) * bins + threadIdx.x] = base;
+                    base += c[k];
+                }
             }
         }
         __syncthreads();
-        uint32_t* kdst = p.key[pass & 1];
-        uint32_t* pdst = p.pos[pass & 1];
         for (int64_t at = lo; at < hi; at += 32 * U) {
             if (!once) load(at);
 #pragma unroll
@@ -233,20 +253,22 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(SortParams p) 
                 if (in && lane == first) to = atomicAdd(cnt + d, uint32_t(__popc(same)));
                 __syncwarp();   // the next items' atomics come after these
                 to = __shfl_sync(0xffffffffu, to, first) + __popc(same & ((1u << lane) - 1));
-                if (in) {
-                    kdst[to] = key[u];
-                    pdst[to] = pos[u];
+                if (!in) continue;
+                // the bitmap was cleared before the pass's first meeting
+                if (pass == 0 && p.present && key[u] < p.vocab) atomicOr(p.present + key[u] / 32, 1u << (key[u] & 31));
+                if (last || !SHARED) {
+                    key_to[to] = key[u];
+                    pos_to[to] = pos[u];
+                } else {
+                    uint32_t* there = cluster.map_shared_rank(list, int(to >> p.cap_log2));
+                    const int64_t slot = to & uint32_t(cap - 1);
+                    there[to_list * cap + slot] = key[u];
+                    there[(2 + to_list) * cap + slot] = pos[u];
                 }
             }
         }
-        cluster.sync();
-    }
-    if (p.present) {
-        const uint32_t* key = p.key[(p.passes - 1) & 1];
-        for (int64_t i = lo + lane; i < hi; i += 32) {
-            const uint32_t k = __ldcg(key + i);
-            if (k < p.vocab && (i == 0 || __ldcg(key + i - 1) != k)) atomicOr(p.present + k / 32, 1u << (k & 31));
-        }
+        // the next pass reads what this one wrote; after the last, no CTA leaves while another reads its totals
+        meet();
     }
 }
 
@@ -467,7 +489,7 @@ template <typename TD, typename TG, bool VEC, int G>
 __global__ void __launch_bounds__(kJoinThreads) embed_join_kernel(SumParams p) {
     using Cols = Columns<TD, VEC, G>;
     constexpr int E = Cols::E, R = kJoinThreads / G;
-    constexpr int U = 4;
+    constexpr int U = 8;
     __shared__ float4 sums[kJoinThreads][E / 4];
     dependency_wait();
     int64_t chunk, slab;
@@ -609,33 +631,37 @@ cudaError_t launch_sum(SumParams p, const SumShape& sh, cudaStream_t s) {
     return launch_group<TD, TG, VEC, kSumThreads>(p, s);
 }
 
-template <typename I>
-cudaError_t launch_sort(const SortParams& p, cudaStream_t s) {
-    const size_t smem = size_t(kSortWarps) * (size_t(1) << p.digit) * 4;
+template <typename I, bool SHARED>
+cudaError_t launch_sort(SortParams p, cudaStream_t s) {
     static bool ready[kOpsMaxDevices];
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
+    const size_t counts = size_t(kSortWarps) * 4;
     if (!ready[dev]) {
-        e = cudaFuncSetAttribute(embed_sort_kernel<I>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                 kSortWarps * (1 << kSortBits) * 4);
+        e = cudaFuncSetAttribute(embed_sort_kernel<I, SHARED>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                 int((counts << kSortBits) + (SHARED ? kSortShared / kSortCluster * 16 : 0)));
         if (e != cudaSuccess) return e;
         ready[dev] = true;
     }
+    unsigned nc = 1;
+    while (nc < kSortCluster && p.n > kSortPer * int64_t(nc)) nc *= 2;
+    p.cap_log2 = 10;
+    while (int64_t(nc) << p.cap_log2 < p.n) ++p.cap_log2;
+    p.cap = SHARED ? int64_t(1) << p.cap_log2 : (p.n + nc * 1024 - 1) / (nc * 1024) * 1024;
     cudaLaunchAttribute attr{};
     attr.id = cudaLaunchAttributeClusterDimension;
-    const unsigned nc = p.n <= kSortAlone ? 1 : kSortCluster;
     attr.val.clusterDim.x = nc;
     attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
     cudaLaunchConfig_t c{};
     c.gridDim = dim3(nc);
     c.blockDim = dim3(kSortThreads);
-    c.dynamicSmemBytes = smem;
+    c.dynamicSmemBytes = (counts << p.digit) + (SHARED ? size_t(16) << p.cap_log2 : 0);
     c.stream = s;
     c.attrs = &attr;
     c.numAttrs = 1;
     cudaGetLastError();
-    return cudaLaunchKernelEx(&c, embed_sort_kernel<I>, p);
+    return cudaLaunchKernelEx(&c, embed_sort_kernel<I, SHARED>, p);
 }
 
 int64_t row_bytes(const lc_rows* r) { return r->stride * elem_size(r->dtype); }
@@ -753,11 +779,13 @@ extern "C" lc_status lc_embed_grad(int device, void* cuda_stream, const lc_rows*
     q.present = accumulate ? nullptr : reinterpret_cast<uint32_t*>(ws + l.present);
     q.passes = (bits + kSortBits - 1) / kSortBits;
     q.digit = (bits + q.passes - 1) / q.passes;
-    cudaError_t e = id_type == LC_I32 ? launch_sort<int32_t>(q, s) : launch_sort<int64_t>(q, s);
+    cudaError_t e;
+    if (ntok <= kSortShared) e = id_type == LC_I32 ? launch_sort<int32_t, true>(q, s) : launch_sort<int64_t, true>(q, s);
+    else e = id_type == LC_I32 ? launch_sort<int32_t, false>(q, s) : launch_sort<int64_t, false>(q, s);
     if (e != cudaSuccess) return ops_launched(call, e);
     SumParams p{};
-    p.key = q.key[(q.passes - 1) & 1];
-    p.pos = q.pos[(q.passes - 1) & 1];
+    p.key = q.key[1];
+    p.pos = q.pos[1];
     p.present = q.present;
     p.dy = static_cast<const uint8_t*>(dy->data);
     p.grad = static_cast<uint8_t*>(grad->data);

@@ -132,7 +132,8 @@ def make_ids(g, t, v, how):
 @pytest.mark.parametrize("how", IDS)
 @pytest.mark.parametrize("t,v,d,dt,gt", [
     (1, 1, 1, F32, F32), (1, 511, 64, BF, F32), (33, 512, 129, BF, BF), (777, 513, 256, F32, BF),
-    (2048, 8000, 256, BF, F32), (2049, 131072, 24, F32, F32), (20011, 40, 1030, BF, BF), (5000, 262145, 8, BF, F32)])
+    (2048, 8000, 256, BF, F32), (2049, 131072, 24, F32, F32), (20011, 40, 1030, BF, BF), (5000, 262145, 8, BF, F32), (8193, 600, 64, F32, F32), (65536, 128256, 8, BF, BF),
+    (70001, 300, 8, BF, F32), (140000, 70000, 16, BF, F32)])
 def test_embed_grad(ops, how, t, v, d, dt, gt):
     g = gen(t + v)
     dy = randn(g, t, d, dtype=dt)
