@@ -79,25 +79,31 @@ def _rows(t, name):
     return lc_rows(t.data_ptr(), stride[0], code, 0)
 
 
-def _on(device, *tensors):
-    if device.type != "cuda":
+def _on(first, *tensors):
+    """The device index that all of them are on."""
+    index = first.get_device()
+    if index < 0:
         raise ValueError("the operators need CUDA tensors")
     for t in tensors:
-        if t is not None and t.device != device:
-            raise ValueError("every tensor must be on %s" % device)
-    return device.index
+        if t is not None and t.get_device() != index:
+            raise ValueError("every tensor must be on %s" % first.device)
+    return index
+
+
+def _like(x):
+    return torch.empty_like(x) if x.is_contiguous() else torch.empty(x.shape, dtype=x.dtype, device=x.device)
 
 
 # the handle of torch's current stream, without a Stream object around it (1 us a call)
 _stream = torch._C._cuda_getCurrentRawStream
 
 
-def _workspace(device, stream, nbytes):
+def _workspace(index, stream, nbytes):
     if not nbytes:
         return None
-    w = _scratch.get((device.index, stream))
+    w = _scratch.get((index, stream))
     if w is None or w.numel() < nbytes:
-        w = _scratch[(device.index, stream)] = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        w = _scratch[(index, stream)] = torch.empty(nbytes, dtype=torch.uint8, device="cuda:%d" % index)
     return w.data_ptr()
 
 
@@ -125,12 +131,11 @@ def _shaped(t, rows, dim, name):
 def embed(table, ids, scale=1.0, out=None):
     """scale * table[ids]: [tokens, dim] in the table's type.  A negative id
     gives a zero row, an id beyond the table a row of NaN."""
-    device = table.device
-    index = _on(device, table, ids, out)
+    index = _on(table, ids, out)
     rt, it = _rows(table, "table"), _ids(ids)
     n, (vocab, dim) = ids.numel(), table.shape
     if out is None:
-        out = torch.empty((n, dim), dtype=table.dtype, device=device)
+        out = torch.empty((n, dim), dtype=table.dtype, device=table.device)
     else:
         _shaped(out, n, dim, "out")
     ro = _rows(out, "out")
@@ -142,8 +147,7 @@ def embed_grad(dy, ids, vocab=None, scale=1.0, grad=None, dtype=None, skip_id=-1
     """The gradient of embed's table, [vocab, dim]: row v is scale times the sum
     of dy over the tokens with id v, in token order; the other rows are zero.
     With accumulate the sums are added to `grad` and the other rows stay."""
-    device = dy.device
-    index = _on(device, dy, ids, grad)
+    index = _on(dy, ids, grad)
     rd, it = _rows(dy, "dy"), _ids(ids)
     n, dim = dy.shape
     if ids.numel() != n:
@@ -153,7 +157,7 @@ def embed_grad(dy, ids, vocab=None, scale=1.0, grad=None, dtype=None, skip_id=-1
             raise ValueError("accumulate needs grad")
         if vocab is None:
             raise ValueError("vocab or grad is needed")
-        grad = torch.empty((vocab, dim), dtype=dtype or dy.dtype, device=device)
+        grad = torch.empty((vocab, dim), dtype=dtype or dy.dtype, device=dy.device)
     else:
         vocab = grad.shape[0]
         _shaped(grad, vocab, dim, "grad")
@@ -161,18 +165,17 @@ def embed_grad(dy, ids, vocab=None, scale=1.0, grad=None, dtype=None, skip_id=-1
     lib, stream = _abi.load(), _stream(index)
     need = lib.lc_embed_grad_workspace(n, vocab, dim)
     check(lib.lc_embed_grad(index, stream, rd, ids.data_ptr(), it, n, scale, skip_id, rg, vocab, dim,
-                            1 if accumulate else 0, _workspace(device, stream, need), need))
+                            1 if accumulate else 0, _workspace(index, stream, need), need))
     return grad
 
 
 def act_save(x, act=None):
     """Keeps x in 8 bits (see Act); `act` is written if given."""
-    device = x.device
-    index = _on(device, x, None if act is None else act.q)
+    index = _on(x, None if act is None else act.q)
     rx = _rows(x, "x")
     n, dim = x.shape
     if act is None:
-        act = Act.empty(n, dim, device)
+        act = Act.empty(n, dim, x.device)
     elif act.rows != n or act.dim != dim:
         raise ValueError("the checkpoint must have %d rows of %d" % (n, dim))
     check(_abi.load().lc_act_save(index, _stream(index), rx, n, dim, act._c()))
@@ -181,11 +184,10 @@ def act_save(x, act=None):
 
 def act_load(act, out=None, dtype=torch.bfloat16):
     """The values of a checkpoint, exact in bfloat16 and in float32."""
-    device = act.q.device
-    index = _on(device, out)
+    index = _on(act.q, out)
     n, dim = act.q.shape[0], act.dim
     if out is None:
-        out = torch.empty((n, dim), dtype=dtype, device=device)
+        out = torch.empty((n, dim), dtype=dtype, device=act.q.device)
     else:
         _shaped(out, n, dim, "out")
     ro = _rows(out, "out")
@@ -202,7 +204,7 @@ def norm(x, weight, bias=None, eps=1e-5, kind="layer", out=None, keep=None):
     new = keep is True
     if new:
         keep = Act.empty(x.shape[0], x.shape[1], device)
-    index = _on(device, x, weight, bias, out, None if keep is None else keep.q)
+    index = _on(x, weight, bias, out, None if keep is None else keep.q)
     rx = _rows(x, "x")
     n, dim = x.shape
     w = _param(weight, dim, "weight")
@@ -212,7 +214,7 @@ def norm(x, weight, bias=None, eps=1e-5, kind="layer", out=None, keep=None):
     if keep is not None and (keep.rows != n or keep.dim != dim):
         raise ValueError("the checkpoint must have %d rows of %d" % (n, dim))
     if out is None:
-        out = torch.empty((n, dim), dtype=x.dtype, device=device)
+        out = _like(x)
     else:
         _shaped(out, n, dim, "out")
     ro = _rows(out, "out")
@@ -233,7 +235,7 @@ def norm_grad(dy, x, weight, mean, rstd, bias=False, dx=None, dweight=None, dbia
     where they are made here; accumulate adds to the ones given."""
     device = dy.device
     kept = isinstance(x, Act)
-    index = _on(device, dy, x.q if kept else x, weight, mean, rstd, dx, dweight, dbias)
+    index = _on(dy, x.q if kept else x, weight, mean, rstd, dx, dweight, dbias)
     rd = _rows(dy, "dy")
     n, dim = dy.shape
     w = _param(weight, dim, "weight")
@@ -245,7 +247,7 @@ def norm_grad(dy, x, weight, mean, rstd, bias=False, dx=None, dweight=None, dbia
     if accumulate and (dweight is None or (bias and dbias is None)):
         raise ValueError("accumulate needs the gradients to add to")
     if dx is None:
-        dx = torch.empty((n, dim), dtype=dy.dtype, device=device)
+        dx = _like(dy)
     else:
         _shaped(dx, n, dim, "dx")
     if dweight is None:
@@ -262,15 +264,14 @@ def norm_grad(dy, x, weight, mean, rstd, bias=False, dx=None, dweight=None, dbia
     check(lib.lc_norm_grad(index, stream, LC_NORM_RMS if mean is None else LC_NORM_LAYER, rd,
                            None if kept else _rows(x, "x"), x._c() if kept else None, n, dim, w,
                            _CODE[weight.dtype], None if mean is None else mean.data_ptr(), rstd.data_ptr(), rdx, pw,
-                           pb, _CODE[dweight.dtype], 1 if accumulate else 0, _workspace(device, stream, need), need))
+                           pb, _CODE[dweight.dtype], 1 if accumulate else 0, _workspace(index, stream, need), need))
     return dx, dweight, dbias
 
 
 def weight_grad(dy, act, grad=None, dtype=torch.float32, accumulate=False):
     """dy^T x for a linear layer's weight [rows of dy, act.dim], with the
     layer's input read from its checkpoint; accumulate adds to `grad`."""
-    device = dy.device
-    index = _on(device, dy, act.q, grad)
+    index = _on(dy, act.q, grad)
     rd = _rows(dy, "dy")
     n, rows = dy.shape
     if act.rows != n:
@@ -278,12 +279,12 @@ def weight_grad(dy, act, grad=None, dtype=torch.float32, accumulate=False):
     if grad is None:
         if accumulate:
             raise ValueError("accumulate needs grad")
-        grad = torch.empty((rows, act.dim), dtype=dtype, device=device)
+        grad = torch.empty((rows, act.dim), dtype=dtype, device=dy.device)
     else:
         _shaped(grad, rows, act.dim, "grad")
     rg = _rows(grad, "grad")
     lib, stream = _abi.load(), _stream(index)
     need = lib.lc_weight_grad_workspace(n, rows, act.dim, rd.dtype)
     check(lib.lc_weight_grad(index, stream, rd, act._c(), n, rows, act.dim, rg, 1 if accumulate else 0,
-                             _workspace(device, stream, need), need))
+                             _workspace(index, stream, need), need))
     return grad
