@@ -127,7 +127,7 @@ struct SortParams {
 // that contribute nothing get the key `vocab` and end up last.
 //   SHARED: between passes an item goes straight to its next place in the shared
 // memory of the CTA that has it there; a list in global memory costs a trip there
-// and a fence of the whole cluster a pass (16381 tokens: 18 us that way, @@ so).
+// and a fence of the whole cluster a pass (16381 tokens: 18 us that way, 13 so).
 template <typename I, bool SHARED>
 __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(SortParams p) {
     extern __shared__ uint32_t sm[];           // counts [warps][digit values], then (SHARED) keys [2][cap], positions [2][cap]

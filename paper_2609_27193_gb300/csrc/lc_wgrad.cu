@@ -191,6 +191,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     const uint32_t tiles = (smem_addr(raw) + 1023) & ~1023u;
     const uint32_t full = smem_addr(bars), empty = full + 8 * kStages, converted = empty + 8 * kStages;
     const uint32_t summed = converted + 8 * kStages, taken = summed + 16, scaled = taken + 16, used = scaled + 16;
+    dependents_may_start();
+    if (threadIdx.x == 32) {
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&xmap) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&ymap) : "memory");
+    }
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; ++i) {
             mbar_init(full + 8 * i, 1);
@@ -379,14 +384,35 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             const float off = failed ? __uint_as_float(0x7fffffffu) : 0.0f;   // NaN after a wait that ran out
             const int k = w.k0 + rank * kHalf + feature_of(quad * 32 + lane);
             const int n0 = w.n0 + half * kAcc;
-            const int cnt = k < p.dim ? p.rows - n0 : 0;
+            const int left = p.rows - n0, cnt = k < p.dim ? left : 0;
             if (p.splits == 1 && p.dw_bf16) {
-                __nv_bfloat16* o = reinterpret_cast<__nv_bfloat16*>(p.dw + int64_t(n0) * p.dw_pitch) + k;
-                const int64_t pitch = p.dw_pitch / 2;
+                // lanes two apart have neighbouring features: of two columns each takes one, with both features, so that
+                // a store has 4 bytes (4096 x 4096 outputs of 64 tokens: 33 us with 2 bytes a store, 28 so)
+                const bool up = lane & 2;
+                const int k2 = k & ~1;
+                const bool second = k2 + 1 < p.dim;
+                __nv_bfloat16* o = reinterpret_cast<__nv_bfloat16*>(p.dw + int64_t(n0 + (up ? 1 : 0)) * p.dw_pitch) + k2;
+                const int64_t step = p.dw_pitch;           // two rows, in elements
+                const bool wide = second && ((reinterpret_cast<uintptr_t>(o) | uintptr_t(p.dw_pitch)) & 3) == 0;
 #pragma unroll
-                for (int j = 0; j < kAcc; ++j) {
-                    if (j < cnt) *o = __float2bfloat16_rn(p.accumulate ? __bfloat162float(*o) + acc[j] + off : acc[j] + off);
-                    o += pitch;
+                for (int j = 0; j < kAcc; j += 2) {
+                    const float got = __shfl_xor_sync(0xffffffffu, up ? acc[j] : acc[j + 1], 2);
+                    float x = (up ? got : acc[j]) + off, y = (up ? acc[j + 1] : got) + off;
+                    if (j + (up ? 1 : 0) < left && k2 < p.dim) {
+                        if (wide) {
+                            uint32_t* at = reinterpret_cast<uint32_t*>(o);
+                            if (p.accumulate) {
+                                const uint32_t old = *at;
+                                x += __uint_as_float(old << 16);
+                                y += __uint_as_float(old & 0xffff0000u);
+                            }
+                            *at = pack_bf16(x, y);
+                        } else {
+                            o[0] = __float2bfloat16_rn(p.accumulate ? __bfloat162float(o[0]) + x : x);
+                            if (second) o[1] = __float2bfloat16_rn(p.accumulate ? __bfloat162float(o[1]) + y : y);
+                        }
+                    }
+                    o += step;
                     asm volatile("" : "+l"(o)::"memory");   // one pointer that moves on, not kAcc of them
                 }
             } else {
@@ -425,26 +451,51 @@ struct StageParams {
 // dy into rows on 16-byte boundaries: a copy, or three bf16 parts that add up to a
 // 32-bit value.  Each part takes the next eight bits of the significand, cut off.
 // An infinity or a NaN stays whole in the first part.
+// A thread takes four columns of a row.
 __global__ void __launch_bounds__(256) wgrad_stage_kernel(StageParams p) {
     dependents_may_start();
-    const int64_t n = p.tok_pad * p.col_pad;
-    for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < n; i += int64_t(gridDim.x) * 256) {
-        const int64_t t = i / p.col_pad, c = i - t * p.col_pad;
-        const bool in = t < p.ntok && c < p.rows;
-        if (!p.f32) {
-            p.out[i] = in ? reinterpret_cast<const __nv_bfloat16*>(p.dy + t * p.dy_pitch)[c] : __float2bfloat16_rn(0.0f);
-            continue;
-        }
-        const float x = in ? reinterpret_cast<const float*>(p.dy + t * p.dy_pitch)[c] : 0.0f;
-        const bool finite = fabsf(x) <= 3.402823466e38f;
-        float rest = x;
+    const int64_t quads = p.col_pad / 4, n = p.tok_pad * p.col_pad;
+    const int64_t item = int64_t(blockIdx.x) * 256 + threadIdx.x;
+    if (item * 4 >= n) return;
+    int64_t t, c;
+    split_item(item, quads, t, c);
+    c *= 4;
+    const uint8_t* row = p.dy + t * p.dy_pitch;
+    uint2* out = reinterpret_cast<uint2*>(p.out + item * 4);
+    if (!p.f32) {
+        uint32_t w[4];
 #pragma unroll
-        for (int k = 0; k < 3; ++k) {
-            float part = __uint_as_float(__float_as_uint(rest) & 0xffff0000u);
-            if (!finite) part = k ? 0.0f : x;
-            p.out[k * n + i] = __float2bfloat16_rn(part);
-            rest -= part;
+        for (int i = 0; i < 4; ++i) w[i] = t < p.ntok && c + i < p.rows ? reinterpret_cast<const uint16_t*>(row)[c + i] : 0u;
+        *out = make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16);
+        return;
+    }
+    float x[4];
+    if (t < p.ntok && c + 4 <= p.rows && (reinterpret_cast<uintptr_t>(row) & 15) == 0) {
+        const float4 v = *reinterpret_cast<const float4*>(row + c * 4);
+        x[0] = v.x;
+        x[1] = v.y;
+        x[2] = v.z;
+        x[3] = v.w;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = t < p.ntok && c + i < p.rows ? reinterpret_cast<const float*>(row)[c + i] : 0.0f;
+    }
+    uint32_t h[4];   // the upper half of what is left
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t bits = __float_as_uint(x[i]);
+            if ((bits & 0x7f800000u) == 0x7f800000u) {
+                // a NaN whose set bits are all cut off stays one
+                h[i] = bits >> 16 | ((bits & 0x7fffffu) ? 0x40u : 0u);
+                x[i] = 0.0f;
+            } else {
+                h[i] = bits >> 16;
+                x[i] -= __uint_as_float(bits & 0xffff0000u);
+            }
         }
+        out[k * n / 4] = make_uint2(h[0] | h[1] << 16, h[2] | h[3] << 16);
     }
 }
 
@@ -455,20 +506,30 @@ struct JoinParams {
     int32_t splits, accumulate, dw_bf16;
 };
 
+// A CTA takes 1024 columns of a row, four a thread.
 __global__ void __launch_bounds__(256) wgrad_join_kernel(JoinParams p) {
     dependency_wait();
     const int64_t n = p.rows * p.dim;
-    for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < n; i += int64_t(gridDim.x) * 256) {
-        const int64_t r = i / p.dim, c = i - r * p.dim;
-        float s = 0.0f;
+    int64_t r, part;
+    split_item(blockIdx.x, (p.dim + 1023) / 1024, r, part);
+    const int64_t c0 = part * 1024 + threadIdx.x;
+    const float* from = p.part + r * p.dim + c0;
+    float s[4] = {};
 #pragma unroll 4
-        for (int k = 0; k < p.splits; ++k) s += p.part[k * n + i];
+    for (int k = 0; k < p.splits; ++k)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (c0 + i * 256 < p.dim) s[i] += from[k * n + i * 256];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int64_t c = c0 + i * 256;
+        if (c >= p.dim) break;
         if (p.dw_bf16) {
             __nv_bfloat16* o = reinterpret_cast<__nv_bfloat16*>(p.dw + r * p.dw_pitch) + c;
-            *o = __float2bfloat16_rn(p.accumulate ? __bfloat162float(*o) + s : s);
+            *o = __float2bfloat16_rn(p.accumulate ? __bfloat162float(*o) + s[i] : s[i]);
         } else {
             float* o = reinterpret_cast<float*>(p.dw + r * p.dw_pitch) + c;
-            *o = p.accumulate ? *o + s : s;
+            *o = p.accumulate ? *o + s[i] : s[i];
         }
     }
 }
@@ -507,7 +568,10 @@ bool encode(CUtensorMap* map, CUtensorMapDataType type, const void* p, int64_t c
 constexpr int64_t al(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
 
 // How a product is cut: output tiles, parts of dy, and splits of the tokens where
-// the tiles alone leave multiprocessors idle (each split at least 4 stages long).
+// the tiles alone leave multiprocessors idle (each split at least 8 stages long: a
+// stage takes half a microsecond, joining the parts four; 512 tokens of 256 -> 1024
+// take 15 us in two splits and 13 in one, 2047 of 2048 -> 512 24 us in one and 19 in
+// four).
 constexpr int kPairs = 76;
 struct Shape {
     int64_t tiles_n, tiles_k, stages_part, stages, splits, per_split;
@@ -520,7 +584,7 @@ Shape shape_of(int64_t ntok, int64_t rows, int64_t dim, int32_t dy_dtype) {
     s.stages = s.stages_part * (dy_dtype == LC_F32 ? 3 : 1);
     const int64_t tiles = s.tiles_n * s.tiles_k;
     s.splits = tiles >= kPairs ? 1 : kPairs / tiles;
-    if (s.splits > (s.stages + 3) / 4) s.splits = (s.stages + 3) / 4;
+    if (s.splits > s.stages / 8) s.splits = s.stages / 8;
     if (s.splits < 1) s.splits = 1;
     s.per_split = (s.stages + s.splits - 1) / s.splits;
     s.splits = (s.stages + s.per_split - 1) / s.per_split;
@@ -624,8 +688,9 @@ extern "C" lc_status lc_weight_grad(int device, void* cuda_stream, const lc_rows
         q.ntok = ntok;
         q.rows = rows;
         q.f32 = f32;
-        const int64_t want = (q.tok_pad * q.col_pad + 1023) / 1024, most = int64_t(ops_sm_count(device)) * 32;
-        wgrad_stage_kernel<<<unsigned(want < most ? want : most), 256, 0, s>>>(q);
+        const int64_t grid = (q.tok_pad * q.col_pad + 1023) / 1024;
+        if (grid > kMost) return fail_status(LC_ERR_INVALID_ARG, "%s: dy is too large", call);
+        wgrad_stage_kernel<<<unsigned(grid), 256, 0, s>>>(q);
         e = cudaGetLastError();
         if (e != cudaSuccess) return ops_launched(call, e);
         ydata = workspace;
@@ -662,8 +727,7 @@ extern "C" lc_status lc_weight_grad(int device, void* cuda_stream, const lc_rows
     e = launch_dependent(wgrad_kernel, 2 * (p.items < pairs ? p.items : pairs), kThreads, kSmem, s, xmap, ymap, p);
     if (e == cudaSuccess && sh.splits > 1) {
         JoinParams j{p.part, p.dw, dw_pitch, rows, dim, p.splits, p.accumulate, p.dw_bf16};
-        const int64_t want = (rows * dim + 1023) / 1024, most = int64_t(ops_sm_count(device)) * 32;
-        e = launch_dependent(wgrad_join_kernel, int(want < most ? want : most), 256, 0, s, j);
+        e = launch_dependent(wgrad_join_kernel, int(rows * ((dim + 1023) / 1024)), 256, 0, s, j);
     }
     return ops_launched(call, e);
 }
