@@ -25,6 +25,8 @@ _CODE = {torch.bfloat16: LC_BF16, torch.float32: LC_F32}
 _IDS = {torch.int32: LC_I32, torch.int64: LC_I64}
 _KIND = {"layer": LC_NORM_LAYER, "rms": LC_NORM_RMS}
 _scratch = {}
+_empty, _empty_like = torch.empty, torch.empty_like
+_f32 = torch.float32
 
 
 class Act:
@@ -52,8 +54,8 @@ class Act:
     def empty(cls, rows, dim, device):
         blocks = -(-int(dim) // LC_ACT_BLOCK)
         act = cls.__new__(cls)
-        act.q = torch.empty((rows, blocks * LC_ACT_BLOCK), dtype=torch.int8, device=device)
-        act.e = torch.empty((rows, blocks), dtype=torch.int8, device=device)
+        act.q = _empty((rows, blocks * LC_ACT_BLOCK), dtype=torch.int8, device=device)
+        act.e = _empty((rows, blocks), dtype=torch.int8, device=device)
         act.dim = int(dim)
         return act
 
@@ -91,7 +93,7 @@ def _on(first, *tensors):
 
 
 def _like(x):
-    return torch.empty_like(x) if x.is_contiguous() else torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    return _empty_like(x) if x.is_contiguous() else _empty(x.shape, dtype=x.dtype, device=x.device)
 
 
 # the handle of torch's current stream, without a Stream object around it (1 us a call)
@@ -110,7 +112,7 @@ def _workspace(index, stream, nbytes):
 def _param(t, dim, name):
     if t.dtype not in _CODE:
         raise TypeError("%s must be bfloat16 or float32, got %s" % (name, t.dtype))
-    if t.dim() != 1 or t.numel() != dim or not t.is_contiguous():
+    if t.shape != (dim,) or not t.is_contiguous():
         raise ValueError("%s must be contiguous with %d elements" % (name, dim))
     return t.data_ptr()
 
@@ -135,10 +137,11 @@ def embed(table, ids, scale=1.0, out=None):
     rt, it = _rows(table, "table"), _ids(ids)
     n, (vocab, dim) = ids.numel(), table.shape
     if out is None:
-        out = torch.empty((n, dim), dtype=table.dtype, device=table.device)
+        out = _empty((n, dim), dtype=table.dtype, device=table.device)
+        ro = lc_rows(out.data_ptr(), dim, rt.dtype, 0)
     else:
         _shaped(out, n, dim, "out")
-    ro = _rows(out, "out")
+        ro = _rows(out, "out")
     check(_abi.load().lc_embed(index, _stream(index), rt, vocab, dim, ids.data_ptr(), it, n, scale, ro))
     return out
 
@@ -157,7 +160,7 @@ def embed_grad(dy, ids, vocab=None, scale=1.0, grad=None, dtype=None, skip_id=-1
             raise ValueError("accumulate needs grad")
         if vocab is None:
             raise ValueError("vocab or grad is needed")
-        grad = torch.empty((vocab, dim), dtype=dtype or dy.dtype, device=dy.device)
+        grad = _empty((vocab, dim), dtype=dtype or dy.dtype, device=dy.device)
     else:
         vocab = grad.shape[0]
         _shaped(grad, vocab, dim, "grad")
@@ -187,7 +190,7 @@ def act_load(act, out=None, dtype=torch.bfloat16):
     index = _on(act.q, out)
     n, dim = act.q.shape[0], act.dim
     if out is None:
-        out = torch.empty((n, dim), dtype=dtype, device=act.q.device)
+        out = _empty((n, dim), dtype=dtype, device=act.q.device)
     else:
         _shaped(out, n, dim, "out")
     ro = _rows(out, "out")
@@ -215,14 +218,15 @@ def norm(x, weight, bias=None, eps=1e-5, kind="layer", out=None, keep=None):
         raise ValueError("the checkpoint must have %d rows of %d" % (n, dim))
     if out is None:
         out = _like(x)
+        ro = lc_rows(out.data_ptr(), dim, rx.dtype, 0)
     else:
         _shaped(out, n, dim, "out")
-    ro = _rows(out, "out")
-    layer = _KIND[kind] == LC_NORM_LAYER
-    rstd = torch.empty(n, dtype=torch.float32, device=device)
-    mean = torch.empty(n, dtype=torch.float32, device=device) if layer else None
-    check(_abi.load().lc_norm(index, _stream(index), _KIND[kind], rx, n, dim, w, b, _CODE[weight.dtype], eps, ro,
-                              mean.data_ptr() if layer else None, rstd.data_ptr(),
+        ro = _rows(out, "out")
+    kind = _KIND[kind]
+    rstd = _empty(n, dtype=_f32, device=device)
+    mean = _empty_like(rstd) if kind == LC_NORM_LAYER else None
+    check(_abi.load().lc_norm(index, _stream(index), kind, rx, n, dim, w, b, _CODE[weight.dtype], eps, ro,
+                              None if mean is None else mean.data_ptr(), rstd.data_ptr(),
                               None if keep is None else keep._c()))
     return (out, mean, rstd, keep) if new else (out, mean, rstd)
 
@@ -241,24 +245,28 @@ def norm_grad(dy, x, weight, mean, rstd, bias=False, dx=None, dweight=None, dbia
     w = _param(weight, dim, "weight")
     if (x.rows, x.dim) != (n, dim) if kept else tuple(x.shape) != (n, dim):
         raise ValueError("x must have dy's shape")
-    for name, t in (("mean", mean), ("rstd", rstd)):
-        if t is not None and (t.dtype != torch.float32 or t.numel() != n or not t.is_contiguous()):
-            raise ValueError("%s must be contiguous float32 with %d elements" % (name, n))
+    for t in (mean, rstd):
+        if t is not None and (t.dtype != _f32 or t.shape != (n,) or not t.is_contiguous()):
+            raise ValueError("mean and rstd must be contiguous float32 with %d elements" % n)
     if accumulate and (dweight is None or (bias and dbias is None)):
         raise ValueError("accumulate needs the gradients to add to")
     if dx is None:
         dx = _like(dy)
+        rdx = lc_rows(dx.data_ptr(), dim, rd.dtype, 0)
     else:
         _shaped(dx, n, dim, "dx")
+        rdx = _rows(dx, "dx")
     if dweight is None:
-        dweight = torch.empty(dim, dtype=dbias.dtype if dbias is not None else dtype, device=device)
-    if dbias is None and bias:
-        dbias = torch.empty(dim, dtype=dweight.dtype, device=device)
-    rdx = _rows(dx, "dx")
+        dweight = _empty(dim, dtype=dbias.dtype if dbias is not None else dtype, device=device)
     pw = _param(dweight, dim, "dweight")
-    pb = None if dbias is None else _param(dbias, dim, "dbias")
-    if dbias is not None and dbias.dtype != dweight.dtype:
-        raise ValueError("dweight and dbias must have one type")
+    pb = None
+    if dbias is not None:
+        pb = _param(dbias, dim, "dbias")
+        if dbias.dtype != dweight.dtype:
+            raise ValueError("dweight and dbias must have one type")
+    elif bias:
+        dbias = _empty_like(dweight)
+        pb = dbias.data_ptr()
     lib, stream = _abi.load(), _stream(index)
     need = lib.lc_norm_grad_workspace(n, dim)
     check(lib.lc_norm_grad(index, stream, LC_NORM_RMS if mean is None else LC_NORM_LAYER, rd,
@@ -279,7 +287,7 @@ def weight_grad(dy, act, grad=None, dtype=torch.float32, accumulate=False):
     if grad is None:
         if accumulate:
             raise ValueError("accumulate needs grad")
-        grad = torch.empty((rows, act.dim), dtype=dtype, device=dy.device)
+        grad = _empty((rows, act.dim), dtype=dtype, device=dy.device)
     else:
         _shaped(grad, rows, act.dim, "grad")
     rg = _rows(grad, "grad")
