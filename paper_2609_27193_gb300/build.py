@@ -3,12 +3,17 @@
 Each .cu under csrc/ is compiled in parallel to an object under _build/,
 then linked into paper_2609_27193_gb300/liblayercheck.so with the CUDA
 runtime linked statically.  Only the lc_* entry points are exported.
+
+The operators' binding over torch tensors (binding/ops_binding.cpp) becomes the
+extension module _ops.so beside it, with g++ and torch's headers, at the same
+time.
 """
 import concurrent.futures as cf
 import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -16,6 +21,8 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "liblayercheck.so")
+BINDING = os.path.join(PKG, "binding", "ops_binding.cpp")
+BINDING_LIB = os.path.join(PKG, "_ops.so")
 
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVFLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC,-ffp-contract=off",
@@ -45,8 +52,50 @@ def up_to_date():
     return all(os.path.getmtime(f) <= t for f in _inputs())
 
 
+def binding_up_to_date():
+    inputs = [BINDING, os.path.join(INCLUDE, "layercheck.h"), os.path.abspath(__file__)]
+    return os.path.exists(BINDING_LIB) and all(os.path.getmtime(f) <= os.path.getmtime(BINDING_LIB) for f in inputs)
+
+
+def compile_binding():
+    """ops_binding.cpp to an object; returns it and torch's library folder."""
+    import torch
+    home = os.path.dirname(torch.__file__)
+    include = [os.path.join(home, "include"), os.path.join(home, "include", "torch", "csrc", "api", "include"),
+               sysconfig.get_paths()["include"], os.path.join(os.path.dirname(os.path.dirname(_nvcc())), "include"),
+               INCLUDE]
+    os.makedirs(BUILD, exist_ok=True)
+    obj = os.path.join(BUILD, "ops_binding.o")
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden",
+           "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI),
+           *[x for d in include for x in ("-isystem" if d != INCLUDE else "-I", d)], "-c", BINDING, "-o", obj]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError("g++ failed on %s:\n%s%s" % (BINDING, r.stdout, r.stderr[-4000:]))
+    return obj, os.path.join(home, "lib")
+
+
+def link_binding(obj, torch_lib):
+    tmp = BINDING_LIB + ".tmp%d" % os.getpid()
+    cmd = ["g++", "-shared", "-o", tmp, obj, "-L", PKG, "-l:liblayercheck.so", "-L", torch_lib, "-ltorch_python",
+           "-ltorch_cpu", "-lc10_cuda", "-lc10", "-Wl,-rpath,$ORIGIN"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError("link failed:\n%s%s" % (r.stdout, r.stderr))
+    os.replace(tmp, BINDING_LIB)
+
+
 def build(force=False, verbose=False, extra_flags=()):
     """Compile and link; returns the library path."""
+    with cf.ThreadPoolExecutor(max_workers=1) as ex:
+        binding = None if binding_up_to_date() and not force else ex.submit(compile_binding)
+        lib = build_library(force, verbose, extra_flags)
+        if binding is not None:
+            link_binding(*binding.result())
+    return lib
+
+
+def build_library(force=False, verbose=False, extra_flags=()):
     if not force and up_to_date():
         return LIB
     nvcc = _nvcc()
@@ -71,7 +120,7 @@ def build(force=False, verbose=False, extra_flags=()):
     with open(vscript, "w") as fh:
         fh.write("{ global: lc_*; local: *; };\n")
     tmp = LIB + ".tmp%d" % os.getpid()
-    cmd = [nvcc, *ARCH, "-shared", "-o", tmp, *[o for o, _ in results],
+    cmd = [nvcc, *ARCH, "-shared", "-o", tmp, *[o for o, _ in results], "-Xlinker", "--soname=liblayercheck.so",
            "-Xlinker", "--version-script=" + vscript, "-cudart", "static"]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
