@@ -11,7 +11,7 @@
 // chunk.  A row that lies inside one chunk is written by it; a row that crosses
 // chunks leaves fp32 partial sums, which a last kernel adds in chunk order.  No
 // floating point atomics: the order of every sum is fixed by the sizes.  The rows
-// without a token are zeroed from a bitmap of the rows that have one.
+// without a token are zeroed from a map of the rows that have one.
 #include <cooperative_groups.h>
 
 #include "lc_ops.cuh"
@@ -26,7 +26,7 @@ constexpr int kSortThreads = 1024;
 constexpr int kSortWarps = kSortThreads / 32;
 constexpr int kSortCluster = 8;
 constexpr int kSortBits = 9;                 // digits of at most 9 bits
-constexpr int64_t kSortPer = 2048;           // tokens of a CTA before the cluster grows
+constexpr int64_t kSortPer = 512;            // tokens of a CTA before the cluster grows
 constexpr int64_t kSortShared = 65536;       // up to this many tokens the list stays in shared memory
 constexpr int kSumThreads = 128;
 constexpr int64_t kMaxTokens = int64_t(1) << 31;
@@ -111,9 +111,8 @@ cudaError_t launch_embed(EmbedParams p, int sms, cudaStream_t s) {
 struct SortParams {
     const void* ids;
     int64_t n, vocab, skip;
-    uint32_t* key[2];      // [1]: the sorted list; [0]: between passes (lists that do not stay in shared memory)
-    uint32_t* pos[2];
-    uint32_t* present;     // bitmap of the rows that have a token (null: not wanted)
+    uint2* list[2];        // (id, position); [1]: sorted; [0]: between passes (lists that do not stay in shared memory)
+    uint8_t* present;      // 1 for the rows that have a token, a byte each (null: not wanted)
     int32_t digit, passes; // bits of a digit, digits
     int64_t cap;           // places of a CTA in the list, a multiple of 1024 (SHARED: 1 << cap_log2)
     int32_t cap_log2;
@@ -130,7 +129,7 @@ struct SortParams {
 // and a fence of the whole cluster a pass (16381 tokens: 18 us that way, 13 so).
 template <typename I, bool SHARED>
 __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(SortParams p) {
-    extern __shared__ uint32_t sm[];           // counts [warps][digit values], then (SHARED) keys [2][cap], positions [2][cap]
+    extern __shared__ uint32_t sm[];           // counts [warps][digit values], then (SHARED) lists [2][cap]
     __shared__ uint32_t tot[1 << kSortBits];
     __shared__ uint32_t warp_sum[kSortWarps];
     dependents_may_start();
@@ -144,15 +143,15 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(SortParams p) 
     const int bins = 1 << p.digit;
     uint32_t* cnt = sm + warp * bins;
     const int64_t cap = p.cap;
-    uint32_t* list = sm + kSortWarps * bins;
+    uint2* list = reinterpret_cast<uint2*>(sm + kSortWarps * bins);
     const int64_t c0 = rank * cap, per = cap / kSortWarps;
     int64_t lo = c0 + warp * per;
     lo = lo < p.n ? lo : p.n;
     const int64_t hi = lo + per < p.n ? lo + per : p.n;
     if (p.present) {
-        const int64_t words = (p.vocab + 31) / 32;
-        for (int64_t i = int64_t(rank) * kSortThreads + threadIdx.x; i < words; i += int64_t(nc) * kSortThreads)
-            p.present[i] = 0;
+        const int64_t vecs = (p.vocab + 15) / 16;   // (the workspace has whole vectors of it)
+        for (int64_t i = int64_t(rank) * kSortThreads + threadIdx.x; i < vecs; i += int64_t(nc) * kSortThreads)
+            reinterpret_cast<uint4*>(p.present)[i] = make_uint4(0, 0, 0, 0);
     }
     constexpr int U = 4;                       // items of a lane that are asked for at once
     const bool once = hi - lo <= 32 * U;       // all of the warp's items: they stay in registers
@@ -162,8 +161,8 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(SortParams p) 
         // the list that this pass reads; the one it writes is the other, the last one's always [1]
         const int to_list = (p.passes - pass) & 1, from = to_list ^ 1;
         // (an index into the parameters' arrays would put them on the stack)
-        const uint32_t *key_from = from ? p.key[1] : p.key[0], *pos_from = from ? p.pos[1] : p.pos[0];
-        uint32_t *key_to = from ? p.key[0] : p.key[1], *pos_to = from ? p.pos[0] : p.pos[1];
+        const uint2* far_from = from ? p.list[1] : p.list[0];
+        uint2* far_to = from ? p.list[0] : p.list[1];
         uint32_t key[U], pos[U];
         auto load = [&](int64_t at) {
 #pragma unroll
@@ -176,11 +175,13 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(SortParams p) 
                     key[u] = uint32_t(id >= 0 && id < p.vocab && id != p.skip ? id : p.vocab);
                     pos[u] = uint32_t(i);
                 } else if constexpr (SHARED) {
-                    key[u] = list[from * cap + (i - c0)];
-                    pos[u] = list[(2 + from) * cap + (i - c0)];
+                    const uint2 v = list[from * cap + (i - c0)];
+                    key[u] = v.x;
+                    pos[u] = v.y;
                 } else {
-                    key[u] = __ldcg(key_from + i);
-                    pos[u] = __ldcg(pos_from + i);
+                    const uint2 v = __ldcg(far_from + i);
+                    key[u] = v.x;
+                    pos[u] = v.y;
                 }
             }
         };
@@ -254,16 +255,13 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(SortParams p) 
                 __syncwarp();   // the next items' atomics come after these
                 to = __shfl_sync(0xffffffffu, to, first) + __popc(same & ((1u << lane) - 1));
                 if (!in) continue;
-                // the bitmap was cleared before the pass's first meeting
-                if (pass == 0 && p.present && key[u] < p.vocab) atomicOr(p.present + key[u] / 32, 1u << (key[u] & 31));
+                // (cleared before the pass's first meeting; a bit each would take atomics, 4 us of 16381 tokens' 15)
+                if (pass == 0 && p.present && key[u] < p.vocab) p.present[key[u]] = 1;
                 if (last || !SHARED) {
-                    key_to[to] = key[u];
-                    pos_to[to] = pos[u];
+                    far_to[to] = make_uint2(key[u], pos[u]);
                 } else {
-                    uint32_t* there = cluster.map_shared_rank(list, int(to >> p.cap_log2));
-                    const int64_t slot = to & uint32_t(cap - 1);
-                    there[to_list * cap + slot] = key[u];
-                    there[(2 + to_list) * cap + slot] = pos[u];
+                    uint2* there = cluster.map_shared_rank(list, int(to >> p.cap_log2));
+                    there[to_list * cap + (to & uint32_t(cap - 1))] = make_uint2(key[u], pos[u]);
                 }
             }
         }
@@ -273,9 +271,8 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(SortParams p) 
 }
 
 struct SumParams {
-    const uint32_t* key;
-    const uint32_t* pos;
-    const uint32_t* present;
+    const uint2* list;    // (id, position), sorted by id
+    const uint8_t* present;
     const uint8_t* dy;
     uint8_t* grad;
     float* part;          // [chunks][2][slabs][G][E]: a chunk's open rows at its start and end
@@ -390,7 +387,7 @@ __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(SumParams p) {
     dependents_may_start();
     const int lane = threadIdx.x & 31;
     if (int64_t(blockIdx.x) >= p.sum_ctas) {
-        // rows without a token: a warp at a time asks for the bits of up to 32 rows and clears what it finds
+        // rows without a token: every warp asks for 32 rows at a time, the CTA clears what they find
         const int64_t r0 = (int64_t(blockIdx.x) - p.sum_ctas) * p.zero_rows;
         const int64_t r1 = r0 + p.zero_rows < p.vocab ? r0 + p.zero_rows : p.vocab;
         const int64_t bytes = p.dim * int64_t(sizeof(TG));
@@ -398,7 +395,7 @@ __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(SumParams p) {
         constexpr int W = kSumThreads / 32;
         for (int64_t first = r0; first < r1; first += 32) {
             const int64_t mine = first + lane;
-            uint32_t empty = __ballot_sync(0xffffffffu, mine < r1 && !(p.present[(mine < r1 ? mine : first) / 32] >> (mine & 31) & 1));
+            uint32_t empty = __ballot_sync(0xffffffffu, mine < r1 && !p.present[mine < r1 ? mine : first]);
             const bool whole = VEC && bytes % 16 == 0;
             if (whole) {
                 // the warp's share of all the rows' vectors
@@ -434,12 +431,13 @@ __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(SumParams p) {
     for (int e = 0; e < E; ++e) acc[e] = 0.0f;
     // 32 entries of the list at a time, one a lane; the next ones are asked for early
     auto entry = [&](int64_t s, uint32_t& key, uint32_t& pos) {
-        key = s < p.n && s <= s1 ? p.key[s] : none;
-        pos = s < s1 ? p.pos[s] : 0;
+        const uint2 v = s < p.n && s <= s1 ? p.list[s] : make_uint2(none, 0);
+        key = v.x;
+        pos = v.y;
     };
     uint32_t key_next, pos_next;
     entry(s0 + lane, key_next, pos_next);
-    const uint32_t before = s0 > 0 ? p.key[s0 - 1] : none;
+    const uint32_t before = s0 > 0 ? p.list[s0 - 1].x : none;
     bool open = __shfl_sync(0xffffffffu, key_next, 0) == before;   // the row began in an earlier chunk
     for (int64_t base = s0; base < s1; base += 32) {
         const uint32_t key32 = key_next, pos32 = pos_next;
@@ -496,7 +494,7 @@ __global__ void __launch_bounds__(kJoinThreads) embed_join_kernel(SumParams p) {
     split_item(blockIdx.x, p.slabs, chunk, slab);
     const int64_t s0 = chunk * p.chunk, s1 = s0 + p.chunk;
     if (s1 >= p.n) return;
-    const uint32_t key = p.key[s1], last = p.key[s1 - 1], before = s0 > 0 ? p.key[s0 - 1] : uint32_t(p.vocab);
+    const uint32_t key = p.list[s1].x, last = p.list[s1 - 1].x, before = s0 > 0 ? p.list[s0 - 1].x : uint32_t(p.vocab);
     if (key == uint32_t(p.vocab) || last != key) return;   // no row crosses this chunk's end
     if (s0 > 0 && before == key) return;                   // it began in an earlier chunk
     // chunks c in (chunk, lo] begin with this row: the largest one, by a search that looks at 32 places at a time,
@@ -505,7 +503,7 @@ __global__ void __launch_bounds__(kJoinThreads) embed_join_kernel(SumParams p) {
     int64_t lo = chunk + 1, hi = p.chunks;                 // key[lo * chunk] == key, hi: beyond
     for (bool near = true; hi - lo > 1; near = false) {
         const int64_t gap = near ? 1 : (hi - lo + 31) / 32, c = lo + gap * (lane + 1);
-        const uint32_t same = __ballot_sync(0xffffffffu, c < hi && p.key[c * p.chunk] == key);
+        const uint32_t same = __ballot_sync(0xffffffffu, c < hi && p.list[c * p.chunk].x == key);
         const int64_t n = __popc(same);                    // sorted: the first n of them
         const int64_t top = lo + gap * (n + 1);
         lo += gap * n;
@@ -561,31 +559,30 @@ __global__ void __launch_bounds__(kJoinThreads) embed_join_kernel(SumParams p) {
 constexpr size_t al256(size_t x) { return (x + 255) & ~size_t(255); }
 
 // Chunks of the sorted list: whole batches of 8 rows, long enough to fill the device
-// a few times over, and no more than 512 of them beyond that, so that a row which
-// all tokens share is joined from no more parts (16381 x 768: 35 us; with 1024 at
-// most 38, with 256 40).
-int64_t chunk_of(int64_t n, int64_t slabs) {
+// a few times over, and beyond that no more than 512 of them for groups of 128
+// threads, 2048 for groups of 32, so that a row which all tokens share is joined from
+// no more parts than that (a join has as many more groups as they are smaller).
+// 16381 x 768: 35 us; with twice as many 38, with half as many 40.
+int64_t chunk_of(int64_t n, int64_t slabs, int64_t group) {
     int64_t c = n * slabs / 4864;
-    if (c < n / 512) c = n / 512;
+    if (c < n * group / 65536) c = n * group / 65536;
     c = (c + 7) / 8 * 8;
     return c < 8 ? 8 : c;
 }
 
 struct GradLayout {
-    size_t key[2], pos[2], present, part, bytes;
+    size_t list[2], present, part, bytes;
 };
 // E: the columns of a thread; more of them are more partial sums a chunk.
 GradLayout grad_layout(int64_t n, int64_t vocab, int64_t part_floats) {
     GradLayout l{};
     size_t at = 0;
     for (int i = 0; i < 2; ++i) {
-        l.key[i] = at;
-        at += al256(size_t(n) * 4);
-        l.pos[i] = at;
-        at += al256(size_t(n) * 4);
+        l.list[i] = at;
+        at += al256(size_t(n) * 8);
     }
     l.present = at;
-    at += al256(size_t((vocab + 31) / 32) * 4);
+    at += al256(size_t(vocab));
     l.part = at;
     l.bytes = at + al256(size_t(part_floats) * 4);
     return l;
@@ -600,7 +597,7 @@ SumShape sum_shape(int64_t n, int64_t dim, int E) {
     SumShape s;
     s.group = dim <= 32 * E ? 32 : dim <= 64 * E ? 64 : kSumThreads;
     s.slabs = (dim + s.group * E - 1) / (s.group * E);
-    s.chunk = chunk_of(n, s.slabs);
+    s.chunk = chunk_of(n, s.slabs, s.group);
     s.chunks = (n + s.chunk - 1) / s.chunk;
     s.part_floats = s.chunks * 2 * s.slabs * s.group * E;
     return s;
@@ -774,11 +771,8 @@ extern "C" lc_status lc_embed_grad(int device, void* cuda_stream, const lc_rows*
     q.n = ntok;
     q.vocab = vocab;
     q.skip = skip_id;
-    for (int i = 0; i < 2; ++i) {
-        q.key[i] = reinterpret_cast<uint32_t*>(ws + l.key[i]);
-        q.pos[i] = reinterpret_cast<uint32_t*>(ws + l.pos[i]);
-    }
-    q.present = accumulate ? nullptr : reinterpret_cast<uint32_t*>(ws + l.present);
+    for (int i = 0; i < 2; ++i) q.list[i] = reinterpret_cast<uint2*>(ws + l.list[i]);
+    q.present = accumulate ? nullptr : ws + l.present;
     q.passes = (bits + kSortBits - 1) / kSortBits;
     q.digit = (bits + q.passes - 1) / q.passes;
     cudaError_t e;
@@ -786,8 +780,7 @@ extern "C" lc_status lc_embed_grad(int device, void* cuda_stream, const lc_rows*
     else e = id_type == LC_I32 ? launch_sort<int32_t, false>(q, s) : launch_sort<int64_t, false>(q, s);
     if (e != cudaSuccess) return ops_launched(call, e);
     SumParams p{};
-    p.key = q.key[1];
-    p.pos = q.pos[1];
+    p.list = q.list[1];
     p.present = q.present;
     p.dy = static_cast<const uint8_t*>(dy->data);
     p.grad = static_cast<uint8_t*>(grad->data);
