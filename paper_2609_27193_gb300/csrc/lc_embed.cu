@@ -10,8 +10,9 @@
 // its rows: a word that half of the tokens share costs no more than any other
 // chunk.  A row that lies inside one chunk is written by it; a row that crosses
 // chunks leaves fp32 partial sums, which a last kernel adds in chunk order.  No
-// floating point atomics: the order of every sum is fixed by the sizes.  The rows
-// without a token are zeroed from a map of the rows that have one.
+// floating point atomics: the order of every sum is fixed by the sizes.  The gradient
+// is zeroed by the multiprocessors that the sort leaves idle: the rows with a token
+// are written twice, which costs less than knowing first which they are.
 #include <cooperative_groups.h>
 
 #include "lc_ops.cuh"
@@ -112,11 +113,42 @@ struct SortParams {
     const void* ids;
     int64_t n, vocab, skip;
     uint2* list[2];        // (id, position); [1]: sorted; [0]: between passes (lists that do not stay in shared memory)
-    uint8_t* present;      // 1 for the rows that have a token, a byte each (null: not wanted)
+    uint8_t* grad;         // zeroed by the CTAs behind the sorting cluster (null: not wanted)
+    int64_t rows, width, pitch;   // of grad, in bytes
     int32_t digit, passes; // bits of a digit, digits
     int64_t cap;           // places of a CTA in the list, a multiple of 1024 (SHARED: 1 << cap_log2)
     int32_t cap_log2;
 };
+
+// Bytes [from, to) of one row, by the CTA's threads.
+__device__ __forceinline__ void zero_span(uint8_t* from, uint8_t* to) {
+    uint8_t* v0 = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(from) + 15) & ~uintptr_t(15));
+    uint8_t* v1 = reinterpret_cast<uint8_t*>(reinterpret_cast<uintptr_t>(to) & ~uintptr_t(15));
+    if (v0 > v1) v0 = v1 = to;
+    // elements have 2 or 4 bytes: the ends are whole pairs of bytes
+    for (uint8_t* e = from + threadIdx.x * 2; e < v0; e += kSortThreads * 2) *reinterpret_cast<uint16_t*>(e) = 0;
+    for (uint8_t* e = v1 + threadIdx.x * 2; e < to; e += kSortThreads * 2) *reinterpret_cast<uint16_t*>(e) = 0;
+#pragma unroll 4
+    for (uint8_t* v = v0 + threadIdx.x * 16; v < v1; v += kSortThreads * 16) st_stream(v, make_uint4(0, 0, 0, 0));
+}
+// Share `cta` of `ctas` of the gradient: every ctas-th piece of kZeroPiece bytes where
+// rows lie back to back, else every ctas-th row.
+constexpr int64_t kZeroPiece = 16 * kSortThreads;
+__device__ __forceinline__ void zero_rows(uint8_t* grad, int64_t rows, int64_t width, int64_t pitch, int cta, int ctas) {
+    if (pitch == width || rows == 1) {
+        const int64_t total = rows * width, head = int64_t(-reinterpret_cast<uintptr_t>(grad) & 15);
+        const int64_t pieces = total > head ? (total - head) / kZeroPiece : 0;
+        uint8_t* v = grad + head + threadIdx.x * 16;
+#pragma unroll 4
+        for (int64_t i = cta; i < pieces; i += ctas) st_stream(v + i * kZeroPiece, make_uint4(0, 0, 0, 0));
+        if (cta == 0) {
+            zero_span(grad, grad + (head < total ? head : total));
+            if (total > head) zero_span(grad + head + pieces * kZeroPiece, grad + total);
+        }
+        return;
+    }
+    for (int64_t r = cta; r < rows; r += ctas) zero_span(grad + r * pitch, grad + r * pitch + width);
+}
 
 // Sorts the tokens by id: least significant digit first, each pass a stable
 // counting sort.  One cluster does it all: every warp owns a contiguous range of
@@ -135,6 +167,10 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(SortParams p) 
     dependents_may_start();
     cg::cluster_group cluster = cg::this_cluster();
     const int rank = int(cluster.block_rank()), nc = int(cluster.num_blocks());
+    if (int(blockIdx.x) >= nc) {
+        zero_rows(p.grad, p.rows, p.width, p.pitch, int(blockIdx.x) - nc, int(gridDim.x) - nc);
+        return;
+    }
     auto meet = [&]() {
         if (nc == 1) __syncthreads();
         else cluster.sync();
@@ -148,11 +184,6 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(SortParams p) 
     int64_t lo = c0 + warp * per;
     lo = lo < p.n ? lo : p.n;
     const int64_t hi = lo + per < p.n ? lo + per : p.n;
-    if (p.present) {
-        const int64_t vecs = (p.vocab + 15) / 16;   // (the workspace has whole vectors of it)
-        for (int64_t i = int64_t(rank) * kSortThreads + threadIdx.x; i < vecs; i += int64_t(nc) * kSortThreads)
-            reinterpret_cast<uint4*>(p.present)[i] = make_uint4(0, 0, 0, 0);
-    }
     constexpr int U = 4;                       // items of a lane that are asked for at once
     const bool once = hi - lo <= 32 * U;       // all of the warp's items: they stay in registers
     for (int pass = 0; pass < p.passes; ++pass) {
@@ -255,8 +286,6 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(SortParams p) 
                 __syncwarp();   // the next items' atomics come after these
                 to = __shfl_sync(0xffffffffu, to, first) + __popc(same & ((1u << lane) - 1));
                 if (!in) continue;
-                // (cleared before the pass's first meeting; a bit each would take atomics, 4 us of 16381 tokens' 15)
-                if (pass == 0 && p.present && key[u] < p.vocab) p.present[key[u]] = 1;
                 if (last || !SHARED) {
                     far_to[to] = make_uint2(key[u], pos[u]);
                 } else {
@@ -272,12 +301,11 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(SortParams p) 
 
 struct SumParams {
     const uint2* list;    // (id, position), sorted by id
-    const uint8_t* present;
     const uint8_t* dy;
     uint8_t* grad;
     float* part;          // [chunks][2][slabs][G][E]: a chunk's open rows at its start and end
     int64_t n, vocab, dim, dy_pitch, grad_pitch;
-    int64_t chunk, chunks, slabs, items, sum_ctas, zero_rows;   // items = chunks * slabs
+    int64_t chunk, chunks, slabs, items;   // items = chunks * slabs
     float scale;
     int32_t accumulate;
 };
@@ -386,38 +414,6 @@ __global__ void __launch_bounds__(kSumThreads) embed_sum_kernel(SumParams p) {
     dependency_wait();
     dependents_may_start();
     const int lane = threadIdx.x & 31;
-    if (int64_t(blockIdx.x) >= p.sum_ctas) {
-        // rows without a token: every warp asks for 32 rows at a time, the CTA clears what they find
-        const int64_t r0 = (int64_t(blockIdx.x) - p.sum_ctas) * p.zero_rows;
-        const int64_t r1 = r0 + p.zero_rows < p.vocab ? r0 + p.zero_rows : p.vocab;
-        const int64_t bytes = p.dim * int64_t(sizeof(TG));
-        const int warp = threadIdx.x >> 5;
-        constexpr int W = kSumThreads / 32;
-        for (int64_t first = r0; first < r1; first += 32) {
-            const int64_t mine = first + lane;
-            uint32_t empty = __ballot_sync(0xffffffffu, mine < r1 && !p.present[mine < r1 ? mine : first]);
-            const bool whole = VEC && bytes % 16 == 0;
-            if (whole) {
-                // the warp's share of all the rows' vectors
-                const int64_t nv = bytes / 16;
-                while (empty) {
-                    const int64_t r = first + __ffs(empty) - 1;
-                    empty &= empty - 1;
-                    uint8_t* row = p.grad + r * p.grad_pitch;
-                    for (int64_t i = threadIdx.x; i < nv; i += kSumThreads) st_stream(row + i * 16, make_uint4(0, 0, 0, 0));
-                }
-                continue;
-            }
-            for (int k = 0; empty; ++k) {
-                const int64_t r = first + __ffs(empty) - 1;
-                empty &= empty - 1;
-                if (k % W != warp) continue;
-                TG* row = reinterpret_cast<TG*>(p.grad + r * p.grad_pitch);
-                for (int64_t i = lane; i < p.dim; i += 32) row[i] = from_f32<TG>(0.0f);
-            }
-        }
-        return;
-    }
     const int64_t item = int64_t(blockIdx.x) * (kSumThreads / G) + int(threadIdx.x) / G;
     if (item >= p.items) return;
     int64_t chunk, slab;
@@ -571,18 +567,16 @@ int64_t chunk_of(int64_t n, int64_t slabs, int64_t group) {
 }
 
 struct GradLayout {
-    size_t list[2], present, part, bytes;
+    size_t list[2], part, bytes;
 };
 // E: the columns of a thread; more of them are more partial sums a chunk.
-GradLayout grad_layout(int64_t n, int64_t vocab, int64_t part_floats) {
+GradLayout grad_layout(int64_t n, int64_t part_floats) {
     GradLayout l{};
     size_t at = 0;
     for (int i = 0; i < 2; ++i) {
         l.list[i] = at;
         at += al256(size_t(n) * 8);
     }
-    l.present = at;
-    at += al256(size_t(vocab));
     l.part = at;
     l.bytes = at + al256(size_t(part_floats) * 4);
     return l;
@@ -605,15 +599,8 @@ SumShape sum_shape(int64_t n, int64_t dim, int E) {
 
 template <typename TD, typename TG, bool VEC, int G>
 cudaError_t launch_group(SumParams p, cudaStream_t s) {
-    p.sum_ctas = (p.items + kSumThreads / G - 1) / (kSumThreads / G);
-    int64_t zero = 0;
-    if (!p.accumulate) {
-        // 16 KB a CTA, whole words of the bitmap where rows are that short
-        p.zero_rows = 16384 / (p.dim * int64_t(sizeof(TG)));
-        p.zero_rows = p.zero_rows < 1 ? 1 : p.zero_rows > 32 ? p.zero_rows / 32 * 32 : p.zero_rows;
-        zero = (p.vocab + p.zero_rows - 1) / p.zero_rows;
-    }
-    cudaError_t e = launch_dependent(embed_sum_kernel<TD, TG, VEC, G>, int(p.sum_ctas + zero), kSumThreads, 0, s, p);
+    const int64_t grid = (p.items + kSumThreads / G - 1) / (kSumThreads / G);
+    cudaError_t e = launch_dependent(embed_sum_kernel<TD, TG, VEC, G>, int(grid), kSumThreads, 0, s, p);
     if (e == cudaSuccess && p.chunks > 1)
         e = launch_dependent(embed_join_kernel<TD, TG, VEC, G>, int(p.items), kJoinThreads, 0, s, p);
     return e;
@@ -631,7 +618,7 @@ cudaError_t launch_sum(SumParams p, const SumShape& sh, cudaStream_t s) {
 }
 
 template <typename I, bool SHARED>
-cudaError_t launch_sort(SortParams p, cudaStream_t s) {
+cudaError_t launch_sort(SortParams p, int sms, cudaStream_t s) {
     static bool ready[kOpsMaxDevices];
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
@@ -653,7 +640,17 @@ cudaError_t launch_sort(SortParams p, cudaStream_t s) {
     attr.val.clusterDim.x = nc;
     attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
     cudaLaunchConfig_t c{};
-    c.gridDim = dim3(nc);
+    // the other multiprocessors zero the gradient meanwhile, from 32 KB a CTA; 512 KB at most, since not every cluster
+    // may find a place at once (1 GB in one CTA a multiprocessor: 229 us, with a second wave as long as the first)
+    int64_t zero = 0;
+    if (p.grad) {
+        const int64_t bytes = p.rows * p.width, want = (bytes + 32767) / 32768, most = sms > int(nc) ? sms - int(nc) : 1;
+        zero = want < most ? want : most;
+        if (zero < bytes / 524288) zero = bytes / 524288;
+        if (zero > 1 << 24) zero = 1 << 24;
+        zero = (zero + nc - 1) / nc * nc;
+    }
+    c.gridDim = dim3(nc + unsigned(zero));
     c.blockDim = dim3(kSortThreads);
     c.dynamicSmemBytes = (counts << p.digit) + (SHARED ? size_t(16) << p.cap_log2 : 0);
     c.stream = s;
@@ -718,7 +715,7 @@ extern "C" uint64_t lc_embed_grad_workspace(int64_t ntok, int64_t vocab, int64_t
         const int64_t f = sum_shape(ntok, dim, E).part_floats;
         floats = f > floats ? f : floats;
     }
-    return grad_layout(ntok, vocab, floats).bytes;
+    return grad_layout(ntok, floats).bytes;
 }
 
 extern "C" lc_status lc_embed_grad(int device, void* cuda_stream, const lc_rows* dy, const void* ids, int32_t id_type,
@@ -764,7 +761,7 @@ extern "C" lc_status lc_embed_grad(int device, void* cuda_stream, const lc_rows*
     const bool vec = aligned16(dy->data) && aligned16(grad->data) && row_bytes(dy) % 16 == 0 && gp % 16 == 0;
     const bool dbf = dy->dtype == LC_BF16, gbf = grad->dtype == LC_BF16;
     const SumShape sh = sum_shape(ntok, dim, vec && dbf ? 8 : 4);
-    const GradLayout l = grad_layout(ntok, vocab, sh.part_floats);
+    const GradLayout l = grad_layout(ntok, sh.part_floats);
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     SortParams q{};
     q.ids = ids;
@@ -772,16 +769,21 @@ extern "C" lc_status lc_embed_grad(int device, void* cuda_stream, const lc_rows*
     q.vocab = vocab;
     q.skip = skip_id;
     for (int i = 0; i < 2; ++i) q.list[i] = reinterpret_cast<uint2*>(ws + l.list[i]);
-    q.present = accumulate ? nullptr : ws + l.present;
+    if (!accumulate) {
+        q.grad = static_cast<uint8_t*>(grad->data);
+        q.rows = vocab;
+        q.width = dim * elem_size(grad->dtype);
+        q.pitch = gp;
+    }
     q.passes = (bits + kSortBits - 1) / kSortBits;
     q.digit = (bits + q.passes - 1) / q.passes;
+    const int sms = ops_sm_count(device);
     cudaError_t e;
-    if (ntok <= kSortShared) e = id_type == LC_I32 ? launch_sort<int32_t, true>(q, s) : launch_sort<int64_t, true>(q, s);
-    else e = id_type == LC_I32 ? launch_sort<int32_t, false>(q, s) : launch_sort<int64_t, false>(q, s);
+    if (ntok <= kSortShared) e = id_type == LC_I32 ? launch_sort<int32_t, true>(q, sms, s) : launch_sort<int64_t, true>(q, sms, s);
+    else e = id_type == LC_I32 ? launch_sort<int32_t, false>(q, sms, s) : launch_sort<int64_t, false>(q, sms, s);
     if (e != cudaSuccess) return ops_launched(call, e);
     SumParams p{};
     p.list = q.list[1];
-    p.present = q.present;
     p.dy = static_cast<const uint8_t*>(dy->data);
     p.grad = static_cast<uint8_t*>(grad->data);
     p.part = reinterpret_cast<float*>(ws + l.part);
