@@ -288,6 +288,7 @@ __global__ void __launch_bounds__(cta_threads(G)) norm_grad_kernel(NormGradParam
     constexpr int V = kVec<T>;
     constexpr int R = cta_threads(G) / G;
     extern __shared__ float2 sums[];
+    dependents_may_start();
     __shared__ __align__(16) float shared[2][2][32];
     int slot = 0;
     const int t = threadIdx.x % G;
@@ -382,7 +383,6 @@ __global__ void __launch_bounds__(cta_threads(G)) norm_grad_kernel(NormGradParam
             for (int i = 0; i < VPT; ++i) store_vec<T, G, VPT, VEC>(p.dx + r * p.dx_pitch, t, i, p.dim, g[i]);
         }
     }
-    dependents_may_start();
     if (!p.want_params) return;
     // one row of sums for the CTA: its groups add theirs in turn
     if constexpr (R > 1) {

@@ -17,8 +17,8 @@
 //   warps 12-19 add up the results
 //
 // The tensor cores add in fp32, but a chain of many products loses more than a sum
-// in registers does (8192 tokens in one chain: 2.5e-6 off; in pieces of 512:
-// 1.2e-7).  So a chain is kChunk stages long; two accumulators in tensor memory
+// in registers does (8192 tokens in one chain: 2.5e-6 off; in pieces of 1024:
+// 1.3e-7).  So a chain is kChunk stages long; two accumulators in tensor memory
 // take turns, and the last eight warps add the finished one to their registers
 // while the other is being filled.  The CTAs are persistent and the stages of one
 // tile follow those of the last, so the outputs are written while the next tile's
@@ -43,7 +43,7 @@ constexpr int kHalf = 128;       // features and columns of dy that a CTA of the
 constexpr int kTile = 2 * kHalf; // of the pair's tile
 constexpr int kTok = 64;         // tokens of a stage
 constexpr int kStages = 5;       // stages in flight
-constexpr int kChunk = 8;        // stages that one accumulator adds up
+constexpr int kChunk = 16;       // stages that one accumulator adds up
 constexpr int kXBytes = kTok * kHalf;              // 8-bit tile
 constexpr int kBox = 64;                           // columns of a copy or operand box: 128 bytes, the swizzle's span
 constexpr int kBoxBytes = kTok * kBox * 2;
