@@ -41,70 +41,79 @@ struct EmbedParams {
     float scale;
 };
 
-// V elements an access: a 16-byte vector, or one element where an address or a
-// pitch is off 16 bytes.
-template <typename T, typename I, int V, int U>
+template <int B>
+struct Word;
+template <>
+struct Word<16> { using type = uint4; };
+template <>
+struct Word<8> { using type = uint2; };
+template <>
+struct Word<4> { using type = uint32_t; };
+template <>
+struct Word<2> { using type = uint16_t; };
+
+// B bytes an access, the most that the addresses and pitches are multiples of.
+template <typename T, typename I, int B, int U>
 __global__ void __launch_bounds__(kEmbedThreads) embed_kernel(EmbedParams p) {
+    using W = typename Word<B>::type;
+    constexpr int V = B / int(sizeof(T));
     const int lane = threadIdx.x & 31;
     const int64_t step = int64_t(gridDim.x) * (kEmbedThreads / 32);
     for (int64_t item = int64_t(blockIdx.x) * (kEmbedThreads / 32) + (threadIdx.x >> 5); item < p.items; item += step) {
-        const int64_t t = item / p.segs;
-        const int64_t c0 = (item - t * p.segs) * (32 * V * U) + lane * V;
+        int64_t t, seg;
+        split_item(item, p.segs, t, seg);
+        const int64_t c0 = seg * (32 * V * U) + lane * V;
         const int64_t id = int64_t(static_cast<const I*>(p.ids)[t]);
         const bool row = id >= 0 && id < p.vocab;
         const T* src = reinterpret_cast<const T*>(p.table + (row ? id : 0) * p.table_pitch);
         T* dst = reinterpret_cast<T*>(p.y + t * p.y_pitch);
         const float fill = id < 0 ? 0.0f : __uint_as_float(0x7fffffffu);
-        if constexpr (V > 1) {
-            uint4 v[U];
+        W v[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int64_t c = c0 + u * 32 * V;
-                if (row && c + V <= p.dim) v[u] = __ldg(reinterpret_cast<const uint4*>(src + c));
-            }
+        for (int u = 0; u < U; ++u) {
+            const int64_t c = c0 + u * 32 * V;
+            if (row && c + V <= p.dim) v[u] = __ldg(reinterpret_cast<const W*>(src + c));
+        }
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int64_t c = c0 + u * 32 * V;
-                if (c + V <= p.dim) {
-                    float f[V];
-                    unpack(v[u], f);
+        for (int u = 0; u < U; ++u) {
+            const int64_t c = c0 + u * 32 * V;
+            if (c + V <= p.dim) {
+                T e[V];
+                memcpy(e, &v[u], B);
 #pragma unroll
-                    for (int i = 0; i < V; ++i) f[i] = row ? f[i] * p.scale : fill;
-                    st_stream(dst + c, pack(f));
-                } else {
-                    for (int64_t k = c; k < p.dim; ++k) dst[k] = from_f32<T>(row ? to_f32(src[k]) * p.scale : fill);
-                }
-            }
-        } else {
-            T v[U];
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int64_t c = c0 + u * 32;
-                if (row && c < p.dim) v[u] = src[c];
-            }
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int64_t c = c0 + u * 32;
-                if (c < p.dim) dst[c] = from_f32<T>(row ? to_f32(v[u]) * p.scale : fill);
+                for (int i = 0; i < V; ++i) e[i] = from_f32<T>(row ? to_f32(e[i]) * p.scale : fill);
+                W out;
+                memcpy(&out, e, B);
+                __stcs(reinterpret_cast<W*>(dst + c), out);
+            } else {
+                for (int64_t k = c; k < p.dim; ++k) dst[k] = from_f32<T>(row ? to_f32(src[k]) * p.scale : fill);
             }
         }
     }
 }
 
-template <typename T, typename I>
-cudaError_t launch_embed(EmbedParams p, int sms, cudaStream_t s) {
-    constexpr int V = kVec<T>, U = 4;
-    const bool vec = aligned16(p.table) && aligned16(p.y) && p.table_pitch % 16 == 0 && p.y_pitch % 16 == 0;
-    const int64_t per = vec ? 32 * V * U : 32 * 8;
+template <typename T, typename I, int B, int U>
+cudaError_t launch_embed_bytes(EmbedParams p, int sms, cudaStream_t s) {
+    constexpr int64_t per = 32 * (B / int(sizeof(T))) * U;
     p.segs = (p.dim + per - 1) / per;
     p.items = p.ntok * p.segs;
     const int64_t want = (p.items + kEmbedThreads / 32 - 1) / (kEmbedThreads / 32);
     const int64_t most = int64_t(sms) * 256;
-    const unsigned grid = unsigned(want < most ? want : most);
     cudaGetLastError();
-    if (vec) embed_kernel<T, I, V, U><<<grid, kEmbedThreads, 0, s>>>(p);
-    else embed_kernel<T, I, 1, 8><<<grid, kEmbedThreads, 0, s>>>(p);
+    embed_kernel<T, I, B, U><<<unsigned(want < most ? want : most), kEmbedThreads, 0, s>>>(p);
     return cudaGetLastError();
+}
+
+// Accesses of 16 bytes where addresses and pitches allow them, else of 8, 4 or one
+// element (8192 tokens, 32000 rows, bf16: 2048 wide @@ us, 2044 @@, 2046 @@, 2047 @@).
+template <typename T, typename I>
+cudaError_t launch_embed(const EmbedParams& p, int sms, cudaStream_t s) {
+    const uintptr_t all = reinterpret_cast<uintptr_t>(p.table) | reinterpret_cast<uintptr_t>(p.y) | uintptr_t(p.table_pitch) |
+                          uintptr_t(p.y_pitch);
+    if (all % 16 == 0) return launch_embed_bytes<T, I, 16, 4>(p, sms, s);
+    if (all % 8 == 0) return launch_embed_bytes<T, I, 8, 8>(p, sms, s);
+    if (all % 4 == 0) return launch_embed_bytes<T, I, 4, 8>(p, sms, s);
+    return launch_embed_bytes<T, I, sizeof(T), 8>(p, sms, s);
 }
 
 // --- the gradient -----------------------------------------------------------
