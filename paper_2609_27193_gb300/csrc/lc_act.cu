@@ -29,7 +29,7 @@ constexpr int kUnroll = 4;   // vectors that a lane has in flight
 // block in 128 / V neighbouring lanes; otherwise kUnroll blocks, a lane every 32nd
 // value of each.
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(kActThreads) act_save_kernel(ActParams p) {
+__global__ void __launch_bounds__(kActThreads, 6) act_save_kernel(ActParams p) {
     constexpr int V = VEC ? kVec<T> : 4, L = VEC ? LC_ACT_BLOCK / V : 32;
     const int lane = threadIdx.x & 31;
     const int64_t item = int64_t(blockIdx.x) * (kActThreads / 32) + (threadIdx.x >> 5);

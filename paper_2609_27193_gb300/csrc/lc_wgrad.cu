@@ -25,9 +25,10 @@
 // products run.
 //
 // A 32-bit dy is split into three bf16 parts that add up to it exactly (8 + 8 + 8
-// bits of significand, cut off, not rounded, so nothing overflows), and a bf16 dy
-// off 16-byte boundaries is copied to aligned rows, both into the workspace by a
-// kernel of their own.  Few output tiles are split over the tokens; the parts are
+// bits of significand, cut off, not rounded, so nothing overflows); a stage then has
+// the tiles of all three, and the operand is made once for them.  That and a bf16 dy
+// off 16-byte boundaries go into aligned rows in the workspace, by a kernel of their
+// own.  Few output tiles are split over the tokens; the parts are
 // added in order by another kernel.
 //
 // Waits are bounded: one that runs out leaves NaN in the outputs.
@@ -42,14 +43,20 @@ namespace {
 constexpr int kHalf = 128;       // features and columns of dy that a CTA of the pair holds
 constexpr int kTile = 2 * kHalf; // of the pair's tile
 constexpr int kTok = 64;         // tokens of a stage
-constexpr int kStages = 5;       // stages in flight
-constexpr int kChunk = 16;       // stages that one accumulator adds up
 constexpr int kXBytes = kTok * kHalf;              // 8-bit tile
 constexpr int kBox = 64;                           // columns of a copy or operand box: 128 bytes, the swizzle's span
 constexpr int kBoxBytes = kTok * kBox * 2;
 constexpr int kOpBytes = kHalf / kBox * kBoxBytes; // a bf16 tile
-constexpr int kLoadBytes = kOpBytes + kXBytes;     // what the copies of a stage bring: dy, 8-bit tile
-constexpr int kStageBytes = kLoadBytes + kOpBytes; // and the operand
+// A stage holds the tiles of all parts of dy (one, or three of a 32-bit dy), the
+// 8-bit tile and the operand made of it, once for all parts.
+template <int PARTS>
+struct StageOf {
+    static constexpr int kLoad = PARTS * kOpBytes + kXBytes;    // what its copies bring
+    static constexpr int kBytes = kLoad + kOpBytes;
+    static constexpr int kStages = PARTS == 1 ? 5 : 3;          // as many as fit
+    static constexpr int kChunk = PARTS == 1 ? 16 : 5;          // stages that one accumulator adds up
+    static constexpr int kSmem = kStages * kBytes + 1024;       // and room to align the tiles to 1024 bytes
+};
 constexpr int kConvWarp = 4, kConvWarps = 8;       // first converter warp (a multiple of 4), their number
 constexpr int kSumWarp = kConvWarp + kConvWarps, kSumWarps = 8;
 constexpr int kThreads = (kSumWarp + kSumWarps) * 32;
@@ -59,7 +66,6 @@ constexpr int kLaunchRegs = 96, kRoleRegs = 40, kConvRegs = 56, kSumRegs = 160;
 static_assert(kConvWarp * 32 * kRoleRegs + kConvWarps * 32 * kConvRegs + kSumWarps * 32 * kSumRegs <= kThreads * kLaunchRegs &&
                   kThreads * kLaunchRegs <= 65536, "registers");
 constexpr int kTmemCols = 512;                     // two accumulators of 256 columns
-constexpr int kSmem = kStages * kStageBytes + 1024;   // and room to align the tiles to 1024 bytes
 constexpr int kAcc = kTile / 2;                    // columns that a thread adds up
 
 // Instruction descriptor: fp32 accumulator, bf16 operands, both with their rows
@@ -73,7 +79,7 @@ struct WgradParams {
     int64_t e_pitch, dw_pitch;
     int32_t ntok, rows, dim;
     int32_t items;         // tiles * splits
-    int32_t ntiles_n, stages, stages_part, splits, per_split;   // stages in all, of a part of dy, of a split
+    int32_t ntiles_n, stages, splits, per_split;   // stages in all, of a split
     int32_t tok_part;      // rows of dy between the parts
     int32_t accumulate, dw_bf16;
 };
@@ -176,8 +182,11 @@ struct Ring {
     }
 };
 
+template <int PARTS>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     wgrad_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CUtensorMap ymap, WgradParams p) {
+    constexpr int kStages = StageOf<PARTS>::kStages, kChunk = StageOf<PARTS>::kChunk;
+    constexpr int kStageBytes = StageOf<PARTS>::kBytes, kLoadBytes = StageOf<PARTS>::kLoad;
     extern __shared__ uint8_t raw[];
     // full and empty: a stage's copies have landed / its products are done (each CTA's own).  converted: both CTAs'
     // operands are in place (the first CTA's).  summed: an accumulator is complete; taken: both CTAs have read it (the
@@ -230,20 +239,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             int it = 0;
             for (int i = pair; i < p.items && ok; i += pairs) {
                 const Item w = item_of(p, i);
-                int part = w.s0 / p.stages_part, t = (w.s0 - part * p.stages_part) * kTok;
+                int t = w.s0 * kTok;
                 for (int s = 0; s < w.stages; ++s, ++it, st.next()) {
                     ok = it < kStages || mbar_wait_bounded(empty + 8 * st.at, st.round ^ 1, kWaitNs);
                     if (!ok) break;
                     const uint32_t at = tiles + st.at * kStageBytes, bar = full + 8 * st.at;
                     mbar_expect_tx(bar, kLoadBytes);
-                    tma_2d(at + kOpBytes, &xmap, w.k0 + rank * kHalf, t, bar);
-                    for (int j = 0; j < kHalf / kBox; ++j)
-                        tma_2d(at + j * kBoxBytes, &ymap, w.n0 + rank * kHalf + j * kBox, part * p.tok_part + t, bar);
+                    tma_2d(at + PARTS * kOpBytes, &xmap, w.k0 + rank * kHalf, t, bar);
+#pragma unroll
+                    for (int part = 0; part < PARTS; ++part)
+                        for (int j = 0; j < kHalf / kBox; ++j)
+                            tma_2d(at + part * kOpBytes + j * kBoxBytes, &ymap, w.n0 + rank * kHalf + j * kBox, part * p.tok_part + t, bar);
                     t += kTok;
-                    if (t >= p.stages_part * kTok) {
-                        t = 0;
-                        ++part;
-                    }
                 }
             }
             // every copy lands before the CTA's memory is given back
@@ -264,8 +271,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                     const uint64_t y = op_desc(tiles + st.at * kStageBytes), x = y + (kLoadBytes >> 4);
                     // 16 tokens are 2048 bytes further
 #pragma unroll
-                    for (int k = 0; k < kTok / 16; ++k)
-                        tc_mma(tmem + acc.at * kTile, x + k * (2048 >> 4), y + k * (2048 >> 4), kIdesc, !first || k > 0);
+                    for (int part = 0; part < PARTS; ++part)
+#pragma unroll
+                        for (int k = 0; k < kTok / 16; ++k)
+                            tc_mma(tmem + acc.at * kTile, x + k * (2048 >> 4), y + part * (kOpBytes >> 4) + k * (2048 >> 4), kIdesc,
+                                   !first || part > 0 || k > 0);
                     tc_commit(empty + 8 * st.at);
                     if (s % kChunk == kChunk - 1 || s == w.stages - 1) {
                         tc_commit(summed + 8 * acc.at);
@@ -285,7 +295,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                     int e[kChunk];
 #pragma unroll
                     for (int j = 0; j < kChunk; ++j) {
-                        const int t = (w.s0 + s + j) % p.stages_part * kTok + t_in;
+                        const int t = (w.s0 + s + j) * kTok + t_in;
                         e[j] = s + j < w.stages && t < p.ntok && f < p.dim ? int(__ldg(ep + int64_t(t) * p.e_pitch)) : 0;
                     }
                     ok = chunk < 2 || mbar_wait_warp(used + 8 * buf, (chunk / 2 - 1) & 1);
@@ -306,7 +316,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         // and the next of the operand's row in box c / 4; piece i of token t lies at i xor (t mod 8).  Lanes of the second
         // box have the neighbour of the others' token, so eight lanes meet in no bank, neither here nor there.
         const int c = lane & 7, t0 = w4 * 16 + ((lane >> 3) ^ (c >> 2));
-        const uint32_t x_off = kOpBytes + t0 * kHalf + c * 16;
+        const uint32_t x_off = PARTS * kOpBytes + t0 * kHalf + c * 16;
         const uint32_t row_off = kLoadBytes + (c >> 2) * kBoxBytes + t0 * 128, piece = uint32_t((c & 3) * 2 ^ (t0 & 7)) << 4;
         const uint32_t first_converted = in_first(converted);
         const uint32_t align = tiles - smem_addr(raw);
@@ -574,17 +584,17 @@ constexpr int64_t al(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
 // four).
 constexpr int kPairs = 76;
 struct Shape {
-    int64_t tiles_n, tiles_k, stages_part, stages, splits, per_split;
+    int64_t tiles_n, tiles_k, stages, splits, per_split;
 };
 Shape shape_of(int64_t ntok, int64_t rows, int64_t dim, int32_t dy_dtype) {
     Shape s;
     s.tiles_n = (rows + kTile - 1) / kTile;
     s.tiles_k = (dim + kTile - 1) / kTile;
-    s.stages_part = (ntok + kTok - 1) / kTok;
-    s.stages = s.stages_part * (dy_dtype == LC_F32 ? 3 : 1);
+    s.stages = (ntok + kTok - 1) / kTok;
     const int64_t tiles = s.tiles_n * s.tiles_k;
     s.splits = tiles >= kPairs ? 1 : kPairs / tiles;
-    if (s.splits > s.stages / 8) s.splits = s.stages / 8;
+    const int64_t least = dy_dtype == LC_F32 ? 4 : 8;   // a stage of three parts takes twice as long
+    if (s.splits > s.stages / least) s.splits = s.stages / least;
     if (s.splits < 1) s.splits = 1;
     s.per_split = (s.stages + s.splits - 1) / s.splits;
     s.splits = (s.stages + s.per_split - 1) / s.per_split;
@@ -594,10 +604,12 @@ int64_t staged_bytes(int64_t ntok, int64_t rows, int32_t dy_dtype) {
     return al(al(ntok, kTok) * al(rows, 64) * 2 * (dy_dtype == LC_F32 ? 3 : 1), 256);
 }
 // Pairs of CTAs that the device holds at once.
+template <int PARTS>
 cudaError_t resident_pairs(int device, int* pairs) {
     static int held[kOpsMaxDevices];
+    constexpr int kSmem = StageOf<PARTS>::kSmem;
     if (!held[device]) {
-        cudaError_t e = cudaFuncSetAttribute(wgrad_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+        cudaError_t e = cudaFuncSetAttribute(wgrad_kernel<PARTS>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
         if (e != cudaSuccess) return e;
         cudaLaunchAttribute attr{};
         attr.id = cudaLaunchAttributeClusterDimension;
@@ -610,13 +622,23 @@ cudaError_t resident_pairs(int device, int* pairs) {
         c.attrs = &attr;
         c.numAttrs = 1;
         int n = 0;
-        e = cudaOccupancyMaxActiveClusters(&n, wgrad_kernel, &c);
+        e = cudaOccupancyMaxActiveClusters(&n, wgrad_kernel<PARTS>, &c);
         if (e != cudaSuccess) return e;
         held[device] = n < 1 ? 1 : n;
     }
     *pairs = held[device];
     return cudaSuccess;
 }
+
+template <int PARTS>
+cudaError_t launch_product(int device, const CUtensorMap& xmap, const CUtensorMap& ymap, const WgradParams& p, cudaStream_t s) {
+    int pairs = 0;
+    const cudaError_t e = resident_pairs<PARTS>(device, &pairs);
+    if (e != cudaSuccess) return e;
+    return launch_dependent(wgrad_kernel<PARTS>, 2 * (p.items < pairs ? p.items : pairs), kThreads, StageOf<PARTS>::kSmem, s, xmap,
+                            ymap, p);
+}
+
 constexpr int64_t kMost = (int64_t(1) << 31) - 1024;
 
 }  // namespace
@@ -715,16 +737,12 @@ extern "C" lc_status lc_weight_grad(int device, void* cuda_stream, const lc_rows
     p.items = int32_t(tiles * sh.splits);
     p.ntiles_n = int32_t(sh.tiles_n);
     p.stages = int32_t(sh.stages);
-    p.stages_part = int32_t(sh.stages_part);
     p.splits = int32_t(sh.splits);
     p.per_split = int32_t(sh.per_split);
     p.tok_part = int32_t(tok_part);
     p.accumulate = accumulate != 0;
     p.dw_bf16 = dw->dtype == LC_BF16;
-    int pairs = 0;
-    e = resident_pairs(device, &pairs);
-    if (e != cudaSuccess) return ops_launched(call, e);
-    e = launch_dependent(wgrad_kernel, 2 * (p.items < pairs ? p.items : pairs), kThreads, kSmem, s, xmap, ymap, p);
+    e = f32 ? launch_product<3>(device, xmap, ymap, p, s) : launch_product<1>(device, xmap, ymap, p, s);
     if (e == cudaSuccess && sh.splits > 1) {
         JoinParams j{p.part, p.dw, dw_pitch, rows, dim, p.splits, p.accumulate, p.dw_bf16};
         e = launch_dependent(wgrad_join_kernel, int(rows * ((dim + 1023) / 1024)), 256, 0, s, j);
