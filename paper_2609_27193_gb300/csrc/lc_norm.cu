@@ -10,11 +10,12 @@
 // its rows.  Each CTA leaves one fp32 row of sums of them, and a second kernel adds
 // those rows in order: two levels, no atomics, the same bits every time.
 //
-// Rows whose addresses and length are multiples of 16 bytes (and enough of them)
+// Rows whose addresses and length are multiples of 16 bytes (and not few and short)
 // stream through shared memory: every group of threads has a ring of rows there, the
 // next ones on their way by bulk copies while it works on one.  In registers as many
 // bytes in flight would leave no room for the work: 16384 rows of 4096 bf16 through
-// a root-mean-square norm 79 us that way, 45 so, their backward from the checkpoint 109 us and 73.
+// a root-mean-square norm 79 us that way, 45 so, their backward from the checkpoint 109 us
+// and 65.
 #include "lc_bulk.cuh"
 #include "lc_ops.cuh"
 
@@ -996,7 +997,14 @@ cudaError_t dispatch_grad(const NormGradParams& p, int sms, cudaStream_t s, int*
     return launch_grad<T, 1024, 2, VEC, KEPT, true>(p, sms, s, ctas);
 }
 
-constexpr int64_t kRingRows = 4;   // rows a multiprocessor from which the rings are taken
+// Whether the rings pay (microseconds through them and directly; bf16 but for the last):
+//   forward    64 rows of 768: 3.1, 3.7; 2432 of 4096: 9.8, 14.3; 2432 of 256: 3.1, 2.7
+//   backward   64 of 4096: 6.4, 8.9; 152 of 768: 6.0, 5.2; 304 of 768: 6.2, 7.1; 608 of 256: 5.2, 4.5; 1216 of 256:
+//              5.2, 5.6; fp32 152 of 1024: 5.8, 4.7; 304 of 1024: 5.8, 6.2
+bool forward_ring(int64_t ntok, int64_t row_bytes) { return row_bytes >= 1024 || ntok >= 4096; }
+bool backward_ring(int64_t ntok, int64_t row_bytes, int sms) {
+    return row_bytes >= 8192 || ntok >= (row_bytes >= 1024 ? 2 * sms : 1024);
+}
 constexpr int64_t kMaxRows = int64_t(1) << 40;
 
 bool plain_params(const void* w, int64_t dim, int32_t dtype) {
@@ -1080,9 +1088,8 @@ extern "C" lc_status lc_norm(int device, void* cuda_stream, int32_t kind, const 
         if (err != cudaSuccess) return ops_launched(call, err);
     }
     cudaError_t err = cudaSuccess;
-    // few rows: a ring's set-up costs more than it hides
     bool done = false;
-    if (vec && dim * e % 16 == 0 && ntok >= kRingRows * sms)
+    if (vec && dim * e % 16 == 0 && forward_ring(ntok, dim * e))
         err = x->dtype == LC_BF16 ? dispatch_norm_ring<__nv_bfloat16>(p, sms, s, &done) : dispatch_norm_ring<float>(p, sms, s, &done);
     if (done || err != cudaSuccess) return ops_launched(call, err);
     if (x->dtype == LC_BF16)
@@ -1194,7 +1201,7 @@ extern "C" lc_status lc_norm_grad(int device, void* cuda_stream, int32_t kind, c
     const int sms = ops_sm_count(device);
     using B = __nv_bfloat16;
     int ctas = 0;
-    if (vec && dim * e % 16 == 0 && ntok >= kRingRows * sms) {
+    if (vec && dim * e % 16 == 0 && backward_ring(ntok, dim * e, sms)) {
         const bool lean = kind == LC_NORM_RMS && !dbias, bf = dy->dtype == LC_BF16;
         auto go = [&](auto f) { err = f(p, sms, s, &ctas); };
         if (bf && x) go(lean ? dispatch_grad_ring<B, false, true> : dispatch_grad_ring<B, false, false>);
