@@ -78,7 +78,7 @@ def compile_binding():
 def link_binding(obj, torch_lib):
     tmp = BINDING_LIB + ".tmp%d" % os.getpid()
     cmd = ["g++", "-shared", "-o", tmp, obj, "-L", PKG, "-l:liblayercheck.so", "-L", torch_lib, "-ltorch_python",
-           "-ltorch_cpu", "-lc10_cuda", "-lc10", "-Wl,-rpath,$ORIGIN"]
+           "-ltorch_cpu", "-ltorch_cuda", "-lc10_cuda", "-lc10", "-Wl,-rpath,$ORIGIN"]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError("link failed:\n%s%s" % (r.stdout, r.stderr))
