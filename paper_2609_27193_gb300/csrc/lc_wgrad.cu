@@ -81,7 +81,7 @@ struct WgradParams {
     int32_t items;         // tiles * splits
     int32_t ntiles_n, stages, splits, per_split;   // stages in all, of a split
     int32_t tok_part;      // rows of dy between the parts
-    int32_t accumulate, dw_bf16;
+    int32_t dw_bf16;
 };
 
 __device__ __forceinline__ void tma_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
@@ -182,7 +182,8 @@ struct Ring {
     }
 };
 
-template <int PARTS>
+// ACC: the outputs are added to (never with splits).
+template <int PARTS, bool ACC>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     wgrad_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CUtensorMap ymap, WgradParams p) {
     constexpr int kStages = StageOf<PARTS>::kStages, kChunk = StageOf<PARTS>::kChunk;
@@ -395,46 +396,70 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             const int k = w.k0 + rank * kHalf + feature_of(quad * 32 + lane);
             const int n0 = w.n0 + half * kAcc;
             const int left = p.rows - n0, cnt = k < p.dim ? left : 0;
+            // ACC and whole tiles have loops of their own: tests inside would make these unrolled loops twice as long,
+            // and their instructions come from memory for a tile or two of few tokens (64 tokens, 4096 -> 4096 in bf16:
+            // 28 us with the tests inside, 16 so)
             if (p.splits == 1 && p.dw_bf16) {
                 // lanes two apart have neighbouring features: of two columns each takes one, with both features, so that
-                // a store has 4 bytes (4096 x 4096 outputs of 64 tokens: 33 us with 2 bytes a store, 28 so)
+                // a store has 4 bytes (33 us with 2 bytes a store)
                 const bool up = lane & 2;
                 const int k2 = k & ~1;
                 const bool second = k2 + 1 < p.dim;
                 __nv_bfloat16* o = reinterpret_cast<__nv_bfloat16*>(p.dw + int64_t(n0 + (up ? 1 : 0)) * p.dw_pitch) + k2;
                 const int64_t step = p.dw_pitch;           // two rows, in elements
                 const bool wide = second && ((reinterpret_cast<uintptr_t>(o) | uintptr_t(p.dw_pitch)) & 3) == 0;
-#pragma unroll
-                for (int j = 0; j < kAcc; j += 2) {
+                auto pair = [&](int j, float& x, float& y) {
                     const float got = __shfl_xor_sync(0xffffffffu, up ? acc[j] : acc[j + 1], 2);
-                    float x = (up ? got : acc[j]) + off, y = (up ? acc[j + 1] : got) + off;
-                    if (j + (up ? 1 : 0) < left && k2 < p.dim) {
-                        if (wide) {
-                            uint32_t* at = reinterpret_cast<uint32_t*>(o);
-                            if (p.accumulate) {
-                                const uint32_t old = *at;
-                                x += __uint_as_float(old << 16);
-                                y += __uint_as_float(old & 0xffff0000u);
-                            }
-                            *at = pack_bf16(x, y);
-                        } else {
-                            o[0] = __float2bfloat16_rn(p.accumulate ? __bfloat162float(o[0]) + x : x);
-                            if (second) o[1] = __float2bfloat16_rn(p.accumulate ? __bfloat162float(o[1]) + y : y);
+                    x = (up ? got : acc[j]) + off;
+                    y = (up ? acc[j + 1] : got) + off;
+                };
+                if (__all_sync(0xffffffffu, wide && left >= kAcc)) {
+#pragma unroll
+                    for (int j = 0; j < kAcc; j += 2) {
+                        float x, y;
+                        pair(j, x, y);
+                        uint32_t* at = reinterpret_cast<uint32_t*>(o);
+                        if constexpr (ACC) {
+                            const uint32_t old = *at;
+                            x += __uint_as_float(old << 16);
+                            y += __uint_as_float(old & 0xffff0000u);
                         }
+                        *at = pack_bf16(x, y);
+                        o += step;
+                        asm volatile("" : "+l"(o)::"memory");   // one pointer that moves on, not kAcc of them
                     }
-                    o += step;
-                    asm volatile("" : "+l"(o)::"memory");   // one pointer that moves on, not kAcc of them
+                } else {
+#pragma unroll
+                    for (int j = 0; j < kAcc; j += 2) {
+                        float x, y;
+                        pair(j, x, y);
+                        if (j + (up ? 1 : 0) < left && k2 < p.dim) {
+                            o[0] = __float2bfloat16_rn(ACC ? __bfloat162float(o[0]) + x : x);
+                            if (second) o[1] = __float2bfloat16_rn(ACC ? __bfloat162float(o[1]) + y : y);
+                        }
+                        o += step;
+                        asm volatile("" : "+l"(o)::"memory");
+                    }
                 }
             } else {
-                const bool add = p.accumulate && p.splits == 1;
+                // (a split product leaves its parts here, and what is added to comes with their sum)
                 float* o = p.splits > 1 ? p.part + (int64_t(w.split) * p.rows + n0) * p.dim + k
                                         : reinterpret_cast<float*>(p.dw + int64_t(n0) * p.dw_pitch) + k;
                 const int64_t pitch = p.splits > 1 ? p.dim : p.dw_pitch / 4;
+                if (__all_sync(0xffffffffu, cnt >= kAcc)) {
 #pragma unroll
-                for (int j = 0; j < kAcc; ++j) {
-                    if (j < cnt) *o = add ? *o + acc[j] + off : acc[j] + off;
-                    o += pitch;
-                    asm volatile("" : "+l"(o)::"memory");
+                    for (int j = 0; j < kAcc; ++j) {
+                        *o = ACC ? *o + acc[j] + off : acc[j] + off;
+                        o += pitch;
+                        asm volatile("" : "+l"(o)::"memory");
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < kAcc; ++j) {
+                        if (j < cnt) *o = ACC ? *o + acc[j] + off : acc[j] + off;
+                        o += pitch;
+                        asm volatile("" : "+l"(o)::"memory");
+                    }
                 }
             }
         }
@@ -604,12 +629,12 @@ int64_t staged_bytes(int64_t ntok, int64_t rows, int32_t dy_dtype) {
     return al(al(ntok, kTok) * al(rows, 64) * 2 * (dy_dtype == LC_F32 ? 3 : 1), 256);
 }
 // Pairs of CTAs that the device holds at once.
-template <int PARTS>
+template <int PARTS, bool ACC>
 cudaError_t resident_pairs(int device, int* pairs) {
     static int held[kOpsMaxDevices];
     constexpr int kSmem = StageOf<PARTS>::kSmem;
     if (!held[device]) {
-        cudaError_t e = cudaFuncSetAttribute(wgrad_kernel<PARTS>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+        cudaError_t e = cudaFuncSetAttribute(wgrad_kernel<PARTS, ACC>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
         if (e != cudaSuccess) return e;
         cudaLaunchAttribute attr{};
         attr.id = cudaLaunchAttributeClusterDimension;
@@ -622,7 +647,7 @@ cudaError_t resident_pairs(int device, int* pairs) {
         c.attrs = &attr;
         c.numAttrs = 1;
         int n = 0;
-        e = cudaOccupancyMaxActiveClusters(&n, wgrad_kernel<PARTS>, &c);
+        e = cudaOccupancyMaxActiveClusters(&n, wgrad_kernel<PARTS, ACC>, &c);
         if (e != cudaSuccess) return e;
         held[device] = n < 1 ? 1 : n;
     }
@@ -630,12 +655,12 @@ cudaError_t resident_pairs(int device, int* pairs) {
     return cudaSuccess;
 }
 
-template <int PARTS>
+template <int PARTS, bool ACC>
 cudaError_t launch_product(int device, const CUtensorMap& xmap, const CUtensorMap& ymap, const WgradParams& p, cudaStream_t s) {
     int pairs = 0;
-    const cudaError_t e = resident_pairs<PARTS>(device, &pairs);
+    const cudaError_t e = resident_pairs<PARTS, ACC>(device, &pairs);
     if (e != cudaSuccess) return e;
-    return launch_dependent(wgrad_kernel<PARTS>, 2 * (p.items < pairs ? p.items : pairs), kThreads, StageOf<PARTS>::kSmem, s, xmap,
+    return launch_dependent(wgrad_kernel<PARTS, ACC>, 2 * (p.items < pairs ? p.items : pairs), kThreads, StageOf<PARTS>::kSmem, s, xmap,
                             ymap, p);
 }
 
@@ -740,11 +765,12 @@ extern "C" lc_status lc_weight_grad(int device, void* cuda_stream, const lc_rows
     p.splits = int32_t(sh.splits);
     p.per_split = int32_t(sh.per_split);
     p.tok_part = int32_t(tok_part);
-    p.accumulate = accumulate != 0;
     p.dw_bf16 = dw->dtype == LC_BF16;
-    e = f32 ? launch_product<3>(device, xmap, ymap, p, s) : launch_product<1>(device, xmap, ymap, p, s);
+    const bool add = accumulate && sh.splits == 1;
+    if (f32) e = add ? launch_product<3, true>(device, xmap, ymap, p, s) : launch_product<3, false>(device, xmap, ymap, p, s);
+    else e = add ? launch_product<1, true>(device, xmap, ymap, p, s) : launch_product<1, false>(device, xmap, ymap, p, s);
     if (e == cudaSuccess && sh.splits > 1) {
-        JoinParams j{p.part, p.dw, dw_pitch, rows, dim, p.splits, p.accumulate, p.dw_bf16};
+        JoinParams j{p.part, p.dw, dw_pitch, rows, dim, p.splits, accumulate != 0, p.dw_bf16};
         e = launch_dependent(wgrad_join_kernel, int(rows * ((dim + 1023) / 1024)), 256, 0, s, j);
     }
     return ops_launched(call, e);
