@@ -131,7 +131,8 @@ def make_ids(g, t, v, how):
 
 @pytest.mark.parametrize("how", IDS)
 @pytest.mark.parametrize("t,v,d,dt,gt", [
-    (1, 1, 1, F32, F32), (1, 511, 64, BF, F32), (33, 512, 129, BF, BF), (777, 513, 256, F32, BF),
+    (1, 1, 1, F32, F32), (1, 511, 64, BF, F32), (33, 512, 129, BF, BF), (64, 70, 2048, BF, F32), (63, 9, 1001, F32, F32),
+    (17, 3000, 520, F32, BF), (65, 70, 200, BF, BF), (777, 513, 256, F32, BF),
     (2048, 8000, 256, BF, F32), (2049, 131072, 24, F32, F32), (20011, 40, 1030, BF, BF), (5000, 262145, 8, BF, F32), (8193, 600, 64, F32, F32), (65536, 128256, 8, BF, BF),
     (70001, 300, 8, BF, F32), (140000, 70000, 16, BF, F32)])
 def test_embed_grad(ops, how, t, v, d, dt, gt):
@@ -150,9 +151,10 @@ def test_embed_grad(ops, how, t, v, d, dt, gt):
 
 
 @pytest.mark.parametrize("gt", [BF, F32])
-def test_embed_grad_accumulate_skip_and_errors_in_ids(ops, gt):
+@pytest.mark.parametrize("t", [50, 700])
+def test_embed_grad_accumulate_skip_and_errors_in_ids(ops, t, gt):
     g = gen(11)
-    t, v, d = 700, 90, 136
+    v, d = 90, 136
     dy = randn(g, t, d, dtype=BF)
     ids = torch.randint(0, v, (t,), generator=g, device="cuda")
     ids[5], ids[6], ids[7] = -7, v, v + 1000
@@ -165,9 +167,10 @@ def test_embed_grad_accumulate_skip_and_errors_in_ids(ops, gt):
 
 
 @pytest.mark.parametrize("dt,gt", [(BF, F32), (F32, BF), (BF, BF)])
-def test_embed_grad_strides(ops, dt, gt):
+@pytest.mark.parametrize("t", [40, 500])
+def test_embed_grad_strides(ops, t, dt, gt):
     g = gen(12)
-    t, v, d = 500, 70, 200
+    v, d = 70, 200
     ids = torch.randint(0, v, (t,), generator=g, device="cuda")
     src = randn(g, t, d, dtype=dt)
     want = ops.embed_grad(src, ids, v, dtype=gt)
@@ -705,11 +708,14 @@ def test_ops_refuse(ops):
     h = _abi.lc_rows(host.data_ptr(), 64, _abi.LC_BF16, 0)
     assert lib.lc_embed(0, None, h, 8, 64, ids.data_ptr(), _abi.LC_I64, 8, 1.0, r) == _abi.LC_ERR_INVALID_ARG
     assert b"not device memory" in lib.lc_last_error()
-    need = lib.lc_embed_grad_workspace(8, 10, 64)
+    many = torch.zeros(100, dtype=torch.int64, device="cuda")
+    long = torch.zeros(100, 64, dtype=BF, device="cuda")
+    need = lib.lc_embed_grad_workspace(100, 10, 64)
     g = torch.zeros(10, 64, device="cuda")
     rg = _abi.lc_rows(g.data_ptr(), 64, _abi.LC_F32, 0)
     ws = torch.zeros(need, dtype=torch.uint8, device="cuda")
-    args = (0, None, r, ids.data_ptr(), _abi.LC_I64, 8, 1.0, -1, rg, 10, 64, 0)
+    rl = _abi.lc_rows(long.data_ptr(), 64, _abi.LC_BF16, 0)
+    args = (0, None, rl, many.data_ptr(), _abi.LC_I64, 100, 1.0, -1, rg, 10, 64, 0)
     assert lib.lc_embed_grad(*args, ws.data_ptr(), need - 1) == _abi.LC_ERR_CAPACITY
     assert lib.lc_embed_grad(*args, ws.data_ptr() + 8, need) == _abi.LC_ERR_INVALID_ARG
     assert lib.lc_embed_grad(*args, None, need) == _abi.LC_ERR_INVALID_ARG

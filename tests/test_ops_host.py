@@ -93,7 +93,7 @@ def test_workspace_sizes(abi):
     assert lib.lc_embed_grad_workspace(-5, 100, 64) == 0
     assert lib.lc_norm_grad_workspace(0, 64) == 0
     sizes = [lib.lc_embed_grad_workspace(n, 1000, 512) for n in (1, 100, 10000, 1000000)]
-    assert sizes == sorted(sizes) and sizes[0] > 0
+    assert sizes == sorted(sizes) and sizes[0] == 0 and sizes[1] > 0      # few tokens need none
     # two lists of ids and positions, and parts that stay far below the gradient's own traffic
     assert sizes[-1] < 16 * 1000000 + 64 * 1024 * 1024
     assert lib.lc_norm_grad_workspace(10 ** 9, 4096) == lib.lc_norm_grad_workspace(10 ** 6, 4096)
