@@ -482,11 +482,11 @@ __device__ __forceinline__ void stage_param(float4* out, const uint8_t* p, bool 
     }
 }
 
-constexpr int fwd_threads(int G) { return 1024; }
+constexpr int kFwdThreads = 1024;   // of a CTA, one a multiprocessor: 64 registers each (with 512: 54 us for 45)
 
 template <typename T, int G, int VPT>
-__global__ void __launch_bounds__(fwd_threads(G), 1) norm_ring_kernel(NormParams p, int depth) {
-    constexpr int V = kVec<T>, NT = fwd_threads(G), R = NT / G;
+__global__ void __launch_bounds__(kFwdThreads, 1) norm_ring_kernel(NormParams p, int depth) {
+    constexpr int V = kVec<T>, NT = kFwdThreads, R = NT / G;
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ __align__(16) float shared[2][1][32];
     __shared__ __align__(8) uint64_t bars[R * kRingMax];
@@ -612,14 +612,15 @@ __global__ void __launch_bounds__(fwd_threads(G), 1) norm_ring_kernel(NormParams
     ring_drain(ring, failed, t);
 }
 
-constexpr int bwd_threads(int G) { return 512; }
+constexpr int kBwdThreads = 512;    // 128 registers each: sums for weight and bias besides the row (rows of 8 values a thread and
+                                    // 1024 threads 104 us for 77, of 32 values and 384 threads 75)
 
 // The backward.  A slot holds the rows of dy and of x (or its 8-bit values; their
 // exponents are asked for a row ahead into registers).
 // LEAN: no means (root-mean-square norm) and no gradient of a bias.
 template <typename T, int G, int VPT, bool KEPT, bool LEAN>
-__global__ void __launch_bounds__(bwd_threads(G), 1) norm_grad_ring_kernel(NormGradParams p, int depth) {
-    constexpr int V = kVec<T>, NT = bwd_threads(G), R = NT / G;
+__global__ void __launch_bounds__(kBwdThreads, 1) norm_grad_ring_kernel(NormGradParams p, int depth) {
+    constexpr int V = kVec<T>, NT = kBwdThreads, R = NT / G;
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ __align__(16) float shared[2][2][32];
     float(*shared1)[1][32] = reinterpret_cast<float(*)[1][32]>(shared);
@@ -867,7 +868,7 @@ int ring_depth(size_t params, int groups, size_t row) {
 
 template <typename T, int G, int VPT>
 cudaError_t launch_norm_ring(const NormParams& p, int sms, cudaStream_t s, bool* done) {
-    constexpr int V = kVec<T>, NT = fwd_threads(G), R = NT / G;
+    constexpr int V = kVec<T>, NT = kFwdThreads, R = NT / G;
     static bool ready[kOpsMaxDevices];
     const size_t params = size_t(VPT) * V * G * 4 * (p.b ? 2 : 1), row = size_t(p.dim) * sizeof(T);
     const int depth = ring_depth(params, R, row);
@@ -897,7 +898,7 @@ cudaError_t dispatch_norm_ring(const NormParams& p, int sms, cudaStream_t s, boo
 
 template <typename T, int G, int VPT, bool KEPT, bool LEAN>
 cudaError_t launch_grad_ring(const NormGradParams& p, int sms, cudaStream_t s, int* ctas) {
-    constexpr int V = kVec<T>, NT = bwd_threads(G), R = NT / G;
+    constexpr int V = kVec<T>, NT = kBwdThreads, R = NT / G;
     static bool ready[kOpsMaxDevices];
     const size_t params = size_t(VPT) * V * G * 4;
     const size_t row = size_t(p.dim) * sizeof(T) + (KEPT ? (size_t(p.dim) + LC_ACT_BLOCK - 1) / LC_ACT_BLOCK * LC_ACT_BLOCK
