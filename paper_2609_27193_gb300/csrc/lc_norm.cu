@@ -869,6 +869,7 @@ int ring_depth(size_t params, int groups, size_t row) {
 template <typename T, int G, int VPT>
 cudaError_t launch_norm_ring(const NormParams& p, int sms, cudaStream_t s, bool* done) {
     constexpr int V = kVec<T>, NT = kFwdThreads, R = NT / G;
+    if (p.dim > G * VPT * V) return cudaErrorInvalidValue;   // every column has a thread
     static bool ready[kOpsMaxDevices];
     const size_t params = size_t(VPT) * V * G * 4 * (p.b ? 2 : 1), row = size_t(p.dim) * sizeof(T);
     const int depth = ring_depth(params, R, row);
@@ -885,7 +886,7 @@ cudaError_t launch_norm_ring(const NormParams& p, int sms, cudaStream_t s, bool*
 template <typename T>
 cudaError_t dispatch_norm_ring(const NormParams& p, int sms, cudaStream_t s, bool* done) {
     constexpr int M = 8 / kVec<T>;          // 16 values a thread, from a warp a row on
-    const int nv = p.dim / kVec<T> / M;
+    const int nv = (p.dim / kVec<T> + M - 1) / M;   // an fp32 row may end half way through its last 8 values
     if (nv <= 32) return launch_norm_ring<T, 32, M>(p, sms, s, done);
     if (nv <= 64) return launch_norm_ring<T, 32, 2 * M>(p, sms, s, done);
     if (nv <= 96) return launch_norm_ring<T, 32, 3 * M>(p, sms, s, done);
@@ -899,6 +900,7 @@ cudaError_t dispatch_norm_ring(const NormParams& p, int sms, cudaStream_t s, boo
 template <typename T, int G, int VPT, bool KEPT, bool LEAN>
 cudaError_t launch_grad_ring(const NormGradParams& p, int sms, cudaStream_t s, int* ctas) {
     constexpr int V = kVec<T>, NT = kBwdThreads, R = NT / G;
+    if (p.dim > G * VPT * V) return cudaErrorInvalidValue;   // every column has a thread
     static bool ready[kOpsMaxDevices];
     const size_t params = size_t(VPT) * V * G * 4;
     const size_t row = size_t(p.dim) * sizeof(T) + (KEPT ? (size_t(p.dim) + LC_ACT_BLOCK - 1) / LC_ACT_BLOCK * LC_ACT_BLOCK
@@ -921,7 +923,7 @@ cudaError_t launch_grad_ring(const NormGradParams& p, int sms, cudaStream_t s, i
 template <typename T, bool KEPT, bool LEAN>
 cudaError_t dispatch_grad_ring(const NormGradParams& p, int sms, cudaStream_t s, int* ctas) {
     constexpr int M = 8 / kVec<T>;
-    const int nv = p.dim / kVec<T> / M;
+    const int nv = (p.dim / kVec<T> + M - 1) / M;   // an fp32 row may end half way through its last 8 values
     if (nv <= 32) return launch_grad_ring<T, 32, M, KEPT, LEAN>(p, sms, s, ctas);
     if (nv <= 64) return launch_grad_ring<T, 32, 2 * M, KEPT, LEAN>(p, sms, s, ctas);
     if (nv <= 96) return launch_grad_ring<T, 32, 3 * M, KEPT, LEAN>(p, sms, s, ctas);

@@ -1,0 +1,67 @@
+"""The operators at the sizes where one shape of a kernel ends and the next begins, with outputs that start as NaN
+and sums that fp32 holds exactly."""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+from tests.test_gpu_ops import BF, F32, SUMS, U, gen, norm_grad_ref, norm_ref, quantize, randn, values, within  # noqa: E402
+
+
+@pytest.fixture(scope="module")
+def ops():
+    from paper_2609_27193_gb300 import ops
+    return ops
+
+
+def whole(g, *shape, dtype=F32, most=3):
+    """Whole numbers of [-most, most]: a sum of up to 2^24 / most of them has no rounding in fp32."""
+    return torch.randint(-most, most + 1, shape, generator=g, device="cuda").to(dtype)
+
+
+# --- norm ------------------------------------------------------------------------------------------------------
+
+# widths at which a group of threads or its vectors change, one 16-byte vector to either side
+EDGES = [(d + s, dt) for d in (256, 512, 768, 1024, 2048, 4096, 8192) for dt, v in ((F32, 4), (BF, 8)) for s in (-v, 0, v)]
+
+
+@pytest.mark.parametrize("kind", ["layer", "rms"])
+@pytest.mark.parametrize("t", [5, 311])
+@pytest.mark.parametrize("d,dt", EDGES)
+def test_norm_between_its_shapes(ops, kind, t, d, dt):
+    """Both directions, directly and through the rings: every column is written and counted."""
+    g = gen(t * d)
+    x = (randn(g, t, d) + (2.0 if kind == "layer" else 0.0)).to(dt)
+    x[:, -4:] *= 4                                        # the last columns weigh in the statistics
+    w = 1 + randn(g, d, dtype=dt, spread=0.2)
+    b = randn(g, d, dtype=dt) if kind == "layer" else None
+    out = torch.full((t, d), math.nan, dtype=dt, device="cuda")
+    keep = ops.Act.empty(t, d, "cuda")
+    keep.q.fill_(55)
+    keep.e.fill_(55)
+    y, mean, rstd = ops.norm(x, w, b, kind=kind, out=out, keep=keep)
+    ref, rmean, rrstd, xhat = norm_ref(x, w, b, kind, 1e-5)
+    a = x.double().abs().mean(1)
+    if mean is not None:
+        within(mean, rmean, SUMS * U * a, "mean")
+    within(rstd, rrstd, (SUMS + 4) * U * rrstd, "rstd")
+    room = ((SUMS + 8) * U * xhat.abs() + (SUMS + 8) * U * (a * rrstd)[:, None]) * w.double().abs()
+    within(y, ref, room + (4 * U * b.double().abs() if b is not None else 0), "y")
+    q, e, _ = quantize(x)
+    assert torch.equal(keep.q, q) and torch.equal(keep.e, e)
+    dy = whole(g, t, d, dtype=dt)
+    for kept in (False, True):
+        seen = values(keep.q, keep.e)[:, :d] if kept else x
+        dx = torch.full((t, d), math.nan, dtype=dt, device="cuda")
+        # without a bias the root-mean-square norm has a form of its own
+        for bias in (True, False):
+            dx.fill_(math.nan)
+            dw = torch.full((d,), math.nan, device="cuda")
+            db = torch.full((d,), math.nan, device="cuda") if bias else None
+            ops.norm_grad(dy, keep if kept else x, w, mean, rstd, dx=dx, dweight=dw, dbias=db)
+            rdx, room, rdw, wroom, rdb, _ = norm_grad_ref(dy, seen, w, mean, rstd)
+            within(dx, rdx, room, "dx")
+            within(dw, rdw, wroom, "dweight")
+            assert db is None or torch.equal(db.double(), rdb)
