@@ -332,7 +332,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                 const int sb = chunk & 1;
                 if (s % kChunk == 0) ok = mbar_wait_warp(scaled + 8 * sb, (chunk >> 1) & 1);
                 if ((it & 1) == group && ok) {
-                    ok = mbar_wait_warp(full + 8 * st.at, st.round);
+                    // The rings are odd, so the other group had this place last, and a wait knows a round by its parity
+                    // alone: where that copy landed later than this group's own ones since, the round before it would
+                    // pass.  The place's last products come first: they are behind that copy, and this round's wait
+                    // for this group.
+                    ok = it < kStages || mbar_wait_warp(empty + 8 * st.at, st.round ^ 1);
+                    ok = ok && mbar_wait_warp(full + 8 * st.at, st.round);
                     const uint8_t* x = raw + align + st.at * kStageBytes + x_off;
                     uint4 q[4];
 #pragma unroll
