@@ -259,6 +259,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             // every copy lands before the CTA's memory is given back
             for (int i = it > kStages ? it - kStages : 0; i < it; ++i)
                 if (!mbar_wait_bounded(full + 8 * (i % kStages), (i / kStages) & 1, kWaitNs)) ok = false;
+            // and so does every arrival that ends a stage's products: they come to both CTAs of the pair, and nobody else
+            // waits for the last round of them.  (Where products are missing one wait runs out, long after the arrivals
+            // of those there are.)
+            bool ended = true;
+            for (int i = it > kStages ? it - kStages : 0; i < it && ended; ++i)
+                ended = mbar_wait_bounded(empty + 8 * (i % kStages), (i / kStages) & 1, kWaitNs);
+            ok = ok && ended;
         } else if (warp == 1 && lane == 0 && rank == 0) {
             Ring<kStages> st;
             Ring<2> acc;

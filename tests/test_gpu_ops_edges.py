@@ -65,3 +65,27 @@ def test_norm_between_its_shapes(ops, kind, t, d, dt):
             within(dx, rdx, room, "dx")
             within(dw, rdw, wroom, "dweight")
             assert db is None or torch.equal(db.double(), rdb)
+
+
+# --- weight gradient -------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dt,gt", [(BF, F32), (BF, BF), (F32, F32), (F32, BF)])
+@pytest.mark.parametrize("t,n,k", [(64, 2560, 2816), (1100, 2500, 2900), (8192, 1030, 5200), (65, 128, 20500), (2049, 4099, 1300)])
+def test_weight_grad_of_several_tiles_a_pair(ops, dt, gt, t, n, k):
+    """More output tiles than the device holds pairs of CTAs: what the rings and accumulators carry from a tile to the
+    next, ends inside a chain, outputs written while the next tile's products run.  Whole numbers, so that every order of
+    adding them gives the same sums: 3 * 3 * 8192 and what is added to stay below 2^24."""
+    g = gen(t + n)
+    dy, x = whole(g, t, n, dtype=dt), whole(g, t, k, dtype=dt)
+    x[:, ::128] = 64.0                                    # with steps of 1 a value is a whole number of them
+    a = ops.act_save(x)
+    assert torch.equal(ops.act_load(a, dtype=dt), x)
+    ref = dy.double().t() @ x.double()
+    out = torch.full((n, k), math.nan, dtype=gt, device="cuda")
+    for _ in range(3):
+        ops.weight_grad(dy, a, grad=out)
+        assert torch.equal(out, ref.to(gt))
+    base = whole(g, n, k, dtype=gt, most=100)
+    out.copy_(base)
+    ops.weight_grad(dy, a, grad=out, accumulate=True)
+    assert torch.equal(out, (ref + base.double()).to(gt))
