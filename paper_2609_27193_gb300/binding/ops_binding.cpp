@@ -9,6 +9,7 @@
 #include <ATen/core/Tensor.h>
 #include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAStream.h>
+#include <cuda_runtime_api.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <map>
@@ -130,14 +131,24 @@ at::Tensor make(at::IntArrayRef size, at::ScalarType type, const at::Tensor& lik
 
 void* stream_of(int index) { return c10::cuda::getCurrentCUDAStream(c10::DeviceIndex(index)).stream(); }
 
-// Scratch of a device and stream: one tensor that grows to the largest call.
-void* workspace(const at::Tensor& like, int index, void* stream, uint64_t bytes) {
-    static auto* held = new std::map<std::pair<int, void*>, at::Tensor>;   // never freed: the driver may be gone by then
-    if (!bytes) return nullptr;
-    at::Tensor& w = (*held)[{index, stream}];
-    if (!w.defined() || uint64_t(w.numel()) < bytes) w = make({int64_t(bytes)}, at::kByte, like);
-    return w.data_ptr();
-}
+// Scratch of one call.  Of a device and stream there is one tensor, which grows to the
+// largest call; the stream's order keeps its users apart.  A call that is captured has a
+// tensor of its own: a graph holds its address for as long as it can be replayed, on any
+// stream, and memory allocated during a capture belongs to the graph.
+struct Scratch {
+    at::Tensor own;
+    void* p = nullptr;
+    Scratch(const at::Tensor& like, int index, void* stream, uint64_t bytes) {
+        static auto* held = new std::map<std::pair<int, void*>, at::Tensor>;   // never freed: the driver may be gone by then
+        if (!bytes) return;
+        cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+        if (cudaStreamIsCapturing(static_cast<cudaStream_t>(stream), &capture) != cudaSuccess)
+            throw std::runtime_error("cannot tell whether the stream is being captured");
+        at::Tensor& w = capture == cudaStreamCaptureStatusNone ? (*held)[{index, stream}] : own;
+        if (!w.defined() || uint64_t(w.numel()) < bytes) w = make({int64_t(bytes)}, at::kByte, like);
+        p = w.data_ptr();
+    }
+};
 
 PyObject* wrapped(const at::Tensor& t) {
     if (t.defined()) return THPVariable_Wrap(t);
@@ -196,8 +207,9 @@ PyObject* embed_grad(PyObject* const* args, Py_ssize_t nargs) {
     const lc_rows rg = rows_of(grad, "grad");
     void* stream = stream_of(index);
     const uint64_t need = lc_embed_grad_workspace(n, vocab, dim);
+    const Scratch scratch(dy, index, stream, need);
     check(lc_embed_grad(index, stream, &rd, ids.data_ptr(), type, n, float(scale), skip, &rg, vocab, dim, accumulate,
-                        workspace(dy, index, stream, need), need));
+                        scratch.p, need));
     return wrapped(grad);
 }
 
@@ -306,9 +318,10 @@ PyObject* norm_grad(PyObject* const* args, Py_ssize_t nargs) {
     if (pb && dbias.scalar_type() != dweight.scalar_type()) throw ValueError("dweight and dbias must have one type");
     void* stream = stream_of(index);
     const uint64_t need = lc_norm_grad_workspace(n, dim);
+    const Scratch scratch(dy, index, stream, need);
     check(lc_norm_grad(index, stream, mean.defined() ? LC_NORM_LAYER : LC_NORM_RMS, &rd, q.defined() ? nullptr : &rx,
                        q.defined() ? &kept : nullptr, n, dim, w, code_of(weight, "weight"), m, r, &rdx, pw, pb,
-                       code_of(dweight, "dweight"), accumulate, workspace(dy, index, stream, need), need));
+                       code_of(dweight, "dweight"), accumulate, scratch.p, need));
     return tuple(dx, dweight, dbias);
 }
 
@@ -334,7 +347,8 @@ PyObject* weight_grad(PyObject* const* args, Py_ssize_t nargs) {
     const lc_act act = act_of(q, e);
     void* stream = stream_of(index);
     const uint64_t need = lc_weight_grad_workspace(n, rows, dim, rd.dtype);
-    check(lc_weight_grad(index, stream, &rd, &act, n, rows, dim, &rg, accumulate, workspace(dy, index, stream, need), need));
+    const Scratch scratch(dy, index, stream, need);
+    check(lc_weight_grad(index, stream, &rd, &act, n, rows, dim, &rg, accumulate, scratch.p, need));
     return wrapped(grad);
 }
 

@@ -6,8 +6,9 @@ Thin binding of the lc_embed / lc_norm / lc_act / lc_weight_grad calls of
 include/layercheck.h over torch CUDA tensors; what is done for every call is in
 C++ (binding/ops_binding.cpp).  Work is enqueued on torch's current stream,
 outputs that are not passed in come from torch's allocator on that stream, and
-scratch is one tensor a device and stream that grows to the largest call (make
-the first call of a size before a stream capture).  There is no CPU fallback.
+scratch is one tensor a device and stream that grows to the largest call.  A call
+inside torch.cuda.graph has scratch of its own from the graph's pool, so graphs
+may be replayed beside other calls and one another.  There is no CPU fallback.
 
 Tensors are rows of their last dimension: [tokens, dim] with any row stride
 (an expanded row, stride 0, may be an input) and bfloat16 or float32 elements.

@@ -89,3 +89,72 @@ def test_weight_grad_of_several_tiles_a_pair(ops, dt, gt, t, n, k):
     out.copy_(base)
     ops.weight_grad(dy, a, grad=out, accumulate=True)
     assert torch.equal(out, (ref + base.double()).to(gt))
+
+
+# --- scratch in graphs -----------------------------------------------------------------------------------------
+
+def graph_inputs(seed, t=700, v=300, d=256, n=192):
+    g = gen(seed)
+    return dict(v=v, ids=torch.randint(0, v, (t,), generator=g, device="cuda"), x=randn(g, t, d, dtype=BF),
+                w=1 + randn(g, d, dtype=BF, spread=0.2), dy=randn(g, t, d, dtype=BF), dz=randn(g, t, n))
+
+
+def graph_step(ops, s):
+    """Every call that takes scratch."""
+    y, mean, rstd = ops.norm(s["x"], s["w"])
+    dx, dw, db = ops.norm_grad(s["dy"], s["x"], s["w"], mean, rstd, bias=True)
+    return [y, dx, dw, db, ops.weight_grad(s["dz"], ops.act_save(s["x"])), ops.embed_grad(dx, s["ids"], s["v"], dtype=F32)]
+
+
+def captured(ops, s, stream):
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        out = graph_step(ops, s)
+    return graph, out
+
+
+def test_a_graph_keeps_its_scratch(ops):
+    """After a larger call on the stream that the graph was captured on, replays write to nobody else's memory."""
+    side = torch.cuda.Stream()
+    s = graph_inputs(51)
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        want = graph_step(ops, s)                         # the scratch that there is before the capture
+    side.synchronize()
+    graph, held = captured(ops, s, side)
+    with torch.cuda.stream(side):
+        big = graph_step(ops, graph_inputs(52, t=9000, v=5000, d=1024, n=512))
+        # whatever was given back is handed out again
+        fills = [torch.full((1 << k,), 0x5a, dtype=torch.uint8, device="cuda") for k in range(12, 25) for _ in range(3)]
+    side.synchronize()
+    for o in held:
+        o.zero_()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(held, want))
+    assert all(bool((f == 0x5a).all()) for f in fills)
+    assert all(bool(torch.isfinite(b).all()) for b in big)
+
+
+def test_graphs_of_one_stream_on_two(ops):
+    """Captured on one stream, replayed side by side."""
+    side, other = torch.cuda.Stream(), torch.cuda.Stream()
+    inputs = [graph_inputs(53, t=20000), graph_inputs(54, t=20000)]
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        wants = [graph_step(ops, s) for s in inputs]
+    side.synchronize()
+    graphs = [captured(ops, s, side) for s in inputs]
+    for _, held in graphs:
+        for o in held:
+            o.zero_()
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for (graph, _), stream in zip(graphs, (side, other)):
+            with torch.cuda.stream(stream):
+                graph.replay()
+    torch.cuda.synchronize()
+    for (_, held), want in zip(graphs, wants):
+        assert all(torch.equal(a, b) for a, b in zip(held, want))
