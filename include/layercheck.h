@@ -649,8 +649,18 @@ lc_status lc_measure_noalloc_debug(int device, void* cuda_stream, const lc_segme
  *     point atomics: the same inputs give the same bits.
  *   - 0 tokens are allowed: outputs per token are untouched, gradients are 0
  *     (or stay as they are with `accumulate`).
+ *   - The waits inside the kernels are bounded like those of lc_measure.  There
+ *     is no context to report one that ran out: what depends on it is NaN
+ *     then, and the next call is not affected.
  * Errors of each: INVALID_ARG (sizes, types, strides, pointers, overlap),
  * CAPACITY (workspace too small), CUDA. */
+
+/* Test switch of those waits, for the calls that the calling host thread makes
+ * from here on: 0, or LC_DEBUG_OPS_STALL, with which the first copy of every
+ * CTA of the weight gradient's product announces 16 bytes that never come.
+ * Errors: INVALID_ARG (other flags). */
+#define LC_DEBUG_OPS_STALL 4
+lc_status lc_ops_debug(int32_t debug_flags);
 
 /* Rows of `dim` elements of type dtype (lc_dtype); row r starts `stride`
  * elements behind row r-1.  Inputs may repeat a row (stride 0), outputs need

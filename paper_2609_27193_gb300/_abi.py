@@ -25,6 +25,7 @@ LC_DRIFT_SNAPSHOT, LC_DRIFT_ACCUMULATE = 0, 1
 LC_COPY_BULK, LC_COPY_THREADS = 0, 1
 LC_DEBUG_BULK_STALL = 1
 LC_DEBUG_MEASURE_STALL = 2
+LC_DEBUG_OPS_STALL = 4
 LC_I32, LC_I64 = 2, 3
 LC_NORM_LAYER, LC_NORM_RMS = 0, 1
 LC_NORM_MAX_DIM = 16384
@@ -151,6 +152,7 @@ SIGNATURES = {
     "lc_store_load_dir": (C.c_int, [ctx_p, C.c_char_p, C.c_int64, P(store_p), C.c_void_p]),
     "lc_manifest_read": (C.c_int, [C.c_char_p, C.c_int32, P(lc_manifest_record), C.c_int64,
                                    P(C.c_int64), P(C.c_int32), P(C.c_uint32), P(C.c_int32)]),
+    "lc_ops_debug": (C.c_int, [C.c_int32]),
     "lc_embed": (C.c_int, [C.c_int, C.c_void_p, P(lc_rows), C.c_int64, C.c_int64, C.c_void_p, C.c_int32,
                            C.c_int64, C.c_float, P(lc_rows)]),
     "lc_embed_grad": (C.c_int, [C.c_int, C.c_void_p, P(lc_rows), C.c_void_p, C.c_int32, C.c_int64, C.c_float,

@@ -18,7 +18,11 @@ bool meet(const Span2& a, const Span2& b) {
     return !(off >= uintptr_t(a.bytes) && off + uintptr_t(b.bytes) <= pitch);
 }
 
+thread_local int32_t debug_flags = 0;
+
 }  // namespace
+
+int ops_stall() { return debug_flags & LC_DEBUG_OPS_STALL ? 1 : 0; }
 
 int ops_sm_count(int device) {
     static int count[kOpsMaxDevices];   // 0: not asked yet (a benign race: every thread writes the same)
@@ -86,3 +90,11 @@ lc_status ops_launched(const char* call, cudaError_t e) {
 }
 
 }  // namespace lc
+
+extern "C" lc_status lc_ops_debug(int32_t flags) {
+    using namespace lc;
+    set_last_error("");
+    if (flags & ~LC_DEBUG_OPS_STALL) return fail_status(LC_ERR_INVALID_ARG, "lc_ops_debug: unknown debug flags 0x%x", unsigned(flags));
+    debug_flags = flags;
+    return LC_OK;
+}

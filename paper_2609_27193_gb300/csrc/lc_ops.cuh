@@ -57,6 +57,9 @@ lc_status ops_check_rows(const char* call, const char* name, const lc_rows* r, i
 lc_status ops_check_act(const char* call, const lc_act* a, int64_t rows, int64_t dim);
 lc_status ops_launched(const char* call, cudaError_t e);
 
+// Whether the calling thread asked for the test switch of the kernels' waits.
+int ops_stall();
+
 // Keeps rows in 8 bits (the norm uses it where it cannot do so on its own pass).
 cudaError_t act_save_rows(const lc_rows* x, const lc_act* a, int64_t ntok, int64_t dim, cudaStream_t s);
 

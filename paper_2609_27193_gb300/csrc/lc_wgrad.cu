@@ -84,6 +84,7 @@ struct WgradParams {
     int32_t ntiles_n, stages, splits, per_split;   // stages in all, of a split
     int32_t tok_part;      // rows of dy between the parts
     int32_t dw_bf16;
+    int32_t stall;         // test switch: the first copy announces 16 bytes that never come
 };
 
 __device__ __forceinline__ void tma_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
@@ -247,7 +248,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                     ok = it < kStages || mbar_wait_bounded(empty + 8 * st.at, st.round ^ 1, kWaitNs);
                     if (!ok) break;
                     const uint32_t at = tiles + st.at * kStageBytes, bar = full + 8 * st.at;
-                    mbar_expect_tx(bar, kLoadBytes);
+                    mbar_expect_tx(bar, kLoadBytes + (it == 0 && p.stall ? 16 : 0));
                     tma_2d(at + PARTS * kOpBytes, &xmap, w.k0 + rank * kHalf, t, bar);
 #pragma unroll
                     for (int part = 0; part < PARTS; ++part)
@@ -345,6 +346,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                     // for this group.
                     ok = it < kStages || mbar_wait_warp(empty + 8 * st.at, st.round ^ 1);
                     ok = ok && mbar_wait_warp(full + 8 * st.at, st.round);
+                    if (!ok) break;   // no arrival: the other CTA's products read this CTA's half of dy
                     const uint8_t* x = raw + align + st.at * kStageBytes + x_off;
                     uint4 q[4];
 #pragma unroll
@@ -780,6 +782,7 @@ extern "C" lc_status lc_weight_grad(int device, void* cuda_stream, const lc_rows
     p.per_split = int32_t(sh.per_split);
     p.tok_part = int32_t(tok_part);
     p.dw_bf16 = dw->dtype == LC_BF16;
+    p.stall = ops_stall();
     const bool add = accumulate && sh.splits == 1;
     if (f32) e = add ? launch_product<3, true>(device, xmap, ymap, p, s) : launch_product<3, false>(device, xmap, ymap, p, s);
     else e = add ? launch_product<1, true>(device, xmap, ymap, p, s) : launch_product<1, false>(device, xmap, ymap, p, s);

@@ -1,0 +1,42 @@
+"""The operators when a wait inside a kernel runs out: a copy announces 16 bytes more than it brings, every wait gives up
+after a second, what depends on it is NaN, and the next call is right."""
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+from tests.test_gpu_ops import BF, F32, gen, randn  # noqa: E402
+
+
+@pytest.fixture()
+def stalled():
+    """Runs a call with the switch on; off again whatever happens."""
+    from paper_2609_27193_gb300 import _abi
+    lib = _abi.load()
+
+    def run(call):
+        _abi.check(lib.lc_ops_debug(_abi.LC_DEBUG_OPS_STALL))
+        try:
+            return call()
+        finally:
+            _abi.check(lib.lc_ops_debug(0))
+            torch.cuda.synchronize()
+    return run
+
+
+@pytest.mark.parametrize("dt,gt", [(BF, F32), (BF, BF), (F32, F32)])
+@pytest.mark.parametrize("t,n,k", [(100, 70, 200), (2100, 300, 500), (300, 2560, 2816)])
+def test_weight_grad(stalled, dt, gt, t, n, k):
+    """One tile, splits that are joined, and several tiles a pair."""
+    from paper_2609_27193_gb300 import ops
+    g = gen(t)
+    dy, a = randn(g, t, n, dtype=dt), ops.act_save(randn(g, t, k, dtype=dt))
+    want = ops.weight_grad(dy, a, dtype=gt)
+    out = torch.zeros_like(want)
+    stalled(lambda: ops.weight_grad(dy, a, grad=out))
+    assert torch.isnan(out).all()
+    ops.weight_grad(dy, a, grad=out)
+    assert torch.equal(out, want)
+    base = randn(g, n, k, dtype=gt)
+    stalled(lambda: ops.weight_grad(dy, a, grad=base, accumulate=True))
+    assert torch.isnan(base).all()
