@@ -452,9 +452,10 @@ __device__ __forceinline__ uint4 lds128(uint32_t addr) {
 
 // The group's wait for its row.  After a wait that ran out nothing is waited for any
 // more: every row that follows becomes NaN, and the groups still meet at their
-// barriers.
+// barriers.  A warp's lanes take one way (another group may set the word between their
+// reads of it).
 __device__ __forceinline__ bool ring_wait(const RowRing& ring, volatile uint32_t* failed) {
-    if (*failed) return false;
+    if (__any_sync(0xffffffffu, *failed)) return false;
     if (mbar_wait_warp(ring.full(), ring.round)) return true;
     *failed = 1;
     return false;
