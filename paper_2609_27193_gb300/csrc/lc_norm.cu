@@ -450,21 +450,23 @@ __device__ __forceinline__ uint4 lds128(uint32_t addr) {
     return v;
 }
 
-// The group's wait for its row.  After a wait that ran out nothing is waited for any
-// more: every row that follows becomes NaN, and the groups still meet at their
-// barriers.  A warp's lanes take one way (another group may set the word between their
-// reads of it).
-__device__ __forceinline__ bool ring_wait(const RowRing& ring, volatile uint32_t* failed) {
-    if (__any_sync(0xffffffffu, *failed)) return false;
+// A warp's wait for its row.  After one that ran out it waits for nothing any more: the
+// rows that follow become NaN, since its part of their sums is, and its group still meets
+// at its barriers.  The outcome is the warp's own; a group whose first warp gave up asks
+// for no more rows, and its others give up where those would be.
+__device__ __forceinline__ bool ring_wait(const RowRing& ring, volatile uint32_t& lost) {
+    if (lost) return false;
     if (mbar_wait_warp(ring.full(), ring.round)) return true;
-    *failed = 1;
+    lost = 1;
     return false;
 }
 
-// After a wait that ran out: what is still on its way lands before the memory is given back.
-__device__ __forceinline__ void ring_drain(const RowRing& ring, uint32_t failed, int t) {
-    if (!failed || t) return;
-    for (int i = 0; i < ring.depth; ++i) mbar_wait_bounded(ring.bar + 8 * i, i < ring.at ? ring.round ^ 1 : ring.round, kDrainNs);
+// After a wait that ran out: what is still on its way lands before the memory is given
+// back.  The rows that were not waited for left the ring's rounds behind, so a wait for
+// each parity: one of them is the round that a place is in.
+__device__ __forceinline__ void ring_drain(const RowRing& ring, uint32_t lost, int t) {
+    if (!lost || t) return;
+    for (int i = 0; i < 2 * ring.depth; ++i) mbar_wait_bounded(ring.bar + 8 * (i >> 1), i & 1, kDrainNs);
 }
 
 // Weight or bias as fp32 in the order in which the threads of a group take them:
@@ -491,7 +493,8 @@ __global__ void __launch_bounds__(kFwdThreads, 1) norm_ring_kernel(NormParams p,
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ __align__(16) float shared[2][1][32];
     __shared__ __align__(8) uint64_t bars[R * kRingMax];
-    __shared__ volatile uint32_t failed;
+    __shared__ uint32_t lost_by[NT / 32];
+    volatile uint32_t& lost = lost_by[threadIdx.x >> 5];
     int slot = 0;
     const int t = threadIdx.x % G, group = threadIdx.x / G;
     float4* params = reinterpret_cast<float4*>(smem);
@@ -505,7 +508,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) norm_ring_kernel(NormParams p,
         mbar_init(smem_addr(bars) + 8 * threadIdx.x, 1);
         mbar_init_fence();
     }
-    if (threadIdx.x == 0) failed = 0;
+    lost = 0;
     __syncthreads();
     // rows of the group: consecutive ones go to different CTAs
     const int64_t step = int64_t(gridDim.x) * R;
@@ -520,7 +523,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) norm_ring_kernel(NormParams p,
     if (p.b) stage_param<V, G, VPT>(params + kParam, p.b, p.w_bf16, p.dim, NT);
     __syncthreads();
     for (; r < p.ntok; r += step) {
-        const bool ok = ring_wait(ring, &failed);
+        const bool ok = ring_wait(ring, lost);
         float f[VPT][V];
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
@@ -535,7 +538,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) norm_ring_kernel(NormParams p,
         }
         // the row has been read by all once they met in a sum
         auto refill = [&]() {
-            if (t == 0 && ahead < p.ntok && !failed) {
+            if (t == 0 && ahead < p.ntok && !lost) {
                 mbar_expect_tx(ring.full(), ring.bytes);
                 bulk_g2s(ring.row(), p.x + ahead * p.x_pitch, ring.bytes, ring.full());
             }
@@ -610,7 +613,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) norm_ring_kernel(NormParams p,
             p.rstd[r] = rstd;
         }
     }
-    ring_drain(ring, failed, t);
+    ring_drain(ring, lost, t);
 }
 
 constexpr int kBwdThreads = 512;    // 128 registers each: sums for weight and bias besides the row (rows of 8 values a thread and
@@ -626,7 +629,8 @@ __global__ void __launch_bounds__(kBwdThreads, 1) norm_grad_ring_kernel(NormGrad
     __shared__ __align__(16) float shared[2][2][32];
     float(*shared1)[1][32] = reinterpret_cast<float(*)[1][32]>(shared);
     __shared__ __align__(8) uint64_t bars[R * kRingMax];
-    __shared__ volatile uint32_t failed;
+    __shared__ uint32_t lost_by[NT / 32];
+    volatile uint32_t& lost = lost_by[threadIdx.x >> 5];
     dependents_may_start();
     int slot = 0;
     const int t = threadIdx.x % G, group = threadIdx.x / G;
@@ -643,7 +647,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) norm_grad_ring_kernel(NormGrad
         mbar_init(smem_addr(bars) + 8 * threadIdx.x, 1);
         mbar_init_fence();
     }
-    if (threadIdx.x == 0) failed = 0;
+    lost = 0;
     __syncthreads();
     const int64_t step = int64_t(gridDim.x) * R;
     int64_t r = int64_t(group) * gridDim.x + blockIdx.x;
@@ -679,7 +683,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) norm_grad_ring_kernel(NormGrad
     };
     row_values(r);
     for (; r < p.ntok; r += step) {
-        const bool ok = ring_wait(ring, &failed);
+        const bool ok = ring_wait(ring, lost);
         float2 a[VPT][V / 2], h[VPT][V / 2];   // dy, then dy w; x, then its normalised value
         const float mu = mean, rs = ok ? rstd : __uint_as_float(0x7fffffffu);
 #pragma unroll
@@ -745,7 +749,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) norm_grad_ring_kernel(NormGrad
             group_sum<G, NT>(s, shared, slot);
         }
         if constexpr (G == 32) __syncwarp();
-        if (t == 0 && ahead < p.ntok && !failed) fetch(ring.at);
+        if (t == 0 && ahead < p.ntok && !lost) fetch(ring.at);
         ahead += step;
         ring.next();
         if (p.dx) {
@@ -764,7 +768,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) norm_grad_ring_kernel(NormGrad
             }
         }
     }
-    ring_drain(ring, failed, t);
+    ring_drain(ring, lost, t);
     if (!p.want_params) return;
     // one row of sums for the CTA: every group leaves its own in the rings' memory (all rows were read), and each
     // column is added over the groups in order
