@@ -36,6 +36,7 @@ struct NormParams {
     int64_t ntok, x_pitch, y_pitch, q_pitch, e_pitch;
     float eps, inv_dim;
     int32_t dim, w_bf16, rms;
+    int32_t stall;        // test switch: a ring's first copy announces 16 bytes that never come
 };
 
 struct NormGradParams {
@@ -51,6 +52,7 @@ struct NormGradParams {
     int64_t ntok, dy_pitch, x_pitch, q_pitch, e_pitch, dx_pitch;
     float inv_dim;
     int32_t dim, w_bf16, rms, want_params;
+    int32_t stall;        // as in NormParams
 };
 
 // The columns that a thread of a group of G holds: VPT vectors of V, 16 bytes each
@@ -516,7 +518,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) norm_ring_kernel(NormParams p,
     int64_t ahead = r;           // first row not asked for
     if (t == 0)
         for (int i = 0; i < depth && ahead < p.ntok; ++i, ahead += step) {
-            mbar_expect_tx(ring.bar + 8 * i, ring.bytes);
+            mbar_expect_tx(ring.bar + 8 * i, ring.bytes + (i == 0 && p.stall ? 16 : 0));
             bulk_g2s(ring.data + i * ring.bytes, p.x + ahead * p.x_pitch, ring.bytes, ring.bar + 8 * i);
         }
     stage_param<V, G, VPT>(params, p.w, p.w_bf16, p.dim, NT);
@@ -652,14 +654,14 @@ __global__ void __launch_bounds__(kBwdThreads, 1) norm_grad_ring_kernel(NormGrad
     const int64_t step = int64_t(gridDim.x) * R;
     int64_t r = int64_t(group) * gridDim.x + blockIdx.x;
     int64_t ahead = r;
-    auto fetch = [&](int at) {
+    auto fetch = [&](int at, uint32_t more) {
         const uint32_t to = ring.data + at * ring.bytes, bar = ring.bar + 8 * at;
-        mbar_expect_tx(bar, ring.bytes);
+        mbar_expect_tx(bar, ring.bytes + more);
         bulk_g2s(to, p.dy + ahead * p.dy_pitch, dy_bytes, bar);
         bulk_g2s(to + dy_bytes, KEPT ? reinterpret_cast<const uint8_t*>(p.q) + ahead * p.q_pitch : p.x + ahead * p.x_pitch, x_bytes, bar);
     };
     if (t == 0)
-        for (int i = 0; i < depth && ahead < p.ntok; ++i, ahead += step) fetch(i);
+        for (int i = 0; i < depth && ahead < p.ntok; ++i, ahead += step) fetch(i, i == 0 && p.stall ? 16 : 0);
     stage_param<V, G, VPT>(params, p.w, p.w_bf16, p.dim, NT);
     __syncthreads();
     float2 dw[VPT][V / 2], db[LEAN ? 1 : VPT][V / 2];
@@ -749,7 +751,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) norm_grad_ring_kernel(NormGrad
             group_sum<G, NT>(s, shared, slot);
         }
         if constexpr (G == 32) __syncwarp();
-        if (t == 0 && ahead < p.ntok && !lost) fetch(ring.at);
+        if (t == 0 && ahead < p.ntok && !lost) fetch(ring.at, 0);
         ahead += step;
         ring.next();
         if (p.dx) {
@@ -770,6 +772,13 @@ __global__ void __launch_bounds__(kBwdThreads, 1) norm_grad_ring_kernel(NormGrad
     }
     ring_drain(ring, lost, t);
     if (!p.want_params) return;
+    if (lost) {
+        // NaN came into dw with h; db has added up whatever was in the row's place
+#pragma unroll
+        for (int i = 0; i < VPT; ++i)
+#pragma unroll
+            for (int j = 0; j < V / 2; ++j) dw[i][j] = db[LEAN ? 0 : i][j] = both(__uint_as_float(0x7fffffffu));
+    }
     // one row of sums for the CTA: every group leaves its own in the rings' memory (all rows were read), and each
     // column is added over the groups in order
     float* out = p.part + int64_t(blockIdx.x) * 2 * p.dim;
@@ -1081,6 +1090,7 @@ extern "C" lc_status lc_norm(int device, void* cuda_stream, int32_t kind, const 
     p.dim = int32_t(dim);
     p.w_bf16 = w_dtype == LC_BF16;
     p.rms = kind == LC_NORM_RMS;
+    p.stall = ops_stall();
     const bool vec = aligned16(p.x) && aligned16(p.y) && aligned16(p.w) && aligned16(p.b) && p.x_pitch % 16 == 0 &&
                      p.y_pitch % 16 == 0;
     const int sms = ops_sm_count(device);
@@ -1204,6 +1214,7 @@ extern "C" lc_status lc_norm_grad(int device, void* cuda_stream, int32_t kind, c
     p.w_bf16 = w_dtype == LC_BF16;
     p.rms = kind == LC_NORM_RMS;
     p.want_params = want;
+    p.stall = ops_stall();
     const bool vec = aligned16(p.dy) && aligned16(p.x) && aligned16(p.dx) && aligned16(p.w) && p.dy_pitch % 16 == 0 &&
                      p.x_pitch % 16 == 0 && p.dx_pitch % 16 == 0;
     const int sms = ops_sm_count(device);

@@ -40,3 +40,27 @@ def test_weight_grad(stalled, dt, gt, t, n, k):
     base = randn(g, n, k, dtype=gt)
     stalled(lambda: ops.weight_grad(dy, a, grad=base, accumulate=True))
     assert torch.isnan(base).all()
+
+
+@pytest.mark.parametrize("kind", ["layer", "rms"])
+@pytest.mark.parametrize("t,d,dt", [(5000, 256, BF), (700, 1024, F32), (400, 4096, BF), (320, 16384, F32)])
+def test_norm(stalled, kind, t, d, dt):
+    """Every group's first row does not come; the rows that follow are not waited for."""
+    from paper_2609_27193_gb300 import ops
+    g = gen(t)
+    x, dy, w = randn(g, t, d, dtype=dt), randn(g, t, d, dtype=dt), 1 + randn(g, d, dtype=dt, spread=0.2)
+    b = randn(g, d, dtype=dt) if kind == "layer" else None
+    want = ops.norm(x, w, b, kind=kind, keep=True)
+    _, mean, rstd, act = want
+    got = stalled(lambda: ops.norm(x, w, b, kind=kind, keep=True))
+    assert torch.isnan(got[0]).all() and torch.isnan(got[2]).all() and (mean is None or torch.isnan(got[1]).all())
+    assert (got[3].e == 127).all() and (got[3].q == 0).all()
+    again = ops.norm(x, w, b, kind=kind, keep=True)
+    assert all(p is q is None or torch.equal(p, q) for p, q in zip(again[:3], want[:3]))
+    assert torch.equal(again[3].q, act.q) and torch.equal(again[3].e, act.e)
+    for seen in (x, act):
+        for bias in (True, False):
+            right = ops.norm_grad(dy, seen, w, mean, rstd, bias=bias)
+            lost = stalled(lambda: ops.norm_grad(dy, seen, w, mean, rstd, bias=bias))
+            assert all(p is None or torch.isnan(p).all() for p in lost)
+            assert all(p is q is None or torch.equal(p, q) for p, q in zip(ops.norm_grad(dy, seen, w, mean, rstd, bias=bias), right))
