@@ -119,8 +119,15 @@ int ids_of(const at::Tensor& t) {
     if (t.dim() != 1 || !t.is_contiguous()) throw ValueError("ids must be 1-D and contiguous");
     return code;
 }
-lc_act act_of(const at::Tensor& q, const at::Tensor& e) {
-    // their layout was checked when the checkpoint was made
+// A checkpoint of n rows of dim values.  What was checked when it was made is checked
+// for every call: its tensors and its width can be other ones by now.
+lc_act act_of(const at::Tensor& q, const at::Tensor& e, int64_t n, int64_t dim) {
+    const int64_t blocks = (dim + LC_ACT_BLOCK - 1) / LC_ACT_BLOCK;
+    if (!q.defined() || !e.defined() || dim < 1 || q.scalar_type() != at::kChar || e.scalar_type() != at::kChar || q.dim() != 2 ||
+        e.dim() != 2 || q.size(0) != n || e.size(0) != n || q.size(1) < blocks * LC_ACT_BLOCK || e.size(1) < blocks ||
+        q.stride(1) != 1 || (e.stride(1) != 1 && e.size(1) > 1))
+        throw ValueError("a checkpoint of " + std::to_string(n) + " rows of " + std::to_string(dim) + " has int8 rows of " +
+                         std::to_string(blocks * LC_ACT_BLOCK) + " values and " + std::to_string(blocks) + " exponents");
     return lc_act{static_cast<int8_t*>(q.data_ptr()), q.stride(0), static_cast<int8_t*>(e.data_ptr()), e.stride(0)};
 }
 
@@ -220,7 +227,7 @@ PyObject* act_save(PyObject* const* args, Py_ssize_t nargs) {
     same_device(index, q);
     same_device(index, e);
     const lc_rows rx = rows_of(x, "x");
-    const lc_act act = act_of(q, e);
+    const lc_act act = act_of(q, e, x.size(0), x.size(1));
     check(lc_act_save(index, stream_of(index), &rx, x.size(0), x.size(1), &act));
     Py_RETURN_NONE;
 }
@@ -232,12 +239,14 @@ PyObject* act_load(PyObject* const* args, Py_ssize_t nargs) {
     at::Tensor out = a.tensor();
     const int64_t dtype = a.integer();
     const int index = cuda_index(q);
+    same_device(index, e);
     same_device(index, out);
+    if (!q.dim()) throw ValueError("a checkpoint has rows");
     const int64_t n = q.size(0);
+    const lc_act act = act_of(q, e, n, dim);
     if (out.defined()) shaped(out, n, dim, "out");
     else out = make({n, dim}, type_of(dtype), q);
     const lc_rows ro = rows_of(out, "out");
-    const lc_act act = act_of(q, e);
     check(lc_act_load(index, stream_of(index), &act, n, dim, &ro));
     return wrapped(out);
 }
@@ -271,7 +280,7 @@ PyObject* norm(PyObject* const* args, Py_ssize_t nargs) {
     const lc_rows ro = rows_of(out, "out");
     const at::Tensor rstd = make({n}, at::kFloat, x), mean = kind == LC_NORM_LAYER ? make({n}, at::kFloat, x) : at::Tensor();
     lc_act keep{};
-    if (q.defined()) keep = act_of(q, e);
+    if (q.defined()) keep = act_of(q, e, n, dim);
     check(lc_norm(index, stream_of(index), kind, &rx, n, dim, w, b, code_of(weight, "weight"), eps, &ro, stat_of(mean, n),
                   stat_of(rstd, n), q.defined() ? &keep : nullptr));
     return tuple(out, mean, rstd);
@@ -298,8 +307,8 @@ PyObject* norm_grad(PyObject* const* args, Py_ssize_t nargs) {
     lc_rows rx{};
     lc_act kept{};
     if (q.defined()) {
-        if (q.size(0) != n || kept_dim != dim) throw ValueError("x must have dy's shape");
-        kept = act_of(q, e);
+        if (kept_dim != dim) throw ValueError("x must have dy's shape");
+        kept = act_of(q, e, n, dim);
     } else {
         cuda_index(x);
         rx = rows_of(x, "x");
@@ -336,7 +345,7 @@ PyObject* weight_grad(PyObject* const* args, Py_ssize_t nargs) {
     for (const at::Tensor* t : {&q, &e, static_cast<const at::Tensor*>(&grad)}) same_device(index, *t);
     const lc_rows rd = rows_of(dy, "dy");
     const int64_t n = dy.size(0), rows = dy.size(1);
-    if (q.size(0) != n) throw ValueError("dy and the checkpoint must have the same number of tokens");
+    const lc_act act = act_of(q, e, n, dim);
     if (grad.defined()) {
         shaped(grad, rows, dim, "grad");
     } else {
@@ -344,7 +353,6 @@ PyObject* weight_grad(PyObject* const* args, Py_ssize_t nargs) {
         grad = make({rows, dim}, type_of(dtype), dy);
     }
     const lc_rows rg = rows_of(grad, "grad");
-    const lc_act act = act_of(q, e);
     void* stream = stream_of(index);
     const uint64_t need = lc_weight_grad_workspace(n, rows, dim, rd.dtype);
     const Scratch scratch(dy, index, stream, need);

@@ -1,0 +1,46 @@
+"""What the operators' binding refuses before anything runs on the GPU."""
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+from tests.test_gpu_ops import BF, gen, randn  # noqa: E402
+
+
+@pytest.fixture(scope="module")
+def ops():
+    from paper_2609_27193_gb300 import ops
+    return ops
+
+
+def test_a_checkpoint_that_changed_after_it_was_made(ops):
+    g = gen(61)
+    t, d = 40, 300
+    x, dy, w = randn(g, t, d, dtype=BF), randn(g, t, d, dtype=BF), torch.ones(d, dtype=BF, device="cuda")
+    good = ops.act_save(x)
+    _, mean, rstd = ops.norm(x, w)
+    want = ops.act_load(good)
+
+    def broken():
+        for field, value in (("q", good.q[:, :256]), ("q", good.q[:t - 1]), ("q", good.q.view(torch.uint8)), ("q", good.q.view(-1)),
+                             ("q", good.q.t().contiguous().t()), ("e", good.e[:, :2]), ("e", good.e[:t - 1]), ("e", good.e.float()),
+                             ("e", good.e.t().contiguous().t()), ("dim", 10 ** 6), ("dim", 0), ("dim", -5), ("e", good.e.cpu())):
+            a = ops.Act(good.q, good.e, d)
+            setattr(a, field, value)
+            yield a
+    for a in broken():
+        with pytest.raises(ValueError):
+            ops.act_load(a)
+        with pytest.raises(ValueError):
+            ops.act_save(x, a)
+        with pytest.raises(ValueError):
+            ops.norm(x, w, keep=a)
+        with pytest.raises(ValueError):
+            ops.norm_grad(dy, a, w, mean, rstd)
+        with pytest.raises(ValueError):
+            ops.weight_grad(dy, a)
+    a = ops.Act(good.q, good.e, d)
+    a.e = None
+    with pytest.raises(ValueError):
+        ops.weight_grad(dy, a)
+    assert torch.equal(ops.act_load(good), want)
