@@ -128,7 +128,9 @@ lc_act act_of(const at::Tensor& q, const at::Tensor& e, int64_t n, int64_t dim) 
         q.stride(1) != 1 || (e.stride(1) != 1 && e.size(1) > 1))
         throw ValueError("a checkpoint of " + std::to_string(n) + " rows of " + std::to_string(dim) + " has int8 rows of " +
                          std::to_string(blocks * LC_ACT_BLOCK) + " values and " + std::to_string(blocks) + " exponents");
-    return lc_act{static_cast<int8_t*>(q.data_ptr()), q.stride(0), static_cast<int8_t*>(e.data_ptr()), e.stride(0)};
+    // (the stride of a single row may be anything)
+    return lc_act{static_cast<int8_t*>(q.data_ptr()), n > 1 ? q.stride(0) : blocks * LC_ACT_BLOCK, static_cast<int8_t*>(e.data_ptr()),
+                  n > 1 ? e.stride(0) : blocks};
 }
 
 // A new tensor on the device of another one (past torch's dispatcher: 1 us less a tensor).

@@ -44,3 +44,14 @@ def test_a_checkpoint_that_changed_after_it_was_made(ops):
     with pytest.raises(ValueError):
         ops.weight_grad(dy, a)
     assert torch.equal(ops.act_load(good), want)
+
+
+def test_one_row_may_have_any_stride(ops):
+    g = gen(62)
+    x, dy = randn(g, 1, 200, dtype=BF), randn(g, 1, 70, dtype=BF)
+    want = ops.act_save(x)
+    a = ops.Act(torch.zeros(256, 1, dtype=torch.int8, device="cuda").t(), torch.zeros(2, 1, dtype=torch.int8, device="cuda").t(), 200)
+    assert a.q.stride() == (1, 1) and a.e.stride() == (1, 1)
+    ops.act_save(x, a)
+    assert torch.equal(a.q, want.q) and torch.equal(a.e, want.e) and torch.equal(ops.act_load(a), ops.act_load(want))
+    assert torch.equal(ops.weight_grad(dy, a), ops.weight_grad(dy, want))
