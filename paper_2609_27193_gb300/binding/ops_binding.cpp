@@ -8,10 +8,12 @@
 
 #include <ATen/core/Tensor.h>
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/core/GradMode.h>
 #include <c10/cuda/CUDAStream.h>
 #include <cuda_runtime_api.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <initializer_list>
 #include <map>
 #include <stdexcept>
 #include <string>
@@ -133,6 +135,16 @@ lc_act act_of(const at::Tensor& q, const at::Tensor& e, int64_t n, int64_t dim) 
                   n > 1 ? e.stride(0) : blocks};
 }
 
+// The forward calls leave no trace for autograd: with it on, what a parameter went into
+// would come out detached, and training would go on without that parameter's gradient.
+void unrecorded(const char* call, std::initializer_list<const at::Tensor*> inputs) {
+    if (!at::GradMode::is_enabled()) return;
+    for (const at::Tensor* t : inputs)
+        if (t->defined() && t->requires_grad())
+            throw std::runtime_error(std::string(call) + " is not recorded by autograd, and an input requires a gradient: call it under "
+                                     "torch.no_grad() or in the forward of a torch.autograd.Function");
+}
+
 // A new tensor on the device of another one (past torch's dispatcher: 1 us less a tensor).
 at::Tensor make(at::IntArrayRef size, at::ScalarType type, const at::Tensor& like) {
     return at::detail::empty_cuda(size, type, like.device(), std::nullopt);
@@ -182,6 +194,7 @@ PyObject* embed(PyObject* const* args, Py_ssize_t nargs) {
     const int index = cuda_index(table), type = ids_of(ids);
     same_device(index, ids);
     same_device(index, out);
+    unrecorded("embed", {&table, &out});
     const lc_rows rt = rows_of(table, "table");
     const int64_t n = ids.numel(), dim = table.size(1);
     if (out.defined()) shaped(out, n, dim, "out");
@@ -272,6 +285,7 @@ PyObject* norm(PyObject* const* args, Py_ssize_t nargs) {
     const int index = cuda_index(x);
     cuda_index(weight);
     for (const at::Tensor* t : {&weight, &bias, static_cast<const at::Tensor*>(&out), &q, &e}) same_device(index, *t);
+    unrecorded("norm", {&x, &weight, &bias, &out});
     const lc_rows rx = rows_of(x, "x");
     const int64_t n = x.size(0), dim = x.size(1);
     const void* w = param_of(weight, dim, "weight");

@@ -10,6 +10,10 @@ scratch is one tensor a device and stream that grows to the largest call.  A cal
 inside torch.cuda.graph has scratch of its own from the graph's pool, so graphs
 may be replayed beside other calls and one another.  There is no CPU fallback.
 
+Autograd records none of this: the gradients are calls too, for training loops
+that write their backward pass themselves and for torch.autograd.Function.
+embed and norm refuse inputs that require a gradient while grad mode is on.
+
 Tensors are rows of their last dimension: [tokens, dim] with any row stride
 (an expanded row, stride 0, may be an input) and bfloat16 or float32 elements.
 """

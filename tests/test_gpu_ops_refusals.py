@@ -55,3 +55,42 @@ def test_one_row_may_have_any_stride(ops):
     ops.act_save(x, a)
     assert torch.equal(a.q, want.q) and torch.equal(a.e, want.e) and torch.equal(ops.act_load(a), ops.act_load(want))
     assert torch.equal(ops.weight_grad(dy, a), ops.weight_grad(dy, want))
+
+
+def test_inputs_that_autograd_would_lose(ops):
+    """A parameter that goes through a forward call would come out detached: refused while grad mode is on."""
+    g = gen(63)
+    t, d = 12, 64
+    x, ids = randn(g, t, d), torch.randint(0, t, (t,), generator=g, device="cuda")
+    w, b = torch.nn.Parameter(torch.ones(d, device="cuda")), torch.nn.Parameter(torch.zeros(d, device="cuda"))
+    table = torch.nn.Parameter(x.clone())
+    for call in (lambda: ops.embed(table, ids), lambda: ops.norm(table, w.detach()), lambda: ops.norm(x, w),
+                 lambda: ops.norm(x, w.detach(), b), lambda: ops.norm(x, w.detach(), out=table)):
+        with pytest.raises(RuntimeError, match="autograd"):
+            call()
+        with torch.no_grad():
+            call()
+    # where torch differentiates by itself, and where nothing requires a gradient
+    with torch.inference_mode():
+        ops.norm(x, w, out=torch.empty_like(x))
+    y, mean, rstd = ops.norm(x, w.detach())
+    ops.norm_grad(y, x, w, mean, rstd)
+
+    class Norm(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, w):
+            y, mean, rstd = ops.norm(x, w)
+            ctx.save_for_backward(x, w, mean, rstd)
+            return y
+
+        @staticmethod
+        def backward(ctx, dy):
+            x, w, mean, rstd = ctx.saved_tensors
+            dx, dw, _ = ops.norm_grad(dy.contiguous(), x, w, mean, rstd)
+            return dx, dw
+    p = x.clone().requires_grad_()
+    Norm.apply(p, w).square().sum().backward()
+    q, v = x.double().requires_grad_(), w.detach().double().requires_grad_()
+    torch.nn.functional.layer_norm(q, (d,), v, None, 1e-5).square().sum().backward()
+    # two fp32 norms of 64 columns and sums of 12 rows: far below this
+    assert (p.grad - q.grad).abs().max() < 1e-4 and (w.grad - v.grad).abs().max() < 1e-4
