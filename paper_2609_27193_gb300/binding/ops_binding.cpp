@@ -144,6 +144,11 @@ void unrecorded(const char* call, std::initializer_list<const at::Tensor*> input
             throw std::runtime_error(std::string(call) + " is not recorded by autograd, and an input requires a gradient: call it under "
                                      "torch.no_grad() or in the forward of a torch.autograd.Function");
 }
+// A tensor that was passed in has other contents now; torch's check of what a backward
+// saved goes by this count (which inference tensors do not have).
+void written(const at::Tensor& t) {
+    if (t.defined() && !t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
 
 // A new tensor on the device of another one (past torch's dispatcher: 1 us less a tensor).
 at::Tensor make(at::IntArrayRef size, at::ScalarType type, const at::Tensor& like) {
@@ -201,6 +206,7 @@ PyObject* embed(PyObject* const* args, Py_ssize_t nargs) {
     else out = make({n, dim}, table.scalar_type(), table);
     const lc_rows ro = rows_of(out, "out");
     check(lc_embed(index, stream_of(index), &rt, table.size(0), dim, ids.data_ptr(), type, n, float(scale), &ro));
+    written(out);
     return wrapped(out);
 }
 
@@ -232,6 +238,7 @@ PyObject* embed_grad(PyObject* const* args, Py_ssize_t nargs) {
     const Scratch scratch(dy, index, stream, need);
     check(lc_embed_grad(index, stream, &rd, ids.data_ptr(), type, n, float(scale), skip, &rg, vocab, dim, accumulate,
                         scratch.p, need));
+    written(grad);
     return wrapped(grad);
 }
 
@@ -244,6 +251,8 @@ PyObject* act_save(PyObject* const* args, Py_ssize_t nargs) {
     const lc_rows rx = rows_of(x, "x");
     const lc_act act = act_of(q, e, x.size(0), x.size(1));
     check(lc_act_save(index, stream_of(index), &rx, x.size(0), x.size(1), &act));
+    written(q);
+    written(e);
     Py_RETURN_NONE;
 }
 
@@ -263,6 +272,7 @@ PyObject* act_load(PyObject* const* args, Py_ssize_t nargs) {
     else out = make({n, dim}, type_of(dtype), q);
     const lc_rows ro = rows_of(out, "out");
     check(lc_act_load(index, stream_of(index), &act, n, dim, &ro));
+    written(out);
     return wrapped(out);
 }
 
@@ -299,6 +309,7 @@ PyObject* norm(PyObject* const* args, Py_ssize_t nargs) {
     if (q.defined()) keep = act_of(q, e, n, dim);
     check(lc_norm(index, stream_of(index), kind, &rx, n, dim, w, b, code_of(weight, "weight"), eps, &ro, stat_of(mean, n),
                   stat_of(rstd, n), q.defined() ? &keep : nullptr));
+    for (const at::Tensor* t : {static_cast<const at::Tensor*>(&out), &q, &e}) written(*t);
     return tuple(out, mean, rstd);
 }
 
@@ -347,6 +358,7 @@ PyObject* norm_grad(PyObject* const* args, Py_ssize_t nargs) {
     check(lc_norm_grad(index, stream, mean.defined() ? LC_NORM_LAYER : LC_NORM_RMS, &rd, q.defined() ? nullptr : &rx,
                        q.defined() ? &kept : nullptr, n, dim, w, code_of(weight, "weight"), m, r, &rdx, pw, pb,
                        code_of(dweight, "dweight"), accumulate, scratch.p, need));
+    for (const at::Tensor* t : {&dx, &dweight, &dbias}) written(*t);
     return tuple(dx, dweight, dbias);
 }
 
@@ -373,6 +385,7 @@ PyObject* weight_grad(PyObject* const* args, Py_ssize_t nargs) {
     const uint64_t need = lc_weight_grad_workspace(n, rows, dim, rd.dtype);
     const Scratch scratch(dy, index, stream, need);
     check(lc_weight_grad(index, stream, &rd, &act, n, rows, dim, &rg, accumulate, scratch.p, need));
+    written(grad);
     return wrapped(grad);
 }
 

@@ -94,3 +94,35 @@ def test_inputs_that_autograd_would_lose(ops):
     torch.nn.functional.layer_norm(q, (d,), v, None, 1e-5).square().sum().backward()
     # two fp32 norms of 64 columns and sums of 12 rows: far below this
     assert (p.grad - q.grad).abs().max() < 1e-4 and (w.grad - v.grad).abs().max() < 1e-4
+
+
+def test_what_is_written_counts_as_written(ops):
+    """torch refuses a backward pass over saved tensors that a call has overwritten."""
+    g = gen(64)
+    t, d = 12, 128
+    x, dy, w = randn(g, t, d), randn(g, t, d), torch.ones(d, device="cuda")
+    ids = torch.randint(0, t, (t,), generator=g, device="cuda")
+    a = ops.act_save(x)
+    _, mean, rstd = ops.norm(x, w)
+
+    def fresh(*shape):
+        return torch.zeros(*shape, device="cuda")
+    o, p, q = fresh(t, d), fresh(d), fresh(d)
+    b = ops.act_save(x)
+    for tensors, call in (((o,), lambda: ops.embed(x, ids, out=o)), ((o,), lambda: ops.embed_grad(dy, ids, grad=o)),
+                          ((b.q, b.e), lambda: ops.act_save(x, b)), ((o,), lambda: ops.act_load(a, out=o)),
+                          ((o, b.q, b.e), lambda: ops.norm(x, w, out=o, keep=b)),
+                          ((o, p, q), lambda: ops.norm_grad(dy, x, w, mean, rstd, dx=o, dweight=p, dbias=q))):
+        before = [v._version for v in tensors]
+        call()
+        assert all(v._version > n for v, n in zip(tensors, before))
+    dw = fresh(d, d)
+    n = dw._version
+    ops.weight_grad(dy, a, grad=dw)
+    assert dw._version > n
+    s = torch.ones(t, d, device="cuda", requires_grad=True)
+    y = s * o
+    with torch.no_grad():
+        ops.norm(x, w, out=o)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.sum().backward()
