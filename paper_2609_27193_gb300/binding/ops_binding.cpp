@@ -24,6 +24,7 @@
 namespace {
 
 PyObject* g_error = nullptr;   // the package's LCError
+PyObject* g_memory = nullptr;  // torch's OutOfMemoryError
 
 struct TypeError : std::runtime_error {
     using std::runtime_error::runtime_error;
@@ -389,10 +390,12 @@ PyObject* weight_grad(PyObject* const* args, Py_ssize_t nargs) {
     return wrapped(grad);
 }
 
-PyObject* set_error(PyObject* const* args, Py_ssize_t nargs) {
-    if (nargs != 1) throw TypeError("wrong number of arguments");
-    Py_XINCREF(args[0]);
+PyObject* set_errors(PyObject* const* args, Py_ssize_t nargs) {
+    if (nargs != 2) throw TypeError("wrong number of arguments");
+    Py_INCREF(args[0]);
     Py_XSETREF(g_error, args[0]);
+    Py_INCREF(args[1]);
+    Py_XSETREF(g_memory, args[1]);
     Py_RETURN_NONE;
 }
 
@@ -414,6 +417,8 @@ PyObject* guarded(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     } catch (const ValueError& e) {
         PyErr_SetString(PyExc_ValueError, e.what());
     } catch (const Raised&) {
+    } catch (const c10::OutOfMemoryError& e) {
+        PyErr_SetString(g_memory ? g_memory : PyExc_MemoryError, e.what_without_backtrace());
     } catch (const std::exception& e) {
         PyErr_SetString(PyExc_RuntimeError, e.what());
     }
@@ -422,7 +427,7 @@ PyObject* guarded(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
 
 #define LC_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(guarded<name>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {LC_METHOD(embed),    LC_METHOD(embed_grad), LC_METHOD(act_save),    LC_METHOD(act_load), LC_METHOD(new_act),
-                         LC_METHOD(norm),     LC_METHOD(norm_grad),  LC_METHOD(weight_grad), LC_METHOD(set_error),
+                         LC_METHOD(norm),     LC_METHOD(norm_grad),  LC_METHOD(weight_grad), LC_METHOD(set_errors),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_ops", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

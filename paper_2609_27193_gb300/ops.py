@@ -25,7 +25,7 @@ from ._abi import LC_ACT_BLOCK, LC_BF16, LC_F32, LC_NORM_LAYER, LC_NORM_RMS
 _abi.load()               # says how to build what is missing
 from . import _ops        # noqa: E402
 
-_ops.set_error(_abi.LCError)
+_ops.set_errors(_abi.LCError, torch.OutOfMemoryError)
 
 __all__ = ["Act", "embed", "embed_grad", "norm", "norm_grad", "act_save", "act_load", "weight_grad"]
 

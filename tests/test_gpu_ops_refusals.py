@@ -126,3 +126,10 @@ def test_what_is_written_counts_as_written(ops):
         ops.norm(x, w, out=o)
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         y.sum().backward()
+
+
+def test_an_output_that_does_not_fit(ops):
+    """16 TB: what a program catches around torch's own allocations it catches here."""
+    dy, ids = torch.zeros(1, 4096, device="cuda"), torch.zeros(1, dtype=torch.int64, device="cuda")
+    with pytest.raises(torch.OutOfMemoryError):
+        ops.embed_grad(dy, ids, 10 ** 9)
