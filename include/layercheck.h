@@ -757,6 +757,10 @@ lc_status lc_weight_grad(int device, void* cuda_stream, const lc_rows* dy, const
                          int64_t rows, int64_t dim, const lc_rows* dw, int32_t accumulate, void* workspace,
                          uint64_t workspace_bytes);
 uint64_t lc_weight_grad_workspace(int64_t ntok, int64_t rows, int64_t dim, int32_t dy_dtype);
+/* What the call needs for this dy (its address and stride; nothing is read): a
+ * 16-bit dy whose rows start on 16-byte boundaries is not copied, which the
+ * size above, enough for any dy of the type, has room for. */
+uint64_t lc_weight_grad_workspace_of(const lc_rows* dy, int64_t ntok, int64_t rows, int64_t dim);
 
 #ifdef __cplusplus
 }

@@ -383,7 +383,7 @@ PyObject* weight_grad(PyObject* const* args, Py_ssize_t nargs) {
     }
     const lc_rows rg = rows_of(grad, "grad");
     void* stream = stream_of(index);
-    const uint64_t need = lc_weight_grad_workspace(n, rows, dim, rd.dtype);
+    const uint64_t need = lc_weight_grad_workspace_of(&rd, n, rows, dim);
     const Scratch scratch(dy, index, stream, need);
     check(lc_weight_grad(index, stream, &rd, &act, n, rows, dim, &rg, accumulate, scratch.p, need));
     written(grad);

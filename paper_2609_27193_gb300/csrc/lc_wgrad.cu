@@ -644,6 +644,13 @@ Shape shape_of(int64_t ntok, int64_t rows, int64_t dim, int32_t dy_dtype) {
 int64_t staged_bytes(int64_t ntok, int64_t rows, int32_t dy_dtype) {
     return al(al(ntok, kTok) * al(rows, 64) * 2 * (dy_dtype == LC_F32 ? 3 : 1), 256);
 }
+// The parts of split tokens lie at the workspace's start, a staged dy behind them.
+int64_t part_bytes(const Shape& s, int64_t rows, int64_t dim) { return s.splits > 1 ? al(s.splits * rows * dim * 4, 256) : 0; }
+// Whether dy has to be staged: 32 bits, or rows that a bulk tensor copy cannot take.
+bool staged_dy(const lc_rows* dy, int64_t rows) {
+    const int64_t pitch = dy->stride * elem_size(dy->dtype);
+    return dy->dtype == LC_F32 || !aligned16(dy->data) || pitch % 16 || pitch < rows * 2;
+}
 // Pairs of CTAs that the device holds at once.
 template <int PARTS, bool ACC>
 cudaError_t resident_pairs(int device, int* pairs) {
@@ -681,6 +688,9 @@ cudaError_t launch_product(int device, const CUtensorMap& xmap, const CUtensorMa
 }
 
 constexpr int64_t kMost = (int64_t(1) << 31) - 1024;
+bool sizes_in_range(int64_t ntok, int64_t rows, int64_t dim) {
+    return ntok > 0 && rows > 0 && dim > 0 && ntok <= kMost && rows <= kMost && dim <= kMost;
+}
 
 }  // namespace
 }  // namespace lc
@@ -688,10 +698,14 @@ constexpr int64_t kMost = (int64_t(1) << 31) - 1024;
 using namespace lc;
 
 extern "C" uint64_t lc_weight_grad_workspace(int64_t ntok, int64_t rows, int64_t dim, int32_t dy_dtype) {
-    if (ntok <= 0 || rows <= 0 || dim <= 0 || ntok > kMost || rows > kMost || dim > kMost || !elem_size(dy_dtype)) return 0;
-    const Shape s = shape_of(ntok, rows, dim, dy_dtype);
-    // rows of dy off 16 bytes, or in 32 bits, are staged; the caller need not know which
-    return uint64_t(staged_bytes(ntok, rows, dy_dtype)) + (s.splits > 1 ? uint64_t(al(s.splits * rows * dim * 4, 256)) : 0);
+    if (!sizes_in_range(ntok, rows, dim) || !elem_size(dy_dtype)) return 0;
+    return uint64_t(staged_bytes(ntok, rows, dy_dtype)) + uint64_t(part_bytes(shape_of(ntok, rows, dim, dy_dtype), rows, dim));
+}
+
+extern "C" uint64_t lc_weight_grad_workspace_of(const lc_rows* dy, int64_t ntok, int64_t rows, int64_t dim) {
+    if (!dy || !sizes_in_range(ntok, rows, dim) || !elem_size(dy->dtype)) return 0;
+    return uint64_t(staged_dy(dy, rows) ? staged_bytes(ntok, rows, dy->dtype) : 0) +
+           uint64_t(part_bytes(shape_of(ntok, rows, dim, dy->dtype), rows, dim));
 }
 
 extern "C" lc_status lc_weight_grad(int device, void* cuda_stream, const lc_rows* dy, const lc_act* x, int64_t ntok,
@@ -706,7 +720,7 @@ extern "C" lc_status lc_weight_grad(int device, void* cuda_stream, const lc_rows
     if (st == LC_OK) st = ops_check_act(call, x, ntok, dim);
     if (st == LC_OK) st = ops_check_rows(call, "dw", dw, rows, dim, true);
     if (st != LC_OK) return st;
-    const uint64_t need = lc_weight_grad_workspace(ntok, rows, dim, dy->dtype);
+    const uint64_t need = lc_weight_grad_workspace_of(dy, ntok, rows, dim);
     if (workspace_bytes < need)
         return fail_status(LC_ERR_CAPACITY, "%s: %llu bytes of workspace, %llu needed", call,
                            (unsigned long long)workspace_bytes, (unsigned long long)need);
@@ -737,14 +751,15 @@ extern "C" lc_status lc_weight_grad(int device, void* cuda_stream, const lc_rows
     if (tiles * sh.splits > kMost) return fail_status(LC_ERR_INVALID_ARG, "%s: too many outputs", call);
     const int64_t dy_pitch = dy->stride * elem_size(dy->dtype);
     const bool f32 = dy->dtype == LC_F32;
-    const bool staged = f32 || !aligned16(dy->data) || dy_pitch % 16 || dy_pitch < rows * 2;
+    const bool staged = staged_dy(dy, rows);
+    uint8_t* const stage = static_cast<uint8_t*>(workspace) + part_bytes(sh, rows, dim);
     const void* ydata = dy->data;
     int64_t ypitch = dy_pitch, yrows = ntok, ycols = rows, tok_part = 0;
     cudaError_t e = cudaSuccess;
     if (staged) {
         StageParams q{};
         q.dy = static_cast<const uint8_t*>(dy->data);
-        q.out = static_cast<__nv_bfloat16*>(workspace);
+        q.out = reinterpret_cast<__nv_bfloat16*>(stage);
         q.dy_pitch = dy_pitch;
         q.tok_pad = al(ntok, kTok);
         q.col_pad = al(rows, 64);
@@ -756,7 +771,7 @@ extern "C" lc_status lc_weight_grad(int device, void* cuda_stream, const lc_rows
         wgrad_stage_kernel<<<unsigned(grid), 256, 0, s>>>(q);
         e = cudaGetLastError();
         if (e != cudaSuccess) return ops_launched(call, e);
-        ydata = workspace;
+        ydata = stage;
         ypitch = q.col_pad * 2;
         ycols = q.col_pad;
         tok_part = q.tok_pad;
@@ -769,7 +784,7 @@ extern "C" lc_status lc_weight_grad(int device, void* cuda_stream, const lc_rows
     WgradParams p{};
     p.e = x->e;
     p.dw = static_cast<uint8_t*>(dw->data);
-    p.part = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + staged_bytes(ntok, rows, dy->dtype));
+    p.part = static_cast<float*>(workspace);
     p.e_pitch = x->e_stride;
     p.dw_pitch = dw_pitch;
     p.ntok = int32_t(ntok);
