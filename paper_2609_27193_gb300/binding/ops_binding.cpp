@@ -161,7 +161,10 @@ void* stream_of(int index) { return c10::cuda::getCurrentCUDAStream(c10::DeviceI
 // Scratch of one call.  Of a device and stream there is one tensor, which grows to the
 // largest call; the stream's order keeps its users apart.  A call that is captured has a
 // tensor of its own: a graph holds its address for as long as it can be replayed, on any
-// stream, and memory allocated during a capture belongs to the graph.
+// stream, and memory allocated during a capture belongs to the graph.  So has a call that
+// needs more than kHeldMost, which the program gets back: such calls write and read tens of
+// megabytes, which takes longer than the allocation's microsecond.
+constexpr uint64_t kHeldMost = 32u << 20;
 struct Scratch {
     at::Tensor own;
     void* p = nullptr;
@@ -171,7 +174,7 @@ struct Scratch {
         cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
         if (cudaStreamIsCapturing(static_cast<cudaStream_t>(stream), &capture) != cudaSuccess)
             throw std::runtime_error("cannot tell whether the stream is being captured");
-        at::Tensor& w = capture == cudaStreamCaptureStatusNone ? (*held)[{index, stream}] : own;
+        at::Tensor& w = capture == cudaStreamCaptureStatusNone && bytes <= kHeldMost ? (*held)[{index, stream}] : own;
         if (!w.defined() || uint64_t(w.numel()) < bytes) w = make({int64_t(bytes)}, at::kByte, like);
         p = w.data_ptr();
     }

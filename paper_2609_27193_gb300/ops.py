@@ -6,9 +6,10 @@ Thin binding of the lc_embed / lc_norm / lc_act / lc_weight_grad calls of
 include/layercheck.h over torch CUDA tensors; what is done for every call is in
 C++ (binding/ops_binding.cpp).  Work is enqueued on torch's current stream,
 outputs that are not passed in come from torch's allocator on that stream, and
-scratch is one tensor a device and stream that grows to the largest call.  A call
-inside torch.cuda.graph has scratch of its own from the graph's pool, so graphs
-may be replayed beside other calls and one another.  There is no CPU fallback.
+scratch up to 32 MB is one tensor a device and stream that grows to the largest
+call (more is allocated for the call).  A call inside torch.cuda.graph has
+scratch of its own from the graph's pool, so graphs may be replayed beside other
+calls and one another.  There is no CPU fallback.
 
 Autograd records none of this: the gradients are calls too, for training loops
 that write their backward pass themselves and for torch.autograd.Function.
