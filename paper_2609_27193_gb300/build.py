@@ -6,9 +6,11 @@ runtime linked statically.  Only the lc_* entry points are exported.
 
 The operators' binding over torch tensors (binding/ops_binding.cpp) becomes the
 extension module _ops.so beside it, with g++ and torch's headers, at the same
-time.
+time.  Without torch there is none: the library and its C ABI need neither.
 """
 import concurrent.futures as cf
+import importlib.metadata
+import importlib.util
 import os
 import shutil
 import subprocess
@@ -23,6 +25,7 @@ BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "liblayercheck.so")
 BINDING = os.path.join(PKG, "binding", "ops_binding.cpp")
 BINDING_LIB = os.path.join(PKG, "_ops.so")
+BINDING_STAMP = os.path.join(BUILD, "ops_binding.for")
 
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVFLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC,-ffp-contract=off",
@@ -52,7 +55,21 @@ def up_to_date():
     return all(os.path.getmtime(f) <= t for f in _inputs())
 
 
+def binding_for():
+    """What the binding is compiled against: the torch and the Python found here; None without torch."""
+    spec = importlib.util.find_spec("torch")
+    if spec is None:
+        return None
+    try:
+        version = importlib.metadata.version("torch")
+    except importlib.metadata.PackageNotFoundError:
+        version = "?"
+    return "torch %s at %s, %s" % (version, spec.origin, sysconfig.get_config_var("SOABI"))
+
+
 def binding_up_to_date():
+    if not os.path.exists(BINDING_STAMP) or open(BINDING_STAMP).read() != binding_for():
+        return False
     inputs = [BINDING, os.path.join(INCLUDE, "layercheck.h"), os.path.abspath(__file__)]
     return os.path.exists(BINDING_LIB) and all(os.path.getmtime(f) <= os.path.getmtime(BINDING_LIB) for f in inputs)
 
@@ -83,12 +100,15 @@ def link_binding(obj, torch_lib):
     if r.returncode != 0:
         raise RuntimeError("link failed:\n%s%s" % (r.stdout, r.stderr))
     os.replace(tmp, BINDING_LIB)
+    with open(BINDING_STAMP, "w") as fh:
+        fh.write(binding_for())
 
 
 def build(force=False, verbose=False, extra_flags=()):
     """Compile and link; returns the library path."""
     with cf.ThreadPoolExecutor(max_workers=1) as ex:
-        binding = None if binding_up_to_date() and not force else ex.submit(compile_binding)
+        wanted = binding_for() is not None and (force or not binding_up_to_date())
+        binding = ex.submit(compile_binding) if wanted else None
         lib = build_library(force, verbose, extra_flags)
         if binding is not None:
             link_binding(*binding.result())

@@ -24,7 +24,11 @@ from . import _abi
 from ._abi import LC_ACT_BLOCK, LC_BF16, LC_F32, LC_NORM_LAYER, LC_NORM_RMS
 
 _abi.load()               # says how to build what is missing
-from . import _ops        # noqa: E402
+try:
+    from . import _ops
+except ImportError as e:
+    raise ImportError("the operators' binding is not built for this torch (run __graft_entry__.build() or "
+                      "python paper_2609_27193_gb300/build.py)") from e
 
 _ops.set_errors(_abi.LCError, torch.OutOfMemoryError)
 
