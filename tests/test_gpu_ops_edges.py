@@ -7,7 +7,8 @@ import pytest
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
-from tests.test_gpu_ops import BF, F32, SUMS, U, gen, norm_grad_ref, norm_ref, quantize, randn, values, within  # noqa: E402
+from tests.test_gpu_ops import (BF, F32, IDS, SUMS, U, gen, make_ids, norm_grad_ref, norm_ref, quantize, randn, values,  # noqa: E402
+                                within)
 
 
 @pytest.fixture(scope="module")
@@ -173,3 +174,41 @@ def test_large_scratch_is_given_back(ops):
     torch.cuda.synchronize()
     assert torch.cuda.memory_allocated() - before <= dw.numel() * 4 + (32 << 20)
     assert torch.equal(dw, ref.float())
+
+
+# --- the sums over tokens, exactly -----------------------------------------------------------------------------
+
+@pytest.mark.parametrize("how", IDS)
+@pytest.mark.parametrize("t,v,d,dt,gt", [
+    (64, 70, 2048, BF, F32), (65, 70, 200, F32, F32), (777, 513, 256, F32, BF), (2049, 131072, 24, F32, F32),
+    (16381, 32000, 768, BF, BF), (20011, 40, 1030, BF, F32), (20011, 40, 1031, BF, F32), (65536, 128256, 8, BF, F32),
+    (65537, 3000, 40, BF, F32), (70001, 300, 8, BF, F32), (140000, 70000, 16, BF, F32), (300000, 5, 129, F32, F32)])
+def test_embed_grad_of_whole_numbers(ops, how, t, v, d, dt, gt):
+    """Sums that fp32 holds exactly (at most 3 * 300000): a token that is lost, doubled or in another row shows,
+    also in a row that all tokens share."""
+    g = gen(t + d)
+    dy = whole(g, t, d, dtype=dt)
+    ids = make_ids(g, t, v, how)
+    ref = torch.zeros(v, d, dtype=torch.float64, device="cuda")
+    keep = ids >= 0
+    ref.index_add_(0, ids[keep], dy[keep].double())
+    grad = torch.full((v, d), math.nan, dtype=gt, device="cuda")
+    ops.embed_grad(dy, ids, grad=grad)
+    assert torch.equal(grad, ref.to(gt))
+    base = whole(g, v, d, dtype=gt, most=100)
+    grad = base.clone()
+    ops.embed_grad(dy, ids, grad=grad, accumulate=True)
+    assert torch.equal(grad, (ref + base.double()).to(gt))
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("t,d", [(5003, 384), (16384, 256), (9000, 1000), (4000, 4096), (3001, 4095), (40000, 24), (700, 16384)])
+def test_norm_bias_gradient_of_whole_numbers(ops, dt, t, d):
+    """dbias exactly, of rows of their own and of one row that all share (stride 0)."""
+    g = gen(t + d)
+    x, w = randn(g, t, d, dtype=dt), torch.ones(d, dtype=dt, device="cuda")
+    _, mean, rstd, act = ops.norm(x, w, keep=True)
+    for dy in (whole(g, t, d, dtype=dt), whole(g, 1, d, dtype=dt).expand(t, d)):
+        for seen in (x, act):
+            _, _, db = ops.norm_grad(dy, seen, w, mean, rstd, bias=True)
+            assert torch.equal(db.double(), dy.double().sum(0))
