@@ -229,6 +229,7 @@ PyObject* embed_grad(PyObject* const* args, Py_ssize_t nargs) {
     const int64_t n = dy.size(0), dim = dy.size(1);
     if (ids.numel() != n) throw ValueError("dy and ids must have the same number of tokens");
     if (grad.defined()) {
+        if (vocab >= 0 && (!grad.dim() || grad.size(0) != vocab)) throw ValueError("grad must have vocab rows");
         vocab = grad.dim() ? grad.size(0) : 0;
         shaped(grad, vocab, dim, "grad");
     } else {

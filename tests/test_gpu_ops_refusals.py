@@ -133,3 +133,13 @@ def test_an_output_that_does_not_fit(ops):
     dy, ids = torch.zeros(1, 4096, device="cuda"), torch.zeros(1, dtype=torch.int64, device="cuda")
     with pytest.raises(torch.OutOfMemoryError):
         ops.embed_grad(dy, ids, 10 ** 9)
+
+
+def test_a_gradient_of_another_vocabulary(ops):
+    dy, ids = torch.ones(3, 16, device="cuda"), torch.tensor([0, 11, 19], device="cuda")
+    grad = torch.zeros(20, 16, device="cuda")
+    with pytest.raises(ValueError, match="vocab"):
+        ops.embed_grad(dy, ids, 10, grad=grad)
+    assert (grad == 0).all()
+    ops.embed_grad(dy, ids, 20, grad=grad)
+    assert (grad[ids] == 1).all() and float(grad.sum()) == 48
