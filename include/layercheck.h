@@ -657,8 +657,9 @@ lc_status lc_measure_noalloc_debug(int device, void* cuda_stream, const lc_segme
 
 /* Test switch of those waits, for the calls that the calling host thread makes
  * from here on: 0, or LC_DEBUG_OPS_STALL, with which the first copy into
- * every ring (the norms' rows, forward and backward; the weight gradient's
- * product) announces 16 bytes that never come.
+ * every ring of the norms' rows (forward and backward), and into the ring of
+ * the second CTA of every pair in the weight gradient's product, announces 16
+ * bytes that never come.
  * Errors: INVALID_ARG (other flags). */
 #define LC_DEBUG_OPS_STALL 4
 lc_status lc_ops_debug(int32_t debug_flags);

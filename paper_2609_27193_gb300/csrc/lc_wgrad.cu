@@ -84,7 +84,7 @@ struct WgradParams {
     int32_t ntiles_n, stages, splits, per_split;   // stages in all, of a split
     int32_t tok_part;      // rows of dy between the parts
     int32_t dw_bf16;
-    int32_t stall;         // test switch: the first copy announces 16 bytes that never come
+    int32_t stall;         // test switch: the second CTA's first copy announces 16 bytes that never come
 };
 
 __device__ __forceinline__ void tma_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
@@ -248,7 +248,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
                     ok = it < kStages || mbar_wait_bounded(empty + 8 * st.at, st.round ^ 1, kWaitNs);
                     if (!ok) break;
                     const uint32_t at = tiles + st.at * kStageBytes, bar = full + 8 * st.at;
-                    mbar_expect_tx(bar, kLoadBytes + (it == 0 && p.stall ? 16 : 0));
+                    mbar_expect_tx(bar, kLoadBytes + (it == 0 && rank == 1 && p.stall ? 16 : 0));
                     tma_2d(at + PARTS * kOpBytes, &xmap, w.k0 + rank * kHalf, t, bar);
 #pragma unroll
                     for (int part = 0; part < PARTS; ++part)

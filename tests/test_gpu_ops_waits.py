@@ -27,7 +27,8 @@ def stalled():
 @pytest.mark.parametrize("dt,gt", [(BF, F32), (BF, BF), (F32, F32)])
 @pytest.mark.parametrize("t,n,k", [(100, 70, 200), (2100, 300, 500), (300, 2560, 2816)])
 def test_weight_grad(stalled, dt, gt, t, n, k):
-    """One tile, splits that are joined, and several tiles a pair."""
+    """One tile, splits that are joined, and several tiles a pair.  The second CTA of a pair misses a copy; the first
+    one's products read half of it."""
     from paper_2609_27193_gb300 import ops
     g = gen(t)
     dy, a = randn(g, t, n, dtype=dt), ops.act_save(randn(g, t, k, dtype=dt))
