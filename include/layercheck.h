@@ -645,8 +645,11 @@ lc_status lc_measure_noalloc_debug(int device, void* cuda_stream, const lc_segme
  *     function returns (0: none needed, NULL allowed), 256-byte aligned.  It
  *     holds nothing between calls.  Calls that may overlap on the GPU need
  *     one each.
- *   - Sums are taken in fp32 in an order that the sizes fix, without floating
- *     point atomics: the same inputs give the same bits.
+ *   - Sums are taken in fp32, without floating point atomics, in an order that
+ *     the sizes, types and strides, the arrays' places relative to 16-byte
+ *     boundaries and the device model fix: the same call gives the same bits,
+ *     in another process too.  The same values elsewhere (rows off 16 bytes)
+ *     may be added in another order.
  *   - 0 tokens are allowed: outputs per token are untouched, gradients are 0
  *     (or stay as they are with `accumulate`).
  *   - The waits inside the kernels are bounded like those of lc_measure.  There
@@ -686,7 +689,8 @@ lc_status lc_embed(int device, void* cuda_stream, const lc_rows* table, int64_t 
                    const void* ids, int32_t id_type, int64_t ntok, float scale, const lc_rows* y);
 
 /* grad[v] = scale * sum of dy[t] over the tokens with ids[t] == v, in
- * ascending t, rounded once to grad's type; every other row is 0.  With
+ * ascending t (a row of many tokens in runs, whose sums are then added in their
+ * order), rounded once to grad's type; every other row is 0.  With
  * accumulate != 0 the sums are added to grad instead and the other rows stay
  * as they are (a tied output projection's gradient, micro-batches).  Ids
  * outside [0, vocab) and the id skip_id (-1: none) contribute nothing.
@@ -752,8 +756,8 @@ uint64_t lc_norm_grad_workspace(int64_t ntok, int64_t dim);
  * kept in 8 bits: dw[n][k] = sum over t of dy[t][n] * x[t][k], `rows` by dim,
  * added to dw with accumulate != 0.  Products and sums are fp32 (tensor cores
  * on bf16 operands, which the checkpoint's values are exactly; a 32-bit dy is
- * split into three bf16 parts that add up to it).  dy and dw may have
- * different types. */
+ * split into three bf16 parts that add up to it, but for bits below 2^-133,
+ * which only values below 2^-110 have).  dy and dw may have different types. */
 lc_status lc_weight_grad(int device, void* cuda_stream, const lc_rows* dy, const lc_act* x, int64_t ntok,
                          int64_t rows, int64_t dim, const lc_rows* dw, int32_t accumulate, void* workspace,
                          uint64_t workspace_bytes);

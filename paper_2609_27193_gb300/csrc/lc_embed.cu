@@ -10,9 +10,10 @@
 // its rows: a word that half of the tokens share costs no more than any other
 // chunk.  A row that lies inside one chunk is written by it; a row that crosses
 // chunks leaves fp32 partial sums, which a last kernel adds in chunk order.  No
-// floating point atomics: the order of every sum is fixed by the sizes.  The gradient
-// is zeroed by the multiprocessors that the sort leaves idle: the rows with a token
-// are written twice, which costs less than knowing first which they are.
+// floating point atomics: the order of every sum is fixed by the sizes, the types and
+// whether rows start on 16-byte boundaries.  The gradient is zeroed by the multiprocessors
+// that the sort leaves idle: the rows with a token are written twice, which costs less
+// than knowing first which they are.
 #include <cooperative_groups.h>
 
 #include "lc_ops.cuh"

@@ -14,8 +14,8 @@
 // stream through shared memory: every group of threads has a ring of rows there, the
 // next ones on their way by bulk copies while it works on one.  In registers as many
 // bytes in flight would leave no room for the work: 16384 rows of 4096 bf16 through
-// a root-mean-square norm 79 us that way, 45 so, their backward from the checkpoint 109 us
-// and 65.
+// a root-mean-square norm 82 us that way, 48 so, their backward from the checkpoint 117 us
+// and 67.
 #include "lc_bulk.cuh"
 #include "lc_ops.cuh"
 
@@ -487,7 +487,7 @@ __device__ __forceinline__ void stage_param(float4* out, const uint8_t* p, bool 
     }
 }
 
-constexpr int kFwdThreads = 1024;   // of a CTA, one a multiprocessor: 64 registers each (with 512: 54 us for 45)
+constexpr int kFwdThreads = 1024;   // of a CTA, one a multiprocessor: 64 registers each (with 512: 55 us for 48)
 
 template <typename T, int G, int VPT>
 __global__ void __launch_bounds__(kFwdThreads, 1) norm_ring_kernel(NormParams p, int depth) {
@@ -618,8 +618,8 @@ __global__ void __launch_bounds__(kFwdThreads, 1) norm_ring_kernel(NormParams p,
     ring_drain(ring, lost, t);
 }
 
-constexpr int kBwdThreads = 512;    // 128 registers each: sums for weight and bias besides the row (rows of 8 values a thread and
-                                    // 1024 threads 104 us for 77, of 32 values and 384 threads 75)
+constexpr int kBwdThreads = 512;    // 128 registers each: sums for weight and bias besides the row (before the
+                                    // arithmetic in pairs 77 us; 8 values a thread and 1024 threads 104, 32 values and 384 threads 75)
 
 // The backward.  A slot holds the rows of dy and of x (or its 8-bit values; their
 // exponents are asked for a row ahead into registers).

@@ -24,9 +24,10 @@
 // tile follow those of the last, so the outputs are written while the next tile's
 // products run.
 //
-// A 32-bit dy is split into three bf16 parts that add up to it exactly (8 + 8 + 8
-// bits of significand, cut off, not rounded, so nothing overflows); a stage then has
-// the tiles of all three, and the operand is made once for them.  That and a bf16 dy
+// A 32-bit dy is split into three bf16 parts that add up to it (8 + 8 + 8 bits of
+// significand, cut off, not rounded, so nothing overflows; exactly, but for bits below
+// bf16's least 2^-133, which only values below 2^-110 have); a stage then has the tiles
+// of all three, and the operand is made once for them.  That and a bf16 dy
 // off 16-byte boundaries go into aligned rows in the workspace, by a kernel of their
 // own.  Few output tiles are split over the tokens; the parts are
 // added in order by another kernel.
@@ -414,7 +415,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             const int left = p.rows - n0, cnt = k < p.dim ? left : 0;
             // ACC and whole tiles have loops of their own: tests inside would make these unrolled loops twice as long,
             // and their instructions come from memory for a tile or two of few tokens (64 tokens, 4096 -> 4096 in bf16:
-            // 28 us with the tests inside, 16 so)
+            // 27 us with the tests inside, 15 so)
             if (p.splits == 1 && p.dw_bf16) {
                 // lanes two apart have neighbouring features: of two columns each takes one, with both features, so that
                 // a store has 4 bytes (33 us with 2 bytes a store)
@@ -500,7 +501,7 @@ struct StageParams {
 };
 
 // dy into rows on 16-byte boundaries: a copy, or three bf16 parts that add up to a
-// 32-bit value.  Each part takes the next eight bits of the significand, cut off.
+// 32-bit value (bits below 2^-133 are lost).  Each part takes the next eight bits of the significand, cut off.
 // An infinity or a NaN stays whole in the first part.
 // A thread takes four columns of a row.
 __global__ void __launch_bounds__(256) wgrad_stage_kernel(StageParams p) {
@@ -621,8 +622,8 @@ constexpr int64_t al(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
 // How a product is cut: output tiles, parts of dy, and splits of the tokens where
 // the tiles alone leave multiprocessors idle (each split at least 8 stages long: a
 // stage takes half a microsecond, joining the parts four; 512 tokens of 256 -> 1024
-// take 15 us in two splits and 13 in one, 2047 of 2048 -> 512 24 us in one and 19 in
-// four).
+// take 9.8 us in one split and 11.8 in two, 2047 of 2048 -> 512 with a 32-bit dy 37 us in
+// one, 29 in two, 22.6 in four and 27 in eight).
 constexpr int kPairs = 76;
 struct Shape {
     int64_t tiles_n, tiles_k, stages, splits, per_split;

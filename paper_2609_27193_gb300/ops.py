@@ -108,7 +108,7 @@ def embed(table, ids, scale=1.0, out=None):
 
 def embed_grad(dy, ids, vocab=None, scale=1.0, grad=None, dtype=None, skip_id=-1, accumulate=False):
     """The gradient of embed's table, [vocab, dim]: row v is scale times the sum
-    of dy over the tokens with id v, in token order; the other rows are zero.
+    of dy over the tokens with id v, in a fixed order; the other rows are zero.
     With accumulate the sums are added to `grad` and the other rows stay."""
     return _ops.embed_grad(dy, ids, -1 if vocab is None else vocab, scale, grad, _dtype(dtype), skip_id, accumulate)
 
