@@ -24,8 +24,8 @@ def stalled():
     return run
 
 
-@pytest.mark.parametrize("dt,gt", [(BF, F32), (BF, BF), (F32, F32)])
-@pytest.mark.parametrize("t,n,k", [(100, 70, 200), (2100, 300, 500), (300, 2560, 2816)])
+@pytest.mark.parametrize("t,n,k,dt,gt", [(100, 70, 200, BF, F32), (2100, 300, 500, F32, F32), (2100, 300, 500, BF, BF),
+                                         (300, 2560, 2816, BF, BF), (300, 2560, 2816, F32, F32)])
 def test_weight_grad(stalled, dt, gt, t, n, k):
     """One tile, splits that are joined, and several tiles a pair.  The second CTA of a pair misses a copy; the first
     one's products read half of it."""
@@ -43,8 +43,8 @@ def test_weight_grad(stalled, dt, gt, t, n, k):
     assert torch.isnan(base).all()
 
 
-@pytest.mark.parametrize("kind", ["layer", "rms"])
-@pytest.mark.parametrize("t,d,dt", [(5000, 256, BF), (700, 1024, F32), (400, 4096, BF), (320, 16384, F32)])
+@pytest.mark.parametrize("t,d,dt,kind", [(5000, 256, BF, "rms"), (700, 1024, F32, "layer"), (400, 4096, BF, "layer"),
+                                         (320, 16384, F32, "rms")])
 def test_norm(stalled, kind, t, d, dt):
     """Every group's first row does not come; the rows that follow are not waited for."""
     from paper_2609_27193_gb300 import ops
