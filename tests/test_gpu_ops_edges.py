@@ -212,3 +212,61 @@ def test_norm_bias_gradient_of_whole_numbers(ops, dt, t, d):
         for seen in (x, act):
             _, _, db = ops.norm_grad(dy, seen, w, mean, rstd, bias=True)
             assert torch.equal(db.double(), dy.double().sum(0))
+
+
+@pytest.mark.parametrize("t", [3000, 70000])
+def test_embed_grad_of_a_vocabulary_of_28_bits(ops, t):
+    """Four digits to sort by, in shared memory and beyond it."""
+    g = gen(t)
+    v = 2 ** 27 + 5
+    ids = torch.randint(0, v, (t,), generator=g, device="cuda")
+    ids[t // 2:] = ids[:t - t // 2]                       # every id at least twice
+    ids[7], ids[8] = v - 1, 2 ** 27
+    dy = whole(g, t, 1)
+    grad = ops.embed_grad(dy, ids, v)
+    ref = torch.zeros(v, 1, device="cuda").index_add_(0, ids, dy)
+    assert torch.equal(grad, ref)
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+def test_rows_far_apart(ops, dt):
+    """Row offsets beyond 32 bits, in elements, for every call."""
+    g = gen(71)
+    t, d, n = 3, 1024, 256
+    far = 2 ** 31 + 64
+    buf = torch.empty(2 * far + 4096, dtype=dt, device="cuda")
+    out = torch.empty(2 * far + 4096, dtype=dt, device="cuda")
+    q8 = torch.zeros(4 * far + 4096, dtype=torch.int8, device="cuda")
+
+    def put(x):
+        v = buf.as_strided(x.shape, (far, 1))
+        v.copy_(x)
+        return v
+
+    def room(*shape):
+        return out.as_strided(shape, (far, 1))
+    x, dy, w = randn(g, t, d, dtype=dt), randn(g, t, d, dtype=dt), 1 + randn(g, d, dtype=dt, spread=0.2)
+    y, mean, rstd, act = ops.norm(x, w, keep=True)
+    kept = ops.Act(q8.as_strided((t, d), (2 * far, 1)), q8[2048:].as_strided((t, d // 128), (2 * far, 1)), d)
+    got = ops.norm(put(x), w, out=room(t, d), keep=kept)
+    assert torch.equal(got[0], y) and torch.equal(got[1], mean) and torch.equal(got[2], rstd)
+    assert torch.equal(kept.q, act.q) and torch.equal(kept.e, act.e)
+    assert torch.equal(ops.act_load(kept, out=room(t, d)), ops.act_load(act, dtype=dt))
+    kept.q.zero_()
+    ops.act_save(put(x), kept)
+    assert torch.equal(kept.q, act.q)
+    want = ops.norm_grad(dy, x, w, mean, rstd, bias=True)
+    for a, b in zip(ops.norm_grad(put(dy), x, w, mean, rstd, bias=True, dx=room(t, d)), want):
+        assert torch.equal(a, b)
+    want = ops.norm_grad(dy, act, w, mean, rstd, bias=True)
+    for a, b in zip(ops.norm_grad(put(dy), kept, w, mean, rstd, bias=True), want):
+        assert torch.equal(a, b)
+    dz = randn(g, t, n, dtype=dt)
+    assert torch.equal(ops.weight_grad(put(dz), kept), ops.weight_grad(dz, act))
+    dz = whole(g, t, 3, dtype=dt)                         # three rows of the output, far apart
+    assert torch.equal(ops.weight_grad(dz, act, grad=room(3, d)), ops.weight_grad(dz, act, dtype=dt))
+    ids = torch.tensor([2, 0, 2], device="cuda")
+    assert torch.equal(ops.embed_grad(put(dy), ids, grad=room(3, d)), ops.embed_grad(dy, ids, 3))
+    many = torch.arange(300, device="cuda") % 3
+    rows = whole(g, 300, d, dtype=dt)
+    assert torch.equal(ops.embed_grad(rows, many, grad=room(3, d)), ops.embed_grad(rows, many, 3))
