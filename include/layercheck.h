@@ -767,6 +767,41 @@ uint64_t lc_weight_grad_workspace(int64_t ntok, int64_t rows, int64_t dim, int32
  * size above, enough for any dy of the type, has room for. */
 uint64_t lc_weight_grad_workspace_of(const lc_rows* dy, int64_t ntok, int64_t rows, int64_t dim);
 
+/* `batch` matrices of rows x cols elements of type dtype (lc_dtype): row r of
+ * matrix b starts at element b * batch_stride + r * stride.  Rows of an output
+ * do not meet. */
+typedef struct {
+    void* data;
+    int64_t stride;
+    int64_t batch_stride;
+    int32_t dtype;
+    int32_t reserved;
+} lc_mats;
+
+/* Updates of weight matrices made nearly orthogonal (the step of the Muon
+ * optimizer): for every matrix, with U the update,
+ *   X = U / (|U|_F + eps),  `steps` (1 to 16) times  A = X X^T,  X = a X + (b A + c A^2) X,
+ *   out = X rounded to bf16,
+ * over the shorter side (X^T X where rows > cols).  coefficients: host array of
+ * steps times a, b, c; what they let singular values in [0, 1] grow to is
+ * bounded (16), and refused above.  update: bf16 or fp32.  out: bf16; it is off
+ * by about 1e-3 of its size before that rounding (operands are fp16; X itself,
+ * sums, diagonals and the norm are held in 32 bits).
+ * momentum (fp32; NULL: U = update): with g the update given it moves first,
+ *   momentum += (1 - beta) (g - momentum),
+ * and U = g + beta (momentum - g) with nesterov != 0, else U = momentum.
+ * A matrix with a NaN or an infinity comes out as NaN, one of zeros as zeros
+ * (with eps = 0 as NaN); the others of the batch are not affected.
+ * A wait that runs out leaves NaN in out; the momentum has moved.
+ * The product kernel is one cooperative launch: calls on two streams at once
+ * follow one another where they do not fit the device together. */
+#define LC_ORTH_MAX_DIM 65536
+lc_status lc_orthogonalize(int device, void* cuda_stream, const lc_mats* update, int64_t batch, int64_t rows,
+                           int64_t cols, const lc_mats* momentum, double beta, int32_t nesterov, int32_t steps,
+                           const double* coefficients, double eps, const lc_mats* out, void* workspace,
+                           uint64_t workspace_bytes);
+uint64_t lc_orthogonalize_workspace(int64_t batch, int64_t rows, int64_t cols);
+
 #ifdef __cplusplus
 }
 #endif

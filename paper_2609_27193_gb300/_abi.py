@@ -30,6 +30,7 @@ LC_I32, LC_I64 = 2, 3
 LC_NORM_LAYER, LC_NORM_RMS = 0, 1
 LC_NORM_MAX_DIM = 16384
 LC_ACT_BLOCK = 128
+LC_ORTH_MAX_DIM = 65536
 LC_SPAN_GATHER, LC_SPAN_D2H, LC_SPAN_H2D, LC_SPAN_SCATTER = 0, 1, 2, 3
 SPAN_NAMES = {0: "gather", 1: "d2h", 2: "h2d", 3: "scatter"}
 
@@ -101,6 +102,11 @@ class lc_act(C.Structure):
     _fields_ = [("q", C.c_void_p), ("q_stride", C.c_int64), ("e", C.c_void_p), ("e_stride", C.c_int64)]
 
 
+class lc_mats(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("stride", C.c_int64), ("batch_stride", C.c_int64), ("dtype", C.c_int32),
+                ("reserved", C.c_int32)]
+
+
 ctx_p = C.c_void_p
 store_p = C.c_void_p
 P = C.POINTER
@@ -170,6 +176,10 @@ SIGNATURES = {
     "lc_weight_grad": (C.c_int, [C.c_int, C.c_void_p, P(lc_rows), P(lc_act), C.c_int64, C.c_int64, C.c_int64,
                                  P(lc_rows), C.c_int32, C.c_void_p, C.c_uint64]),
     "lc_weight_grad_workspace_of": (C.c_uint64, [P(lc_rows), C.c_int64, C.c_int64, C.c_int64]),
+    "lc_orthogonalize": (C.c_int, [C.c_int, C.c_void_p, P(lc_mats), C.c_int64, C.c_int64, C.c_int64, P(lc_mats),
+                                   C.c_double, C.c_int32, C.c_int32, C.c_void_p, C.c_double, P(lc_mats), C.c_void_p,
+                                   C.c_uint64]),
+    "lc_orthogonalize_workspace": (C.c_uint64, [C.c_int64, C.c_int64, C.c_int64]),
     "lc_weight_grad_workspace": (C.c_uint64, [C.c_int64, C.c_int64, C.c_int64, C.c_int32]),
 }
 

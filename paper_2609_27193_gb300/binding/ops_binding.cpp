@@ -394,6 +394,60 @@ PyObject* weight_grad(PyObject* const* args, Py_ssize_t nargs) {
     return wrapped(grad);
 }
 
+// A matrix or a batch of them; a single one has any batch stride, as a single row has any stride.
+lc_mats mats_of(const at::Tensor& t, const char* name) {
+    lc_mats m{};
+    m.dtype = code_of(t, name);
+    const int64_t d = t.dim();
+    if (d != 2 && d != 3) throw ValueError(std::string(name) + " must be a matrix or a batch of matrices");
+    if (t.stride(d - 1) != 1 && t.size(d - 1) > 1) throw ValueError(std::string(name) + " must have contiguous rows");
+    m.data = t.data_ptr();
+    m.stride = t.size(d - 2) > 1 ? t.stride(d - 2) : t.size(d - 1);
+    m.batch_stride = d == 3 && t.size(0) > 1 ? t.stride(0) : t.size(d - 2) * m.stride;
+    return m;
+}
+
+PyObject* orthogonalize(PyObject* const* args, Py_ssize_t nargs) {
+    Args a(args, nargs, 7);
+    const at::Tensor update = a.tensor(), momentum = a.tensor();
+    const double beta = a.number();
+    const bool nesterov = a.truth();
+    char* packed = nullptr;
+    Py_ssize_t bytes = 0;
+    if (PyBytes_AsStringAndSize(args[a.at++], &packed, &bytes) < 0) throw Raised{};
+    const double eps = a.number();
+    at::Tensor out = a.tensor();
+    const int index = cuda_index(update);
+    same_device(index, momentum);
+    same_device(index, out);
+    unrecorded("orthogonalize", {&update, &momentum, &out});
+    const lc_mats mu = mats_of(update, "update");
+    lc_mats mm{};
+    if (momentum.defined()) {
+        if (momentum.sizes() != update.sizes()) throw ValueError("momentum must have the update's shape");
+        if (momentum.scalar_type() != at::kFloat) throw TypeError("momentum must be float32");
+        mm = mats_of(momentum, "momentum");
+    }
+    if (out.defined()) {
+        if (out.sizes() != update.sizes()) throw ValueError("out must have the update's shape");
+        if (out.scalar_type() != at::kBFloat16) throw TypeError("out must be bfloat16");
+    } else {
+        out = make(update.sizes(), at::kBFloat16, update);
+    }
+    const lc_mats mo = mats_of(out, "out");
+    const int64_t d = update.dim(), batch = d == 3 ? update.size(0) : 1, rows = update.size(d - 2), cols = update.size(d - 1);
+    if (rows < 1 || cols < 1) throw ValueError("update must have rows and columns");
+    void* stream = stream_of(index);
+    const uint64_t need = lc_orthogonalize_workspace(batch, rows, cols);
+    const Scratch scratch(update, index, stream, need);
+    check(lc_orthogonalize(index, stream, &mu, batch, rows, cols, momentum.defined() ? &mm : nullptr, beta, nesterov,
+                           int32_t(bytes / Py_ssize_t(3 * sizeof(double))), reinterpret_cast<const double*>(packed), eps, &mo, scratch.p,
+                           need));
+    written(momentum);
+    written(out);
+    return wrapped(out);
+}
+
 PyObject* set_errors(PyObject* const* args, Py_ssize_t nargs) {
     if (nargs != 2) throw TypeError("wrong number of arguments");
     Py_INCREF(args[0]);
@@ -431,7 +485,8 @@ PyObject* guarded(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
 
 #define LC_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(guarded<name>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {LC_METHOD(embed),    LC_METHOD(embed_grad), LC_METHOD(act_save),    LC_METHOD(act_load), LC_METHOD(new_act),
-                         LC_METHOD(norm),     LC_METHOD(norm_grad),  LC_METHOD(weight_grad), LC_METHOD(set_errors),
+                         LC_METHOD(norm),     LC_METHOD(norm_grad),  LC_METHOD(weight_grad), LC_METHOD(orthogonalize),
+                         LC_METHOD(set_errors),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_ops", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1,0 +1,1091 @@
+// lc_orth.cu -- an update of a weight matrix made nearly orthogonal by
+// Newton-Schulz products: X = U / (|U| + eps), and `steps` times
+//
+//   A = X X^T,   X <- a X + (b A + c A^2) X
+//
+// over the shorter side (a matrix with more rows than columns is worked on
+// transposed).  Each step takes a singular value s to a s + b s^3 + c s^5.
+//
+// Three kernels: one moves the momentum and leaves sums of squares, one writes X
+// in the products' layout, one does all products.  The products are on the 5th-generation
+// tensor cores, fp16 operands and fp32 sums:
+//
+//   * The state X is kept in 32 bits, as an fp16 number and the fp16 rest of it times 2^11.  The
+//     first part is the operand, both are read where X itself is added.  (With one fp16 number
+//     as state, a matrix of 8 directions over noise of 1e-4 came out 4e-2 off, so 6e-4; bf16 operands 3e-1.)
+//   * The diagonals of A and of B = b A + c A^2 are far larger than the rest and stay in fp32, beside
+//     the operands: A^2 = A0^2 + (d_i + d_j) A0 + d^2, and X's row i is multiplied by a + e_i.  That
+//     halves the error (512 x 1024: 1.7e-3 to 5e-4 off before the output's rounding of 1.7e-3).
+//   * Operands are scaled by powers of two.  No element of X, A or B is larger than the matrix's
+//     largest singular value, which the coefficients bound, so nothing overflows fp16.
+//   * A and B are symmetric: the tiles on and above the diagonal are computed, and a product reads the
+//     others as transposes of those, which the tensor core takes either way.
+//
+// Matrices lie in the workspace in boxes of 64 x 64, rows of 128 bytes swizzled as the operands are
+// in shared memory, so that a box is one contiguous bulk copy and the same box serves with its rows along the
+// reduction or across it.
+//
+// The product kernel is one cooperative launch: its CTAs go through the 3 * steps
+// products together, with a barrier of the whole grid between them.  Two CTAs of a cluster share
+// tiles of 256 x 256 (PAIR), or a CTA has one of 128 x 128.  Warp 0 brings the operands, warp 1 issues
+// the products into two accumulators in turn, warps 4-11 turn the finished one into the next operand.
+//
+// Waits are bounded: where one runs out the CTA's outputs are NaN, and with the next
+// barrier everybody's.
+#include <cuda_fp16.h>
+
+#include <cmath>
+
+#include "lc_bulk.cuh"
+#include "lc_ops.cuh"
+
+namespace lc {
+namespace {
+
+constexpr int kBox = 64;                    // rows and columns of a box
+constexpr int kBoxBytes = kBox * kBox * 2;
+constexpr int kCtaRows = 128;               // rows of an operand in a CTA
+constexpr int kOperand = 2 * kBoxBytes;
+constexpr int kStageBytes = 2 * kOperand;
+constexpr int kStages = 6;
+constexpr int kSumWarp = 4, kSumWarps = 8;  // the first (a multiple of 4) of the warps that read the accumulators, and their number
+constexpr int kThreads = (kSumWarp + kSumWarps) * 32;
+constexpr int kSmem = kStages * kStageBytes + 1024;
+constexpr int kMaxSteps = 16;
+constexpr int kNormCtas = 512;              // most partial sums of squares of a matrix
+
+template <bool PAIR>
+struct TileOf {
+    static constexpr int kTile = PAIR ? 256 : 128;
+    // fp32 accumulator, fp16 operands; which way their rows lie is added for each product
+    static constexpr uint32_t kIdesc = 1u << 4 | uint32_t(kTile / 8) << 17 | uint32_t(kTile / 16) << 24;
+};
+
+struct OrthStep {
+    float a, b, c, scale;    // scale: of B's operand
+};
+struct OrthParams {
+    uint32_t* count;         // arrivals at the grid's barriers
+    uint32_t* arrived;       // [batch * tiles][CTAs of a tile]: splits of a product that are done
+    float* d;                // [batch][mp]: diagonal of A
+    float* e;                // [batch][mp]: diagonal of B
+    uint8_t* x[2];           // operand of X, of even and odd steps
+    uint8_t* rest;           // what it lacks of X, times 2^11
+    uint8_t* sa;             // A without its diagonal
+    uint8_t* sb;             // B without it
+    float* part;             // splits' sums
+    uint8_t* out;
+    int64_t out_pitch, out_batch;   // bytes
+    uint64_t limit_ns;
+    float x_scale, a_scale;
+    int32_t batch, m, n;     // of X as it is worked on (m <= n)
+    int32_t bm, bn;          // boxes of m and n
+    int32_t steps, splits[3];  // of the reductions of A, A^2 and B X (the last always 1)
+    int32_t turned;          // out is X^T
+    int32_t wide;            // out takes 16-byte stores
+    int32_t stall;
+    OrthStep step[kMaxSteps];
+};
+
+__device__ __forceinline__ uint32_t cluster_addr(uint32_t bar, int rank) {
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(bar), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ void arrive_at(uint32_t cluster_bar) {
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+}
+__device__ __forceinline__ void cluster_meet() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// Once the products issued so far are done: an arrival at the barrier (of both CTAs).
+template <bool PAIR>
+__device__ __forceinline__ void commit(uint32_t bar) {
+    if constexpr (PAIR)
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
+                     "h"(uint16_t(3))
+                     : "memory");
+    else
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+template <bool PAIR>
+__device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t add) {
+    if constexpr (PAIR)
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+                     "l"(a), "l"(b), "r"(idesc), "r"(add)
+                     : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+                     "l"(a), "l"(b), "r"(idesc), "r"(add)
+                     : "memory");
+}
+// Descriptor of an operand: two boxes, 8 rows of 128 bytes 1024 bytes apart.  Rows
+// along the reduction: the boxes hold 64 columns of the output each.
+__device__ __forceinline__ uint64_t operand_desc(uint32_t addr) {
+    return uint64_t((addr & 0x3ffffu) >> 4) | uint64_t(kBoxBytes >> 4) << 16 | uint64_t(1024 >> 4) << 32 | uint64_t(1) << 46 |
+           uint64_t(2) << 61;
+}
+
+__device__ __forceinline__ void tmem_ld32(uint32_t addr, float (&f)[32]) {
+    uint32_t r[32];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,"
+        "%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n\ttcgen05.wait::ld.sync.aligned;"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
+          "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
+          "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(addr)
+        : "memory");
+#pragma unroll
+    for (int i = 0; i < 32; ++i) f[i] = __uint_as_float(r[i]);
+}
+
+// What other CTAs wrote in this launch is read past L1.
+__device__ __forceinline__ uint4 ld_l2(const void* p) { return __ldcg(static_cast<const uint4*>(p)); }
+
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+    const __half2 h = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ float2 unpack_f16(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
+
+// 16-byte piece `p` (of 8) of row r in a box.
+__device__ __forceinline__ uint32_t piece_at(int r, int p) { return uint32_t(r) * 128 + uint32_t((p ^ (r & 7)) * 16); }
+
+// X's value as its operand and the rest: hi + lo * 2^-11.
+constexpr float kRest = 2048.0f;
+__device__ __forceinline__ void split_pair(float x, float y, uint32_t& hi, uint32_t& lo) {
+    hi = pack_f16(x, y);
+    const float2 h = unpack_f16(hi);
+    lo = pack_f16((x - h.x) * kRest, (y - h.y) * kRest);
+}
+
+// One piece of a product: a tile, or a split of its reduction.
+struct Item {
+    int mat, i, j, split, s0, stages, tile;
+};
+template <bool PAIR>
+__device__ __forceinline__ Item item_of(const OrthParams& p, int phase, int at) {
+    constexpr int T = TileOf<PAIR>::kTile;
+    const int tm = p.bm * kBox / T, tn = p.bn * kBox / T;
+    const int all = phase == 0 ? p.bn : p.bm, splits = p.splits[phase];
+    Item w;
+    const int t = at / splits;
+    w.split = at - t * splits;
+    const int per = (all + splits - 1) / splits;
+    w.s0 = w.split * per;
+    w.stages = min(per, all - w.s0);
+    w.tile = t;
+    if (phase == 2) {
+        const int tiles = tm * tn;
+        w.mat = t / tiles;
+        const int k = t - w.mat * tiles;
+        w.j = k / tm;
+        w.i = k - w.j * tm;
+    } else {
+        const int tiles = tm * (tm + 1) / 2;
+        w.mat = t / tiles;
+        const int k = t - w.mat * tiles;
+        // column j holds tiles [j (j + 1) / 2, ...)
+        int j = int((sqrtf(8.0f * float(k) + 1.0f) - 1.0f) * 0.5f);
+        while (j * (j + 1) / 2 > k) --j;
+        while ((j + 1) * (j + 2) / 2 <= k) ++j;
+        w.j = j;
+        w.i = k - j * (j + 1) / 2;
+    }
+    return w;
+}
+template <bool PAIR>
+__device__ __forceinline__ int items_of(const OrthParams& p, int phase) {
+    constexpr int T = TileOf<PAIR>::kTile;
+    const int tm = p.bm * kBox / T, tn = p.bn * kBox / T;
+    return p.batch * (phase == 2 ? tm * tn : tm * (tm + 1) / 2) * p.splits[phase];
+}
+
+template <int N>
+struct Ring {
+    int at = 0;
+    uint32_t round = 0;
+    __device__ __forceinline__ void next() {
+        if (++at == N) {
+            at = 0;
+            round ^= 1;
+        }
+    }
+};
+
+// Until `want` CTAs have arrived.
+__device__ __forceinline__ bool grid_wait(const uint32_t* count, uint32_t want, uint64_t limit_ns) {
+    uint64_t t0 = 0;
+    for (uint64_t it = 1;; ++it) {
+        uint32_t v;
+        asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(count) : "memory");
+        if (v >= want) return true;
+        if (it % 64) continue;
+        const uint64_t t = global_ns();
+        if (t0 == 0) t0 = t;
+        else if (t - t0 > limit_ns || it > (uint64_t(1) << 40)) return false;
+    }
+}
+// A wait for the grid, in shared memory: as long as the grid may take.
+__device__ __forceinline__ bool wait_long(uint32_t bar, uint32_t parity, uint64_t limit_ns) {
+    uint64_t t0 = 0;
+    for (uint64_t it = 1;; ++it) {
+        if (mbar_try_wait(bar, parity)) return true;
+        if (it % kPollsPerTime) continue;
+        const uint64_t t = global_ns();
+        if (t0 == 0) t0 = t;
+        else if (t - t0 > limit_ns || it > (uint64_t(1) << 40)) return false;
+    }
+}
+
+// The warps that read the accumulators take one way: a wait that only some of them gave up on
+// would leave the others at their barrier.
+__device__ __forceinline__ bool sum_warps_agree(bool ok) {
+    uint32_t r;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, 1, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+        : "=r"(r)
+        : "r"(uint32_t(ok)), "n"(kSumWarps * 32)
+        : "memory");
+    return r != 0;
+}
+
+// Where a row of the output lies, and element c of it.
+__device__ __forceinline__ __nv_bfloat16* out_at(const OrthParams& p, int mat, int r, int c) {
+    uint8_t* base = p.out + int64_t(mat) * p.out_batch;
+    return p.turned ? reinterpret_cast<__nv_bfloat16*>(base + int64_t(c) * p.out_pitch) + r
+                    : reinterpret_cast<__nv_bfloat16*>(base + int64_t(r) * p.out_pitch) + c;
+}
+// 32 columns from c of row r.
+__device__ __forceinline__ void store_out(const OrthParams& p, int mat, int r, int c, const float (&f)[32]) {
+    if (r >= p.m) return;
+    __nv_bfloat16* o = out_at(p, mat, r, c);
+    if (p.turned) {
+        const int64_t step = p.out_pitch / 2;
+#pragma unroll
+        for (int k = 0; k < 32; ++k)
+            if (c + k < p.n) o[k * step] = __float2bfloat16_rn(f[k]);
+    } else if (p.wide && c + 32 <= p.n) {
+#pragma unroll
+        for (int k = 0; k < 32; k += 8)
+            *reinterpret_cast<uint4*>(o + k) = make_uint4(pack_bf16(f[k], f[k + 1]), pack_bf16(f[k + 2], f[k + 3]),
+                                                          pack_bf16(f[k + 4], f[k + 5]), pack_bf16(f[k + 6], f[k + 7]));
+    } else {
+#pragma unroll
+        for (int k = 0; k < 32; ++k)
+            if (c + k < p.n) o[k] = __float2bfloat16_rn(f[k]);
+    }
+}
+
+template <bool PAIR>
+__global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_constant__ OrthParams p) {
+    constexpr int T = TileOf<PAIR>::kTile, kCtas = PAIR ? 2 : 1;
+    constexpr int kCols = T / 2;             // columns of the tile that a warp of the second group reads
+    constexpr int kTmemCols = 2 * T;
+    extern __shared__ uint8_t raw[];
+    // full and empty: a stage's copies have landed / its products are done (each CTA's own).  peer: the other CTA's copies
+    // have landed (the first CTA's).  summed: an accumulator is complete; taken: it has been read (the first CTA's).
+    // go: the grid has come to the next product.
+    __shared__ __align__(8) uint64_t bars[3 * kStages + 5];
+    __shared__ uint32_t tmem_base, last;
+    __shared__ volatile uint32_t failed;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = PAIR ? int(blockIdx.x & 1) : 0, unit = int(blockIdx.x) / kCtas, units = int(gridDim.x) / kCtas;
+    const uint32_t ring = (smem_addr(raw) + 1023) & ~1023u;
+    const uint32_t full = smem_addr(bars), empty = full + 8 * kStages, peer = empty + 8 * kStages;
+    const uint32_t summed = peer + 8 * kStages, taken = summed + 16, go = taken + 16;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kStages; ++i) {
+            mbar_init(full + 8 * i, 1);
+            mbar_init(empty + 8 * i, 1);
+            mbar_init(peer + 8 * i, 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(summed + 8 * i, 1);
+            mbar_init(taken + 8 * i, kCtas * kSumWarps);
+        }
+        mbar_init(go, 1);
+        failed = 0;
+        mbar_init_fence();
+    }
+    if (warp == 1) {
+        if constexpr (PAIR) {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem_base)), "r"(kTmemCols) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem_base)), "r"(kTmemCols) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+        }
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if constexpr (PAIR) cluster_meet();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = tmem_base;
+    const int phases = 3 * p.steps;
+    const int64_t x_bytes = int64_t(p.bm) * p.bn * kBoxBytes, s_bytes = int64_t(p.bm) * p.bm * kBoxBytes;
+
+    if (warp == 0 && lane == 0) {
+        // --- the operands ---
+        Ring<kStages> st;
+        int it = 0;
+        bool ok = true;
+        for (int ph = 0; ph < phases && ok; ++ph) {
+            const int phase = ph % 3;
+            if (ph) ok = grid_wait(p.count, uint32_t(ph) * gridDim.x, p.limit_ns);
+            if (!ok) break;
+            asm volatile("fence.proxy.async.global;" ::: "memory");   // what they wrote is read by copies
+            mbar_arrive(go);
+            const uint8_t* x = p.x[ph / 3 & 1];
+            const int items = items_of<PAIR>(p, phase);
+            for (int i = unit; i < items && ok; i += units) {
+                const Item w = item_of<PAIR>(p, phase, i);
+                // first box row or column of this CTA's part of either operand
+                const int left = w.i * (T / kBox) + rank * 2, right = w.j * (T / kBox) + rank * 2;
+                const uint8_t* xm = x + w.mat * x_bytes;
+                const uint8_t* sm = (phase == 1 ? p.sa : p.sb) + w.mat * s_bytes;
+                for (int s = 0; s < w.stages; ++s, ++it, st.next()) {
+                    ok = it < kStages || mbar_wait_bounded(empty + 8 * st.at, st.round ^ 1, kWaitNs);
+                    if (!ok) break;
+                    const int k = w.s0 + s, kt = k / (T / kBox);
+                    const uint32_t to = ring + st.at * kStageBytes, bar = full + 8 * st.at;
+                    mbar_expect_tx(bar, kStageBytes + (it == 0 && rank == kCtas - 1 && p.stall ? 16 : 0));
+                    // two boxes, one above the other or side by side
+                    auto above = [&](uint32_t at, const uint8_t* base, int width, int r, int c) {
+                        bulk_g2s(at, base + (int64_t(r) * width + c) * kBoxBytes, kBoxBytes, bar);
+                        bulk_g2s(at + kBoxBytes, base + (int64_t(r + 1) * width + c) * kBoxBytes, kBoxBytes, bar);
+                    };
+                    auto beside = [&](uint32_t at, const uint8_t* base, int width, int r, int c) {
+                        bulk_g2s(at, base + (int64_t(r) * width + c) * kBoxBytes, kOperand, bar);
+                    };
+                    if (phase == 0) {
+                        above(to, xm, p.bn, left, k);
+                        above(to + kOperand, xm, p.bn, right, k);
+                    } else {
+                        if (w.i <= kt) above(to, sm, p.bm, left, k);
+                        else beside(to, sm, p.bm, k, left);
+                        if (phase == 2) beside(to + kOperand, xm, p.bn, k, right);
+                        else if (w.j <= kt) above(to + kOperand, sm, p.bm, right, k);
+                        else beside(to + kOperand, sm, p.bm, k, right);
+                    }
+                }
+            }
+        }
+        // every copy lands, and every arrival that ends a stage's products, before the CTA's memory is given back
+        for (int i = it > kStages ? it - kStages : 0; i < it; ++i)
+            if (!mbar_wait_bounded(full + 8 * (i % kStages), (i / kStages) & 1, kWaitNs)) ok = false;
+        bool ended = true;
+        for (int i = it > kStages ? it - kStages : 0; i < it && ended; ++i)
+            ended = mbar_wait_bounded(empty + 8 * (i % kStages), (i / kStages) & 1, kWaitNs);
+        if (!ok || !ended) failed = 1;
+    } else if (warp == 1 && lane == 0) {
+        // --- the products; in the second CTA of a pair: word of its copies for the first ---
+        Ring<kStages> st;
+        Ring<2> acc;
+        const uint32_t first_peer = PAIR ? cluster_addr(peer, 0) : 0;
+        int chunk = 0;
+        bool ok = true;
+        for (int ph = 0; ph < phases && ok; ++ph) {
+            const int phase = ph % 3;
+            const int items = items_of<PAIR>(p, phase);
+            for (int i = unit; i < items && ok; i += units) {
+                const Item w = item_of<PAIR>(p, phase, i);
+                // (a first stage comes once the grid has come here)
+                if (rank) {
+                    for (int s = 0; s < w.stages && ok; ++s, st.next()) {
+                        ok = wait_long(full + 8 * st.at, st.round, s ? kWaitNs : p.limit_ns);
+                        if (ok) arrive_at(first_peer + 8 * st.at);
+                    }
+                    continue;
+                }
+                if (chunk >= 2) ok = mbar_wait_bounded(taken + 8 * acc.at, acc.round ^ 1, kWaitNs);
+                for (int s = 0; s < w.stages && ok; ++s, st.next()) {
+                    ok = wait_long(full + 8 * st.at, st.round, s ? kWaitNs : p.limit_ns);
+                    if (PAIR && ok) ok = wait_long(peer + 8 * st.at, st.round, s ? kWaitNs : p.limit_ns);
+                    if (!ok) break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    const int kt = (w.s0 + s) / (T / kBox);
+                    // rows along the reduction: 16 of them are 2048 bytes further; across it 16 columns are 32 bytes
+                    const bool ta = phase && w.i > kt, tb = phase == 2 || (phase == 1 && w.j > kt);
+                    const uint64_t l = operand_desc(ring + st.at * kStageBytes), r = l + (kOperand >> 4);
+                    const uint32_t idesc = TileOf<PAIR>::kIdesc | (ta ? 1u << 15 : 0u) | (tb ? 1u << 16 : 0u);
+                    const int la = ta ? 2048 >> 4 : 2, lb = tb ? 2048 >> 4 : 2;
+#pragma unroll
+                    for (int k = 0; k < kBox / 16; ++k)
+                        mma<PAIR>(tmem + acc.at * T, l + k * la, r + k * lb, idesc, s > 0 || k > 0);
+                    commit<PAIR>(empty + 8 * st.at);
+                }
+                if (ok) commit<PAIR>(summed + 8 * acc.at);
+                acc.next();
+                ++chunk;
+            }
+        }
+        if (!ok) failed = 1;
+    } else if (warp >= kSumWarp) {
+        // --- what comes of an accumulator ---
+        const int quad = warp & 3, half = (warp - kSumWarp) >> 2, t = threadIdx.x - kSumWarp * 32;
+        const int row = quad * 32 + lane;                 // of this CTA's 128
+        const uint32_t first_taken = PAIR ? cluster_addr(taken, 0) : taken;
+        const uint32_t from = tmem + (uint32_t(quad * 32) << 16) + half * kCols;
+        Ring<2> acc;
+        bool ok = true;
+        for (int ph = 0; ph < phases; ++ph) {
+            const int phase = ph % 3, step = ph / 3;
+            const bool final = ph == phases - 1;
+            ok = sum_warps_agree(wait_long(go, ph & 1, p.limit_ns));
+            if (!ok) break;
+            const OrthStep co = p.step[step];
+            const int splits = p.splits[phase], items = items_of<PAIR>(p, phase);
+            for (int i = unit; i < items; i += units, acc.next()) {
+                const Item w = item_of<PAIR>(p, phase, i);
+                ok = sum_warps_agree(mbar_wait_warp(summed + 8 * acc.at, acc.round));
+                if (!ok) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const int gr = w.i * T + rank * kCtaRows + row, gc = w.j * T + half * kCols;
+                bool mine = true;
+                const float* parts = nullptr;
+                if (splits > 1) {
+                    // the split that comes last adds them all up, in their order
+                    constexpr int kPart = kCtaRows * T;
+                    float* mypart = p.part + (int64_t(w.tile) * kCtas + rank) * splits * kPart + half * kCols * kCtaRows + row;
+                    parts = mypart;
+                    mypart += int64_t(w.split) * kPart;
+#pragma unroll 1
+                    for (int c = 0; c < kCols; c += 32) {
+                        float f[32];
+                        tmem_ld32(from + acc.at * T + c, f);
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) __stcg(mypart + (c + k) * kCtaRows, f[k]);
+                    }
+                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) arrive_at(first_taken + 8 * acc.at);
+                    __threadfence();
+                    asm volatile("bar.sync 1, %0;" ::"n"(kSumWarps * 32) : "memory");
+                    if (t == 0) {
+                        uint32_t* a = p.arrived + w.tile * kCtas + rank;
+                        const uint32_t n = atomicAdd(a, 1u);
+                        last = n == uint32_t(splits - 1);
+                        if (last) *a = 0;            // for the next product
+                        __threadfence();
+                    }
+                    asm volatile("bar.sync 1, %0;" ::"n"(kSumWarps * 32) : "memory");
+                    mine = last;
+                }
+                float scale, dr = 0.0f;
+                if (phase == 0) scale = 1.0f / (p.x_scale * p.x_scale);
+                else if (phase == 1) scale = 1.0f / (p.a_scale * p.a_scale), dr = __ldcg(p.d + int64_t(w.mat) * p.bm * kBox + gr);
+                else scale = 1.0f / co.scale, dr = co.a + __ldcg(p.e + int64_t(w.mat) * p.bm * kBox + gr);
+#pragma unroll 1
+                for (int c = 0; c < kCols && mine; c += 32) {
+                    float f[32];
+                    if (splits > 1) {
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) f[k] = __ldcg(parts + (c + k) * kCtaRows);
+#pragma unroll 1
+                        for (int s = 1; s < splits; ++s)
+#pragma unroll
+                            for (int k = 0; k < 32; ++k) f[k] += __ldcg(parts + int64_t(s) * (kCtaRows * T) + (c + k) * kCtaRows);
+                    } else {
+                        tmem_ld32(from + acc.at * T + c, f);
+                    }
+                    const int col = gc + c, bc = col / kBox, br = gr / kBox, p0 = col % kBox / 8;
+                    if (phase == 0) {
+                        uint8_t* o = p.sa + w.mat * s_bytes + (int64_t(br) * p.bm + bc) * kBoxBytes;
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) {
+                            f[k] *= scale;
+                            if (col + k == gr) {
+                                p.d[int64_t(w.mat) * p.bm * kBox + gr] = f[k];
+                                f[k] = 0.0f;
+                            }
+                            f[k] *= p.a_scale;
+                        }
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            *reinterpret_cast<uint4*>(o + piece_at(gr % kBox, p0 + k)) =
+                                make_uint4(pack_f16(f[8 * k], f[8 * k + 1]), pack_f16(f[8 * k + 2], f[8 * k + 3]),
+                                           pack_f16(f[8 * k + 4], f[8 * k + 5]), pack_f16(f[8 * k + 6], f[8 * k + 7]));
+                    } else if (phase == 1) {
+                        const int64_t off = w.mat * s_bytes + (int64_t(br) * p.bm + bc) * kBoxBytes;
+                        const float* dc = p.d + int64_t(w.mat) * p.bm * kBox + col;
+                        const float a_back = 1.0f / p.a_scale;
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const uint32_t at = piece_at(gr % kBox, p0 + k);
+                            const uint4 a = ld_l2(p.sa + off + at);
+                            const float4 d0 = __ldcg(reinterpret_cast<const float4*>(dc + 8 * k)), d1 = __ldcg(reinterpret_cast<const float4*>(dc + 8 * k + 4));
+                            const float dj[8] = {d0.x, d0.y, d0.z, d0.w, d1.x, d1.y, d1.z, d1.w};
+                            const uint32_t aw[4] = {a.x, a.y, a.z, a.w};
+                            float v[8];
+#pragma unroll
+                            for (int m = 0; m < 8; ++m) {
+                                const float2 a2 = unpack_f16(aw[m / 2]);
+                                const float a0 = (m & 1 ? a2.y : a2.x) * a_back;
+                                if (col + 8 * k + m == gr) {
+                                    // (A0 is zero there)
+                                    const float e = co.b * dr + co.c * (f[8 * k + m] * scale + dr * dr);
+                                    p.e[int64_t(w.mat) * p.bm * kBox + gr] = e;
+                                    v[m] = 0.0f;
+                                } else {
+                                    v[m] = (co.b * a0 + co.c * (f[8 * k + m] * scale + (dr + dj[m]) * a0)) * co.scale;
+                                }
+                            }
+                            *reinterpret_cast<uint4*>(p.sb + off + at) =
+                                make_uint4(pack_f16(v[0], v[1]), pack_f16(v[2], v[3]), pack_f16(v[4], v[5]), pack_f16(v[6], v[7]));
+                        }
+                    } else {
+                        const int64_t off = w.mat * x_bytes + (int64_t(br) * p.bn + bc) * kBoxBytes;
+                        const uint8_t* xi = p.x[step & 1] + off;
+                        uint8_t* xo = p.x[step & 1 ^ 1] + off;
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const uint32_t at = piece_at(gr % kBox, p0 + k);
+                            const uint4 h = ld_l2(xi + at), l = ld_l2(p.rest + off + at);
+                            const uint32_t hw[4] = {h.x, h.y, h.z, h.w}, lw[4] = {l.x, l.y, l.z, l.w};
+                            uint32_t hn[4], ln[4];
+#pragma unroll
+                            for (int m = 0; m < 4; ++m) {
+                                const float2 hv = unpack_f16(hw[m]), lv = unpack_f16(lw[m]);
+                                float& v0 = f[8 * k + 2 * m];
+                                float& v1 = f[8 * k + 2 * m + 1];
+                                v0 = fmaf(dr, fmaf(lv.x, 1.0f / kRest, hv.x), v0 * scale);
+                                v1 = fmaf(dr, fmaf(lv.y, 1.0f / kRest, hv.y), v1 * scale);
+                                if (!final) split_pair(v0, v1, hn[m], ln[m]);
+                            }
+                            if (!final) {
+                                *reinterpret_cast<uint4*>(xo + at) = make_uint4(hn[0], hn[1], hn[2], hn[3]);
+                                *reinterpret_cast<uint4*>(p.rest + off + at) = make_uint4(ln[0], ln[1], ln[2], ln[3]);
+                            }
+                        }
+                        if (final) {
+                            const float back = 1.0f / p.x_scale;
+#pragma unroll
+                            for (int k = 0; k < 32; ++k) f[k] *= back;
+                            store_out(p, w.mat, gr, col, f);
+                        }
+                    }
+                }
+                if (splits == 1) {
+                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) arrive_at(first_taken + 8 * acc.at);
+                }
+            }
+            if (!ok) break;
+            if (!final) {
+                asm volatile("fence.proxy.async.global;" ::: "memory");
+                __threadfence();
+                asm volatile("bar.sync 1, %0;" ::"n"(kSumWarps * 32) : "memory");
+                if (t == 0) asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(p.count) : "memory");
+            }
+        }
+        if (!ok) {
+            failed = 1;
+            // NaN where this CTA's outputs would be
+            float f[32];
+#pragma unroll
+            for (int k = 0; k < 32; ++k) f[k] = __uint_as_float(0x7fffffffu);
+            const int items = items_of<PAIR>(p, 2);
+            for (int i = unit; i < items; i += units) {
+                const Item w = item_of<PAIR>(p, 2, i);
+                for (int c = 0; c < kCols; c += 32)
+                    store_out(p, w.mat, w.i * T + rank * kCtaRows + row, w.j * T + half * kCols + c, f);
+            }
+        }
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    }
+    __syncwarp();
+    __syncthreads();
+    if constexpr (PAIR) cluster_meet();   // the other CTA's barriers and operands are used until here
+    if (warp == 1) {
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        if constexpr (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+        else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+    }
+}
+
+// --- before the products -----------------------------------------------------------
+
+struct PrepParams {
+    const uint8_t* u;
+    uint8_t* m;              // momentum (null: none)
+    float2* part;            // [batch][parts]
+    uint32_t* zero;          // counters of the product kernel
+    uint8_t* hi;
+    uint8_t* rest;
+    int64_t u_pitch, u_batch, m_pitch, m_batch;   // bytes
+    int64_t rows, cols;      // as given; one long row where they are contiguous
+    int32_t nzero, parts;
+    float beta, x_scale;
+    double eps;
+    int32_t u_bf16, nesterov, turned, bm, bn;
+    int32_t wide;            // rows on 16-byte boundaries
+};
+
+// Values c .. c + 7 of a row, zero beyond its end.
+__device__ __forceinline__ void load8(const uint8_t* row, bool bf16, bool wide, int64_t c, int64_t cols, float (&f)[8]) {
+    if (wide && c + 8 <= cols) {
+        if (bf16) {
+            unpack(*reinterpret_cast<const uint4*>(row + c * 2), f);
+        } else {
+            const float4 a = *reinterpret_cast<const float4*>(row + c * 4), b = *reinterpret_cast<const float4*>(row + c * 4 + 16);
+            f[0] = a.x, f[1] = a.y, f[2] = a.z, f[3] = a.w, f[4] = b.x, f[5] = b.y, f[6] = b.z, f[7] = b.w;
+        }
+        return;
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+        f[k] = c + k >= cols ? 0.0f : bf16 ? to_f32(reinterpret_cast<const __nv_bfloat16*>(row)[c + k]) : reinterpret_cast<const float*>(row)[c + k];
+}
+// The momentum after a gradient, and the update that comes of both.
+__device__ __forceinline__ float moved(const PrepParams& p, float m, float g) { return fmaf(1.0f - p.beta, g - m, m); }
+__device__ __forceinline__ float update_of(const PrepParams& p, float m, float g) { return p.nesterov ? fmaf(p.beta, m - g, g) : m; }
+
+// Moves the momentum and leaves sums of the update's squares, one pair a CTA: as they are, and of values
+// times 2^-80 for a matrix whose squares leave fp32's range.
+__global__ void __launch_bounds__(256) orth_norm_kernel(PrepParams p) {
+    __shared__ float2 sums[8];
+    const int mat = blockIdx.y;
+    if (mat == 0)
+        for (int i = int(blockIdx.x) * 256 + int(threadIdx.x); i < p.nzero; i += p.parts * 256) p.zero[i] = 0;
+    const uint8_t* u = p.u + int64_t(mat) * p.u_batch;
+    uint8_t* m = p.m ? p.m + int64_t(mat) * p.m_batch : nullptr;
+    const int64_t width = (p.cols + 7) / 8, all = p.rows * width;
+    float s1 = 0.0f, s2 = 0.0f;
+    for (int64_t at = int64_t(blockIdx.x) * 256 + threadIdx.x; at < all; at += int64_t(p.parts) * 256) {
+        int64_t r, c;
+        split_item(at, width, r, c);
+        c *= 8;
+        float f[8];
+        load8(u + r * p.u_pitch, p.u_bf16, p.wide, c, p.cols, f);
+        if (m) {
+            float v[8];
+            float* row = reinterpret_cast<float*>(m + r * p.m_pitch);
+            load8(reinterpret_cast<const uint8_t*>(row), false, p.wide, c, p.cols, v);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                v[k] = moved(p, v[k], f[k]);
+                f[k] = update_of(p, v[k], f[k]);
+            }
+            if (p.wide && c + 8 <= p.cols) {
+                *reinterpret_cast<float4*>(row + c) = make_float4(v[0], v[1], v[2], v[3]);
+                *reinterpret_cast<float4*>(row + c + 4) = make_float4(v[4], v[5], v[6], v[7]);
+            } else {
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (c + k < p.cols) row[c + k] = v[k];
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            s1 = fmaf(f[k], f[k], s1);
+            const float small = f[k] * 0x1p-80f;
+            s2 = fmaf(small, small, s2);
+        }
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+        s1 += __shfl_xor_sync(0xffffffffu, s1, o);
+        s2 += __shfl_xor_sync(0xffffffffu, s2, o);
+    }
+    if (threadIdx.x % 32 == 0) sums[threadIdx.x / 32] = make_float2(s1, s2);
+    __syncthreads();
+    if (threadIdx.x) return;
+    for (int w = 1; w < 8; ++w) {
+        s1 += sums[w].x;
+        s2 += sums[w].y;
+    }
+    p.part[int64_t(mat) * p.parts + blockIdx.x] = make_float2(s1, s2);
+}
+
+// The update over its norm as X: operand and rest, box by box.
+__global__ void __launch_bounds__(256) orth_split_kernel(PrepParams p) {
+    __shared__ float2 sums[8];
+    __shared__ float factor[2];
+    __shared__ float tile[kBox][kBox + 1];
+    const int mat = blockIdx.y, t = threadIdx.x;
+    float s1 = 0.0f, s2 = 0.0f;
+    for (int i = t; i < p.parts; i += 256) {
+        const float2 v = p.part[int64_t(mat) * p.parts + i];
+        s1 += v.x;
+        s2 += v.y;
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+        s1 += __shfl_xor_sync(0xffffffffu, s1, o);
+        s2 += __shfl_xor_sync(0xffffffffu, s2, o);
+    }
+    if (t % 32 == 0) sums[t / 32] = make_float2(s1, s2);
+    __syncthreads();
+    if (t == 0) {
+        for (int w = 1; w < 8; ++w) {
+            s1 += sums[w].x;
+            s2 += sums[w].y;
+        }
+        // squares beyond the range: values and norm times 2^-64
+        const bool large = s1 > 3.402823466e38f;
+        const double norm = large ? sqrt(double(s2)) * 0x1p80 : sqrt(double(s1));
+        factor[0] = large ? 0x1p-64f : 1.0f;
+        factor[1] = float(double(p.x_scale) / (norm + p.eps) * (large ? 0x1p64 : 1.0));
+    }
+    __syncthreads();
+    const float f0 = factor[0], f1 = factor[1];
+    const uint8_t* u = p.u + int64_t(mat) * p.u_batch;
+    const uint8_t* m = p.m ? p.m + int64_t(mat) * p.m_batch : nullptr;
+    const int r = t / 4, c = t % 4 * 16;     // a thread's row and its 16 columns of it
+    const int64_t boxes = int64_t(p.bm) * p.bn;
+    for (int64_t box = blockIdx.x; box < boxes; box += gridDim.x) {
+        const int64_t br = box / p.bn, bc = box - br * p.bn;
+        // the box of U: where X is turned, (bc, br)
+        const int64_t ur = (p.turned ? bc : br) * kBox + r, uc = (p.turned ? br : bc) * kBox + c;
+        float f[16];
+        if (ur < p.rows && uc < p.cols) {
+            float h[8];
+#pragma unroll
+            for (int k = 0; k < 16; k += 8) {
+                load8(u + ur * p.u_pitch, p.u_bf16, p.wide, uc + k, p.cols, h);
+                if (m) {
+                    float v[8];
+                    load8(m + ur * p.m_pitch, false, p.wide, uc + k, p.cols, v);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) h[j] = update_of(p, v[j], h[j]);
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) f[k + j] = uc + k + j < p.cols ? h[j] * f0 * f1 : 0.0f;
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < 16; ++k) f[k] = 0.0f;
+        }
+        if (p.turned) {
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < 16; ++k) tile[r][c + k] = f[k];
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < 16; ++k) f[k] = tile[c + k][r];
+        }
+        const int64_t off = (int64_t(mat) * boxes + box) * kBoxBytes;
+#pragma unroll
+        for (int k = 0; k < 16; k += 8) {
+            uint32_t hi[4], lo[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) split_pair(f[k + 2 * j], f[k + 2 * j + 1], hi[j], lo[j]);
+            const uint32_t at = piece_at(r, (c + k) / 8);
+            *reinterpret_cast<uint4*>(p.hi + off + at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+            *reinterpret_cast<uint4*>(p.rest + off + at) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+        }
+    }
+}
+
+// --- host -------------------------------------------------------------------------
+
+constexpr int64_t al(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
+
+// How a call is cut, and where its parts lie in the workspace.
+struct Plan {
+    int64_t batch, m, n, bm, bn, tm, tn;
+    bool pair, turned;
+    int ctas;                 // of a tile
+    int64_t splits[3], items[3], parts;
+    int64_t counters, norm, d, e, x0, x1, rest, sa, sb, part, bytes;
+};
+constexpr int kPairs = 76;    // pairs of CTAs that the device holds
+constexpr int64_t kPairFrom = 1024;
+
+Plan plan_of(int64_t batch, int64_t rows, int64_t cols) {
+    Plan q{};
+    q.batch = batch;
+    q.turned = rows > cols;
+    q.m = q.turned ? cols : rows;
+    q.n = q.turned ? rows : cols;
+    q.pair = q.m >= kPairFrom;
+    q.ctas = q.pair ? 2 : 1;
+    const int64_t T = q.pair ? 256 : 128, units = q.pair ? kPairs : 2 * kPairs;
+    q.tm = al(q.m, T) / T;
+    q.tn = al(q.n, T) / T;
+    q.bm = q.tm * T / kBox;
+    q.bn = q.tn * T / kBox;
+    const int64_t half = batch * q.tm * (q.tm + 1) / 2;
+    for (int k = 0; k < 3; ++k) {
+        const int64_t tiles = k == 2 ? batch * q.tm * q.tn : half, stages = k == 0 ? q.bn : q.bm;
+        int64_t s = k == 2 ? 1 : units / tiles;
+        if (s > stages / 4) s = stages / 4;
+        if (s < 1) s = 1;
+        const int64_t per = (stages + s - 1) / s;
+        q.splits[k] = (stages + per - 1) / per;
+        q.items[k] = tiles * q.splits[k];
+    }
+    q.parts = al(q.m * q.n, 4096) / 4096;
+    if (q.parts > kNormCtas) q.parts = kNormCtas;
+    int64_t at = 0;
+    auto take = [&](int64_t bytes) {
+        const int64_t here = at;
+        at += al(bytes, 256);
+        return here;
+    };
+    const int64_t x = batch * q.bm * q.bn * kBoxBytes, sq = batch * q.bm * q.bm * kBoxBytes, diag = batch * q.bm * kBox * 4;
+    const int64_t most = q.splits[0] > q.splits[1] ? q.splits[0] : q.splits[1];
+    q.counters = take((1 + half * q.ctas) * 4);
+    q.norm = take(batch * q.parts * 8);
+    q.d = take(diag);
+    q.e = take(diag);
+    q.x0 = take(x);
+    q.x1 = take(x);
+    q.rest = take(x);
+    q.sa = take(sq);
+    q.sb = take(sq);
+    q.part = take(most > 1 ? half * most * T * T * 4 : 0);
+    q.bytes = at;
+    return q;
+}
+
+// Largest magnitude of y -> a y + b y^3 + c y^5 on [0, r], and of b y^2 + c y^4.
+double most_of(double a, double b, double c, double r) {
+    auto f = [&](double y2) { return std::fabs(std::sqrt(y2) * (a + y2 * (b + y2 * c))); };
+    double most = f(r * r);
+    // a + 3 b y^2 + 5 c y^4 = 0
+    const double disc = 9 * b * b - 20 * a * c;
+    if (disc >= 0)
+        for (double s : {-1.0, 1.0}) {
+            const double y2 = c != 0 ? (-3 * b + s * std::sqrt(disc)) / (10 * c) : b != 0 ? -a / (3 * b) : -1.0;
+            if (y2 > 0 && y2 < r * r) most = std::fmax(most, f(y2));
+        }
+    return most;
+}
+double most_of_b(double b, double c, double r) {
+    auto f = [&](double y2) { return std::fabs(y2 * (b + y2 * c)); };
+    double most = f(r * r);
+    if (c != 0 && -b / (2 * c) > 0 && -b / (2 * c) < r * r) most = std::fmax(most, f(-b / (2 * c)));
+    return most;
+}
+// The largest power of two that takes `most` to no more than half of fp16's range.
+float room_for(double most) {
+    int k = 0;
+    std::frexp(32768.0 / std::fmax(most, 1.0), &k);
+    return float(std::ldexp(1.0, k - 1 > 15 ? 15 : k - 1));
+}
+
+template <bool PAIR>
+cudaError_t resident(int device, int* n) {
+    static int held[kOpsMaxDevices];
+    if (!held[device]) {
+        cudaError_t e = cudaFuncSetAttribute(orth_product_kernel<PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+        if (e != cudaSuccess) return e;
+        int k = 0;
+        if (PAIR) {
+            cudaLaunchAttribute attr{};
+            attr.id = cudaLaunchAttributeClusterDimension;
+            attr.val.clusterDim.x = 2;
+            attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+            cudaLaunchConfig_t c{};
+            c.gridDim = dim3(2 * kPairs);
+            c.blockDim = dim3(kThreads);
+            c.dynamicSmemBytes = kSmem;
+            c.attrs = &attr;
+            c.numAttrs = 1;
+            e = cudaOccupancyMaxActiveClusters(&k, orth_product_kernel<PAIR>, &c);
+        } else {
+            e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&k, orth_product_kernel<PAIR>, kThreads, kSmem);
+            k *= ops_sm_count(device);
+        }
+        if (e != cudaSuccess) return e;
+        if (k < 1) return cudaErrorCooperativeLaunchTooLarge;
+        held[device] = k;
+    }
+    *n = held[device];
+    return cudaSuccess;
+}
+
+template <bool PAIR>
+cudaError_t launch_products(int device, const OrthParams& p, const Plan& q, cudaStream_t s) {
+    int units = 0;
+    cudaError_t e = resident<PAIR>(device, &units);
+    if (e != cudaSuccess) return e;
+    int64_t want = 1;
+    for (int64_t i : q.items) want = i > want ? i : want;
+    if (want < units) units = int(want);
+    cudaLaunchAttribute attr[2] = {};
+    attr[0].id = cudaLaunchAttributeCooperative;
+    attr[0].val.cooperative = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = 2;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t c{};
+    c.gridDim = dim3(unsigned(units * q.ctas));
+    c.blockDim = dim3(kThreads);
+    c.dynamicSmemBytes = kSmem;
+    c.stream = s;
+    c.attrs = attr;
+    c.numAttrs = PAIR ? 2 : 1;
+    cudaGetLastError();
+    return cudaLaunchKernelEx(&c, orth_product_kernel<PAIR>, p);
+}
+
+// Checks of one array of matrices; the whole of it as one span.
+lc_status check_mats(const char* call, const char* name, const lc_mats* a, int64_t batch, int64_t rows, int64_t cols, bool out,
+                     Span2* span) {
+    if (!a) return fail_status(LC_ERR_INVALID_ARG, "%s: %s is NULL", call, name);
+    const int e = elem_size(a->dtype);
+    if (!e) return fail_status(LC_ERR_INVALID_ARG, "%s: %s has unknown dtype %d", call, name, int(a->dtype));
+    if (reinterpret_cast<uintptr_t>(a->data) % uintptr_t(e))
+        return fail_status(LC_ERR_INVALID_ARG, "%s: %s is not element-aligned", call, name);
+    constexpr int64_t kFar = int64_t(1) << 40;
+    if (a->stride < 0 || a->batch_stride < 0 || a->stride > kFar || a->batch_stride > kFar)
+        return fail_status(LC_ERR_INVALID_ARG, "%s: %s has strides %lld and %lld", call, name, (long long)a->batch_stride,
+                           (long long)a->stride);
+    // an output's rows do not meet: matrix after matrix, or row after row of all of them
+    const int64_t st = rows > 1 ? a->stride : 0, bs = batch > 1 ? a->batch_stride : 0;
+    if (out && !((rows == 1 || st >= cols) && (batch <= 1 || bs >= (rows - 1) * st + cols)) &&
+        !((batch <= 1 || bs >= cols) && (rows == 1 || st >= (batch - 1) * bs + cols)))
+        return fail_status(LC_ERR_INVALID_ARG, "%s: rows of %s overlap (strides %lld and %lld)", call, name,
+                           (long long)a->batch_stride, (long long)a->stride);
+    *span = {name, a->data, batch > 0 ? 1 : 0, ((batch - 1) * bs + (rows - 1) * st + cols) * e, 0, out};
+    return LC_OK;
+}
+
+bool rows_wide(const void* p, int64_t pitch, int64_t batch_pitch) { return aligned16(p) && pitch % 16 == 0 && batch_pitch % 16 == 0; }
+
+bool orth_sizes(int64_t batch, int64_t rows, int64_t cols) {
+    return batch >= 0 && batch <= 65535 && rows > 0 && cols > 0 && rows <= LC_ORTH_MAX_DIM && cols <= LC_ORTH_MAX_DIM &&
+           batch * ((rows + 127) / 128) * ((cols + 127) / 128) < (int64_t(1) << 30);
+}
+
+}  // namespace
+}  // namespace lc
+
+using namespace lc;
+
+extern "C" uint64_t lc_orthogonalize_workspace(int64_t batch, int64_t rows, int64_t cols) {
+    if (!orth_sizes(batch, rows, cols) || batch == 0) return 0;
+    return uint64_t(plan_of(batch, rows, cols).bytes);
+}
+
+extern "C" lc_status lc_orthogonalize(int device, void* cuda_stream, const lc_mats* update, int64_t batch, int64_t rows,
+                                      int64_t cols, const lc_mats* momentum, double beta, int32_t nesterov, int32_t steps,
+                                      const double* coefficients, double eps, const lc_mats* out, void* workspace,
+                                      uint64_t workspace_bytes) {
+    const char* call = "lc_orthogonalize";
+    set_last_error("");
+    if (!orth_sizes(batch, rows, cols))
+        return fail_status(LC_ERR_INVALID_ARG, "%s: %lld matrices of %lld x %lld (at most LC_ORTH_MAX_DIM = %d a side)", call,
+                           (long long)batch, (long long)rows, (long long)cols, LC_ORTH_MAX_DIM);
+    if (steps < 1 || steps > kMaxSteps || !coefficients)
+        return fail_status(LC_ERR_INVALID_ARG, "%s: 1 to %d steps with three coefficients each are needed", call, kMaxSteps);
+    if (!(eps >= 0.0) || eps > 1e30) return fail_status(LC_ERR_INVALID_ARG, "%s: eps %g", call, eps);
+    if (momentum && !(beta >= 0.0 && beta < 1.0)) return fail_status(LC_ERR_INVALID_ARG, "%s: beta %g", call, beta);
+    Span2 spans[4];
+    int n = 0;
+    lc_status st = check_mats(call, "update", update, batch, rows, cols, false, &spans[n++]);
+    if (st == LC_OK && momentum) st = check_mats(call, "momentum", momentum, batch, rows, cols, true, &spans[n++]);
+    if (st == LC_OK) st = check_mats(call, "out", out, batch, rows, cols, true, &spans[n++]);
+    if (st != LC_OK) return st;
+    if (momentum && momentum->dtype != LC_F32) return fail_status(LC_ERR_INVALID_ARG, "%s: the momentum is kept in fp32", call);
+    if (out->dtype != LC_BF16) return fail_status(LC_ERR_INVALID_ARG, "%s: out is bf16", call);
+    const Plan q = plan_of(batch, rows, cols);
+    // what no singular value exceeds at any step, from which the operands' scales follow
+    OrthParams p{};
+    double r = 1.0, most = 1.0;
+    for (int k = 0; k < steps; ++k) {
+        const double a = coefficients[3 * k], b = coefficients[3 * k + 1], c = coefficients[3 * k + 2];
+        if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c) || std::fabs(a) > 1e3 || std::fabs(b) > 1e3 || std::fabs(c) > 1e3)
+            return fail_status(LC_ERR_INVALID_ARG, "%s: coefficients %g, %g, %g", call, a, b, c);
+        const double in_b = most_of_b(b, c, r);
+        p.step[k] = {float(a), float(b), float(c), room_for(in_b)};
+        r = most_of(a, b, c, r);
+        if (!(r <= 16.0) || in_b > 16384.0)
+            return fail_status(LC_ERR_INVALID_ARG, "%s: the coefficients of step %d let singular values grow to %g", call, k, r);
+        most = std::fmax(most, r);
+    }
+    p.a_scale = room_for(most * most);
+    p.x_scale = room_for(most);
+    // elements of about 1 where the matrix has no structure: sqrt(m n) times those of X
+    const float middle = float(std::ldexp(1.0, std::ilogb(std::sqrt(double(q.m) * double(q.n)))));
+    if (middle < p.x_scale) p.x_scale = middle;
+    const uint64_t need = batch ? uint64_t(q.bytes) : 0;
+    if (workspace_bytes < need)
+        return fail_status(LC_ERR_CAPACITY, "%s: %llu bytes of workspace, %llu needed", call, (unsigned long long)workspace_bytes,
+                           (unsigned long long)need);
+    if (need && reinterpret_cast<uintptr_t>(workspace) % 256)
+        return fail_status(LC_ERR_INVALID_ARG, "%s: the workspace is not 256-byte aligned", call);
+    OnDevice cur(device);
+    spans[n++] = {"workspace", workspace, need ? 1 : 0, int64_t(need), 0, true};
+    st = ops_check(call, device, spans, n);
+    if (st != LC_OK) return st;
+    if (!cur.ok) return fail_status(LC_ERR_CUDA, "%s: cannot make device %d current", call, device);
+    if (!batch) return LC_OK;
+    uint8_t* const w = static_cast<uint8_t*>(workspace);
+    cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+    PrepParams a{};
+    const int ue = elem_size(update->dtype);
+    a.u = static_cast<const uint8_t*>(update->data);
+    a.u_pitch = update->stride * ue;
+    a.u_batch = update->batch_stride * ue;
+    a.wide = rows_wide(a.u, rows > 1 ? a.u_pitch : 0, batch > 1 ? a.u_batch : 0);
+    if (momentum) {
+        a.m = static_cast<uint8_t*>(momentum->data);
+        a.m_pitch = momentum->stride * 4;
+        a.m_batch = momentum->batch_stride * 4;
+        a.wide = a.wide && rows_wide(a.m, rows > 1 ? a.m_pitch : 0, batch > 1 ? a.m_batch : 0);
+    }
+    a.part = reinterpret_cast<float2*>(w + q.norm);
+    a.zero = reinterpret_cast<uint32_t*>(w + q.counters);
+    a.nzero = int32_t((q.norm - q.counters) / 4);
+    a.parts = int32_t(q.parts);
+    a.hi = w + q.x0;
+    a.rest = w + q.rest;
+    a.rows = rows;
+    a.cols = cols;
+    a.beta = float(beta);
+    a.x_scale = p.x_scale;
+    a.eps = eps;
+    a.u_bf16 = update->dtype == LC_BF16;
+    a.nesterov = nesterov != 0;
+    a.turned = q.turned;
+    a.bm = int32_t(q.bm);
+    a.bn = int32_t(q.bn);
+    PrepParams flat = a;
+    if (update->stride == cols && (!momentum || momentum->stride == cols)) {
+        flat.rows = 1;
+        flat.cols = rows * cols;
+        flat.wide = rows_wide(a.u, 0, batch > 1 ? a.u_batch : 0) && (!momentum || rows_wide(a.m, 0, batch > 1 ? a.m_batch : 0));
+    }
+    cudaGetLastError();
+    orth_norm_kernel<<<dim3(unsigned(q.parts), unsigned(batch)), 256, 0, s>>>(flat);
+    cudaError_t err = cudaGetLastError();
+    if (err != cudaSuccess) return ops_launched(call, err);
+    const int64_t boxes = q.bm * q.bn, most_ctas = int64_t(ops_sm_count(device)) * 8;
+    orth_split_kernel<<<dim3(unsigned(boxes < most_ctas ? boxes : most_ctas), unsigned(batch)), 256, 0, s>>>(a);
+    err = cudaGetLastError();
+    if (err != cudaSuccess) return ops_launched(call, err);
+    p.count = reinterpret_cast<uint32_t*>(w + q.counters);
+    p.arrived = p.count + 1;
+    p.d = reinterpret_cast<float*>(w + q.d);
+    p.e = reinterpret_cast<float*>(w + q.e);
+    p.x[0] = w + q.x0;
+    p.x[1] = w + q.x1;
+    p.rest = w + q.rest;
+    p.sa = w + q.sa;
+    p.sb = w + q.sb;
+    p.part = reinterpret_cast<float*>(w + q.part);
+    p.out = static_cast<uint8_t*>(out->data);
+    p.out_pitch = out->stride * 2;
+    p.out_batch = out->batch_stride * 2;
+    // the grid may be a second ahead of a CTA, and as much longer as a product takes at a twentieth of the tensor cores' rate
+    p.limit_ns = kWaitNs + uint64_t(2.0 * double(batch) * double(q.m) * double(q.m) * double(q.n) * 1e-5);
+    p.batch = int32_t(batch);
+    p.m = int32_t(q.m);
+    p.n = int32_t(q.n);
+    p.bm = int32_t(q.bm);
+    p.bn = int32_t(q.bn);
+    p.steps = steps;
+    for (int k = 0; k < 3; ++k) p.splits[k] = int32_t(q.splits[k]);
+    p.turned = q.turned;
+    p.wide = rows_wide(p.out, rows > 1 ? p.out_pitch : 0, batch > 1 ? p.out_batch : 0);
+    p.stall = ops_stall();
+    err = q.pair ? launch_products<true>(device, p, q, s) : launch_products<false>(device, p, q, s);
+    return ops_launched(call, err);
+}

@@ -18,6 +18,9 @@ embed and norm refuse inputs that require a gradient while grad mode is on.
 Tensors are rows of their last dimension: [tokens, dim] with any row stride
 (an expanded row, stride 0, may be an input) and bfloat16 or float32 elements.
 """
+import functools
+import struct
+
 import torch
 
 from . import _abi
@@ -32,7 +35,8 @@ except ImportError as e:
 
 _ops.set_errors(_abi.LCError, torch.OutOfMemoryError)
 
-__all__ = ["Act", "embed", "embed_grad", "norm", "norm_grad", "act_save", "act_load", "weight_grad"]
+__all__ = ["Act", "embed", "embed_grad", "norm", "norm_grad", "act_save", "act_load", "weight_grad",
+           "orthogonalize"]
 
 _CODE = {torch.bfloat16: LC_BF16, torch.float32: LC_F32}
 _KIND = {"layer": LC_NORM_LAYER, "rms": LC_NORM_RMS}
@@ -153,3 +157,26 @@ def weight_grad(dy, act, grad=None, dtype=torch.float32, accumulate=False):
     """dy^T x for a linear layer's weight [rows of dy, act.dim], with the
     layer's input read from its checkpoint; accumulate adds to `grad`."""
     return _ops.weight_grad(dy, act.q, act.e, act.dim, grad, _dtype(dtype), accumulate)
+
+
+@functools.lru_cache(maxsize=64)
+def _packed(steps, coefficients):
+    """The coefficients of every step as the library takes them: three doubles each."""
+    if not 1 <= steps <= 16:
+        raise ValueError("1 to 16 steps, not %d" % steps)
+    every = coefficients if isinstance(coefficients[0], tuple) else (coefficients,) * steps
+    if len(every) != steps or any(len(c) != 3 for c in every):
+        raise ValueError("three coefficients for every step, or for each of %d" % steps)
+    return struct.pack("%dd" % (3 * steps), *(x for c in every for x in c))
+
+
+def orthogonalize(update, momentum=None, beta=0.95, nesterov=True, steps=5, coefficients=(3.4445, -4.7750, 2.0315),
+                  eps=1e-7, out=None):
+    """The update of a weight matrix, [rows, cols], or of a batch of them, [batch, rows, cols], made nearly orthogonal:
+    X = U / (|U| + eps), then `steps` times A = X X^T, X = a X + (b A + c A^2) X, in bfloat16.  coefficients: (a, b, c),
+    or a sequence of one triple a step.  U is the update, or with `momentum` (float32, written) what comes of it:
+    momentum += (1 - beta) (update - momentum), and U = update + beta (momentum - update), without nesterov the
+    momentum itself."""
+    if not isinstance(coefficients, tuple) or not all(isinstance(c, (int, float, tuple)) for c in coefficients):
+        coefficients = tuple(tuple(c) if hasattr(c, "__len__") else c for c in coefficients)
+    return _ops.orthogonalize(update, momentum, beta, nesterov, _packed(steps, coefficients), eps, out)
