@@ -661,8 +661,8 @@ lc_status lc_measure_noalloc_debug(int device, void* cuda_stream, const lc_segme
 /* Test switch of those waits, for the calls that the calling host thread makes
  * from here on: 0, or LC_DEBUG_OPS_STALL, with which the first copy into
  * every ring of the norms' rows (forward and backward), and into the ring of
- * the second CTA of every pair in the weight gradient's product, announces 16
- * bytes that never come.
+ * the last CTA of every tile of the weight gradient's and of
+ * lc_orthogonalize's products, announces 16 bytes that never come.
  * Errors: INVALID_ARG (other flags). */
 #define LC_DEBUG_OPS_STALL 4
 lc_status lc_ops_debug(int32_t debug_flags);
@@ -751,6 +751,30 @@ lc_status lc_norm_grad(int device, void* cuda_stream, int32_t kind, const lc_row
                        const float* mean, const float* rstd, const lc_rows* dx, void* dweight, void* dbias,
                        int32_t g_dtype, int32_t accumulate, void* workspace, uint64_t workspace_bytes);
 uint64_t lc_norm_grad_workspace(int64_t ntok, int64_t dim);
+
+/* The root-mean-square norm of a residual sum: s = x + residual, rstd = 1 /
+ * sqrt(mean of s^2 + eps), y = s * rstd * weight, dim <= LC_NORM_MAX_DIM.  sum
+ * receives s (it may be the residual itself: the same address, stride and
+ * type), y (nullable) the norm, rstd ntok fp32.  keep and y8 (nullable): s and y
+ * are also kept in 8 bits, as by lc_act_save; without y, y8 is needed.  Each output is
+ * rounded once, from fp32: y is the norm of s as it was before its rounding.
+ * x and y have one type, residual and sum one: the same, or bf16 and fp32. */
+lc_status lc_add_norm(int device, void* cuda_stream, const lc_rows* x, const lc_rows* residual, int64_t ntok,
+                      int64_t dim, const void* weight, int32_t w_dtype, double eps, const lc_rows* sum,
+                      const lc_rows* y, float* rstd, const lc_act* keep, const lc_act* y8);
+
+/* Gradients of lc_add_norm from dy (of y), dsum (of the sum, from what reads it
+ * later on), the sum (or its checkpoint `kept`; exactly one of them) and rstd:
+ * with h = sum * rstd and a = dy * weight,
+ *   dx = dsum + rstd * (a - h * mean(a * h)),  dweight = sum over t of dy * h.
+ * dx is the gradient of x and of the residual alike; it has dsum's type and may
+ * be dsum itself (the same address and stride).  dweight: dim elements of
+ * g_dtype, added to with accumulate != 0.  The workspace is
+ * lc_norm_grad_workspace's. */
+lc_status lc_add_norm_grad(int device, void* cuda_stream, const lc_rows* dy, const lc_rows* dsum, const lc_rows* sum,
+                           const lc_act* kept, int64_t ntok, int64_t dim, const void* weight, int32_t w_dtype,
+                           const float* rstd, const lc_rows* dx, void* dweight, int32_t g_dtype, int32_t accumulate,
+                           void* workspace, uint64_t workspace_bytes);
 
 /* The gradient of a linear layer's weight (y = x W^T) with the layer's input
  * kept in 8 bits: dw[n][k] = sum over t of dy[t][n] * x[t][k], `rows` by dim,

@@ -173,6 +173,11 @@ SIGNATURES = {
                                C.c_int64, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, P(lc_rows),
                                C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_uint64]),
     "lc_norm_grad_workspace": (C.c_uint64, [C.c_int64, C.c_int64]),
+    "lc_add_norm": (C.c_int, [C.c_int, C.c_void_p, P(lc_rows), P(lc_rows), C.c_int64, C.c_int64, C.c_void_p, C.c_int32,
+                              C.c_double, P(lc_rows), P(lc_rows), C.c_void_p, P(lc_act), P(lc_act)]),
+    "lc_add_norm_grad": (C.c_int, [C.c_int, C.c_void_p, P(lc_rows), P(lc_rows), P(lc_rows), P(lc_act), C.c_int64,
+                                   C.c_int64, C.c_void_p, C.c_int32, C.c_void_p, P(lc_rows), C.c_void_p, C.c_int32,
+                                   C.c_int32, C.c_void_p, C.c_uint64]),
     "lc_weight_grad": (C.c_int, [C.c_int, C.c_void_p, P(lc_rows), P(lc_act), C.c_int64, C.c_int64, C.c_int64,
                                  P(lc_rows), C.c_int32, C.c_void_p, C.c_uint64]),
     "lc_weight_grad_workspace_of": (C.c_uint64, [P(lc_rows), C.c_int64, C.c_int64, C.c_int64]),

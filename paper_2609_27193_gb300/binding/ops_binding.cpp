@@ -367,6 +367,86 @@ PyObject* norm_grad(PyObject* const* args, Py_ssize_t nargs) {
     return tuple(dx, dweight, dbias);
 }
 
+PyObject* add_norm(PyObject* const* args, Py_ssize_t nargs) {
+    Args a(args, nargs, 11);
+    const at::Tensor x = a.tensor(), residual = a.tensor(), weight = a.tensor();
+    const double eps = a.number();
+    at::Tensor out = a.tensor();
+    const bool want = a.truth();
+    at::Tensor sum = a.tensor();
+    const at::Tensor q = a.tensor(), e = a.tensor(), yq = a.tensor(), ye = a.tensor();
+    const int index = cuda_index(x);
+    cuda_index(residual);
+    cuda_index(weight);
+    for (const at::Tensor* t : {&residual, &weight, static_cast<const at::Tensor*>(&out), static_cast<const at::Tensor*>(&sum), &q, &e, &yq, &ye})
+        same_device(index, *t);
+    unrecorded("add_norm", {&x, &residual, &weight, &out, &sum});
+    const lc_rows rx = rows_of(x, "x"), rr = rows_of(residual, "residual");
+    const int64_t n = x.size(0), dim = x.size(1);
+    shaped(residual, n, dim, "residual");
+    const void* w = param_of(weight, dim, "weight");
+    if (sum.defined()) shaped(sum, n, dim, "sum");
+    else sum = make({n, dim}, residual.scalar_type(), x);
+    const lc_rows rs = rows_of(sum, "sum");
+    lc_rows ro{};
+    if (out.defined()) shaped(out, n, dim, "out");
+    else if (want) out = make({n, dim}, x.scalar_type(), x);
+    if (out.defined()) ro = rows_of(out, "out");
+    const at::Tensor rstd = make({n}, at::kFloat, x);
+    lc_act keep{}, y8{};
+    if (q.defined()) keep = act_of(q, e, n, dim);
+    if (yq.defined()) y8 = act_of(yq, ye, n, dim);
+    check(lc_add_norm(index, stream_of(index), &rx, &rr, n, dim, w, code_of(weight, "weight"), eps, &rs, out.defined() ? &ro : nullptr,
+                      stat_of(rstd, n), q.defined() ? &keep : nullptr, yq.defined() ? &y8 : nullptr));
+    for (const at::Tensor* t : {static_cast<const at::Tensor*>(&sum), static_cast<const at::Tensor*>(&out), &q, &e, &yq, &ye}) written(*t);
+    return tuple(sum, out, rstd);
+}
+
+PyObject* add_norm_grad(PyObject* const* args, Py_ssize_t nargs) {
+    Args a(args, nargs, 12);
+    const at::Tensor dy = a.tensor(), dsum = a.tensor(), total = a.tensor(), q = a.tensor(), e = a.tensor();
+    const int64_t kept_dim = a.integer();
+    const at::Tensor weight = a.tensor(), rstd = a.tensor();
+    at::Tensor dx = a.tensor(), dweight = a.tensor();
+    const int64_t dtype = a.integer();
+    const bool accumulate = a.truth();
+    const int index = cuda_index(dy);
+    cuda_index(dsum);
+    cuda_index(weight);
+    cuda_index(rstd);
+    for (const at::Tensor* t : {&dsum, &total, &q, &e, &weight, &rstd, static_cast<const at::Tensor*>(&dx), static_cast<const at::Tensor*>(&dweight)})
+        same_device(index, *t);
+    const lc_rows rd = rows_of(dy, "dy"), rr = rows_of(dsum, "dsum");
+    const int64_t n = dy.size(0), dim = dy.size(1);
+    shaped(dsum, n, dim, "dsum");
+    const void* w = param_of(weight, dim, "weight");
+    lc_rows rs{};
+    lc_act kept{};
+    if (q.defined()) {
+        if (kept_dim != dim) throw ValueError("the sum must have dy's shape");
+        kept = act_of(q, e, n, dim);
+    } else {
+        cuda_index(total);
+        rs = rows_of(total, "the sum");
+        shaped(total, n, dim, "the sum");
+    }
+    const float* r = stat_of(rstd, n);
+    if (accumulate && !dweight.defined()) throw ValueError("accumulate needs the gradient to add to");
+    if (dx.defined()) shaped(dx, n, dim, "dx");
+    else dx = make({n, dim}, dsum.scalar_type(), dy);
+    if (!dweight.defined()) dweight = make({dim}, type_of(dtype), dy);
+    const lc_rows rdx = rows_of(dx, "dx");
+    void* pw = param_of(dweight, dim, "dweight");
+    void* stream = stream_of(index);
+    const uint64_t need = lc_norm_grad_workspace(n, dim);
+    const Scratch scratch(dy, index, stream, need);
+    check(lc_add_norm_grad(index, stream, &rd, &rr, q.defined() ? nullptr : &rs, q.defined() ? &kept : nullptr, n, dim, w,
+                           code_of(weight, "weight"), r, &rdx, pw, code_of(dweight, "dweight"), accumulate, scratch.p, need));
+    written(dx);
+    written(dweight);
+    return tuple(dx, dweight);
+}
+
 PyObject* weight_grad(PyObject* const* args, Py_ssize_t nargs) {
     Args a(args, nargs, 7);
     const at::Tensor dy = a.tensor(), q = a.tensor(), e = a.tensor();
@@ -485,8 +565,8 @@ PyObject* guarded(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
 
 #define LC_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(guarded<name>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {LC_METHOD(embed),    LC_METHOD(embed_grad), LC_METHOD(act_save),    LC_METHOD(act_load), LC_METHOD(new_act),
-                         LC_METHOD(norm),     LC_METHOD(norm_grad),  LC_METHOD(weight_grad), LC_METHOD(orthogonalize),
-                         LC_METHOD(set_errors),
+                         LC_METHOD(norm),     LC_METHOD(norm_grad),  LC_METHOD(weight_grad), LC_METHOD(add_norm),
+                         LC_METHOD(add_norm_grad), LC_METHOD(orthogonalize), LC_METHOD(set_errors),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_ops", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1,5 +1,5 @@
 // lc_ops.cuh -- what the operators of a training step (lc_embed.cu, lc_act.cu,
-// lc_norm.cu, lc_wgrad.cu) share: checks of their arguments on the host, and
+// lc_norm.cu, lc_addnorm.cu, lc_wgrad.cu, lc_orth.cu) share: checks of their arguments on the host, and
 // element and vector access in fp32 whatever the arrays' type on the device.
 #pragma once
 
@@ -62,6 +62,11 @@ int ops_stall();
 
 // Keeps rows in 8 bits (the norm uses it where it cannot do so on its own pass).
 cudaError_t act_save_rows(const lc_rows* x, const lc_act* a, int64_t ntok, int64_t dim, cudaStream_t s);
+
+// Adds up the rows of sums that the CTAs of a norm's backward left for weight and bias
+// ([rows][2][dim], at most kGradCtas rows; dw and db may be null).
+constexpr int kGradCtas = 608;
+cudaError_t norm_fold(const float* part, int rows, int dim, void* dw, void* db, bool bf16, bool accumulate, cudaStream_t s);
 
 inline Span2 span_of(const char* name, const lc_rows* r, int64_t rows, int64_t dim, bool out) {
     const int e = elem_size(r->dtype);

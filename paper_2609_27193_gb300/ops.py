@@ -1,9 +1,10 @@
 """Operators of a training step around the fused optimizer: the embedding
-lookup, layer and root-mean-square norms, activations kept in 8 bits for the
-backward pass, and the gradients of them that adamw_step_measure reads.
+lookup, layer and root-mean-square norms, the norm of a residual sum, activations
+kept in 8 bits for the backward pass, the gradients of them that
+adamw_step_measure reads, and updates of matrices made orthogonal.
 
-Thin binding of the lc_embed / lc_norm / lc_act / lc_weight_grad calls of
-include/layercheck.h over torch CUDA tensors; what is done for every call is in
+Thin binding of the lc_embed / lc_norm / lc_add_norm / lc_act / lc_weight_grad /
+lc_orthogonalize calls of include/layercheck.h over torch CUDA tensors; what is done for every call is in
 C++ (binding/ops_binding.cpp).  Work is enqueued on torch's current stream,
 outputs that are not passed in come from torch's allocator on that stream, and
 scratch up to 32 MB is one tensor a device and stream that grows to the largest
@@ -13,10 +14,12 @@ calls and one another.  There is no CPU fallback.
 
 Autograd records none of this: the gradients are calls too, for training loops
 that write their backward pass themselves and for torch.autograd.Function.
-embed and norm refuse inputs that require a gradient while grad mode is on.
+embed, norm, add_norm and orthogonalize refuse inputs that require a gradient while
+grad mode is on.
 
 Tensors are rows of their last dimension: [tokens, dim] with any row stride
-(an expanded row, stride 0, may be an input) and bfloat16 or float32 elements.
+(an expanded row, stride 0, may be an input) and bfloat16 or float32 elements;
+updates of matrices are [rows, cols] or [batch, rows, cols].
 """
 import functools
 import struct
@@ -35,8 +38,8 @@ except ImportError as e:
 
 _ops.set_errors(_abi.LCError, torch.OutOfMemoryError)
 
-__all__ = ["Act", "embed", "embed_grad", "norm", "norm_grad", "act_save", "act_load", "weight_grad",
-           "orthogonalize"]
+__all__ = ["Act", "embed", "embed_grad", "norm", "norm_grad", "act_save", "act_load", "add_norm", "add_norm_grad",
+           "weight_grad", "orthogonalize"]
 
 _CODE = {torch.bfloat16: LC_BF16, torch.float32: LC_F32}
 _KIND = {"layer": LC_NORM_LAYER, "rms": LC_NORM_RMS}
@@ -151,6 +154,32 @@ def norm_grad(dy, x, weight, mean, rstd, bias=False, dx=None, dweight=None, dbia
         return _ops.norm_grad(dy, None, x.q, x.e, x.dim, weight, mean, rstd, bias, dx, dweight, dbias, _dtype(dtype),
                               accumulate)
     return _ops.norm_grad(dy, x, None, None, 0, weight, mean, rstd, bias, dx, dweight, dbias, _dtype(dtype), accumulate)
+
+
+def add_norm(x, residual, weight, eps=1e-5, out=None, sum=None, keep=None, out8=None):
+    """The residual sum x + residual and its root-mean-square norm y, in one pass.  Returns (sum, y, rstd), and after
+    them the checkpoints made here: keep=True keeps the sum in 8 bits, out8=True keeps y; either may be an Act that
+    is written.  sum: where the sum goes, the residual itself if wanted.  out=False: y is wanted in 8 bits only (and
+    returned as None).  The sum has the residual's type and y has x's: both the same, or a float32 residual around
+    bfloat16 branches."""
+    kept = None if keep is None or keep is False else _for(keep, x)
+    y8 = None if out8 is None or out8 is False else _for(out8, x)
+    result = _ops.add_norm(x, residual, weight, eps, None if out is False else out, out is not False, sum,
+                           *((None, None) if kept is None else (kept.q, kept.e)),
+                           *((None, None) if y8 is None else (y8.q, y8.e)))
+    if keep is True:
+        result = (*result, kept)
+    return (*result, y8) if out8 is True else result
+
+
+def add_norm_grad(dy, dsum, total, weight, rstd, dx=None, dweight=None, dtype=torch.float32, accumulate=False):
+    """Gradients of add_norm: (dx, dweight).  dx belongs to x and to the residual alike: what comes through the norm
+    from dy, and dsum, the sum's own gradient; dx may be dsum itself.  total: the sum, or its checkpoint (Act).
+    dweight is of `dtype` where it is made here; accumulate adds to the one given."""
+    if isinstance(total, Act):
+        return _ops.add_norm_grad(dy, dsum, None, total.q, total.e, total.dim, weight, rstd, dx, dweight, _dtype(dtype),
+                                  accumulate)
+    return _ops.add_norm_grad(dy, dsum, total, None, None, 0, weight, rstd, dx, dweight, _dtype(dtype), accumulate)
 
 
 def weight_grad(dy, act, grad=None, dtype=torch.float32, accumulate=False):
