@@ -10,9 +10,8 @@
 // in the products' layout, one does all products.  The products are on the 5th-generation
 // tensor cores, fp16 operands and fp32 sums:
 //
-//   * The state X is kept in 32 bits, as an fp16 number and the fp16 rest of it times 2^11.  The
-//     first part is the operand, both are read where X itself is added.  (With one fp16 number
-//     as state, a matrix of 8 directions over noise of 1e-4 came out 4e-2 off, so 6e-4; bf16 operands 3e-1.)
+//   * The state X is kept in fp32 beside its operand.  (With the fp16 number as state a matrix
+//     of 8 directions over noise of 1e-4 came out 4e-2 off, so 6e-4; with bf16 3e-1.)
 //   * The diagonals of A and of B = b A + c A^2 are far larger than the rest and stay in fp32, beside
 //     the operands: A^2 = A0^2 + (d_i + d_j) A0 + d^2, and X's row i is multiplied by a + e_i.  That
 //     halves the error (512 x 1024: 1.7e-3 to 5e-4 off before the output's rounding of 1.7e-3).
@@ -50,7 +49,8 @@ constexpr int kStageBytes = 2 * kOperand;
 constexpr int kStages = 6;
 constexpr int kSumWarp = 4, kSumWarps = 8;  // the first (a multiple of 4) of the warps that read the accumulators, and their number
 constexpr int kThreads = (kSumWarp + kSumWarps) * 32;
-constexpr int kSmem = kStages * kStageBytes + 1024;
+// the ring, half a box for each of the warps that write operands, and room to align them to 1024 bytes
+constexpr int kSmem = kStages * kStageBytes + kSumWarps * kBoxBytes / 2 + 1024;
 constexpr int kMaxSteps = 16;
 constexpr int kNormCtas = 512;              // most partial sums of squares of a matrix
 
@@ -66,12 +66,13 @@ struct OrthStep {
 };
 struct OrthParams {
     uint32_t* count;         // arrivals at the grid's barriers
-    uint32_t* arrived;       // [batch * tiles][CTAs of a tile]: splits of a product that are done
+    uint32_t* arrived;       // [A, A^2][tiles][CTAs of a tile]: splits of a product that are done
     float* d;                // [batch][mp]: diagonal of A
     float* e;                // [batch][mp]: diagonal of B
     uint8_t* x[2];           // operand of X, of even and odd steps
-    uint8_t* rest;           // what it lacks of X, times 2^11
-    uint8_t* sa;             // A without its diagonal
+    uint8_t* xf;             // X in fp32, times x_scale
+    uint8_t* af;             // A without its diagonal, in fp32
+    uint8_t* sa;             // its operand
     uint8_t* sb;             // B without it
     float* part;             // splits' sums
     uint8_t* out;
@@ -80,6 +81,7 @@ struct OrthParams {
     float x_scale, a_scale;
     int32_t batch, m, n;     // of X as it is worked on (m <= n)
     int32_t bm, bn;          // boxes of m and n
+    int32_t tiles;           // of A, of all matrices
     int32_t steps, splits[3];  // of the reductions of A, A^2 and B X (the last always 1)
     int32_t turned;          // out is X^T
     int32_t wide;            // out takes 16-byte stores
@@ -141,25 +143,13 @@ __device__ __forceinline__ void tmem_ld32(uint32_t addr, float (&f)[32]) {
     for (int i = 0; i < 32; ++i) f[i] = __uint_as_float(r[i]);
 }
 
-// What other CTAs wrote in this launch is read past L1.
-__device__ __forceinline__ uint4 ld_l2(const void* p) { return __ldcg(static_cast<const uint4*>(p)); }
-
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
     const __half2 h = __floats2half2_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&h);
 }
-__device__ __forceinline__ float2 unpack_f16(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
 
 // 16-byte piece `p` (of 8) of row r in a box.
 __device__ __forceinline__ uint32_t piece_at(int r, int p) { return uint32_t(r) * 128 + uint32_t((p ^ (r & 7)) * 16); }
-
-// X's value as its operand and the rest: hi + lo * 2^-11.
-constexpr float kRest = 2048.0f;
-__device__ __forceinline__ void split_pair(float x, float y, uint32_t& hi, uint32_t& lo) {
-    hi = pack_f16(x, y);
-    const float2 h = unpack_f16(hi);
-    lo = pack_f16((x - h.x) * kRest, (y - h.y) * kRest);
-}
 
 // One piece of a product: a tile, or a split of its reduction.
 struct Item {
@@ -252,32 +242,143 @@ __device__ __forceinline__ bool sum_warps_agree(bool ok) {
     return r != 0;
 }
 
-// Where a row of the output lies, and element c of it.
-__device__ __forceinline__ __nv_bfloat16* out_at(const OrthParams& p, int mat, int r, int c) {
-    uint8_t* base = p.out + int64_t(mat) * p.out_batch;
-    return p.turned ? reinterpret_cast<__nv_bfloat16*>(base + int64_t(c) * p.out_pitch) + r
-                    : reinterpret_cast<__nv_bfloat16*>(base + int64_t(r) * p.out_pitch) + c;
+__device__ __forceinline__ void sts128(uint32_t addr, const uint4& v) {
+    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
-// 32 columns from c of row r.
-__device__ __forceinline__ void store_out(const OrthParams& p, int mat, int r, int c, const float (&f)[32]) {
-    if (r >= p.m) return;
-    __nv_bfloat16* o = out_at(p, mat, r, c);
-    if (p.turned) {
-        const int64_t step = p.out_pitch / 2;
+__device__ __forceinline__ uint4 lds128(uint32_t addr) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint32_t lds16(uint32_t addr) {
+    uint16_t v;
+    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(addr) : "memory");
+    return v;
+}
+
+// A warp's 32 rows of 64 columns of the output, from its 4 KB of staging in shared memory (rows of 128
+// bytes, swizzled).  r0, c0: the first row and column.
+__device__ __forceinline__ void store_rows(const OrthParams& p, int mat, int r0, int c0, uint32_t stage, int lane) {
+    uint8_t* base = p.out + int64_t(mat) * p.out_batch;
+    if (p.wide && c0 + kBox <= p.n) {
+        const int piece = lane % 8;
 #pragma unroll
-        for (int k = 0; k < 32; ++k)
-            if (c + k < p.n) o[k * step] = __float2bfloat16_rn(f[k]);
-    } else if (p.wide && c + 32 <= p.n) {
-#pragma unroll
-        for (int k = 0; k < 32; k += 8)
-            *reinterpret_cast<uint4*>(o + k) = make_uint4(pack_bf16(f[k], f[k + 1]), pack_bf16(f[k + 2], f[k + 3]),
-                                                          pack_bf16(f[k + 4], f[k + 5]), pack_bf16(f[k + 6], f[k + 7]));
-    } else {
-#pragma unroll
-        for (int k = 0; k < 32; ++k)
-            if (c + k < p.n) o[k] = __float2bfloat16_rn(f[k]);
+        for (int k = 0; k < 8; ++k) {
+            const int r = k * 4 + lane / 8;
+            const uint4 v = lds128(stage + piece_at(r, piece));
+            if (r0 + r < p.m) *reinterpret_cast<uint4*>(base + int64_t(r0 + r) * p.out_pitch + c0 * 2 + piece * 16) = v;
+        }
+        return;
+    }
+#pragma unroll 4
+    for (int k = 0; k < 64; ++k) {
+        const int r = k / 2, c = k % 2 * 32 + lane;
+        const uint32_t v = lds16(stage + piece_at(r, c / 8) + c % 8 * 2);
+        if (r0 + r < p.m && c0 + c < p.n) *reinterpret_cast<uint16_t*>(base + int64_t(r0 + r) * p.out_pitch + (c0 + c) * 2) = uint16_t(v);
     }
 }
+// A row's columns c .. c + 31 of an output that is X^T: the lanes' rows are neighbours there.
+__device__ __forceinline__ void store_turned(const OrthParams& p, int mat, int r, int c, const float (&f)[32]) {
+    if (r >= p.m) return;
+    uint8_t* o = p.out + int64_t(mat) * p.out_batch + int64_t(c) * p.out_pitch + int64_t(r) * 2;
+#pragma unroll
+    for (int k = 0; k < 32; ++k)
+        if (c + k < p.n) *reinterpret_cast<__nv_bfloat16*>(o + k * p.out_pitch) = __float2bfloat16_rn(f[k]);
+}
+
+// Where fp32 matrices keep row r: rows in groups of 32, four columns of a group's rows after another, so that
+// a warp with a row a lane reads and writes 512 bytes at once.
+__device__ __forceinline__ int64_t row_at(int64_t mat, int rows, int cols, int r) {
+    return ((mat * (rows / 32) + r / 32) * (cols / 4)) * 512 + r % 32 * 16;
+}
+__device__ __forceinline__ int quad_at(int c) { return c / 4 * 512; }
+
+// A row of a product's tile on its way to the next operand, 8 or 32 columns at a time.
+struct Finish {
+    const OrthParams& p;
+    const OrthStep& co;
+    const int phase, gr;
+    const bool final;
+    const int mat;
+    uint8_t* state;          // the row of A or of X in fp32
+    uint8_t* out;            // the next operand: the row of boxes
+    int64_t diag;            // of the matrix's first diagonal element
+    float scale, dr;
+    float4 next[8], now[8];  // what is read beside the accumulator: A or X
+    float d_next, d_now;     // A's diagonal, of a column a lane
+
+    __device__ __forceinline__ Finish(const OrthParams& q, int ph, int step, bool fin, int m, int r)
+        : p(q), co(q.step[step]), phase(ph), gr(r), final(fin), mat(m) {
+        const int cols = (phase == 2 ? p.bn : p.bm) * kBox;
+        state = (phase == 2 ? p.xf : p.af) + row_at(mat, p.bm * kBox, cols, gr);
+        out = (phase == 0 ? p.sa : phase == 1 ? p.sb : p.x[step & 1 ^ 1]) + (int64_t(mat) * p.bm + gr / kBox) * (cols / kBox) * kBoxBytes;
+        diag = int64_t(mat) * p.bm * kBox;
+        if (phase == 0) {
+            scale = 1.0f / (p.x_scale * p.x_scale);
+            dr = 0.0f;
+        } else if (phase == 1) {
+            scale = 1.0f / (p.a_scale * p.a_scale);
+            dr = __ldcg(p.d + diag + gr);
+        } else {
+            scale = 1.0f / co.scale;
+            dr = co.a + __ldcg(p.e + diag + gr);
+        }
+    }
+    template <int N>
+    __device__ __forceinline__ void ask(int col, int lane) {
+        if (phase == 0) return;
+#pragma unroll
+        for (int k = 0; k < 2 * N; ++k) next[k] = __ldcg(reinterpret_cast<const float4*>(state + quad_at(col + 4 * k)));
+        if (phase == 1) d_next = __ldcg(p.d + diag + col + lane % (8 * N));
+    }
+    template <int N>
+    __device__ __forceinline__ void take() {
+#pragma unroll
+        for (int k = 0; k < 2 * N; ++k) now[k] = next[k];
+        d_now = d_next;
+    }
+    // Columns col .. col + 7 (all lanes): f from the accumulator, and what becomes of it as the next operand; k: which of the
+    // eights asked for.
+    __device__ __forceinline__ uint4 piece(int col, int k, float* f) {
+        const float old[8] = {now[2 * k].x, now[2 * k].y, now[2 * k].z, now[2 * k].w, now[2 * k + 1].x, now[2 * k + 1].y, now[2 * k + 1].z, now[2 * k + 1].w};
+        const bool diagonal = col <= gr && gr < col + 8;
+        float v[8], sc;
+        if (phase == 0) {
+#pragma unroll
+            for (int m = 0; m < 8; ++m) {
+                f[m] *= scale;
+                if (diagonal && col + m == gr) {
+                    __stcg(p.d + diag + gr, f[m]);
+                    f[m] = 0.0f;
+                }
+                v[m] = f[m];
+            }
+            sc = p.a_scale;
+        } else if (phase == 1) {
+#pragma unroll
+            for (int m = 0; m < 8; ++m) {
+                const float dj = __shfl_sync(0xffffffffu, d_now, 8 * k + m);
+                v[m] = co.b * old[m] + co.c * (f[m] * scale + (dr + dj) * old[m]);
+                if (diagonal && col + m == gr) {
+                    // (A is zero there)
+                    __stcg(p.e + diag + gr, co.b * dr + co.c * (f[m] * scale + dr * dr));
+                    v[m] = 0.0f;
+                }
+            }
+            sc = co.scale;
+        } else {
+#pragma unroll
+            for (int m = 0; m < 8; ++m) f[m] = v[m] = fmaf(dr, old[m], f[m] * scale);
+            sc = 1.0f;
+        }
+        if (phase == 0 || (phase == 2 && !final)) {
+            __stcg(reinterpret_cast<float4*>(state + quad_at(col)), make_float4(v[0], v[1], v[2], v[3]));
+            __stcg(reinterpret_cast<float4*>(state + quad_at(col + 4)), make_float4(v[4], v[5], v[6], v[7]));
+        }
+        return make_uint4(pack_f16(v[0] * sc, v[1] * sc), pack_f16(v[2] * sc, v[3] * sc), pack_f16(v[4] * sc, v[5] * sc),
+                          pack_f16(v[6] * sc, v[7] * sc));
+    }
+};
 
 template <bool PAIR>
 __global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_constant__ OrthParams p) {
@@ -289,7 +390,7 @@ __global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_
     // have landed (the first CTA's).  summed: an accumulator is complete; taken: it has been read (the first CTA's).
     // go: the grid has come to the next product.
     __shared__ __align__(8) uint64_t bars[3 * kStages + 5];
-    __shared__ uint32_t tmem_base, last;
+    __shared__ uint32_t tmem_base;
     __shared__ volatile uint32_t failed;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = PAIR ? int(blockIdx.x & 1) : 0, unit = int(blockIdx.x) / kCtas, units = int(gridDim.x) / kCtas;
@@ -429,6 +530,7 @@ __global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_
         const int row = quad * 32 + lane;                 // of this CTA's 128
         const uint32_t first_taken = PAIR ? cluster_addr(taken, 0) : taken;
         const uint32_t from = tmem + (uint32_t(quad * 32) << 16) + half * kCols;
+        const uint32_t stage = ring + kStages * kStageBytes + (warp - kSumWarp) * (kBoxBytes / 2);
         Ring<2> acc;
         bool ok = true;
         for (int ph = 0; ph < phases; ++ph) {
@@ -436,146 +538,118 @@ __global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_
             const bool final = ph == phases - 1;
             ok = sum_warps_agree(wait_long(go, ph & 1, p.limit_ns));
             if (!ok) break;
-            const OrthStep co = p.step[step];
             const int splits = p.splits[phase], items = items_of<PAIR>(p, phase);
             for (int i = unit; i < items; i += units, acc.next()) {
                 const Item w = item_of<PAIR>(p, phase, i);
-                ok = sum_warps_agree(mbar_wait_warp(summed + 8 * acc.at, acc.round));
-                if (!ok) break;
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const int gr = w.i * T + rank * kCtaRows + row, gc = w.j * T + half * kCols;
-                bool mine = true;
-                const float* parts = nullptr;
-                if (splits > 1) {
-                    // the split that comes last adds them all up, in their order
-                    constexpr int kPart = kCtaRows * T;
-                    float* mypart = p.part + (int64_t(w.tile) * kCtas + rank) * splits * kPart + half * kCols * kCtaRows + row;
-                    parts = mypart;
-                    mypart += int64_t(w.split) * kPart;
+                Finish fin(p, phase, step, final, w.mat, w.i * T + rank * kCtaRows + row);
+                const int c0 = w.j * T + half * kCols;
+                if (splits == 1) {
+                    // what is read beside the accumulator is on its way before that is complete, and then 32 columns ahead
+                    fin.ask<4>(c0, lane);
+                    ok = sum_warps_agree(mbar_wait_warp(summed + 8 * acc.at, acc.round));
+                    if (!ok) break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll 1
                     for (int c = 0; c < kCols; c += 32) {
                         float f[32];
                         tmem_ld32(from + acc.at * T + c, f);
-#pragma unroll
-                        for (int k = 0; k < 32; ++k) __stcg(mypart + (c + k) * kCtaRows, f[k]);
-                    }
-                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                    __syncwarp();
-                    if (lane == 0) arrive_at(first_taken + 8 * acc.at);
-                    __threadfence();
-                    asm volatile("bar.sync 1, %0;" ::"n"(kSumWarps * 32) : "memory");
-                    if (t == 0) {
-                        uint32_t* a = p.arrived + w.tile * kCtas + rank;
-                        const uint32_t n = atomicAdd(a, 1u);
-                        last = n == uint32_t(splits - 1);
-                        if (last) *a = 0;            // for the next product
-                        __threadfence();
-                    }
-                    asm volatile("bar.sync 1, %0;" ::"n"(kSumWarps * 32) : "memory");
-                    mine = last;
-                }
-                float scale, dr = 0.0f;
-                if (phase == 0) scale = 1.0f / (p.x_scale * p.x_scale);
-                else if (phase == 1) scale = 1.0f / (p.a_scale * p.a_scale), dr = __ldcg(p.d + int64_t(w.mat) * p.bm * kBox + gr);
-                else scale = 1.0f / co.scale, dr = co.a + __ldcg(p.e + int64_t(w.mat) * p.bm * kBox + gr);
-#pragma unroll 1
-                for (int c = 0; c < kCols && mine; c += 32) {
-                    float f[32];
-                    if (splits > 1) {
-#pragma unroll
-                        for (int k = 0; k < 32; ++k) f[k] = __ldcg(parts + (c + k) * kCtaRows);
-#pragma unroll 1
-                        for (int s = 1; s < splits; ++s)
-#pragma unroll
-                            for (int k = 0; k < 32; ++k) f[k] += __ldcg(parts + int64_t(s) * (kCtaRows * T) + (c + k) * kCtaRows);
-                    } else {
-                        tmem_ld32(from + acc.at * T + c, f);
-                    }
-                    const int col = gc + c, bc = col / kBox, br = gr / kBox, p0 = col % kBox / 8;
-                    if (phase == 0) {
-                        uint8_t* o = p.sa + w.mat * s_bytes + (int64_t(br) * p.bm + bc) * kBoxBytes;
-#pragma unroll
-                        for (int k = 0; k < 32; ++k) {
-                            f[k] *= scale;
-                            if (col + k == gr) {
-                                p.d[int64_t(w.mat) * p.bm * kBox + gr] = f[k];
-                                f[k] = 0.0f;
-                            }
-                            f[k] *= p.a_scale;
+                        if (c + 32 == kCols) {
+                            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                            __syncwarp();
+                            if (lane == 0) arrive_at(first_taken + 8 * acc.at);
                         }
-#pragma unroll
-                        for (int k = 0; k < 4; ++k)
-                            *reinterpret_cast<uint4*>(o + piece_at(gr % kBox, p0 + k)) =
-                                make_uint4(pack_f16(f[8 * k], f[8 * k + 1]), pack_f16(f[8 * k + 2], f[8 * k + 3]),
-                                           pack_f16(f[8 * k + 4], f[8 * k + 5]), pack_f16(f[8 * k + 6], f[8 * k + 7]));
-                    } else if (phase == 1) {
-                        const int64_t off = w.mat * s_bytes + (int64_t(br) * p.bm + bc) * kBoxBytes;
-                        const float* dc = p.d + int64_t(w.mat) * p.bm * kBox + col;
-                        const float a_back = 1.0f / p.a_scale;
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            const uint32_t at = piece_at(gr % kBox, p0 + k);
-                            const uint4 a = ld_l2(p.sa + off + at);
-                            const float4 d0 = __ldcg(reinterpret_cast<const float4*>(dc + 8 * k)), d1 = __ldcg(reinterpret_cast<const float4*>(dc + 8 * k + 4));
-                            const float dj[8] = {d0.x, d0.y, d0.z, d0.w, d1.x, d1.y, d1.z, d1.w};
-                            const uint32_t aw[4] = {a.x, a.y, a.z, a.w};
-                            float v[8];
-#pragma unroll
-                            for (int m = 0; m < 8; ++m) {
-                                const float2 a2 = unpack_f16(aw[m / 2]);
-                                const float a0 = (m & 1 ? a2.y : a2.x) * a_back;
-                                if (col + 8 * k + m == gr) {
-                                    // (A0 is zero there)
-                                    const float e = co.b * dr + co.c * (f[8 * k + m] * scale + dr * dr);
-                                    p.e[int64_t(w.mat) * p.bm * kBox + gr] = e;
-                                    v[m] = 0.0f;
-                                } else {
-                                    v[m] = (co.b * a0 + co.c * (f[8 * k + m] * scale + (dr + dj[m]) * a0)) * co.scale;
-                                }
-                            }
-                            *reinterpret_cast<uint4*>(p.sb + off + at) =
-                                make_uint4(pack_f16(v[0], v[1]), pack_f16(v[2], v[3]), pack_f16(v[4], v[5]), pack_f16(v[6], v[7]));
+                        fin.take<4>();
+                        if (c + 32 < kCols) fin.ask<4>(c0 + c + 32, lane);
+                        if (c % kBox == 0) {
+                            // the staging's last rows have been read
+                            if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                            __syncwarp();
                         }
-                    } else {
-                        const int64_t off = w.mat * x_bytes + (int64_t(br) * p.bn + bc) * kBoxBytes;
-                        const uint8_t* xi = p.x[step & 1] + off;
-                        uint8_t* xo = p.x[step & 1 ^ 1] + off;
+                        uint4 v[4];
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            const uint32_t at = piece_at(gr % kBox, p0 + k);
-                            const uint4 h = ld_l2(xi + at), l = ld_l2(p.rest + off + at);
-                            const uint32_t hw[4] = {h.x, h.y, h.z, h.w}, lw[4] = {l.x, l.y, l.z, l.w};
-                            uint32_t hn[4], ln[4];
-#pragma unroll
-                            for (int m = 0; m < 4; ++m) {
-                                const float2 hv = unpack_f16(hw[m]), lv = unpack_f16(lw[m]);
-                                float& v0 = f[8 * k + 2 * m];
-                                float& v1 = f[8 * k + 2 * m + 1];
-                                v0 = fmaf(dr, fmaf(lv.x, 1.0f / kRest, hv.x), v0 * scale);
-                                v1 = fmaf(dr, fmaf(lv.y, 1.0f / kRest, hv.y), v1 * scale);
-                                if (!final) split_pair(v0, v1, hn[m], ln[m]);
-                            }
-                            if (!final) {
-                                *reinterpret_cast<uint4*>(xo + at) = make_uint4(hn[0], hn[1], hn[2], hn[3]);
-                                *reinterpret_cast<uint4*>(p.rest + off + at) = make_uint4(ln[0], ln[1], ln[2], ln[3]);
-                            }
-                        }
+                        for (int k = 0; k < 4; ++k) v[k] = fin.piece(c0 + c + 8 * k, k, f + 8 * k);
                         if (final) {
                             const float back = 1.0f / p.x_scale;
 #pragma unroll
                             for (int k = 0; k < 32; ++k) f[k] *= back;
-                            store_out(p, w.mat, gr, col, f);
+                            if (p.turned) {
+                                store_turned(p, w.mat, fin.gr, c0 + c, f);
+                                continue;
+                            }
+#pragma unroll
+                            for (int k = 0; k < 4; ++k)
+                                v[k] = make_uint4(pack_bf16(f[8 * k], f[8 * k + 1]), pack_bf16(f[8 * k + 2], f[8 * k + 3]),
+                                                  pack_bf16(f[8 * k + 4], f[8 * k + 5]), pack_bf16(f[8 * k + 6], f[8 * k + 7]));
+                        }
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) sts128(stage + piece_at(lane, c % kBox / 8 + k), v[k]);
+                        if (c % kBox == 0) continue;
+                        // 32 rows of a box are one piece of memory
+                        const int col = c0 + c - 32;
+                        if (final) {
+                            __syncwarp();
+                            store_rows(p, w.mat, fin.gr - lane, col, stage, lane);
+                            __syncwarp();
+                        } else {
+                            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                            __syncwarp();
+                            if (lane == 0) {
+                                bulk_s2g(fin.out + int64_t(col / kBox) * kBoxBytes + quad % 2 * (kBoxBytes / 2), stage, kBoxBytes / 2);
+                                asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                            }
                         }
                     }
+                    continue;
                 }
-                if (splits == 1) {
-                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                    __syncwarp();
-                    if (lane == 0) arrive_at(first_taken + 8 * acc.at);
+                // every CTA with a split of the tile leaves its sums and takes a share of the columns of all of them,
+                // added in the splits' order (the items are no more than the CTAs, so all splits are on their way)
+                ok = sum_warps_agree(mbar_wait_warp(summed + 8 * acc.at, acc.round));
+                if (!ok) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                constexpr int kPart = kCtaRows * T;
+                float* parts = p.part + (int64_t(w.tile) * kCtas + rank) * splits * kPart + row;
+                float* mine = parts + int64_t(w.split) * kPart + half * kCols * kCtaRows;
+#pragma unroll 1
+                for (int c = 0; c < kCols; c += 32) {
+                    float f[32];
+                    tmem_ld32(from + acc.at * T + c, f);
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) __stcg(mine + (c + k) * kCtaRows, f[k]);
+                }
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) arrive_at(first_taken + 8 * acc.at);
+                __threadfence();
+                asm volatile("bar.sync 1, %0;" ::"n"(kSumWarps * 32) : "memory");
+                uint32_t* arrived = p.arrived + ((phase * p.tiles + w.tile) * kCtas + rank);
+                if (t == 0) asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(arrived) : "memory");
+                // (the counters only grow: this product's splits come on top of the earlier steps')
+                bool came = true;
+                if (lane == 0) came = grid_wait(arrived, uint32_t(splits) * uint32_t(step + 1), kWaitNs);
+                ok = sum_warps_agree(__all_sync(0xffffffffu, came));
+                if (!ok) break;
+#pragma unroll 1
+                for (int k = w.split * 2 + half; k < T / 8; k += splits * 2) {
+                    float f[8];
+                    const float* at = parts + k * 8 * kCtaRows;
+                    fin.ask<1>(w.j * T + k * 8, lane);
+#pragma unroll
+                    for (int m = 0; m < 8; ++m) f[m] = __ldcg(at + m * kCtaRows);
+#pragma unroll 1
+                    for (int s = 1; s < splits; ++s) {
+                        at += kPart;
+#pragma unroll
+                        for (int m = 0; m < 8; ++m) f[m] += __ldcg(at + m * kCtaRows);
+                    }
+                    fin.take<1>();
+                    const int col = w.j * T + k * 8;
+                    const uint4 v = fin.piece(col, 0, f);
+                    *reinterpret_cast<uint4*>(fin.out + int64_t(col / kBox) * kBoxBytes + piece_at(fin.gr % kBox, col % kBox / 8)) = v;
                 }
             }
             if (!ok) break;
             if (!final) {
+                if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
                 asm volatile("fence.proxy.async.global;" ::: "memory");
                 __threadfence();
                 asm volatile("bar.sync 1, %0;" ::"n"(kSumWarps * 32) : "memory");
@@ -584,15 +658,16 @@ __global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_
         }
         if (!ok) {
             failed = 1;
+            // what is on its way out of shared memory ends first
+            if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
             // NaN where this CTA's outputs would be
-            float f[32];
-#pragma unroll
-            for (int k = 0; k < 32; ++k) f[k] = __uint_as_float(0x7fffffffu);
             const int items = items_of<PAIR>(p, 2);
             for (int i = unit; i < items; i += units) {
                 const Item w = item_of<PAIR>(p, 2, i);
-                for (int c = 0; c < kCols; c += 32)
-                    store_out(p, w.mat, w.i * T + rank * kCtaRows + row, w.j * T + half * kCols + c, f);
+                const int r = w.i * T + rank * kCtaRows + row;
+                for (int c = w.j * T + half * kCols; c < min(w.j * T + (half + 1) * kCols, p.n) && r < p.m; ++c)
+                    *reinterpret_cast<uint16_t*>(p.out + int64_t(w.mat) * p.out_batch + int64_t(p.turned ? c : r) * p.out_pitch +
+                                                 int64_t(p.turned ? r : c) * 2) = 0x7fff;
             }
         }
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -615,7 +690,7 @@ struct PrepParams {
     float2* part;            // [batch][parts]
     uint32_t* zero;          // counters of the product kernel
     uint8_t* hi;
-    uint8_t* rest;
+    uint8_t* xf;
     int64_t u_pitch, u_batch, m_pitch, m_batch;   // bytes
     int64_t rows, cols;      // as given; one long row where they are contiguous
     int32_t nzero, parts;
@@ -701,7 +776,7 @@ __global__ void __launch_bounds__(256) orth_norm_kernel(PrepParams p) {
     p.part[int64_t(mat) * p.parts + blockIdx.x] = make_float2(s1, s2);
 }
 
-// The update over its norm as X: operand and rest, box by box.
+// The update over its norm as X: operand and fp32, box by box.
 __global__ void __launch_bounds__(256) orth_split_kernel(PrepParams p) {
     __shared__ float2 sums[8];
     __shared__ float factor[2];
@@ -769,15 +844,13 @@ __global__ void __launch_bounds__(256) orth_split_kernel(PrepParams p) {
             for (int k = 0; k < 16; ++k) f[k] = tile[c + k][r];
         }
         const int64_t off = (int64_t(mat) * boxes + box) * kBoxBytes;
+        uint8_t* const xf = p.xf + row_at(mat, p.bm * kBox, p.bn * kBox, int(br) * kBox + r) + quad_at(int(bc) * kBox + c);
 #pragma unroll
-        for (int k = 0; k < 16; k += 8) {
-            uint32_t hi[4], lo[4];
+        for (int k = 0; k < 16; k += 4) *reinterpret_cast<float4*>(xf + quad_at(k)) = make_float4(f[k], f[k + 1], f[k + 2], f[k + 3]);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) split_pair(f[k + 2 * j], f[k + 2 * j + 1], hi[j], lo[j]);
-            const uint32_t at = piece_at(r, (c + k) / 8);
-            *reinterpret_cast<uint4*>(p.hi + off + at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-            *reinterpret_cast<uint4*>(p.rest + off + at) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-        }
+        for (int k = 0; k < 16; k += 8)
+            *reinterpret_cast<uint4*>(p.hi + off + piece_at(r, (c + k) / 8)) =
+                make_uint4(pack_f16(f[k], f[k + 1]), pack_f16(f[k + 2], f[k + 3]), pack_f16(f[k + 4], f[k + 5]), pack_f16(f[k + 6], f[k + 7]));
     }
 }
 
@@ -791,7 +864,7 @@ struct Plan {
     bool pair, turned;
     int ctas;                 // of a tile
     int64_t splits[3], items[3], parts;
-    int64_t counters, norm, d, e, x0, x1, rest, sa, sb, part, bytes;
+    int64_t counters, norm, d, e, x0, x1, xf, af, sa, sb, part, bytes;
 };
 constexpr int kPairs = 76;    // pairs of CTAs that the device holds
 constexpr int64_t kPairFrom = 1024;
@@ -829,13 +902,14 @@ Plan plan_of(int64_t batch, int64_t rows, int64_t cols) {
     };
     const int64_t x = batch * q.bm * q.bn * kBoxBytes, sq = batch * q.bm * q.bm * kBoxBytes, diag = batch * q.bm * kBox * 4;
     const int64_t most = q.splits[0] > q.splits[1] ? q.splits[0] : q.splits[1];
-    q.counters = take((1 + half * q.ctas) * 4);
+    q.counters = take((1 + 2 * half * q.ctas) * 4);
     q.norm = take(batch * q.parts * 8);
     q.d = take(diag);
     q.e = take(diag);
     q.x0 = take(x);
     q.x1 = take(x);
-    q.rest = take(x);
+    q.xf = take(2 * x);
+    q.af = take(2 * sq);
     q.sa = take(sq);
     q.sb = take(sq);
     q.part = take(most > 1 ? half * most * T * T * 4 : 0);
@@ -901,12 +975,20 @@ cudaError_t resident(int device, int* n) {
 }
 
 template <bool PAIR>
-cudaError_t launch_products(int device, const OrthParams& p, const Plan& q, cudaStream_t s) {
+cudaError_t launch_products(int device, OrthParams& p, const Plan& q, cudaStream_t s) {
     int units = 0;
     cudaError_t e = resident<PAIR>(device, &units);
     if (e != cudaSuccess) return e;
     int64_t want = 1;
-    for (int64_t i : q.items) want = i > want ? i : want;
+    for (int k = 0; k < 3; ++k) {
+        int64_t items = q.items[k];
+        // splits wait for one another, so each needs a CTA of its own
+        if (p.splits[k] > 1 && items > units) {
+            items /= p.splits[k];
+            p.splits[k] = 1;
+        }
+        want = items > want ? items : want;
+    }
     if (want < units) units = int(want);
     cudaLaunchAttribute attr[2] = {};
     attr[0].id = cudaLaunchAttributeCooperative;
@@ -1036,7 +1118,7 @@ extern "C" lc_status lc_orthogonalize(int device, void* cuda_stream, const lc_ma
     a.nzero = int32_t((q.norm - q.counters) / 4);
     a.parts = int32_t(q.parts);
     a.hi = w + q.x0;
-    a.rest = w + q.rest;
+    a.xf = w + q.xf;
     a.rows = rows;
     a.cols = cols;
     a.beta = float(beta);
@@ -1067,7 +1149,8 @@ extern "C" lc_status lc_orthogonalize(int device, void* cuda_stream, const lc_ma
     p.e = reinterpret_cast<float*>(w + q.e);
     p.x[0] = w + q.x0;
     p.x[1] = w + q.x1;
-    p.rest = w + q.rest;
+    p.xf = w + q.xf;
+    p.af = w + q.af;
     p.sa = w + q.sa;
     p.sb = w + q.sb;
     p.part = reinterpret_cast<float*>(w + q.part);
@@ -1082,6 +1165,7 @@ extern "C" lc_status lc_orthogonalize(int device, void* cuda_stream, const lc_ma
     p.bm = int32_t(q.bm);
     p.bn = int32_t(q.bn);
     p.steps = steps;
+    p.tiles = int32_t(q.items[0] / q.splits[0]);
     for (int k = 0; k < 3; ++k) p.splits[k] = int32_t(q.splits[k]);
     p.turned = q.turned;
     p.wide = rows_wide(p.out, rows > 1 ? p.out_pitch : 0, batch > 1 ? p.out_batch : 0);

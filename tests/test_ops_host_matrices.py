@@ -70,13 +70,14 @@ def test_refusals_before_the_device(abi):
 
 
 def test_workspace(abi):
-    """Room for X three times and two square matrices, in fp16, padded to whole tiles; none for sizes that are refused."""
+    """Room for X in fp32 and twice in fp16, and for A in fp32, A and B in fp16, padded to whole tiles; none for sizes that
+    are refused."""
     size = abi.load().lc_orthogonalize_workspace
     for b, m, n in ((1, 1, 1), (1, 256, 256), (8, 1024, 256), (1, 4096, 14336), (3, 515, 1023)):
         lo, hi = sorted((m, n))
-        assert size(b, m, n) >= b * (3 * lo * hi + 2 * lo * lo) * 2
+        assert size(b, m, n) >= b * 8 * (lo * hi + lo * lo)
         assert size(b, m, n) == size(b, n, m)
-        assert size(b, m, n) < b * (3 * (lo + 256) * (hi + 256) + 2 * (lo + 256) ** 2) * 2 + (152 << 18)
+        assert size(b, m, n) < b * 8 * (lo + 256) * (hi + 256) * 2 + (152 << 18)
     for bad in ((0, 4, 4), (1, 0, 4), (1, 4, 0), (1, 4, abi.LC_ORTH_MAX_DIM + 1), (65536, 4, 4), (-1, 4, 4)):
         assert size(*bad) == 0
 
