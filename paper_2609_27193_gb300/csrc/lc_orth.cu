@@ -26,8 +26,8 @@
 //
 // The product kernel is one cooperative launch: its CTAs go through the 3 * steps
 // products together, with a barrier of the whole grid between them.  Two CTAs of a cluster share
-// tiles of 256 x 256 (PAIR), or a CTA has one of 128 x 128.  Warp 0 brings the operands, warp 1 issues
-// the products into two accumulators in turn, warps 4-11 turn the finished one into the next operand.
+// tiles of 256 x 256 (PAIR), or a CTA has one of 128 x 64.  Warp 0 brings the operands, warp 1 issues
+// the products into two accumulators in turn, warps 4-19 turn the finished one into the next operand.
 //
 // Waits are bounded: where one runs out the CTA's outputs are NaN, and with the next
 // barrier everybody's.
@@ -43,22 +43,30 @@ namespace {
 
 constexpr int kBox = 64;                    // rows and columns of a box
 constexpr int kBoxBytes = kBox * kBox * 2;
-constexpr int kCtaRows = 128;               // rows of an operand in a CTA
-constexpr int kOperand = 2 * kBoxBytes;
-constexpr int kStageBytes = 2 * kOperand;
-constexpr int kStages = 6;
-constexpr int kSumWarp = 4, kSumWarps = 8;  // the first (a multiple of 4) of the warps that read the accumulators, and their number
+constexpr int kCtaRows = 128;               // rows of the left operand in a CTA
+constexpr int kSumWarp = 4, kSumWarps = 16; // the first (a multiple of 4) of the warps that read the accumulators, and their number
 constexpr int kThreads = (kSumWarp + kSumWarps) * 32;
-// the ring, half a box for each of the warps that write operands, and room to align them to 1024 bytes
-constexpr int kSmem = kStages * kStageBytes + kSumWarps * kBoxBytes / 2 + 1024;
+constexpr int kChunk = 16;                  // columns that such a warp works on at a time
 constexpr int kMaxSteps = 16;
 constexpr int kNormCtas = 512;              // most partial sums of squares of a matrix
 
+// A tile is kRows x kCols, of one CTA or of a pair of them with half of the rows each.
 template <bool PAIR>
 struct TileOf {
-    static constexpr int kTile = PAIR ? 256 : 128;
+    static constexpr int kCtas = PAIR ? 2 : 1;
+    static constexpr int kRows = kCtaRows * kCtas, kCols = PAIR ? 256 : 64;
+    static constexpr int kSide = kRows / kBox;                 // boxes of a block on the diagonal
+    static constexpr int kLeft = 2 * kBoxBytes;                // of a stage: the left operand, and the CTA's part of the right one
+    static constexpr int kRightBoxes = kCols / kCtas / kBox;
+    static constexpr int kStageBytes = kLeft + kRightBoxes * kBoxBytes;
+    static constexpr int kStages = PAIR ? 5 : 8;
+    static constexpr int kWarpCols = kCols / 4;                // columns of a warp, 32 rows of them
+    static constexpr int kShare = kBox / kWarpCols;            // warps that fill half a box of staging
+    static constexpr int kStaging = kSumWarps / kShare * (kBoxBytes / 2);
+    static constexpr int kSmem = kStages * kStageBytes + kStaging + 1024;   // and room to align them to 1024 bytes
+    static constexpr int kTmemCols = 2 * kCols;
     // fp32 accumulator, fp16 operands; which way their rows lie is added for each product
-    static constexpr uint32_t kIdesc = 1u << 4 | uint32_t(kTile / 8) << 17 | uint32_t(kTile / 16) << 24;
+    static constexpr uint32_t kIdesc = 1u << 4 | uint32_t(kCols / 8) << 17 | uint32_t(kRows / 16) << 24;
 };
 
 struct OrthStep {
@@ -128,19 +136,17 @@ __device__ __forceinline__ uint64_t operand_desc(uint32_t addr) {
            uint64_t(2) << 61;
 }
 
-__device__ __forceinline__ void tmem_ld32(uint32_t addr, float (&f)[32]) {
-    uint32_t r[32];
+__device__ __forceinline__ void tmem_ld16(uint32_t addr, float (&f)[16]) {
+    uint32_t r[16];
     asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,"
-        "%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n\ttcgen05.wait::ld.sync.aligned;"
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
         : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
-          "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
-          "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
         : "r"(addr)
         : "memory");
 #pragma unroll
-    for (int i = 0; i < 32; ++i) f[i] = __uint_as_float(r[i]);
+    for (int i = 0; i < 16; ++i) f[i] = __uint_as_float(r[i]);
 }
 
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
@@ -151,14 +157,15 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
 // 16-byte piece `p` (of 8) of row r in a box.
 __device__ __forceinline__ uint32_t piece_at(int r, int p) { return uint32_t(r) * 128 + uint32_t((p ^ (r & 7)) * 16); }
 
-// One piece of a product: a tile, or a split of its reduction.
+// One piece of a product: a tile, or a split of its reduction.  i: the block of kRows rows, j: of kCols columns, jb: the
+// block on the diagonal that the columns are part of.
 struct Item {
-    int mat, i, j, split, s0, stages, tile;
+    int mat, i, j, jb, split, s0, stages, tile;
 };
 template <bool PAIR>
 __device__ __forceinline__ Item item_of(const OrthParams& p, int phase, int at) {
-    constexpr int T = TileOf<PAIR>::kTile;
-    const int tm = p.bm * kBox / T, tn = p.bn * kBox / T;
+    constexpr int kIn = TileOf<PAIR>::kRows / TileOf<PAIR>::kCols;   // tiles beside one another in such a block
+    const int tm = p.bm / TileOf<PAIR>::kSide, tn = p.bn * kBox / TileOf<PAIR>::kCols;
     const int all = phase == 0 ? p.bn : p.bm, splits = p.splits[phase];
     Item w;
     const int t = at / splits;
@@ -173,24 +180,26 @@ __device__ __forceinline__ Item item_of(const OrthParams& p, int phase, int at) 
         const int k = t - w.mat * tiles;
         w.j = k / tm;
         w.i = k - w.j * tm;
+        w.jb = 0;
     } else {
-        const int tiles = tm * (tm + 1) / 2;
+        const int tiles = tm * (tm + 1) / 2 * kIn;
         w.mat = t / tiles;
-        const int k = t - w.mat * tiles;
-        // column j holds tiles [j (j + 1) / 2, ...)
+        const int k = (t - w.mat * tiles) / kIn;
+        // block column j holds blocks [j (j + 1) / 2, ...)
         int j = int((sqrtf(8.0f * float(k) + 1.0f) - 1.0f) * 0.5f);
         while (j * (j + 1) / 2 > k) --j;
         while ((j + 1) * (j + 2) / 2 <= k) ++j;
-        w.j = j;
+        w.jb = j;
         w.i = k - j * (j + 1) / 2;
+        w.j = j * kIn + t % kIn;
     }
     return w;
 }
 template <bool PAIR>
 __device__ __forceinline__ int items_of(const OrthParams& p, int phase) {
-    constexpr int T = TileOf<PAIR>::kTile;
-    const int tm = p.bm * kBox / T, tn = p.bn * kBox / T;
-    return p.batch * (phase == 2 ? tm * tn : tm * (tm + 1) / 2) * p.splits[phase];
+    constexpr int kIn = TileOf<PAIR>::kRows / TileOf<PAIR>::kCols;
+    const int tm = p.bm / TileOf<PAIR>::kSide, tn = p.bn * kBox / TileOf<PAIR>::kCols;
+    return p.batch * (phase == 2 ? tm * tn : tm * (tm + 1) / 2 * kIn) * p.splits[phase];
 }
 
 template <int N>
@@ -256,33 +265,34 @@ __device__ __forceinline__ uint32_t lds16(uint32_t addr) {
     return v;
 }
 
-// A warp's 32 rows of 64 columns of the output, from its 4 KB of staging in shared memory (rows of 128
-// bytes, swizzled).  r0, c0: the first row and column.
-__device__ __forceinline__ void store_rows(const OrthParams& p, int mat, int r0, int c0, uint32_t stage, int lane) {
+// 32 rows of 64 columns of the output, from 4 KB of staging in shared memory (rows of 128 bytes,
+// swizzled), by SHARE warps of which this is the `part`th.  r0, c0: the first row and column.
+template <int SHARE>
+__device__ __forceinline__ void store_rows(const OrthParams& p, int mat, int r0, int c0, uint32_t stage, int part, int lane) {
     uint8_t* base = p.out + int64_t(mat) * p.out_batch;
     if (p.wide && c0 + kBox <= p.n) {
         const int piece = lane % 8;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const int r = k * 4 + lane / 8;
+        for (int k = 0; k < 8 / SHARE; ++k) {
+            const int r = (k * SHARE + part) * 4 + lane / 8;
             const uint4 v = lds128(stage + piece_at(r, piece));
             if (r0 + r < p.m) *reinterpret_cast<uint4*>(base + int64_t(r0 + r) * p.out_pitch + c0 * 2 + piece * 16) = v;
         }
         return;
     }
 #pragma unroll 4
-    for (int k = 0; k < 64; ++k) {
+    for (int k = part; k < 64; k += SHARE) {
         const int r = k / 2, c = k % 2 * 32 + lane;
         const uint32_t v = lds16(stage + piece_at(r, c / 8) + c % 8 * 2);
         if (r0 + r < p.m && c0 + c < p.n) *reinterpret_cast<uint16_t*>(base + int64_t(r0 + r) * p.out_pitch + (c0 + c) * 2) = uint16_t(v);
     }
 }
-// A row's columns c .. c + 31 of an output that is X^T: the lanes' rows are neighbours there.
-__device__ __forceinline__ void store_turned(const OrthParams& p, int mat, int r, int c, const float (&f)[32]) {
+// A row's columns c .. c + 15 of an output that is X^T: the lanes' rows are neighbours there.
+__device__ __forceinline__ void store_turned(const OrthParams& p, int mat, int r, int c, const float (&f)[kChunk]) {
     if (r >= p.m) return;
     uint8_t* o = p.out + int64_t(mat) * p.out_batch + int64_t(c) * p.out_pitch + int64_t(r) * 2;
 #pragma unroll
-    for (int k = 0; k < 32; ++k)
+    for (int k = 0; k < kChunk; ++k)
         if (c + k < p.n) *reinterpret_cast<__nv_bfloat16*>(o + k * p.out_pitch) = __float2bfloat16_rn(f[k]);
 }
 
@@ -293,7 +303,7 @@ __device__ __forceinline__ int64_t row_at(int64_t mat, int rows, int cols, int r
 }
 __device__ __forceinline__ int quad_at(int c) { return c / 4 * 512; }
 
-// A row of a product's tile on its way to the next operand, 8 or 32 columns at a time.
+// A row of a product's tile on its way to the next operand, 8 or 16 columns at a time.
 struct Finish {
     const OrthParams& p;
     const OrthStep& co;
@@ -303,8 +313,8 @@ struct Finish {
     uint8_t* state;          // the row of A or of X in fp32
     uint8_t* out;            // the next operand: the row of boxes
     int64_t diag;            // of the matrix's first diagonal element
-    float scale, dr;
-    float4 next[8], now[8];  // what is read beside the accumulator: A or X
+    float scale, cs, dr;
+    float4 next[4], now[4];  // what is read beside the accumulator: A or X
     float d_next, d_now;     // A's diagonal, of a column a lane
 
     __device__ __forceinline__ Finish(const OrthParams& q, int ph, int step, bool fin, int m, int r)
@@ -313,11 +323,13 @@ struct Finish {
         state = (phase == 2 ? p.xf : p.af) + row_at(mat, p.bm * kBox, cols, gr);
         out = (phase == 0 ? p.sa : phase == 1 ? p.sb : p.x[step & 1 ^ 1]) + (int64_t(mat) * p.bm + gr / kBox) * (cols / kBox) * kBoxBytes;
         diag = int64_t(mat) * p.bm * kBox;
+        cs = 0.0f;
         if (phase == 0) {
             scale = 1.0f / (p.x_scale * p.x_scale);
             dr = 0.0f;
         } else if (phase == 1) {
             scale = 1.0f / (p.a_scale * p.a_scale);
+            cs = co.c * scale;
             dr = __ldcg(p.d + diag + gr);
         } else {
             scale = 1.0f / co.scale;
@@ -341,50 +353,62 @@ struct Finish {
     // eights asked for.
     __device__ __forceinline__ uint4 piece(int col, int k, float* f) {
         const float old[8] = {now[2 * k].x, now[2 * k].y, now[2 * k].z, now[2 * k].w, now[2 * k + 1].x, now[2 * k + 1].y, now[2 * k + 1].z, now[2 * k + 1].w};
-        const bool diagonal = col <= gr && gr < col + 8;
-        float v[8], sc;
+        // the warp's rows meet these columns on the diagonal: seldom
+        const bool diagonal = phase < 2 && (col & ~31) == (gr & ~31);
+        float sc = 1.0f;
         if (phase == 0) {
 #pragma unroll
-            for (int m = 0; m < 8; ++m) {
-                f[m] *= scale;
-                if (diagonal && col + m == gr) {
-                    __stcg(p.d + diag + gr, f[m]);
-                    f[m] = 0.0f;
-                }
-                v[m] = f[m];
+            for (int m = 0; m < 8; ++m) f[m] *= scale;
+            if (diagonal) {
+#pragma unroll
+                for (int m = 0; m < 8; ++m)
+                    if (col + m == gr) {
+                        __stcg(p.d + diag + gr, f[m]);
+                        f[m] = 0.0f;
+                    }
             }
             sc = p.a_scale;
         } else if (phase == 1) {
+            // b A0 + c (A0^2 + (d_i + d_j) A0)
+            float on[8];
+            if (diagonal) {
+#pragma unroll
+                for (int m = 0; m < 8; ++m) on[m] = f[m];
+            }
+            const float bc = fmaf(co.c, dr, co.b);
 #pragma unroll
             for (int m = 0; m < 8; ++m) {
                 const float dj = __shfl_sync(0xffffffffu, d_now, 8 * k + m);
-                v[m] = co.b * old[m] + co.c * (f[m] * scale + (dr + dj) * old[m]);
-                if (diagonal && col + m == gr) {
-                    // (A is zero there)
-                    __stcg(p.e + diag + gr, co.b * dr + co.c * (f[m] * scale + dr * dr));
-                    v[m] = 0.0f;
-                }
+                f[m] = fmaf(fmaf(co.c, dj, bc), old[m], cs * f[m]);
+            }
+            if (diagonal) {
+#pragma unroll
+                for (int m = 0; m < 8; ++m)
+                    if (col + m == gr) {
+                        // (A0 is zero there)
+                        __stcg(p.e + diag + gr, fmaf(cs, on[m], dr * bc));
+                        f[m] = 0.0f;
+                    }
             }
             sc = co.scale;
         } else {
 #pragma unroll
-            for (int m = 0; m < 8; ++m) f[m] = v[m] = fmaf(dr, old[m], f[m] * scale);
-            sc = 1.0f;
+            for (int m = 0; m < 8; ++m) f[m] = fmaf(dr, old[m], f[m] * scale);
         }
         if (phase == 0 || (phase == 2 && !final)) {
-            __stcg(reinterpret_cast<float4*>(state + quad_at(col)), make_float4(v[0], v[1], v[2], v[3]));
-            __stcg(reinterpret_cast<float4*>(state + quad_at(col + 4)), make_float4(v[4], v[5], v[6], v[7]));
+            __stcg(reinterpret_cast<float4*>(state + quad_at(col)), make_float4(f[0], f[1], f[2], f[3]));
+            __stcg(reinterpret_cast<float4*>(state + quad_at(col + 4)), make_float4(f[4], f[5], f[6], f[7]));
         }
-        return make_uint4(pack_f16(v[0] * sc, v[1] * sc), pack_f16(v[2] * sc, v[3] * sc), pack_f16(v[4] * sc, v[5] * sc),
-                          pack_f16(v[6] * sc, v[7] * sc));
+        return make_uint4(pack_f16(f[0] * sc, f[1] * sc), pack_f16(f[2] * sc, f[3] * sc), pack_f16(f[4] * sc, f[5] * sc),
+                          pack_f16(f[6] * sc, f[7] * sc));
     }
 };
 
 template <bool PAIR>
 __global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_constant__ OrthParams p) {
-    constexpr int T = TileOf<PAIR>::kTile, kCtas = PAIR ? 2 : 1;
-    constexpr int kCols = T / 2;             // columns of the tile that a warp of the second group reads
-    constexpr int kTmemCols = 2 * T;
+    using Tile = TileOf<PAIR>;
+    constexpr int kCtas = Tile::kCtas, kStages = Tile::kStages, kStageBytes = Tile::kStageBytes, kCols = Tile::kCols;
+    constexpr int kWarpCols = Tile::kWarpCols, kTmemCols = Tile::kTmemCols, kSide = Tile::kSide;
     extern __shared__ uint8_t raw[];
     // full and empty: a stage's copies have landed / its products are done (each CTA's own).  peer: the other CTA's copies
     // have landed (the first CTA's).  summed: an accumulator is complete; taken: it has been read (the first CTA's).
@@ -444,32 +468,33 @@ __global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_
             for (int i = unit; i < items && ok; i += units) {
                 const Item w = item_of<PAIR>(p, phase, i);
                 // first box row or column of this CTA's part of either operand
-                const int left = w.i * (T / kBox) + rank * 2, right = w.j * (T / kBox) + rank * 2;
+                const int left = w.i * kSide + rank * 2, right = w.j * (kCols / kBox) + rank * Tile::kRightBoxes;
                 const uint8_t* xm = x + w.mat * x_bytes;
                 const uint8_t* sm = (phase == 1 ? p.sa : p.sb) + w.mat * s_bytes;
                 for (int s = 0; s < w.stages; ++s, ++it, st.next()) {
                     ok = it < kStages || mbar_wait_bounded(empty + 8 * st.at, st.round ^ 1, kWaitNs);
                     if (!ok) break;
-                    const int k = w.s0 + s, kt = k / (T / kBox);
+                    const int k = w.s0 + s, kt = k / kSide;
                     const uint32_t to = ring + st.at * kStageBytes, bar = full + 8 * st.at;
                     mbar_expect_tx(bar, kStageBytes + (it == 0 && rank == kCtas - 1 && p.stall ? 16 : 0));
-                    // two boxes, one above the other or side by side
-                    auto above = [&](uint32_t at, const uint8_t* base, int width, int r, int c) {
-                        bulk_g2s(at, base + (int64_t(r) * width + c) * kBoxBytes, kBoxBytes, bar);
-                        bulk_g2s(at + kBoxBytes, base + (int64_t(r + 1) * width + c) * kBoxBytes, kBoxBytes, bar);
+                    // boxes one above the other, or side by side
+                    auto above = [&](uint32_t at, const uint8_t* base, int width, int r, int c, int n) {
+                        for (int m = 0; m < n; ++m)
+                            bulk_g2s(at + m * kBoxBytes, base + (int64_t(r + m) * width + c) * kBoxBytes, kBoxBytes, bar);
                     };
-                    auto beside = [&](uint32_t at, const uint8_t* base, int width, int r, int c) {
-                        bulk_g2s(at, base + (int64_t(r) * width + c) * kBoxBytes, kOperand, bar);
+                    auto beside = [&](uint32_t at, const uint8_t* base, int width, int r, int c, int n) {
+                        bulk_g2s(at, base + (int64_t(r) * width + c) * kBoxBytes, n * kBoxBytes, bar);
                     };
+                    constexpr int kRight = Tile::kRightBoxes;
                     if (phase == 0) {
-                        above(to, xm, p.bn, left, k);
-                        above(to + kOperand, xm, p.bn, right, k);
+                        above(to, xm, p.bn, left, k, 2);
+                        above(to + Tile::kLeft, xm, p.bn, right, k, kRight);
                     } else {
-                        if (w.i <= kt) above(to, sm, p.bm, left, k);
-                        else beside(to, sm, p.bm, k, left);
-                        if (phase == 2) beside(to + kOperand, xm, p.bn, k, right);
-                        else if (w.j <= kt) above(to + kOperand, sm, p.bm, right, k);
-                        else beside(to + kOperand, sm, p.bm, k, right);
+                        if (w.i <= kt) above(to, sm, p.bm, left, k, 2);
+                        else beside(to, sm, p.bm, k, left, 2);
+                        if (phase == 2) beside(to + Tile::kLeft, xm, p.bn, k, right, kRight);
+                        else if (w.jb <= kt) above(to + Tile::kLeft, sm, p.bm, right, k, kRight);
+                        else beside(to + Tile::kLeft, sm, p.bm, k, right, kRight);
                     }
                 }
             }
@@ -507,15 +532,15 @@ __global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_
                     if (PAIR && ok) ok = wait_long(peer + 8 * st.at, st.round, s ? kWaitNs : p.limit_ns);
                     if (!ok) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const int kt = (w.s0 + s) / (T / kBox);
+                    const int kt = (w.s0 + s) / kSide;
                     // rows along the reduction: 16 of them are 2048 bytes further; across it 16 columns are 32 bytes
-                    const bool ta = phase && w.i > kt, tb = phase == 2 || (phase == 1 && w.j > kt);
-                    const uint64_t l = operand_desc(ring + st.at * kStageBytes), r = l + (kOperand >> 4);
-                    const uint32_t idesc = TileOf<PAIR>::kIdesc | (ta ? 1u << 15 : 0u) | (tb ? 1u << 16 : 0u);
+                    const bool ta = phase && w.i > kt, tb = phase == 2 || (phase == 1 && w.jb > kt);
+                    const uint64_t l = operand_desc(ring + st.at * kStageBytes), r = l + (Tile::kLeft >> 4);
+                    const uint32_t idesc = Tile::kIdesc | (ta ? 1u << 15 : 0u) | (tb ? 1u << 16 : 0u);
                     const int la = ta ? 2048 >> 4 : 2, lb = tb ? 2048 >> 4 : 2;
 #pragma unroll
                     for (int k = 0; k < kBox / 16; ++k)
-                        mma<PAIR>(tmem + acc.at * T, l + k * la, r + k * lb, idesc, s > 0 || k > 0);
+                        mma<PAIR>(tmem + acc.at * kCols, l + k * la, r + k * lb, idesc, s > 0 || k > 0);
                     commit<PAIR>(empty + 8 * st.at);
                 }
                 if (ok) commit<PAIR>(summed + 8 * acc.at);
@@ -526,11 +551,18 @@ __global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_
         if (!ok) failed = 1;
     } else if (warp >= kSumWarp) {
         // --- what comes of an accumulator ---
-        const int quad = warp & 3, half = (warp - kSumWarp) >> 2, t = threadIdx.x - kSumWarp * 32;
+        const int quad = warp & 3, group = (warp - kSumWarp) >> 2, t = threadIdx.x - kSumWarp * 32;
         const int row = quad * 32 + lane;                 // of this CTA's 128
         const uint32_t first_taken = PAIR ? cluster_addr(taken, 0) : taken;
-        const uint32_t from = tmem + (uint32_t(quad * 32) << 16) + half * kCols;
-        const uint32_t stage = ring + kStages * kStageBytes + (warp - kSumWarp) * (kBoxBytes / 2);
+        const uint32_t from = tmem + (uint32_t(quad * 32) << 16) + group * kWarpCols;
+        // half a box of staging, filled by kShare warps with the same rows; the first of them stores it
+        constexpr int kShare = Tile::kShare;
+        const int part = group % kShare;
+        const uint32_t stage = ring + kStages * kStageBytes + (group / kShare * 4 + quad) * (kBoxBytes / 2);
+        auto stage_meet = [&]() {
+            if constexpr (kShare == 1) __syncwarp();
+            else asm volatile("bar.sync %0, %1;" ::"r"(2 + group / kShare * 4 + quad), "n"(kShare * 32) : "memory");
+        };
         Ring<2> acc;
         bool ok = true;
         for (int ph = 0; ph < phases; ++ph) {
@@ -541,63 +573,58 @@ __global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_
             const int splits = p.splits[phase], items = items_of<PAIR>(p, phase);
             for (int i = unit; i < items; i += units, acc.next()) {
                 const Item w = item_of<PAIR>(p, phase, i);
-                Finish fin(p, phase, step, final, w.mat, w.i * T + rank * kCtaRows + row);
-                const int c0 = w.j * T + half * kCols;
+                Finish fin(p, phase, step, final, w.mat, w.i * Tile::kRows + rank * kCtaRows + row);
+                const int c0 = w.j * kCols + group * kWarpCols;
                 if (splits == 1) {
-                    // what is read beside the accumulator is on its way before that is complete, and then 32 columns ahead
-                    fin.ask<4>(c0, lane);
+                    // what is read beside the accumulator is on its way before that is complete, and then a chunk ahead
+                    fin.ask<2>(c0, lane);
                     ok = sum_warps_agree(mbar_wait_warp(summed + 8 * acc.at, acc.round));
                     if (!ok) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    // the staging's last rows have been read
+                    if (part == 0 && lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                    stage_meet();
 #pragma unroll 1
-                    for (int c = 0; c < kCols; c += 32) {
-                        float f[32];
-                        tmem_ld32(from + acc.at * T + c, f);
-                        if (c + 32 == kCols) {
+                    for (int c = 0; c < kWarpCols; c += kChunk) {
+                        float f[kChunk];
+                        tmem_ld16(from + acc.at * kCols + c, f);
+                        if (c + kChunk == kWarpCols) {
                             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                             __syncwarp();
                             if (lane == 0) arrive_at(first_taken + 8 * acc.at);
                         }
-                        fin.take<4>();
-                        if (c + 32 < kCols) fin.ask<4>(c0 + c + 32, lane);
-                        if (c % kBox == 0) {
-                            // the staging's last rows have been read
-                            if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-                            __syncwarp();
-                        }
-                        uint4 v[4];
+                        fin.take<2>();
+                        if (c + kChunk < kWarpCols) fin.ask<2>(c0 + c + kChunk, lane);
+                        uint4 v[2];
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) v[k] = fin.piece(c0 + c + 8 * k, k, f + 8 * k);
+                        for (int k = 0; k < 2; ++k) v[k] = fin.piece(c0 + c + 8 * k, k, f + 8 * k);
                         if (final) {
                             const float back = 1.0f / p.x_scale;
 #pragma unroll
-                            for (int k = 0; k < 32; ++k) f[k] *= back;
+                            for (int k = 0; k < kChunk; ++k) f[k] *= back;
                             if (p.turned) {
                                 store_turned(p, w.mat, fin.gr, c0 + c, f);
                                 continue;
                             }
 #pragma unroll
-                            for (int k = 0; k < 4; ++k)
+                            for (int k = 0; k < 2; ++k)
                                 v[k] = make_uint4(pack_bf16(f[8 * k], f[8 * k + 1]), pack_bf16(f[8 * k + 2], f[8 * k + 3]),
                                                   pack_bf16(f[8 * k + 4], f[8 * k + 5]), pack_bf16(f[8 * k + 6], f[8 * k + 7]));
                         }
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) sts128(stage + piece_at(lane, c % kBox / 8 + k), v[k]);
-                        if (c % kBox == 0) continue;
-                        // 32 rows of a box are one piece of memory
-                        const int col = c0 + c - 32;
-                        if (final) {
-                            __syncwarp();
-                            store_rows(p, w.mat, fin.gr - lane, col, stage, lane);
-                            __syncwarp();
-                        } else {
-                            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                            __syncwarp();
-                            if (lane == 0) {
-                                bulk_s2g(fin.out + int64_t(col / kBox) * kBoxBytes + quad % 2 * (kBoxBytes / 2), stage, kBoxBytes / 2);
-                                asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-                            }
+                        for (int k = 0; k < 2; ++k) sts128(stage + piece_at(lane, (c0 + c) % kBox / 8 + k), v[k]);
+                    }
+                    // 32 rows of a box are one piece of memory
+                    const int col = c0 - c0 % kBox;
+                    if (!final) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    stage_meet();
+                    if (!final) {
+                        if (part == 0 && lane == 0) {
+                            bulk_s2g(fin.out + int64_t(col / kBox) * kBoxBytes + quad % 2 * (kBoxBytes / 2), stage, kBoxBytes / 2);
+                            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
                         }
+                    } else if (!p.turned) {
+                        store_rows<kShare>(p, w.mat, fin.gr - lane, col, stage, part, lane);
                     }
                     continue;
                 }
@@ -606,15 +633,15 @@ __global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_
                 ok = sum_warps_agree(mbar_wait_warp(summed + 8 * acc.at, acc.round));
                 if (!ok) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                constexpr int kPart = kCtaRows * T;
+                constexpr int kPart = kCtaRows * kCols;
                 float* parts = p.part + (int64_t(w.tile) * kCtas + rank) * splits * kPart + row;
-                float* mine = parts + int64_t(w.split) * kPart + half * kCols * kCtaRows;
+                float* mine = parts + int64_t(w.split) * kPart + group * kWarpCols * kCtaRows;
 #pragma unroll 1
-                for (int c = 0; c < kCols; c += 32) {
-                    float f[32];
-                    tmem_ld32(from + acc.at * T + c, f);
+                for (int c = 0; c < kWarpCols; c += kChunk) {
+                    float f[kChunk];
+                    tmem_ld16(from + acc.at * kCols + c, f);
 #pragma unroll
-                    for (int k = 0; k < 32; ++k) __stcg(mine + (c + k) * kCtaRows, f[k]);
+                    for (int k = 0; k < kChunk; ++k) __stcg(mine + (c + k) * kCtaRows, f[k]);
                 }
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                 __syncwarp();
@@ -629,20 +656,25 @@ __global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_
                 ok = sum_warps_agree(__all_sync(0xffffffffu, came));
                 if (!ok) break;
 #pragma unroll 1
-                for (int k = w.split * 2 + half; k < T / 8; k += splits * 2) {
-                    float f[8];
+                for (int k = w.split * 4 + group; k < kCols / 8; k += splits * 4) {
+                    const int col = w.j * kCols + k * 8;
+                    fin.ask<1>(col, lane);
                     const float* at = parts + k * 8 * kCtaRows;
-                    fin.ask<1>(w.j * T + k * 8, lane);
-#pragma unroll
-                    for (int m = 0; m < 8; ++m) f[m] = __ldcg(at + m * kCtaRows);
+                    // four splits' loads at a time
+                    float f[8] = {};
 #pragma unroll 1
-                    for (int s = 1; s < splits; ++s) {
-                        at += kPart;
+                    for (int s = 0; s < splits; s += 4, at += 4 * kPart) {
+                        float g[4][8];
 #pragma unroll
-                        for (int m = 0; m < 8; ++m) f[m] += __ldcg(at + m * kCtaRows);
+                        for (int h = 0; h < 4; ++h)
+#pragma unroll
+                            for (int m = 0; m < 8; ++m) g[h][m] = s + h < splits ? __ldcg(at + h * kPart + m * kCtaRows) : 0.0f;
+#pragma unroll
+                        for (int h = 0; h < 4; ++h)
+#pragma unroll
+                            for (int m = 0; m < 8; ++m) f[m] += g[h][m];
                     }
                     fin.take<1>();
-                    const int col = w.j * T + k * 8;
                     const uint4 v = fin.piece(col, 0, f);
                     *reinterpret_cast<uint4*>(fin.out + int64_t(col / kBox) * kBoxBytes + piece_at(fin.gr % kBox, col % kBox / 8)) = v;
                 }
@@ -664,8 +696,8 @@ __global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_
             const int items = items_of<PAIR>(p, 2);
             for (int i = unit; i < items; i += units) {
                 const Item w = item_of<PAIR>(p, 2, i);
-                const int r = w.i * T + rank * kCtaRows + row;
-                for (int c = w.j * T + half * kCols; c < min(w.j * T + (half + 1) * kCols, p.n) && r < p.m; ++c)
+                const int r = w.i * Tile::kRows + rank * kCtaRows + row, c0 = w.j * kCols + group * kWarpCols;
+                for (int c = c0; c < min(c0 + kWarpCols, p.n) && r < p.m; ++c)
                     *reinterpret_cast<uint16_t*>(p.out + int64_t(w.mat) * p.out_batch + int64_t(p.turned ? c : r) * p.out_pitch +
                                                  int64_t(p.turned ? r : c) * 2) = 0x7fff;
             }
@@ -877,16 +909,17 @@ Plan plan_of(int64_t batch, int64_t rows, int64_t cols) {
     q.n = q.turned ? rows : cols;
     q.pair = q.m >= kPairFrom;
     q.ctas = q.pair ? 2 : 1;
-    const int64_t T = q.pair ? 256 : 128, units = q.pair ? kPairs : 2 * kPairs;
-    q.tm = al(q.m, T) / T;
-    q.tn = al(q.n, T) / T;
-    q.bm = q.tm * T / kBox;
-    q.bn = q.tn * T / kBox;
-    const int64_t half = batch * q.tm * (q.tm + 1) / 2;
+    const int64_t rows_of = q.pair ? TileOf<true>::kRows : TileOf<false>::kRows, cols_of = q.pair ? TileOf<true>::kCols : TileOf<false>::kCols;
+    const int64_t units = q.pair ? kPairs : 2 * kPairs;
+    q.tm = al(q.m, rows_of) / rows_of;
+    q.tn = al(q.n, cols_of) / cols_of;
+    q.bm = q.tm * rows_of / kBox;
+    q.bn = q.tn * cols_of / kBox;
+    const int64_t half = batch * q.tm * (q.tm + 1) / 2 * (rows_of / cols_of);
     for (int k = 0; k < 3; ++k) {
         const int64_t tiles = k == 2 ? batch * q.tm * q.tn : half, stages = k == 0 ? q.bn : q.bm;
         int64_t s = k == 2 ? 1 : units / tiles;
-        if (s > stages / 4) s = stages / 4;
+        if (s > stages / 16) s = stages / 16;
         if (s < 1) s = 1;
         const int64_t per = (stages + s - 1) / s;
         q.splits[k] = (stages + per - 1) / per;
@@ -912,7 +945,7 @@ Plan plan_of(int64_t batch, int64_t rows, int64_t cols) {
     q.af = take(2 * sq);
     q.sa = take(sq);
     q.sb = take(sq);
-    q.part = take(most > 1 ? half * most * T * T * 4 : 0);
+    q.part = take(most > 1 ? half * most * rows_of * cols_of * 4 : 0);
     q.bytes = at;
     return q;
 }
@@ -947,7 +980,7 @@ template <bool PAIR>
 cudaError_t resident(int device, int* n) {
     static int held[kOpsMaxDevices];
     if (!held[device]) {
-        cudaError_t e = cudaFuncSetAttribute(orth_product_kernel<PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+        cudaError_t e = cudaFuncSetAttribute(orth_product_kernel<PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize, TileOf<PAIR>::kSmem);
         if (e != cudaSuccess) return e;
         int k = 0;
         if (PAIR) {
@@ -958,12 +991,12 @@ cudaError_t resident(int device, int* n) {
             cudaLaunchConfig_t c{};
             c.gridDim = dim3(2 * kPairs);
             c.blockDim = dim3(kThreads);
-            c.dynamicSmemBytes = kSmem;
+            c.dynamicSmemBytes = TileOf<PAIR>::kSmem;
             c.attrs = &attr;
             c.numAttrs = 1;
             e = cudaOccupancyMaxActiveClusters(&k, orth_product_kernel<PAIR>, &c);
         } else {
-            e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&k, orth_product_kernel<PAIR>, kThreads, kSmem);
+            e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&k, orth_product_kernel<PAIR>, kThreads, TileOf<PAIR>::kSmem);
             k *= ops_sm_count(device);
         }
         if (e != cudaSuccess) return e;
@@ -999,7 +1032,7 @@ cudaError_t launch_products(int device, OrthParams& p, const Plan& q, cudaStream
     cudaLaunchConfig_t c{};
     c.gridDim = dim3(unsigned(units * q.ctas));
     c.blockDim = dim3(kThreads);
-    c.dynamicSmemBytes = kSmem;
+    c.dynamicSmemBytes = TileOf<PAIR>::kSmem;
     c.stream = s;
     c.attrs = attr;
     c.numAttrs = PAIR ? 2 : 1;
