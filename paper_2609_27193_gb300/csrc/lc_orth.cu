@@ -106,6 +106,7 @@ __device__ __forceinline__ void arrive_at(uint32_t cluster_bar) {
     asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
 __device__ __forceinline__ void cluster_meet() {
+    __syncwarp();
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 // Once the products issued so far are done: an arrival at the barrier (of both CTAs).
@@ -886,6 +887,425 @@ __global__ void __launch_bounds__(256) orth_split_kernel(PrepParams p) {
     }
 }
 
+// --- small matrices --------------------------------------------------------------------
+
+// Up to 128 rows: a cluster has a matrix, each CTA up to 256 of its columns for the whole call, from the
+// update to the output.  X lies in tensor memory in fp32 and in shared memory as operand.  A step needs the
+// other CTAs once: their parts of A are added up, each CTA a share of the columns, through the cluster's shared
+// memory, and A goes to all; A^2 is computed by each (128 x 128 x 128 takes less than sending it).
+constexpr int kSmallRows = 128, kSmallCols = 256, kSmallThreads = 512, kSmallCtas = 8;
+constexpr int kQuadPitch = kSmallRows * 16 + 16;   // of fp32 staging: four columns of all rows; 16 more keep eight quads of a row in eight banks
+// X's operand, A's, and the other CTAs' sums; staging lies over them
+constexpr int kSmallX = kSmallRows * kSmallCols * 2, kSmallA = kSmallRows * kSmallRows * 2, kSmallSums = kSmallRows * kSmallRows * 4;
+constexpr int kSmallSmem = kSmallX + kSmallA + kSmallSums + 1024;
+static_assert(kSmallCols / 4 * kQuadPitch <= kSmallX + kSmallA + kSmallSums, "staging");
+
+struct SmallParams {
+    const uint8_t* u;
+    uint8_t* m;
+    uint8_t* out;
+    int64_t u_pitch, u_batch, m_pitch, m_batch, out_pitch, out_batch;   // bytes
+    int64_t rows, cols;      // as given
+    double eps;
+    float beta, x_scale, a_scale;
+    int32_t ctas, u_bf16, nesterov, turned, steps;
+    int32_t wide, out_wide;  // rows on 16-byte boundaries
+    OrthStep step[kMaxSteps];
+};
+
+__device__ __forceinline__ void tmem_st16(uint32_t addr, const float (&f)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};\n\t"
+        "tcgen05.wait::st.sync.aligned;" ::"r"(addr),
+        "f"(f[0]), "f"(f[1]), "f"(f[2]), "f"(f[3]), "f"(f[4]), "f"(f[5]), "f"(f[6]), "f"(f[7]), "f"(f[8]), "f"(f[9]), "f"(f[10]), "f"(f[11]),
+        "f"(f[12]), "f"(f[13]), "f"(f[14]), "f"(f[15])
+        : "memory");
+}
+__device__ __forceinline__ float4 lds_quad(uint32_t addr) {
+    const uint4 v = lds128(addr);
+    return make_float4(__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z), __uint_as_float(v.w));
+}
+// Stores into a CTA of the cluster.
+__device__ __forceinline__ void st_cluster(uint32_t addr, const float4& v) {
+    asm volatile("st.shared::cluster.v4.f32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
+}
+__device__ __forceinline__ void st_cluster(uint32_t addr, const float2& v) {
+    asm volatile("st.shared::cluster.v2.f32 [%0], {%1,%2};" ::"r"(addr), "f"(v.x), "f"(v.y) : "memory");
+}
+__device__ __forceinline__ void st_cluster(uint32_t addr, const uint2& v) {
+    asm volatile("st.shared::cluster.v2.u32 [%0], {%1,%2};" ::"r"(addr), "r"(v.x), "r"(v.y) : "memory");
+}
+__device__ __forceinline__ void st_cluster(uint32_t addr, float v) {
+    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
+}
+
+// Where an operand of 128 rows keeps row r's columns c .. c + 7: boxes of 64 columns, two of rows each.
+__device__ __forceinline__ uint32_t small_at(int r, int c) { return (c / kBox * 2 + r / kBox) * kBoxBytes + piece_at(r % kBox, c % kBox / 8); }
+// Descriptor of an operand whose rows run along the reduction; the next 64 columns are two boxes further.
+__device__ __forceinline__ uint64_t small_desc(uint32_t addr) {
+    return uint64_t((addr & 0x3ffffu) >> 4) | uint64_t(2 * kBoxBytes >> 4) << 16 | uint64_t(1024 >> 4) << 32 | uint64_t(1) << 46 | uint64_t(2) << 61;
+}
+
+__device__ __forceinline__ float element(const uint8_t* row, bool bf16, int64_t c) {
+    return bf16 ? to_f32(reinterpret_cast<const __nv_bfloat16*>(row)[c]) : reinterpret_cast<const float*>(row)[c];
+}
+// Values c .. c + 3 of a row, zero beyond its end.
+__device__ __forceinline__ float4 load_quad(const uint8_t* row, bool bf16, bool wide, int64_t c, int64_t cols) {
+    if (wide && c + 4 <= cols) {
+        if (!bf16) return *reinterpret_cast<const float4*>(row + c * 4);
+        const uint2 v = *reinterpret_cast<const uint2*>(row + c * 2);
+        return make_float4(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u), __uint_as_float(v.y << 16),
+                           __uint_as_float(v.y & 0xffff0000u));
+    }
+    return make_float4(c < cols ? element(row, bf16, c) : 0.0f, c + 1 < cols ? element(row, bf16, c + 1) : 0.0f,
+                       c + 2 < cols ? element(row, bf16, c + 2) : 0.0f, c + 3 < cols ? element(row, bf16, c + 3) : 0.0f);
+}
+
+// K: a CTA's columns over 64.
+template <int K>
+__global__ void __launch_bounds__(kSmallThreads, 1) orth_small_kernel(const __grid_constant__ SmallParams p) {
+    constexpr int kN = 64 * K, kMine = kN / 4;   // columns of the CTA, of a thread
+    extern __shared__ uint8_t raw[];
+    __shared__ __align__(8) uint64_t done_bar;
+    __shared__ uint32_t tmem_base;
+    __shared__ __align__(16) float d[kSmallRows], e[kSmallRows];
+    __shared__ float2 sums[kSmallThreads / 32], all[kSmallCtas];
+    __shared__ float factor[2];
+    const int t = threadIdx.x, warp = t >> 5, lane = t & 31, quad = warp & 3, group = warp >> 2, row = quad * 32 + lane;
+    const int C = p.ctas, rank = int(blockIdx.x) % C, mat = int(blockIdx.x) / C;
+    const uint32_t xs = (smem_addr(raw) + 1023) & ~1023u, as = xs + kSmallX, ss = as + kSmallA, done = smem_addr(&done_bar);
+    if (t == 0) {
+        mbar_init(done, 1);
+        mbar_init_fence();
+    }
+    if (warp == 0) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem_base)), "r"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    // --- the update, and its norm ---
+    const uint8_t* u = p.u + int64_t(mat) * p.u_batch;
+    uint8_t* m = p.m ? p.m + int64_t(mat) * p.m_batch : nullptr;
+    const int64_t first = int64_t(rank) * kN;    // X's first column here
+    const int64_t n = p.turned ? p.rows : p.cols;
+    const int rows = int(p.turned ? p.cols : p.rows);
+    auto updated = [&](float v, float& mom) {
+        mom = fmaf(1.0f - p.beta, v - mom, mom);
+        return p.nesterov ? fmaf(p.beta, mom - v, v) : mom;
+    };
+    float x[kMine], s1 = 0.0f, s2 = 0.0f;
+    auto count = [&](float v) {
+        s1 = fmaf(v, v, s1);
+        v *= 0x1p-80f;
+        s2 = fmaf(v, v, s2);
+    };
+    if (p.turned) {
+        // a lane's row is a column of the update
+#pragma unroll
+        for (int k = 0; k < kMine; ++k) {
+            const int64_t c = first + group * kMine + k;
+            const bool in = row < rows && c < n;
+            x[k] = in ? element(u + c * p.u_pitch, p.u_bf16, row) : 0.0f;
+        }
+        if (m) {
+#pragma unroll
+            for (int k = 0; k < kMine; ++k) {
+                const int64_t c = first + group * kMine + k;
+                if (row < rows && c < n) {
+                    float* at = reinterpret_cast<float*>(m + c * p.m_pitch) + row;
+                    float v = *at;
+                    x[k] = updated(x[k], v);
+                    *at = v;
+                }
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kMine; ++k) count(x[k]);
+    } else {
+        // eight lanes a row, four rows a warp; through shared memory to a row a lane
+#pragma unroll 4
+        for (int i = warp; i < kN / 32 * (kSmallRows / 4); i += kSmallThreads / 32) {
+            const int q = i % (kN / 32) * 8 + lane % 8, r = i / (kN / 32) * 4 + lane / 8;
+            const int64_t c = first + q * 4;
+            float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            if (r < rows && c < n) {
+                v = load_quad(u + r * p.u_pitch, p.u_bf16, p.wide, c, n);
+                if (m) {
+                    float* at = reinterpret_cast<float*>(m + r * p.m_pitch) + c;
+                    float4 w = load_quad(reinterpret_cast<const uint8_t*>(at - c), false, p.wide, c, n);
+                    v.x = updated(v.x, w.x);
+                    v.y = updated(v.y, w.y);
+                    v.z = updated(v.z, w.z);
+                    v.w = updated(v.w, w.w);
+                    if (p.wide && c + 4 <= n) {
+                        *reinterpret_cast<float4*>(at) = w;
+                    } else {
+                        at[0] = w.x;
+                        if (c + 1 < n) at[1] = w.y;
+                        if (c + 2 < n) at[2] = w.z;
+                        if (c + 3 < n) at[3] = w.w;
+                    }
+                }
+                count(v.x);
+                count(v.y);
+                count(v.z);
+                count(v.w);
+            }
+            sts128(xs + q * kQuadPitch + r * 16, make_uint4(__float_as_uint(v.x), __float_as_uint(v.y), __float_as_uint(v.z), __float_as_uint(v.w)));
+        }
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+        s1 += __shfl_xor_sync(0xffffffffu, s1, o);
+        s2 += __shfl_xor_sync(0xffffffffu, s2, o);
+    }
+    if (lane == 0) sums[warp] = make_float2(s1, s2);
+    __syncthreads();
+    if (!p.turned) {
+#pragma unroll
+        for (int k = 0; k < kMine; k += 4) {
+            const float4 v = lds_quad(xs + (group * kMine + k) / 4 * kQuadPitch + row * 16);
+            x[k] = v.x;
+            x[k + 1] = v.y;
+            x[k + 2] = v.z;
+            x[k + 3] = v.w;
+        }
+    }
+    if (t < C) {
+        s1 = s2 = 0.0f;
+        for (int w = 0; w < kSmallThreads / 32; ++w) {
+            s1 += sums[w].x;
+            s2 += sums[w].y;
+        }
+        st_cluster(cluster_addr(smem_addr(&all[rank]), t), make_float2(s1, s2));
+    }
+    cluster_meet();
+    if (t == 0) {
+        s1 = s2 = 0.0f;
+        for (int k = 0; k < C; ++k) {
+            s1 += all[k].x;
+            s2 += all[k].y;
+        }
+        const bool large = s1 > 3.402823466e38f;
+        const double norm = large ? sqrt(double(s2)) * 0x1p80 : sqrt(double(s1));
+        factor[0] = large ? 0x1p-64f : 1.0f;
+        factor[1] = float(double(p.x_scale) / (norm + p.eps) * (large ? 0x1p64 : 1.0));
+    }
+    __syncthreads();
+    const uint32_t tmem = tmem_base, mine = uint32_t(quad * 32) << 16;
+    const uint32_t state = tmem + mine + kSmallCols + group * kMine;
+    const bool real = row < rows;
+    {
+        const float f0 = factor[0], f1 = factor[1];
+#pragma unroll
+        for (int c = 0; c < kMine; c += 16) {
+            float f[16];
+#pragma unroll
+            for (int k = 0; k < 16; ++k) f[k] = real && first + group * kMine + c + k < n ? x[c + k] * f0 * f1 : 0.0f;
+            tmem_st16(state + c, f);
+#pragma unroll
+            for (int k = 0; k < 16; k += 8)
+                sts128(xs + small_at(row, group * kMine + c + k), make_uint4(pack_f16(f[k], f[k + 1]), pack_f16(f[k + 2], f[k + 3]),
+                                                                            pack_f16(f[k + 4], f[k + 5]), pack_f16(f[k + 6], f[k + 7])));
+        }
+    }
+    // --- the steps ---
+    uint8_t* const out = p.out + int64_t(mat) * p.out_batch;
+    const float x_back = 1.0f / p.x_scale;
+    uint32_t round = 0;
+    bool ok = true;
+    // everybody's writes are in place, one thread issues the products, and everybody waits for them
+    auto products = [&](auto issue) {
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+        __syncthreads();
+        if (warp == 0) {
+            if (lane == 0) {
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                issue();
+                commit<false>(done);
+            }
+            __syncwarp();
+        }
+        ok = mbar_wait_bounded(done, round, kWaitNs) && ok;
+        round ^= 1;
+        __syncwarp();
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    };
+    constexpr uint32_t kFormat = 1u << 4 | uint32_t(kSmallRows / 16) << 24;
+    constexpr uint32_t kSquare = kFormat | uint32_t(kSmallRows / 8) << 17, kOnX = kFormat | uint32_t(kN / 8) << 17 | 1u << 16;
+    const uint32_t from = tmem + mine + group * 32;
+    for (int step = 0; step < p.steps; ++step) {
+        const OrthStep co = p.step[step];
+        // A, of this CTA's columns
+        products([&]() {
+#pragma unroll
+            for (int j = 0; j < K; ++j)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const uint64_t o = operand_desc(xs + j * 2 * kBoxBytes) + 2 * k;
+                    mma<false>(tmem, o, o, kSquare, j > 0 || k > 0);
+                }
+        });
+        const float a_scale = 1.0f / (p.x_scale * p.x_scale);
+        float f[32];
+        {
+            float g[16];
+#pragma unroll
+            for (int c = 0; c < 32; c += 16) {
+                tmem_ld16(from + c, g);
+#pragma unroll
+                for (int k = 0; k < 16; ++k) f[c + k] = ok ? g[k] * a_scale : __uint_as_float(0x7fffffffu);
+            }
+        }
+        if (C == 1) {
+#pragma unroll
+            for (int k = 0; k < 32; ++k)
+                if (group * 32 + k == row) {
+                    d[row] = f[k];
+                    f[k] = 0.0f;
+                }
+#pragma unroll
+            for (int k = 0; k < 32; k += 8)
+                sts128(as + small_at(row, group * 32 + k),
+                       make_uint4(pack_f16(f[k] * p.a_scale, f[k + 1] * p.a_scale), pack_f16(f[k + 2] * p.a_scale, f[k + 3] * p.a_scale),
+                                  pack_f16(f[k + 4] * p.a_scale, f[k + 5] * p.a_scale), pack_f16(f[k + 6] * p.a_scale, f[k + 7] * p.a_scale)));
+        } else {
+            // four columns of all rows are one piece; a CTA adds up 32 / C of them, in the CTAs' order
+            const int each = 32 / C;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int q = group * 8 + k;
+                st_cluster(cluster_addr(ss + ((rank * each + q % each) * kSmallRows + row) * 16, q / each),
+                           make_float4(f[4 * k], f[4 * k + 1], f[4 * k + 2], f[4 * k + 3]));
+            }
+            cluster_meet();
+            for (int i = t; i < each * kSmallRows; i += kSmallThreads) {
+                const int r = i % kSmallRows, c = (rank * each + i / kSmallRows) * 4;
+                float4 v = lds_quad(ss + i * 16);
+                for (int k = 1; k < C; ++k) {
+                    const float4 w = lds_quad(ss + (k * each * kSmallRows + i) * 16);
+                    v.x += w.x;
+                    v.y += w.y;
+                    v.z += w.z;
+                    v.w += w.w;
+                }
+                if (c <= r && r < c + 4) {
+                    const float on = r == c ? v.x : r == c + 1 ? v.y : r == c + 2 ? v.z : v.w;
+                    for (int k = 0; k < C; ++k) st_cluster(cluster_addr(smem_addr(&d[r]), k), on);
+                    v.x = r == c ? 0.0f : v.x;
+                    v.y = r == c + 1 ? 0.0f : v.y;
+                    v.z = r == c + 2 ? 0.0f : v.z;
+                    v.w = r == c + 3 ? 0.0f : v.w;
+                }
+                const uint2 w = make_uint2(pack_f16(v.x * p.a_scale, v.y * p.a_scale), pack_f16(v.z * p.a_scale, v.w * p.a_scale));
+                const uint32_t at = as + small_at(r, c) + c % 8 * 2;
+                for (int k = 0; k < C; ++k) st_cluster(cluster_addr(at, k), w);
+            }
+            asm volatile("fence.proxy.async;" ::: "memory");
+            cluster_meet();
+        }
+        // A0^2, and B in A's place
+        products([&]() {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const uint64_t o = operand_desc(as + k / 4 * 2 * kBoxBytes) + 2 * (k % 4);
+                mma<false>(tmem, o, o, kSquare, k > 0);
+            }
+        });
+        {
+            const float back = 1.0f / p.a_scale, cs = co.c * back * back, dr = d[row], bc = fmaf(co.c, dr, co.b);
+#pragma unroll
+            for (int c = 0; c < 32; c += 16) {
+                float g[16];
+                tmem_ld16(from + c, g);
+#pragma unroll
+                for (int k = 0; k < 16; k += 8) {
+                    const int col = group * 32 + c + k;
+                    const uint32_t at = as + small_at(row, col);
+                    const uint4 a = lds128(at);
+                    const uint32_t aw[4] = {a.x, a.y, a.z, a.w};
+                    float v[8];
+#pragma unroll
+                    for (int h = 0; h < 8; ++h) {
+                        const float2 a2 = __half22float2(*reinterpret_cast<const __half2*>(&aw[h / 2]));
+                        v[h] = fmaf(fmaf(co.c, d[col + h], bc), (h & 1 ? a2.y : a2.x) * back, cs * g[k + h]) * co.scale;
+                        if (col + h == row) {
+                            // (A0 is zero there)
+                            e[row] = fmaf(cs, g[k + h], dr * bc);
+                            v[h] = 0.0f;
+                        }
+                    }
+                    sts128(at, make_uint4(pack_f16(v[0], v[1]), pack_f16(v[2], v[3]), pack_f16(v[4], v[5]), pack_f16(v[6], v[7])));
+                }
+            }
+        }
+        // X
+        products([&]() {
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                mma<false>(tmem, operand_desc(as + k / 4 * 2 * kBoxBytes) + 2 * (k % 4),
+                           small_desc(xs + k / 4 * kBoxBytes) + (2048 >> 4) * (k % 4), kOnX, k > 0);
+        });
+        const float back = 1.0f / co.scale, keep = co.a + e[row];
+#pragma unroll
+        for (int c = 0; c < kMine; c += 16) {
+            float g[16], h[16];
+            tmem_ld16(tmem + mine + group * kMine + c, g);
+            tmem_ld16(state + c, h);
+#pragma unroll
+            for (int k = 0; k < 16; ++k) g[k] = fmaf(keep, h[k], g[k] * back);
+            if (step < p.steps - 1) {
+                tmem_st16(state + c, g);
+#pragma unroll
+                for (int k = 0; k < 16; k += 8)
+                    sts128(xs + small_at(row, group * kMine + c + k), make_uint4(pack_f16(g[k], g[k + 1]), pack_f16(g[k + 2], g[k + 3]),
+                                                                                pack_f16(g[k + 4], g[k + 5]), pack_f16(g[k + 6], g[k + 7])));
+                continue;
+            }
+            // --- the output ---
+#pragma unroll
+            for (int k = 0; k < 16; ++k) g[k] = ok ? g[k] * x_back : __uint_as_float(0x7fffffffu);
+            if (p.turned) {
+#pragma unroll
+                for (int k = 0; k < 16; ++k) {
+                    const int64_t to = first + group * kMine + c + k;
+                    if (real && to < n) reinterpret_cast<__nv_bfloat16*>(out + to * p.out_pitch)[row] = __float2bfloat16_rn(g[k]);
+                }
+            } else {
+                // the operands have been read: their place is staging again
+#pragma unroll
+                for (int k = 0; k < 16; k += 4)
+                    sts128(xs + (group * kMine + c + k) / 4 * kQuadPitch + row * 16,
+                           make_uint4(__float_as_uint(g[k]), __float_as_uint(g[k + 1]), __float_as_uint(g[k + 2]), __float_as_uint(g[k + 3])));
+            }
+        }
+    }
+    if (!p.turned) {
+        __syncthreads();
+        for (int i = warp; i < kN / 32 * (kSmallRows / 4); i += kSmallThreads / 32) {
+            const int q = i % (kN / 32) * 8 + lane % 8, r = i / (kN / 32) * 4 + lane / 8;
+            const int64_t c = first + q * 4;
+            if (r >= rows || c >= n) continue;
+            const float4 v = lds_quad(xs + q * kQuadPitch + r * 16);
+            __nv_bfloat16* o = reinterpret_cast<__nv_bfloat16*>(out + r * p.out_pitch) + c;
+            if (p.out_wide && c + 4 <= n) {
+                *reinterpret_cast<uint2*>(o) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+            } else {
+                o[0] = __float2bfloat16_rn(v.x);
+                if (c + 1 < n) o[1] = __float2bfloat16_rn(v.y);
+                if (c + 2 < n) o[2] = __float2bfloat16_rn(v.z);
+                if (c + 3 < n) o[3] = __float2bfloat16_rn(v.w);
+            }
+        }
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if (warp == 0) {
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+    }
+}
+
 // --- host -------------------------------------------------------------------------
 
 constexpr int64_t al(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
@@ -1040,6 +1460,41 @@ cudaError_t launch_products(int device, OrthParams& p, const Plan& q, cudaStream
     return cudaLaunchKernelEx(&c, orth_product_kernel<PAIR>, p);
 }
 
+// CTAs and columns over 64 of each that a small matrix takes (0: it is not one).
+struct Small {
+    int ctas, blocks;
+};
+Small small_of(int64_t m, int64_t n) {
+    if (m > kSmallRows || n > kSmallCols * kSmallCtas) return {0, 0};
+    int c = 1;
+    while (int64_t(c) * kSmallCols < n) c *= 2;
+    return {c, int((n + c * 64 - 1) / (c * 64))};
+}
+template <int K>
+cudaError_t launch_small(const SmallParams& p, int64_t batch, cudaStream_t s) {
+    static bool ready[kOpsMaxDevices];
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess && !ready[dev]) {
+        e = cudaFuncSetAttribute(orth_small_kernel<K>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmallSmem);
+        ready[dev] = e == cudaSuccess;
+    }
+    if (e != cudaSuccess) return e;
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = unsigned(p.ctas);
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cudaLaunchConfig_t c{};
+    c.gridDim = dim3(unsigned(batch * p.ctas));
+    c.blockDim = dim3(kSmallThreads);
+    c.dynamicSmemBytes = kSmallSmem;
+    c.stream = s;
+    c.attrs = &attr;
+    c.numAttrs = 1;
+    cudaGetLastError();
+    return cudaLaunchKernelEx(&c, orth_small_kernel<K>, p);
+}
+
 // Checks of one array of matrices; the whole of it as one span.
 lc_status check_mats(const char* call, const char* name, const lc_mats* a, int64_t batch, int64_t rows, int64_t cols, bool out,
                      Span2* span) {
@@ -1076,6 +1531,7 @@ using namespace lc;
 
 extern "C" uint64_t lc_orthogonalize_workspace(int64_t batch, int64_t rows, int64_t cols) {
     if (!orth_sizes(batch, rows, cols) || batch == 0) return 0;
+    if (small_of(rows < cols ? rows : cols, rows < cols ? cols : rows).ctas) return 0;
     return uint64_t(plan_of(batch, rows, cols).bytes);
 }
 
@@ -1120,7 +1576,8 @@ extern "C" lc_status lc_orthogonalize(int device, void* cuda_stream, const lc_ma
     // elements of about 1 where the matrix has no structure: sqrt(m n) times those of X
     const float middle = float(std::ldexp(1.0, std::ilogb(std::sqrt(double(q.m) * double(q.n)))));
     if (middle < p.x_scale) p.x_scale = middle;
-    const uint64_t need = batch ? uint64_t(q.bytes) : 0;
+    const Small small = small_of(q.m, q.n);
+    const uint64_t need = lc_orthogonalize_workspace(batch, rows, cols);
     if (workspace_bytes < need)
         return fail_status(LC_ERR_CAPACITY, "%s: %llu bytes of workspace, %llu needed", call, (unsigned long long)workspace_bytes,
                            (unsigned long long)need);
@@ -1162,6 +1619,35 @@ extern "C" lc_status lc_orthogonalize(int device, void* cuda_stream, const lc_ma
     a.turned = q.turned;
     a.bm = int32_t(q.bm);
     a.bn = int32_t(q.bn);
+    if (small.ctas) {
+        SmallParams o{};
+        o.u = a.u;
+        o.u_pitch = a.u_pitch;
+        o.u_batch = a.u_batch;
+        o.m = a.m;
+        o.m_pitch = a.m_pitch;
+        o.m_batch = a.m_batch;
+        o.out = static_cast<uint8_t*>(out->data);
+        o.out_pitch = out->stride * 2;
+        o.out_batch = out->batch_stride * 2;
+        o.rows = rows;
+        o.cols = cols;
+        o.eps = eps;
+        o.beta = float(beta);
+        o.x_scale = p.x_scale;
+        o.a_scale = p.a_scale;
+        o.ctas = small.ctas;
+        o.u_bf16 = a.u_bf16;
+        o.nesterov = a.nesterov;
+        o.turned = a.turned;
+        o.steps = steps;
+        o.wide = a.wide;
+        o.out_wide = rows_wide(o.out, rows > 1 ? o.out_pitch : 0, batch > 1 ? o.out_batch : 0);
+        for (int k = 0; k < steps; ++k) o.step[k] = p.step[k];
+        cudaError_t (*const launch[])(const SmallParams&, int64_t, cudaStream_t) = {launch_small<1>, launch_small<2>, launch_small<3>,
+                                                                                   launch_small<4>};
+        return ops_launched(call, launch[small.blocks - 1](o, batch, s));
+    }
     PrepParams flat = a;
     if (update->stride == cols && (!momentum || momentum->stride == cols)) {
         flat.rows = 1;

@@ -65,15 +65,17 @@ def test_refusals_before_the_device(abi):
     says(b"overlap", b=2, o=mats(batch=95, stride=96 * 2))
     says(b"grow", coef=(17.0, 0.0, 0.0))
     says(b"coefficients", coef=(float("inf"), 0.0, 0.0))
-    says(b"workspace", size=16)
-    says(b"256-byte", ws=8192 + 16)
+    says(b"workspace", m=640, size=16, n=96 * 8, u=mats(stride=768), o=mats(1 << 30, stride=768))
+    says(b"256-byte", m=640, n=96 * 8, u=mats(stride=768), o=mats(1 << 30, stride=768), ws=8192 + 16)
 
 
 def test_workspace(abi):
     """Room for X in fp32 and twice in fp16, and for A in fp32, A and B in fp16, padded to whole tiles; none for sizes that
     are refused."""
     size = abi.load().lc_orthogonalize_workspace
-    for b, m, n in ((1, 1, 1), (1, 256, 256), (8, 1024, 256), (1, 4096, 14336), (3, 515, 1023)):
+    for b, m, n in ((1, 1, 1), (5, 128, 2048), (1, 100, 20)):
+        assert size(b, m, n) == size(b, n, m) == 0            # small ones stay in a cluster's memory
+    for b, m, n in ((1, 129, 129), (1, 128, 2049), (1, 256, 256), (8, 1024, 256), (1, 4096, 14336), (3, 515, 1023)):
         lo, hi = sorted((m, n))
         assert size(b, m, n) >= b * 8 * (lo * hi + lo * lo)
         assert size(b, m, n) == size(b, n, m)
