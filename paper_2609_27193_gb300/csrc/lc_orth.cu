@@ -361,20 +361,21 @@ struct Finish {
 #pragma unroll
             for (int m = 0; m < 8; ++m) f[m] *= scale;
             if (diagonal) {
+                float on = 0.0f;
 #pragma unroll
-                for (int m = 0; m < 8; ++m)
-                    if (col + m == gr) {
-                        __stcg(p.d + diag + gr, f[m]);
-                        f[m] = 0.0f;
-                    }
+                for (int m = 0; m < 8; ++m) {
+                    on = col + m == gr ? f[m] : on;
+                    f[m] = col + m == gr ? 0.0f : f[m];
+                }
+                if (col <= gr && gr < col + 8) __stcg(p.d + diag + gr, on);
             }
             sc = p.a_scale;
         } else if (phase == 1) {
             // b A0 + c (A0^2 + (d_i + d_j) A0)
-            float on[8];
+            float on = 0.0f;
             if (diagonal) {
 #pragma unroll
-                for (int m = 0; m < 8; ++m) on[m] = f[m];
+                for (int m = 0; m < 8; ++m) on = col + m == gr ? f[m] : on;
             }
             const float bc = fmaf(co.c, dr, co.b);
 #pragma unroll
@@ -384,12 +385,9 @@ struct Finish {
             }
             if (diagonal) {
 #pragma unroll
-                for (int m = 0; m < 8; ++m)
-                    if (col + m == gr) {
-                        // (A0 is zero there)
-                        __stcg(p.e + diag + gr, fmaf(cs, on[m], dr * bc));
-                        f[m] = 0.0f;
-                    }
+                for (int m = 0; m < 8; ++m) f[m] = col + m == gr ? 0.0f : f[m];
+                // (A0 is zero there)
+                if (col <= gr && gr < col + 8) __stcg(p.e + diag + gr, fmaf(cs, on, dr * bc));
             }
             sc = co.scale;
         } else {
@@ -647,7 +645,6 @@ __global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                 __syncwarp();
                 if (lane == 0) arrive_at(first_taken + 8 * acc.at);
-                __threadfence();
                 asm volatile("bar.sync 1, %0;" ::"n"(kSumWarps * 32) : "memory");
                 uint32_t* arrived = p.arrived + ((phase * p.tiles + w.tile) * kCtas + rank);
                 if (t == 0) asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(arrived) : "memory");
@@ -683,8 +680,7 @@ __global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_
             if (!ok) break;
             if (!final) {
                 if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
-                asm volatile("fence.proxy.async.global;" ::: "memory");
-                __threadfence();
+                if (splits > 1) asm volatile("fence.proxy.async.global;" ::: "memory");   // (those store operands themselves)
                 asm volatile("bar.sync 1, %0;" ::"n"(kSumWarps * 32) : "memory");
                 if (t == 0) asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(p.count) : "memory");
             }
@@ -891,12 +887,13 @@ __global__ void __launch_bounds__(256) orth_split_kernel(PrepParams p) {
 
 // Up to 128 rows: a cluster has a matrix, each CTA up to 256 of its columns for the whole call, from the
 // update to the output.  X lies in tensor memory in fp32 and in shared memory as operand.  A step needs the
-// other CTAs once: their parts of A are added up, each CTA a share of the columns, through the cluster's shared
+// other CTAs once: their parts of A are added up, each CTA a share of the rows, through the cluster's shared
 // memory, and A goes to all; A^2 is computed by each (128 x 128 x 128 takes less than sending it).
 constexpr int kSmallRows = 128, kSmallCols = 256, kSmallThreads = 512, kSmallCtas = 8;
 constexpr int kQuadPitch = kSmallRows * 16 + 16;   // of fp32 staging: four columns of all rows; 16 more keep eight quads of a row in eight banks
 // X's operand, A's, and the other CTAs' sums; staging lies over them
-constexpr int kSmallX = kSmallRows * kSmallCols * 2, kSmallA = kSmallRows * kSmallRows * 2, kSmallSums = kSmallRows * kSmallRows * 4;
+constexpr int kSmallX = kSmallRows * kSmallCols * 2, kSmallA = kSmallRows * kSmallRows * 2;
+constexpr int kSmallSums = kSmallRows * kSmallRows * 4 + kSmallCtas * 32 * 16;
 constexpr int kSmallSmem = kSmallX + kSmallA + kSmallSums + 1024;
 static_assert(kSmallCols / 4 * kQuadPitch <= kSmallX + kSmallA + kSmallSums, "staging");
 
@@ -932,8 +929,8 @@ __device__ __forceinline__ void st_cluster(uint32_t addr, const float4& v) {
 __device__ __forceinline__ void st_cluster(uint32_t addr, const float2& v) {
     asm volatile("st.shared::cluster.v2.f32 [%0], {%1,%2};" ::"r"(addr), "f"(v.x), "f"(v.y) : "memory");
 }
-__device__ __forceinline__ void st_cluster(uint32_t addr, const uint2& v) {
-    asm volatile("st.shared::cluster.v2.u32 [%0], {%1,%2};" ::"r"(addr), "r"(v.x), "r"(v.y) : "memory");
+__device__ __forceinline__ void st_cluster(uint32_t addr, const uint4& v) {
+    asm volatile("st.shared::cluster.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
 __device__ __forceinline__ void st_cluster(uint32_t addr, float v) {
     asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
@@ -961,6 +958,30 @@ __device__ __forceinline__ float4 load_quad(const uint8_t* row, bool bf16, bool 
                        c + 2 < cols ? element(row, bf16, c + 2) : 0.0f, c + 3 < cols ? element(row, bf16, c + 3) : 0.0f);
 }
 
+__device__ __forceinline__ void sts_quad(uint32_t addr, const float4& v) {
+    sts128(addr, make_uint4(__float_as_uint(v.x), __float_as_uint(v.y), __float_as_uint(v.z), __float_as_uint(v.w)));
+}
+// Four by four values and their transpose.
+__device__ __forceinline__ void turn(float4 (&v)[4]) {
+    const float4 a = v[0], b = v[1], c = v[2], d = v[3];
+    v[0] = make_float4(a.x, b.x, c.x, d.x);
+    v[1] = make_float4(a.y, b.y, c.y, d.y);
+    v[2] = make_float4(a.z, b.z, c.z, d.z);
+    v[3] = make_float4(a.w, b.w, c.w, d.w);
+}
+// Four values of an output's row of `cols` from c.
+__device__ __forceinline__ void store_quad(uint8_t* row, bool wide, int64_t c, int64_t cols, const float4& v) {
+    __nv_bfloat16* o = reinterpret_cast<__nv_bfloat16*>(row) + c;
+    if (wide && c + 4 <= cols) {
+        *reinterpret_cast<uint2*>(o) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+        return;
+    }
+    if (c < cols) o[0] = __float2bfloat16_rn(v.x);
+    if (c + 1 < cols) o[1] = __float2bfloat16_rn(v.y);
+    if (c + 2 < cols) o[2] = __float2bfloat16_rn(v.z);
+    if (c + 3 < cols) o[3] = __float2bfloat16_rn(v.w);
+}
+
 // K: a CTA's columns over 64.
 template <int K>
 __global__ void __launch_bounds__(kSmallThreads, 1) orth_small_kernel(const __grid_constant__ SmallParams p) {
@@ -982,46 +1003,69 @@ __global__ void __launch_bounds__(kSmallThreads, 1) orth_small_kernel(const __gr
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem_base)), "r"(512) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    // (the others' shared memory is written once they have started)
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
     // --- the update, and its norm ---
     const uint8_t* u = p.u + int64_t(mat) * p.u_batch;
     uint8_t* m = p.m ? p.m + int64_t(mat) * p.m_batch : nullptr;
     const int64_t first = int64_t(rank) * kN;    // X's first column here
     const int64_t n = p.turned ? p.rows : p.cols;
     const int rows = int(p.turned ? p.cols : p.rows);
-    auto updated = [&](float v, float& mom) {
-        mom = fmaf(1.0f - p.beta, v - mom, mom);
-        return p.nesterov ? fmaf(p.beta, mom - v, v) : mom;
+    float s1 = 0.0f, s2 = 0.0f;
+    auto count = [&](const float4& f) {
+        for (float v : {f.x, f.y, f.z, f.w}) {
+            s1 = fmaf(v, v, s1);
+            v *= 0x1p-80f;
+            s2 = fmaf(v, v, s2);
+        }
     };
-    float x[kMine], s1 = 0.0f, s2 = 0.0f;
-    auto count = [&](float v) {
-        s1 = fmaf(v, v, s1);
-        v *= 0x1p-80f;
-        s2 = fmaf(v, v, s2);
+    // values c .. c + 3 of a row of `cols` move its momentum and become what comes of it
+    auto move = [&](float* at, int64_t c, int64_t cols, float4& v) {
+        float4 w = load_quad(reinterpret_cast<const uint8_t*>(at), false, p.wide, c, cols);
+        auto one = [&](float& x, float& mom) {
+            mom = fmaf(1.0f - p.beta, x - mom, mom);
+            x = p.nesterov ? fmaf(p.beta, mom - x, x) : mom;
+        };
+        one(v.x, w.x);
+        one(v.y, w.y);
+        one(v.z, w.z);
+        one(v.w, w.w);
+        at += c;
+        if (p.wide && c + 4 <= cols) {
+            *reinterpret_cast<float4*>(at) = w;
+        } else {
+            at[0] = w.x;
+            if (c + 1 < cols) at[1] = w.y;
+            if (c + 2 < cols) at[2] = w.z;
+            if (c + 3 < cols) at[3] = w.w;
+        }
     };
+    // through shared memory to a row a lane
     if (p.turned) {
-        // a lane's row is a column of the update
+        // a row of the update is a column of X: a lane has four neighbours of four of them
+        for (int q = warp; q < kN / 4; q += kSmallThreads / 32) {
+            const int r = lane * 4;
+            float4 v[4];
 #pragma unroll
-        for (int k = 0; k < kMine; ++k) {
-            const int64_t c = first + group * kMine + k;
-            const bool in = row < rows && c < n;
-            x[k] = in ? element(u + c * p.u_pitch, p.u_bf16, row) : 0.0f;
-        }
-        if (m) {
-#pragma unroll
-            for (int k = 0; k < kMine; ++k) {
-                const int64_t c = first + group * kMine + k;
-                if (row < rows && c < n) {
-                    float* at = reinterpret_cast<float*>(m + c * p.m_pitch) + row;
-                    float v = *at;
-                    x[k] = updated(x[k], v);
-                    *at = v;
-                }
+            for (int k = 0; k < 4; ++k) {
+                const int64_t c = first + q * 4 + k;
+                v[k] = c < n ? load_quad(u + c * p.u_pitch, p.u_bf16, p.wide, r, rows) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
             }
-        }
+            if (m) {
 #pragma unroll
-        for (int k = 0; k < kMine; ++k) count(x[k]);
+                for (int k = 0; k < 4; ++k)
+                    if (first + q * 4 + k < n && r < rows) move(reinterpret_cast<float*>(m + (first + q * 4 + k) * p.m_pitch), r, rows, v[k]);
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) count(v[k]);
+            turn(v);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) sts_quad(xs + q * kQuadPitch + (r + k) * 16, v[k]);
+        }
     } else {
-        // eight lanes a row, four rows a warp; through shared memory to a row a lane
+        // eight lanes a row, four rows a warp
 #pragma unroll 4
         for (int i = warp; i < kN / 32 * (kSmallRows / 4); i += kSmallThreads / 32) {
             const int q = i % (kN / 32) * 8 + lane % 8, r = i / (kN / 32) * 4 + lane / 8;
@@ -1029,28 +1073,10 @@ __global__ void __launch_bounds__(kSmallThreads, 1) orth_small_kernel(const __gr
             float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
             if (r < rows && c < n) {
                 v = load_quad(u + r * p.u_pitch, p.u_bf16, p.wide, c, n);
-                if (m) {
-                    float* at = reinterpret_cast<float*>(m + r * p.m_pitch) + c;
-                    float4 w = load_quad(reinterpret_cast<const uint8_t*>(at - c), false, p.wide, c, n);
-                    v.x = updated(v.x, w.x);
-                    v.y = updated(v.y, w.y);
-                    v.z = updated(v.z, w.z);
-                    v.w = updated(v.w, w.w);
-                    if (p.wide && c + 4 <= n) {
-                        *reinterpret_cast<float4*>(at) = w;
-                    } else {
-                        at[0] = w.x;
-                        if (c + 1 < n) at[1] = w.y;
-                        if (c + 2 < n) at[2] = w.z;
-                        if (c + 3 < n) at[3] = w.w;
-                    }
-                }
-                count(v.x);
-                count(v.y);
-                count(v.z);
-                count(v.w);
+                if (m) move(reinterpret_cast<float*>(m + r * p.m_pitch), c, n, v);
+                count(v);
             }
-            sts128(xs + q * kQuadPitch + r * 16, make_uint4(__float_as_uint(v.x), __float_as_uint(v.y), __float_as_uint(v.z), __float_as_uint(v.w)));
+            sts_quad(xs + q * kQuadPitch + r * 16, v);
         }
     }
 #pragma unroll
@@ -1060,16 +1086,17 @@ __global__ void __launch_bounds__(kSmallThreads, 1) orth_small_kernel(const __gr
     }
     if (lane == 0) sums[warp] = make_float2(s1, s2);
     __syncthreads();
-    if (!p.turned) {
+    float x[kMine];
 #pragma unroll
-        for (int k = 0; k < kMine; k += 4) {
-            const float4 v = lds_quad(xs + (group * kMine + k) / 4 * kQuadPitch + row * 16);
-            x[k] = v.x;
-            x[k + 1] = v.y;
-            x[k + 2] = v.z;
-            x[k + 3] = v.w;
-        }
+    for (int k = 0; k < kMine; k += 4) {
+        const float4 v = lds_quad(xs + (group * kMine + k) / 4 * kQuadPitch + row * 16);
+        x[k] = v.x;
+        x[k + 1] = v.y;
+        x[k + 2] = v.z;
+        x[k + 3] = v.w;
     }
+    __syncwarp();
+    asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
     if (t < C) {
         s1 = s2 = 0.0f;
         for (int w = 0; w < kSmallThreads / 32; ++w) {
@@ -1091,6 +1118,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) orth_small_kernel(const __gr
         factor[1] = float(double(p.x_scale) / (norm + p.eps) * (large ? 0x1p64 : 1.0));
     }
     __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = tmem_base, mine = uint32_t(quad * 32) << 16;
     const uint32_t state = tmem + mine + kSmallCols + group * kMine;
     const bool real = row < rows;
@@ -1146,60 +1174,72 @@ __global__ void __launch_bounds__(kSmallThreads, 1) orth_small_kernel(const __gr
                     mma<false>(tmem, o, o, kSquare, j > 0 || k > 0);
                 }
         });
-        const float a_scale = 1.0f / (p.x_scale * p.x_scale);
+        // A as its operand, times a_scale; the diagonal (in the warps whose columns are their rows) by itself
+        const bool diagonal = group == quad;
+        const float to_a = p.a_scale / (p.x_scale * p.x_scale), nan = __uint_as_float(0x7fffffffu);
         float f[32];
-        {
+#pragma unroll
+        for (int c = 0; c < 32; c += 16) {
             float g[16];
+            tmem_ld16(from + c, g);
 #pragma unroll
-            for (int c = 0; c < 32; c += 16) {
-                tmem_ld16(from + c, g);
+            for (int k = 0; k < 16; ++k) f[c + k] = g[k];
+        }
+        if (!ok) {
 #pragma unroll
-                for (int k = 0; k < 16; ++k) f[c + k] = ok ? g[k] * a_scale : __uint_as_float(0x7fffffffu);
-            }
+            for (int k = 0; k < 32; ++k) f[k] = nan;
         }
         if (C == 1) {
+            if (diagonal) {
+                float on = 0.0f;
 #pragma unroll
-            for (int k = 0; k < 32; ++k)
-                if (group * 32 + k == row) {
-                    d[row] = f[k];
-                    f[k] = 0.0f;
+                for (int k = 0; k < 32; ++k) {
+                    on = k == lane ? f[k] : on;
+                    f[k] = k == lane ? 0.0f : f[k];
                 }
-#pragma unroll
-            for (int k = 0; k < 32; k += 8)
-                sts128(as + small_at(row, group * 32 + k),
-                       make_uint4(pack_f16(f[k] * p.a_scale, f[k + 1] * p.a_scale), pack_f16(f[k + 2] * p.a_scale, f[k + 3] * p.a_scale),
-                                  pack_f16(f[k + 4] * p.a_scale, f[k + 5] * p.a_scale), pack_f16(f[k + 6] * p.a_scale, f[k + 7] * p.a_scale)));
-        } else {
-            // four columns of all rows are one piece; a CTA adds up 32 / C of them, in the CTAs' order
-            const int each = 32 / C;
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const int q = group * 8 + k;
-                st_cluster(cluster_addr(ss + ((rank * each + q % each) * kSmallRows + row) * 16, q / each),
-                           make_float4(f[4 * k], f[4 * k + 1], f[4 * k + 2], f[4 * k + 3]));
+                d[row] = on * to_a;
             }
+#pragma unroll
+            for (int k = 0; k < 32; k += 8) {
+                uint32_t w[4];
+#pragma unroll
+                for (int h = 0; h < 4; ++h) {
+                    const float2 v = mul2(make_float2(f[k + 2 * h], f[k + 2 * h + 1]), both(to_a));
+                    w[h] = pack_f16(v.x, v.y);
+                }
+                sts128(as + small_at(row, group * 32 + k), make_uint4(w[0], w[1], w[2], w[3]));
+            }
+        } else {
+            // a CTA adds up 128 / C rows, in the CTAs' order; four columns of these rows are one piece (and 16 bytes more,
+            // so that pieces of a row lie in different banks)
+            const int each = kSmallRows / C, pitch = each * 16 + 16;
+            const uint32_t to = cluster_addr(ss + rank * 32 * pitch + row % each * 16, row / each);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) st_cluster(to + (group * 8 + k) * pitch, make_float4(f[4 * k], f[4 * k + 1], f[4 * k + 2], f[4 * k + 3]));
             cluster_meet();
-            for (int i = t; i < each * kSmallRows; i += kSmallThreads) {
-                const int r = i % kSmallRows, c = (rank * each + i / kSmallRows) * 4;
-                float4 v = lds_quad(ss + i * 16);
-                for (int k = 1; k < C; ++k) {
-                    const float4 w = lds_quad(ss + (k * each * kSmallRows + i) * 16);
-                    v.x += w.x;
-                    v.y += w.y;
-                    v.z += w.z;
-                    v.w += w.w;
+            for (int i = t; i < each * 16; i += kSmallThreads) {
+                // eight columns of a row, eight neighbours of which a lane group sends on as 128 bytes
+                const int r = i / 16, c = i % 16 * 8, full = rank * each + r;
+                float v[8] = {};
+                for (int k = 0; k < C; ++k) {
+                    const uint32_t at = ss + (k * 32 + c / 4) * pitch + r * 16;
+                    const float4 a = lds_quad(at), b = lds_quad(at + pitch);
+                    v[0] += a.x, v[1] += a.y, v[2] += a.z, v[3] += a.w;
+                    v[4] += b.x, v[5] += b.y, v[6] += b.z, v[7] += b.w;
                 }
-                if (c <= r && r < c + 4) {
-                    const float on = r == c ? v.x : r == c + 1 ? v.y : r == c + 2 ? v.z : v.w;
-                    for (int k = 0; k < C; ++k) st_cluster(cluster_addr(smem_addr(&d[r]), k), on);
-                    v.x = r == c ? 0.0f : v.x;
-                    v.y = r == c + 1 ? 0.0f : v.y;
-                    v.z = r == c + 2 ? 0.0f : v.z;
-                    v.w = r == c + 3 ? 0.0f : v.w;
+                float on = 0.0f;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    v[k] *= to_a;
+                    on = c + k == full ? v[k] : on;
+                    v[k] = c + k == full ? 0.0f : v[k];
                 }
-                const uint2 w = make_uint2(pack_f16(v.x * p.a_scale, v.y * p.a_scale), pack_f16(v.z * p.a_scale, v.w * p.a_scale));
-                const uint32_t at = as + small_at(r, c) + c % 8 * 2;
-                for (int k = 0; k < C; ++k) st_cluster(cluster_addr(at, k), w);
+                const uint4 w = make_uint4(pack_f16(v[0], v[1]), pack_f16(v[2], v[3]), pack_f16(v[4], v[5]), pack_f16(v[6], v[7]));
+                const uint32_t at = as + small_at(full, c), d_at = smem_addr(&d[full]);
+                for (int k = 0; k < C; ++k) {
+                    st_cluster(cluster_addr(at, k), w);
+                    if (c / 8 == full / 8) st_cluster(cluster_addr(d_at, k), on);
+                }
             }
             asm volatile("fence.proxy.async;" ::: "memory");
             cluster_meet();
@@ -1213,29 +1253,40 @@ __global__ void __launch_bounds__(kSmallThreads, 1) orth_small_kernel(const __gr
             }
         });
         {
-            const float back = 1.0f / p.a_scale, cs = co.c * back * back, dr = d[row], bc = fmaf(co.c, dr, co.b);
+            // b A0 + c (A0^2 + (d_i + d_j) A0), times B's scale; here A0, d and A0^2 are times a_scale (A0^2 twice)
+            const float back = 1.0f / p.a_scale, dr = d[row], to_b = co.c * back * back * co.scale;
+            const float2 cs = both(to_b), bc = both(fmaf(to_b, dr, co.b * back * co.scale));
 #pragma unroll
             for (int c = 0; c < 32; c += 16) {
                 float g[16];
                 tmem_ld16(from + c, g);
+                if (diagonal) {
+                    // (A0 is zero there)
+                    float on = 0.0f;
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) {
+                        on = c + k == lane ? g[k] : on;
+                        g[k] = c + k == lane ? 0.0f : g[k];
+                    }
+                    const float dt = dr * back;
+                    if (lane / 16 == c / 16) e[row] = fmaf(co.c * back * back, on, dt * fmaf(co.c, dt, co.b));
+                }
 #pragma unroll
                 for (int k = 0; k < 16; k += 8) {
                     const int col = group * 32 + c + k;
                     const uint32_t at = as + small_at(row, col);
                     const uint4 a = lds128(at);
                     const uint32_t aw[4] = {a.x, a.y, a.z, a.w};
-                    float v[8];
+                    const float4 d0 = *reinterpret_cast<const float4*>(d + col), d1 = *reinterpret_cast<const float4*>(d + col + 4);
+                    const float2 dj[4] = {make_float2(d0.x, d0.y), make_float2(d0.z, d0.w), make_float2(d1.x, d1.y), make_float2(d1.z, d1.w)};
+                    uint32_t w[4];
 #pragma unroll
-                    for (int h = 0; h < 8; ++h) {
-                        const float2 a2 = __half22float2(*reinterpret_cast<const __half2*>(&aw[h / 2]));
-                        v[h] = fmaf(fmaf(co.c, d[col + h], bc), (h & 1 ? a2.y : a2.x) * back, cs * g[k + h]) * co.scale;
-                        if (col + h == row) {
-                            // (A0 is zero there)
-                            e[row] = fmaf(cs, g[k + h], dr * bc);
-                            v[h] = 0.0f;
-                        }
+                    for (int h = 0; h < 4; ++h) {
+                        const float2 a2 = __half22float2(*reinterpret_cast<const __half2*>(&aw[h]));
+                        const float2 v = fma2(fma2(cs, dj[h], bc), a2, mul2(cs, make_float2(g[k + 2 * h], g[k + 2 * h + 1])));
+                        w[h] = pack_f16(v.x, v.y);
                     }
-                    sts128(at, make_uint4(pack_f16(v[0], v[1]), pack_f16(v[2], v[3]), pack_f16(v[4], v[5]), pack_f16(v[6], v[7])));
+                    sts128(at, make_uint4(w[0], w[1], w[2], w[3]));
                 }
             }
         }
@@ -1253,7 +1304,11 @@ __global__ void __launch_bounds__(kSmallThreads, 1) orth_small_kernel(const __gr
             tmem_ld16(tmem + mine + group * kMine + c, g);
             tmem_ld16(state + c, h);
 #pragma unroll
-            for (int k = 0; k < 16; ++k) g[k] = fmaf(keep, h[k], g[k] * back);
+            for (int k = 0; k < 16; k += 2) {
+                const float2 v = fma2(both(keep), make_float2(h[k], h[k + 1]), mul2(make_float2(g[k], g[k + 1]), both(back)));
+                g[k] = v.x;
+                g[k + 1] = v.y;
+            }
             if (step < p.steps - 1) {
                 tmem_st16(state + c, g);
 #pragma unroll
@@ -1265,37 +1320,28 @@ __global__ void __launch_bounds__(kSmallThreads, 1) orth_small_kernel(const __gr
             // --- the output ---
 #pragma unroll
             for (int k = 0; k < 16; ++k) g[k] = ok ? g[k] * x_back : __uint_as_float(0x7fffffffu);
-            if (p.turned) {
+            // the operands have been read: their place is staging again
 #pragma unroll
-                for (int k = 0; k < 16; ++k) {
-                    const int64_t to = first + group * kMine + c + k;
-                    if (real && to < n) reinterpret_cast<__nv_bfloat16*>(out + to * p.out_pitch)[row] = __float2bfloat16_rn(g[k]);
-                }
-            } else {
-                // the operands have been read: their place is staging again
-#pragma unroll
-                for (int k = 0; k < 16; k += 4)
-                    sts128(xs + (group * kMine + c + k) / 4 * kQuadPitch + row * 16,
-                           make_uint4(__float_as_uint(g[k]), __float_as_uint(g[k + 1]), __float_as_uint(g[k + 2]), __float_as_uint(g[k + 3])));
-            }
+            for (int k = 0; k < 16; k += 4)
+                sts_quad(xs + (group * kMine + c + k) / 4 * kQuadPitch + row * 16, make_float4(g[k], g[k + 1], g[k + 2], g[k + 3]));
         }
     }
-    if (!p.turned) {
-        __syncthreads();
+    __syncthreads();
+    if (p.turned) {
+        for (int q = warp; q < kN / 4; q += kSmallThreads / 32) {
+            const int r = lane * 4;
+            float4 v[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] = lds_quad(xs + q * kQuadPitch + (r + k) * 16);
+            turn(v);
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (first + q * 4 + k < n) store_quad(out + (first + q * 4 + k) * p.out_pitch, p.out_wide, r, rows, v[k]);
+        }
+    } else {
         for (int i = warp; i < kN / 32 * (kSmallRows / 4); i += kSmallThreads / 32) {
             const int q = i % (kN / 32) * 8 + lane % 8, r = i / (kN / 32) * 4 + lane / 8;
-            const int64_t c = first + q * 4;
-            if (r >= rows || c >= n) continue;
-            const float4 v = lds_quad(xs + q * kQuadPitch + r * 16);
-            __nv_bfloat16* o = reinterpret_cast<__nv_bfloat16*>(out + r * p.out_pitch) + c;
-            if (p.out_wide && c + 4 <= n) {
-                *reinterpret_cast<uint2*>(o) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
-            } else {
-                o[0] = __float2bfloat16_rn(v.x);
-                if (c + 1 < n) o[1] = __float2bfloat16_rn(v.y);
-                if (c + 2 < n) o[2] = __float2bfloat16_rn(v.z);
-                if (c + 3 < n) o[3] = __float2bfloat16_rn(v.w);
-            }
+            if (r < rows) store_quad(out + r * p.out_pitch, p.out_wide, first + q * 4, n, lds_quad(xs + q * kQuadPitch + r * 16));
         }
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
