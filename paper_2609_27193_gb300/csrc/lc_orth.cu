@@ -48,7 +48,7 @@ constexpr int kSumWarp = 4, kSumWarps = 16; // the first (a multiple of 4) of th
 constexpr int kThreads = (kSumWarp + kSumWarps) * 32;
 constexpr int kChunk = 16;                  // columns that such a warp works on at a time
 constexpr int kMaxSteps = 16;
-constexpr int kNormCtas = 512;              // most partial sums of squares of a matrix
+constexpr int kNormCtas = 1216;              // most partial sums of squares of a matrix
 
 // A tile is kRows x kCols, of one CTA or of a pair of them with half of the rows each.
 template <bool PAIR>
@@ -137,6 +137,15 @@ __device__ __forceinline__ uint64_t operand_desc(uint32_t addr) {
            uint64_t(2) << 61;
 }
 
+__device__ __forceinline__ void tmem_ld8(uint32_t addr, float (&f)[8]) {
+    uint32_t r[8];
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];\n\ttcgen05.wait::ld.sync.aligned;"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                 : "r"(addr)
+                 : "memory");
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(r[i]);
+}
 __device__ __forceinline__ void tmem_ld16(uint32_t addr, float (&f)[16]) {
     uint32_t r[16];
     asm volatile(
@@ -634,17 +643,17 @@ __global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 constexpr int kPart = kCtaRows * kCols;
                 float* parts = p.part + (int64_t(w.tile) * kCtas + rank) * splits * kPart + row;
-                float* mine = parts + int64_t(w.split) * kPart + group * kWarpCols * kCtaRows;
+                float* mine = parts + int64_t(w.split) * kPart;
+                const uint32_t sums = tmem + (uint32_t(quad * 32) << 16) + acc.at * kCols;
+                // eight columns are a piece; pieces 4 s .. 4 s + 3 are split s's, and so on, one for each group of warps
 #pragma unroll 1
-                for (int c = 0; c < kWarpCols; c += kChunk) {
-                    float f[kChunk];
-                    tmem_ld16(from + acc.at * kCols + c, f);
+                for (int k = group; k < kCols / 8; k += 4) {
+                    if (k / 4 % splits == w.split) continue;
+                    float f[8];
+                    tmem_ld8(sums + k * 8, f);
 #pragma unroll
-                    for (int k = 0; k < kChunk; ++k) __stcg(mine + (c + k) * kCtaRows, f[k]);
+                    for (int m = 0; m < 8; ++m) __stcg(mine + (k * 8 + m) * kCtaRows, f[m]);
                 }
-                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                __syncwarp();
-                if (lane == 0) arrive_at(first_taken + 8 * acc.at);
                 asm volatile("bar.sync 1, %0;" ::"n"(kSumWarps * 32) : "memory");
                 uint32_t* arrived = p.arrived + ((phase * p.tiles + w.tile) * kCtas + rank);
                 if (t == 0) asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(arrived) : "memory");
@@ -657,25 +666,29 @@ __global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_
                 for (int k = w.split * 4 + group; k < kCols / 8; k += splits * 4) {
                     const int col = w.j * kCols + k * 8;
                     fin.ask<1>(col, lane);
+                    float own[8], f[8] = {};
+                    tmem_ld8(sums + k * 8, own);
                     const float* at = parts + k * 8 * kCtaRows;
-                    // four splits' loads at a time
-                    float f[8] = {};
+                    // three splits' loads at a time
 #pragma unroll 1
-                    for (int s = 0; s < splits; s += 4, at += 4 * kPart) {
-                        float g[4][8];
+                    for (int s = 0; s < splits; s += 3, at += 3 * kPart) {
+                        float g[3][8];
 #pragma unroll
-                        for (int h = 0; h < 4; ++h)
+                        for (int h = 0; h < 3; ++h)
 #pragma unroll
-                            for (int m = 0; m < 8; ++m) g[h][m] = s + h < splits ? __ldcg(at + h * kPart + m * kCtaRows) : 0.0f;
+                            for (int m = 0; m < 8; ++m) g[h][m] = s + h < splits && s + h != w.split ? __ldcg(at + h * kPart + m * kCtaRows) : 0.0f;
 #pragma unroll
-                        for (int h = 0; h < 4; ++h)
+                        for (int h = 0; h < 3; ++h)
 #pragma unroll
-                            for (int m = 0; m < 8; ++m) f[m] += g[h][m];
+                            for (int m = 0; m < 8; ++m) f[m] += s + h == w.split ? own[m] : g[h][m];
                     }
                     fin.take<1>();
                     const uint4 v = fin.piece(col, 0, f);
                     *reinterpret_cast<uint4*>(fin.out + int64_t(col / kBox) * kBoxBytes + piece_at(fin.gr % kBox, col % kBox / 8)) = v;
                 }
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) arrive_at(first_taken + 8 * acc.at);
             }
             if (!ok) break;
             if (!final) {
@@ -889,7 +902,7 @@ __global__ void __launch_bounds__(256) orth_split_kernel(PrepParams p) {
 // update to the output.  X lies in tensor memory in fp32 and in shared memory as operand.  A step needs the
 // other CTAs once: their parts of A are added up, each CTA a share of the rows, through the cluster's shared
 // memory, and A goes to all; A^2 is computed by each (128 x 128 x 128 takes less than sending it).
-constexpr int kSmallRows = 128, kSmallCols = 256, kSmallThreads = 512, kSmallCtas = 8;
+constexpr int kSmallRows = 128, kSmallCols = 256, kSmallThreads = 512, kSmallCtas = 16;
 constexpr int kQuadPitch = kSmallRows * 16 + 16;   // of fp32 staging: four columns of all rows; 16 more keep eight quads of a row in eight banks
 // X's operand, A's, and the other CTAs' sums; staging lies over them
 constexpr int kSmallX = kSmallRows * kSmallCols * 2, kSmallA = kSmallRows * kSmallRows * 2;
@@ -1361,36 +1374,53 @@ struct Plan {
     int64_t batch, m, n, bm, bn, tm, tn;
     bool pair, turned;
     int ctas;                 // of a tile
-    int64_t splits[3], items[3], parts;
+    int64_t splits[3], items[3], half, parts;   // half: tiles of A
     int64_t counters, norm, d, e, x0, x1, xf, af, sa, sb, part, bytes;
 };
 constexpr int kPairs = 76;    // pairs of CTAs that the device holds
-constexpr int64_t kPairFrom = 1024;
+
+// One way of cutting, and what it takes: a product's stages one after the other, as often as its pieces go round the
+// device, and the splits' exchange.  A stage takes 0.36 us on a pair's tile (0.30 where nothing but copies is done), 0.30
+// on a single CTA's, which does an eighth of the work.  What comes on top of each product (4.5 us: copies' latency, the
+// accumulators, the barrier) is the same for both.
+double cut(Plan& q, bool pair) {
+    q.pair = pair;
+    q.ctas = pair ? TileOf<true>::kCtas : TileOf<false>::kCtas;
+    const int64_t rows = pair ? TileOf<true>::kRows : TileOf<false>::kRows, cols = pair ? TileOf<true>::kCols : TileOf<false>::kCols;
+    const int64_t units = pair ? kPairs : 2 * kPairs;
+    const double stage = pair ? 0.36 : 0.30, exchange = pair ? 6.0 : 3.0;
+    q.tm = al(q.m, rows) / rows;
+    q.tn = al(q.n, cols) / cols;
+    q.bm = q.tm * rows / kBox;
+    q.bn = q.tn * cols / kBox;
+    const int64_t half = q.batch * q.tm * (q.tm + 1) / 2 * (rows / cols);
+    double all = 0.0;
+    for (int k = 0; k < 3; ++k) {
+        const int64_t tiles = k == 2 ? q.batch * q.tm * q.tn : half, stages = k == 0 ? q.bn : q.bm;
+        const int64_t most = k == 2 || tiles >= units ? 1 : units / tiles;
+        double best = 0.0;
+        for (int64_t s = 1; s <= most && s <= stages && s <= 32; ++s) {
+            const int64_t per = (stages + s - 1) / s;
+            const double t = double((tiles * s + units - 1) / units * per) * stage + (s > 1 ? exchange : 0.0);
+            if (s > 1 && t >= best) continue;
+            best = t;
+            q.splits[k] = (stages + per - 1) / per;
+            q.items[k] = tiles * q.splits[k];
+        }
+        all += best;
+    }
+    q.half = half;
+    return all;
+}
 
 Plan plan_of(int64_t batch, int64_t rows, int64_t cols) {
-    Plan q{};
+    Plan q{}, single{};
     q.batch = batch;
     q.turned = rows > cols;
     q.m = q.turned ? cols : rows;
     q.n = q.turned ? rows : cols;
-    q.pair = q.m >= kPairFrom;
-    q.ctas = q.pair ? 2 : 1;
-    const int64_t rows_of = q.pair ? TileOf<true>::kRows : TileOf<false>::kRows, cols_of = q.pair ? TileOf<true>::kCols : TileOf<false>::kCols;
-    const int64_t units = q.pair ? kPairs : 2 * kPairs;
-    q.tm = al(q.m, rows_of) / rows_of;
-    q.tn = al(q.n, cols_of) / cols_of;
-    q.bm = q.tm * rows_of / kBox;
-    q.bn = q.tn * cols_of / kBox;
-    const int64_t half = batch * q.tm * (q.tm + 1) / 2 * (rows_of / cols_of);
-    for (int k = 0; k < 3; ++k) {
-        const int64_t tiles = k == 2 ? batch * q.tm * q.tn : half, stages = k == 0 ? q.bn : q.bm;
-        int64_t s = k == 2 ? 1 : units / tiles;
-        if (s > stages / 16) s = stages / 16;
-        if (s < 1) s = 1;
-        const int64_t per = (stages + s - 1) / s;
-        q.splits[k] = (stages + per - 1) / per;
-        q.items[k] = tiles * q.splits[k];
-    }
+    single = q;
+    if (cut(single, false) <= cut(q, true)) q = single;
     q.parts = al(q.m * q.n, 4096) / 4096;
     if (q.parts > kNormCtas) q.parts = kNormCtas;
     int64_t at = 0;
@@ -1400,8 +1430,11 @@ Plan plan_of(int64_t batch, int64_t rows, int64_t cols) {
         return here;
     };
     const int64_t x = batch * q.bm * q.bn * kBoxBytes, sq = batch * q.bm * q.bm * kBoxBytes, diag = batch * q.bm * kBox * 4;
-    const int64_t most = q.splits[0] > q.splits[1] ? q.splits[0] : q.splits[1];
-    q.counters = take((1 + 2 * half * q.ctas) * 4);
+    const int64_t tile = q.pair ? TileOf<true>::kRows * TileOf<true>::kCols : TileOf<false>::kRows * TileOf<false>::kCols;
+    int64_t most = 0;
+    for (int k = 0; k < 2; ++k)
+        if (q.splits[k] > 1 && q.splits[k] > most) most = q.splits[k];
+    q.counters = take((1 + 2 * q.half * q.ctas) * 4);
     q.norm = take(batch * q.parts * 8);
     q.d = take(diag);
     q.e = take(diag);
@@ -1411,7 +1444,7 @@ Plan plan_of(int64_t batch, int64_t rows, int64_t cols) {
     q.af = take(2 * sq);
     q.sa = take(sq);
     q.sb = take(sq);
-    q.part = take(most > 1 ? half * most * rows_of * cols_of * 4 : 0);
+    q.part = take(q.half * most * tile * 4);
     q.bytes = at;
     return q;
 }
@@ -1523,6 +1556,7 @@ cudaError_t launch_small(const SmallParams& p, int64_t batch, cudaStream_t s) {
     cudaError_t e = cudaGetDevice(&dev);
     if (e == cudaSuccess && !ready[dev]) {
         e = cudaFuncSetAttribute(orth_small_kernel<K>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmallSmem);
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(orth_small_kernel<K>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
         ready[dev] = e == cudaSuccess;
     }
     if (e != cudaSuccess) return e;
@@ -1730,7 +1764,7 @@ extern "C" lc_status lc_orthogonalize(int device, void* cuda_stream, const lc_ma
     p.bm = int32_t(q.bm);
     p.bn = int32_t(q.bn);
     p.steps = steps;
-    p.tiles = int32_t(q.items[0] / q.splits[0]);
+    p.tiles = int32_t(q.half);
     for (int k = 0; k < 3; ++k) p.splits[k] = int32_t(q.splits[k]);
     p.turned = q.turned;
     p.wide = rows_wide(p.out, rows > 1 ? p.out_pitch : 0, batch > 1 ? p.out_batch : 0);

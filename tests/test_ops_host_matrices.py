@@ -73,9 +73,9 @@ def test_workspace(abi):
     """Room for X in fp32 and twice in fp16, and for A in fp32, A and B in fp16, padded to whole tiles; none for sizes that
     are refused."""
     size = abi.load().lc_orthogonalize_workspace
-    for b, m, n in ((1, 1, 1), (5, 128, 2048), (1, 100, 20)):
+    for b, m, n in ((1, 1, 1), (5, 128, 4096), (1, 100, 20)):
         assert size(b, m, n) == size(b, n, m) == 0            # small ones stay in a cluster's memory
-    for b, m, n in ((1, 129, 129), (1, 128, 2049), (1, 256, 256), (8, 1024, 256), (1, 4096, 14336), (3, 515, 1023)):
+    for b, m, n in ((1, 129, 129), (1, 128, 4097), (1, 256, 256), (8, 1024, 256), (1, 4096, 14336), (3, 515, 1023)):
         lo, hi = sorted((m, n))
         assert size(b, m, n) >= b * 8 * (lo * hi + lo * lo)
         assert size(b, m, n) == size(b, n, m)
