@@ -50,23 +50,22 @@ constexpr int kChunk = 16;                  // columns that such a warp works on
 constexpr int kMaxSteps = 16;
 constexpr int kNormCtas = 1216;              // most partial sums of squares of a matrix
 
-// A tile is kRows x kCols, of one CTA or of a pair of them with half of the rows each.
+// A tile is of one CTA, 128 x 64, or of a pair of them with half of the rows each, 256 x 256 or 256 x 128 (kRows x up to
+// kCols).
 template <bool PAIR>
 struct TileOf {
     static constexpr int kCtas = PAIR ? 2 : 1;
     static constexpr int kRows = kCtaRows * kCtas, kCols = PAIR ? 256 : 64;
     static constexpr int kSide = kRows / kBox;                 // boxes of a block on the diagonal
     static constexpr int kLeft = 2 * kBoxBytes;                // of a stage: the left operand, and the CTA's part of the right one
-    static constexpr int kRightBoxes = kCols / kCtas / kBox;
-    static constexpr int kStageBytes = kLeft + kRightBoxes * kBoxBytes;
+    static constexpr int kStageBytes = kLeft + kCols / kCtas / kBox * kBoxBytes;
     static constexpr int kStages = PAIR ? 5 : 8;
-    static constexpr int kWarpCols = kCols / 4;                // columns of a warp, 32 rows of them
-    static constexpr int kShare = kBox / kWarpCols;            // warps that fill half a box of staging
-    static constexpr int kStaging = kSumWarps / kShare * (kBoxBytes / 2);
+    // a warp has 32 rows of a quarter of the columns; half a box of staging for as many warps as fill 64 columns
+    static constexpr int kStaging = kSumWarps * (kCols / 4) / kBox * (kBoxBytes / 2);
     static constexpr int kSmem = kStages * kStageBytes + kStaging + 1024;   // and room to align them to 1024 bytes
     static constexpr int kTmemCols = 2 * kCols;
-    // fp32 accumulator, fp16 operands; which way their rows lie is added for each product
-    static constexpr uint32_t kIdesc = 1u << 4 | uint32_t(kCols / 8) << 17 | uint32_t(kRows / 16) << 24;
+    // fp32 accumulator, fp16 operands; columns, and which way their rows lie, are added for each product
+    static constexpr uint32_t kIdesc = 1u << 4 | uint32_t(kRows / 16) << 24;
 };
 
 struct OrthStep {
@@ -89,7 +88,8 @@ struct OrthParams {
     float x_scale, a_scale;
     int32_t batch, m, n;     // of X as it is worked on (m <= n)
     int32_t bm, bn;          // boxes of m and n
-    int32_t tiles;           // of A, of all matrices
+    int32_t tiles;           // of A, of all matrices, at most
+    int32_t cols[3];         // of a pair's tile
     int32_t steps, splits[3];  // of the reductions of A, A^2 and B X (the last always 1)
     int32_t turned;          // out is X^T
     int32_t wide;            // out takes 16-byte stores
@@ -167,15 +167,18 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
 // 16-byte piece `p` (of 8) of row r in a box.
 __device__ __forceinline__ uint32_t piece_at(int r, int p) { return uint32_t(r) * 128 + uint32_t((p ^ (r & 7)) * 16); }
 
-// One piece of a product: a tile, or a split of its reduction.  i: the block of kRows rows, j: of kCols columns, jb: the
+template <bool PAIR>
+__device__ __forceinline__ int cols_of(const OrthParams& p, int phase) { return PAIR ? p.cols[phase] : TileOf<PAIR>::kCols; }
+
+// One piece of a product: a tile, or a split of its reduction.  i: the block of kRows rows, j: of the tile's columns, jb: the
 // block on the diagonal that the columns are part of.
 struct Item {
     int mat, i, j, jb, split, s0, stages, tile;
 };
 template <bool PAIR>
 __device__ __forceinline__ Item item_of(const OrthParams& p, int phase, int at) {
-    constexpr int kIn = TileOf<PAIR>::kRows / TileOf<PAIR>::kCols;   // tiles beside one another in such a block
-    const int tm = p.bm / TileOf<PAIR>::kSide, tn = p.bn * kBox / TileOf<PAIR>::kCols;
+    const int cols = cols_of<PAIR>(p, phase), in = TileOf<PAIR>::kRows / cols;   // tiles beside one another in such a block
+    const int tm = p.bm / TileOf<PAIR>::kSide, tn = p.bn * kBox / cols;
     const int all = phase == 0 ? p.bn : p.bm, splits = p.splits[phase];
     Item w;
     const int t = at / splits;
@@ -192,24 +195,24 @@ __device__ __forceinline__ Item item_of(const OrthParams& p, int phase, int at) 
         w.i = k - w.j * tm;
         w.jb = 0;
     } else {
-        const int tiles = tm * (tm + 1) / 2 * kIn;
+        const int tiles = tm * (tm + 1) / 2 * in;
         w.mat = t / tiles;
-        const int k = (t - w.mat * tiles) / kIn;
+        const int k = (t - w.mat * tiles) / in;
         // block column j holds blocks [j (j + 1) / 2, ...)
         int j = int((sqrtf(8.0f * float(k) + 1.0f) - 1.0f) * 0.5f);
         while (j * (j + 1) / 2 > k) --j;
         while ((j + 1) * (j + 2) / 2 <= k) ++j;
         w.jb = j;
         w.i = k - j * (j + 1) / 2;
-        w.j = j * kIn + t % kIn;
+        w.j = j * in + t % in;
     }
     return w;
 }
 template <bool PAIR>
 __device__ __forceinline__ int items_of(const OrthParams& p, int phase) {
-    constexpr int kIn = TileOf<PAIR>::kRows / TileOf<PAIR>::kCols;
-    const int tm = p.bm / TileOf<PAIR>::kSide, tn = p.bn * kBox / TileOf<PAIR>::kCols;
-    return p.batch * (phase == 2 ? tm * tn : tm * (tm + 1) / 2 * kIn) * p.splits[phase];
+    const int cols = cols_of<PAIR>(p, phase);
+    const int tm = p.bm / TileOf<PAIR>::kSide, tn = p.bn * kBox / cols;
+    return p.batch * (phase == 2 ? tm * tn : tm * (tm + 1) / 2 * (TileOf<PAIR>::kRows / cols)) * p.splits[phase];
 }
 
 template <int N>
@@ -276,22 +279,21 @@ __device__ __forceinline__ uint32_t lds16(uint32_t addr) {
 }
 
 // 32 rows of 64 columns of the output, from 4 KB of staging in shared memory (rows of 128 bytes,
-// swizzled), by SHARE warps of which this is the `part`th.  r0, c0: the first row and column.
-template <int SHARE>
-__device__ __forceinline__ void store_rows(const OrthParams& p, int mat, int r0, int c0, uint32_t stage, int part, int lane) {
+// swizzled), by `share` warps of which this is the `part`th.  r0, c0: the first row and column.
+__device__ __forceinline__ void store_rows(const OrthParams& p, int mat, int r0, int c0, uint32_t stage, int share, int part, int lane) {
     uint8_t* base = p.out + int64_t(mat) * p.out_batch;
     if (p.wide && c0 + kBox <= p.n) {
         const int piece = lane % 8;
-#pragma unroll
-        for (int k = 0; k < 8 / SHARE; ++k) {
-            const int r = (k * SHARE + part) * 4 + lane / 8;
+#pragma unroll 2
+        for (int k = part; k < 8; k += share) {
+            const int r = k * 4 + lane / 8;
             const uint4 v = lds128(stage + piece_at(r, piece));
             if (r0 + r < p.m) *reinterpret_cast<uint4*>(base + int64_t(r0 + r) * p.out_pitch + c0 * 2 + piece * 16) = v;
         }
         return;
     }
 #pragma unroll 4
-    for (int k = part; k < 64; k += SHARE) {
+    for (int k = part; k < 64; k += share) {
         const int r = k / 2, c = k % 2 * 32 + lane;
         const uint32_t v = lds16(stage + piece_at(r, c / 8) + c % 8 * 2);
         if (r0 + r < p.m && c0 + c < p.n) *reinterpret_cast<uint16_t*>(base + int64_t(r0 + r) * p.out_pitch + (c0 + c) * 2) = uint16_t(v);
@@ -415,8 +417,8 @@ struct Finish {
 template <bool PAIR>
 __global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_constant__ OrthParams p) {
     using Tile = TileOf<PAIR>;
-    constexpr int kCtas = Tile::kCtas, kStages = Tile::kStages, kStageBytes = Tile::kStageBytes, kCols = Tile::kCols;
-    constexpr int kWarpCols = Tile::kWarpCols, kTmemCols = Tile::kTmemCols, kSide = Tile::kSide;
+    constexpr int kCtas = Tile::kCtas, kStages = Tile::kStages, kStageBytes = Tile::kStageBytes;
+    constexpr int kCols = Tile::kCols, kTmemCols = Tile::kTmemCols, kSide = Tile::kSide;
     extern __shared__ uint8_t raw[];
     // full and empty: a stage's copies have landed / its products are done (each CTA's own).  peer: the other CTA's copies
     // have landed (the first CTA's).  summed: an accumulator is complete; taken: it has been read (the first CTA's).
@@ -472,11 +474,11 @@ __global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_
             asm volatile("fence.proxy.async.global;" ::: "memory");   // what they wrote is read by copies
             mbar_arrive(go);
             const uint8_t* x = p.x[ph / 3 & 1];
-            const int items = items_of<PAIR>(p, phase);
+            const int items = items_of<PAIR>(p, phase), boxes = cols_of<PAIR>(p, phase) / kCtas / kBox;   // of the right operand
             for (int i = unit; i < items && ok; i += units) {
                 const Item w = item_of<PAIR>(p, phase, i);
                 // first box row or column of this CTA's part of either operand
-                const int left = w.i * kSide + rank * 2, right = w.j * (kCols / kBox) + rank * Tile::kRightBoxes;
+                const int left = w.i * kSide + rank * 2, right = (w.j * kCtas + rank) * boxes;
                 const uint8_t* xm = x + w.mat * x_bytes;
                 const uint8_t* sm = (phase == 1 ? p.sa : p.sb) + w.mat * s_bytes;
                 for (int s = 0; s < w.stages; ++s, ++it, st.next()) {
@@ -484,7 +486,7 @@ __global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_
                     if (!ok) break;
                     const int k = w.s0 + s, kt = k / kSide;
                     const uint32_t to = ring + st.at * kStageBytes, bar = full + 8 * st.at;
-                    mbar_expect_tx(bar, kStageBytes + (it == 0 && rank == kCtas - 1 && p.stall ? 16 : 0));
+                    mbar_expect_tx(bar, Tile::kLeft + boxes * kBoxBytes + (it == 0 && rank == kCtas - 1 && p.stall ? 16 : 0));
                     // boxes one above the other, or side by side
                     auto above = [&](uint32_t at, const uint8_t* base, int width, int r, int c, int n) {
                         for (int m = 0; m < n; ++m)
@@ -493,16 +495,15 @@ __global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_
                     auto beside = [&](uint32_t at, const uint8_t* base, int width, int r, int c, int n) {
                         bulk_g2s(at, base + (int64_t(r) * width + c) * kBoxBytes, n * kBoxBytes, bar);
                     };
-                    constexpr int kRight = Tile::kRightBoxes;
                     if (phase == 0) {
                         above(to, xm, p.bn, left, k, 2);
-                        above(to + Tile::kLeft, xm, p.bn, right, k, kRight);
+                        above(to + Tile::kLeft, xm, p.bn, right, k, boxes);
                     } else {
                         if (w.i <= kt) above(to, sm, p.bm, left, k, 2);
                         else beside(to, sm, p.bm, k, left, 2);
-                        if (phase == 2) beside(to + Tile::kLeft, xm, p.bn, k, right, kRight);
-                        else if (w.jb <= kt) above(to + Tile::kLeft, sm, p.bm, right, k, kRight);
-                        else beside(to + Tile::kLeft, sm, p.bm, k, right, kRight);
+                        if (phase == 2) beside(to + Tile::kLeft, xm, p.bn, k, right, boxes);
+                        else if (w.jb <= kt) above(to + Tile::kLeft, sm, p.bm, right, k, boxes);
+                        else beside(to + Tile::kLeft, sm, p.bm, k, right, boxes);
                     }
                 }
             }
@@ -524,6 +525,7 @@ __global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_
         for (int ph = 0; ph < phases && ok; ++ph) {
             const int phase = ph % 3;
             const int items = items_of<PAIR>(p, phase);
+            const uint32_t format = Tile::kIdesc | uint32_t(cols_of<PAIR>(p, phase) / 8) << 17;
             for (int i = unit; i < items && ok; i += units) {
                 const Item w = item_of<PAIR>(p, phase, i);
                 // (a first stage comes once the grid has come here)
@@ -544,7 +546,7 @@ __global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_
                     // rows along the reduction: 16 of them are 2048 bytes further; across it 16 columns are 32 bytes
                     const bool ta = phase && w.i > kt, tb = phase == 2 || (phase == 1 && w.jb > kt);
                     const uint64_t l = operand_desc(ring + st.at * kStageBytes), r = l + (Tile::kLeft >> 4);
-                    const uint32_t idesc = Tile::kIdesc | (ta ? 1u << 15 : 0u) | (tb ? 1u << 16 : 0u);
+                    const uint32_t idesc = format | (ta ? 1u << 15 : 0u) | (tb ? 1u << 16 : 0u);
                     const int la = ta ? 2048 >> 4 : 2, lb = tb ? 2048 >> 4 : 2;
 #pragma unroll
                     for (int k = 0; k < kBox / 16; ++k)
@@ -562,15 +564,7 @@ __global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_
         const int quad = warp & 3, group = (warp - kSumWarp) >> 2, t = threadIdx.x - kSumWarp * 32;
         const int row = quad * 32 + lane;                 // of this CTA's 128
         const uint32_t first_taken = PAIR ? cluster_addr(taken, 0) : taken;
-        const uint32_t from = tmem + (uint32_t(quad * 32) << 16) + group * kWarpCols;
-        // half a box of staging, filled by kShare warps with the same rows; the first of them stores it
-        constexpr int kShare = Tile::kShare;
-        const int part = group % kShare;
-        const uint32_t stage = ring + kStages * kStageBytes + (group / kShare * 4 + quad) * (kBoxBytes / 2);
-        auto stage_meet = [&]() {
-            if constexpr (kShare == 1) __syncwarp();
-            else asm volatile("bar.sync %0, %1;" ::"r"(2 + group / kShare * 4 + quad), "n"(kShare * 32) : "memory");
-        };
+        const uint32_t from = tmem + (uint32_t(quad * 32) << 16);
         Ring<2> acc;
         bool ok = true;
         for (int ph = 0; ph < phases; ++ph) {
@@ -579,10 +573,18 @@ __global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_
             ok = sum_warps_agree(wait_long(go, ph & 1, p.limit_ns));
             if (!ok) break;
             const int splits = p.splits[phase], items = items_of<PAIR>(p, phase);
+            const int cols = cols_of<PAIR>(p, phase), warp_cols = cols / 4;
+            // half a box of staging, filled by `share` warps with the same rows; the first of them stores it
+            const int share = kBox / warp_cols, part = group % share, place = group / share * 4 + quad;
+            const uint32_t stage = ring + kStages * kStageBytes + place * (kBoxBytes / 2);
+            auto stage_meet = [&]() {
+                if (share == 1) __syncwarp();
+                else asm volatile("bar.sync %0, %1;" ::"r"(2 + place), "r"(share * 32) : "memory");
+            };
             for (int i = unit; i < items; i += units, acc.next()) {
                 const Item w = item_of<PAIR>(p, phase, i);
                 Finish fin(p, phase, step, final, w.mat, w.i * Tile::kRows + rank * kCtaRows + row);
-                const int c0 = w.j * kCols + group * kWarpCols;
+                const int c0 = w.j * cols + group * warp_cols;
                 if (splits == 1) {
                     // what is read beside the accumulator is on its way before that is complete, and then a chunk ahead
                     fin.ask<2>(c0, lane);
@@ -593,16 +595,16 @@ __global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_
                     if (part == 0 && lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
                     stage_meet();
 #pragma unroll 1
-                    for (int c = 0; c < kWarpCols; c += kChunk) {
+                    for (int c = 0; c < warp_cols; c += kChunk) {
                         float f[kChunk];
-                        tmem_ld16(from + acc.at * kCols + c, f);
-                        if (c + kChunk == kWarpCols) {
+                        tmem_ld16(from + acc.at * kCols + group * warp_cols + c, f);
+                        if (c + kChunk == warp_cols) {
                             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                             __syncwarp();
                             if (lane == 0) arrive_at(first_taken + 8 * acc.at);
                         }
                         fin.take<2>();
-                        if (c + kChunk < kWarpCols) fin.ask<2>(c0 + c + kChunk, lane);
+                        if (c + kChunk < warp_cols) fin.ask<2>(c0 + c + kChunk, lane);
                         uint4 v[2];
 #pragma unroll
                         for (int k = 0; k < 2; ++k) v[k] = fin.piece(c0 + c + 8 * k, k, f + 8 * k);
@@ -632,7 +634,7 @@ __global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_
                             asm volatile("cp.async.bulk.commit_group;" ::: "memory");
                         }
                     } else if (!p.turned) {
-                        store_rows<kShare>(p, w.mat, fin.gr - lane, col, stage, part, lane);
+                        store_rows(p, w.mat, fin.gr - lane, col, stage, share, part, lane);
                     }
                     continue;
                 }
@@ -641,13 +643,13 @@ __global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_
                 ok = sum_warps_agree(mbar_wait_warp(summed + 8 * acc.at, acc.round));
                 if (!ok) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                constexpr int kPart = kCtaRows * kCols;
-                float* parts = p.part + (int64_t(w.tile) * kCtas + rank) * splits * kPart + row;
-                float* mine = parts + int64_t(w.split) * kPart;
-                const uint32_t sums = tmem + (uint32_t(quad * 32) << 16) + acc.at * kCols;
+                const int size = kCtaRows * cols;
+                float* parts = p.part + (int64_t(w.tile) * kCtas + rank) * splits * size + row;
+                float* mine = parts + int64_t(w.split) * size;
+                const uint32_t sums = from + acc.at * kCols;
                 // eight columns are a piece; pieces 4 s .. 4 s + 3 are split s's, and so on, one for each group of warps
 #pragma unroll 1
-                for (int k = group; k < kCols / 8; k += 4) {
+                for (int k = group; k < cols / 8; k += 4) {
                     if (k / 4 % splits == w.split) continue;
                     float f[8];
                     tmem_ld8(sums + k * 8, f);
@@ -663,20 +665,20 @@ __global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_
                 ok = sum_warps_agree(__all_sync(0xffffffffu, came));
                 if (!ok) break;
 #pragma unroll 1
-                for (int k = w.split * 4 + group; k < kCols / 8; k += splits * 4) {
-                    const int col = w.j * kCols + k * 8;
+                for (int k = w.split * 4 + group; k < cols / 8; k += splits * 4) {
+                    const int col = w.j * cols + k * 8;
                     fin.ask<1>(col, lane);
                     float own[8], f[8] = {};
                     tmem_ld8(sums + k * 8, own);
                     const float* at = parts + k * 8 * kCtaRows;
                     // three splits' loads at a time
 #pragma unroll 1
-                    for (int s = 0; s < splits; s += 3, at += 3 * kPart) {
+                    for (int s = 0; s < splits; s += 3, at += 3 * size) {
                         float g[3][8];
 #pragma unroll
                         for (int h = 0; h < 3; ++h)
 #pragma unroll
-                            for (int m = 0; m < 8; ++m) g[h][m] = s + h < splits && s + h != w.split ? __ldcg(at + h * kPart + m * kCtaRows) : 0.0f;
+                            for (int m = 0; m < 8; ++m) g[h][m] = s + h < splits && s + h != w.split ? __ldcg(at + h * size + m * kCtaRows) : 0.0f;
 #pragma unroll
                         for (int h = 0; h < 3; ++h)
 #pragma unroll
@@ -706,8 +708,8 @@ __global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_
             const int items = items_of<PAIR>(p, 2);
             for (int i = unit; i < items; i += units) {
                 const Item w = item_of<PAIR>(p, 2, i);
-                const int r = w.i * Tile::kRows + rank * kCtaRows + row, c0 = w.j * kCols + group * kWarpCols;
-                for (int c = c0; c < min(c0 + kWarpCols, p.n) && r < p.m; ++c)
+                const int cols = cols_of<PAIR>(p, 2), r = w.i * Tile::kRows + rank * kCtaRows + row, c0 = w.j * cols + group * (cols / 4);
+                for (int c = c0; c < min(c0 + cols / 4, p.n) && r < p.m; ++c)
                     *reinterpret_cast<uint16_t*>(p.out + int64_t(w.mat) * p.out_batch + int64_t(p.turned ? c : r) * p.out_pitch +
                                                  int64_t(p.turned ? r : c) * 2) = 0x7fff;
             }
@@ -1371,45 +1373,48 @@ constexpr int64_t al(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
 
 // How a call is cut, and where its parts lie in the workspace.
 struct Plan {
-    int64_t batch, m, n, bm, bn, tm, tn;
+    int64_t batch, m, n, bm, bn, tm;
     bool pair, turned;
     int ctas;                 // of a tile
-    int64_t splits[3], items[3], half, parts;   // half: tiles of A
+    int64_t cols[3], splits[3], tiles[3], items[3], half, parts;   // half: tiles of A, at most
     int64_t counters, norm, d, e, x0, x1, xf, af, sa, sb, part, bytes;
 };
 constexpr int kPairs = 76;    // pairs of CTAs that the device holds
 
 // One way of cutting, and what it takes: a product's stages one after the other, as often as its pieces go round the
-// device, and the splits' exchange.  A stage takes 0.36 us on a pair's tile (0.30 where nothing but copies is done), 0.30
-// on a single CTA's, which does an eighth of the work.  What comes on top of each product (4.5 us: copies' latency, the
-// accumulators, the barrier) is the same for both.
+// device, and what becomes of the last accumulator.  A stage takes 0.36 us on a pair's tile, of 128 columns as of 256 (0.31
+// with a quarter of the products: the copies' 64 bytes a cycle and multiprocessor), and 0.30 on a single CTA's, a quarter or
+// half of that.  An accumulator takes 4, 2 and 1 us, and its splits' exchange 11, 6.5 and 5.5.  What comes on top of each
+// product (3.5 us: the copies' latency, the barrier) is the same for all.
 double cut(Plan& q, bool pair) {
     q.pair = pair;
     q.ctas = pair ? TileOf<true>::kCtas : TileOf<false>::kCtas;
-    const int64_t rows = pair ? TileOf<true>::kRows : TileOf<false>::kRows, cols = pair ? TileOf<true>::kCols : TileOf<false>::kCols;
+    const int64_t rows = pair ? TileOf<true>::kRows : TileOf<false>::kRows, widest = pair ? TileOf<true>::kCols : TileOf<false>::kCols;
     const int64_t units = pair ? kPairs : 2 * kPairs;
-    const double stage = pair ? 0.36 : 0.30, exchange = pair ? 6.0 : 3.0;
     q.tm = al(q.m, rows) / rows;
-    q.tn = al(q.n, cols) / cols;
     q.bm = q.tm * rows / kBox;
-    q.bn = q.tn * cols / kBox;
-    const int64_t half = q.batch * q.tm * (q.tm + 1) / 2 * (rows / cols);
+    q.bn = al(q.n, widest) / kBox;
     double all = 0.0;
     for (int k = 0; k < 3; ++k) {
-        const int64_t tiles = k == 2 ? q.batch * q.tm * q.tn : half, stages = k == 0 ? q.bn : q.bm;
-        const int64_t most = k == 2 || tiles >= units ? 1 : units / tiles;
-        double best = 0.0;
-        for (int64_t s = 1; s <= most && s <= stages && s <= 32; ++s) {
-            const int64_t per = (stages + s - 1) / s;
-            const double t = double((tiles * s + units - 1) / units * per) * stage + (s > 1 ? exchange : 0.0);
-            if (s > 1 && t >= best) continue;
-            best = t;
-            q.splits[k] = (stages + per - 1) / per;
-            q.items[k] = tiles * q.splits[k];
+        const int64_t stages = k == 0 ? q.bn : q.bm;
+        double best = -1.0;
+        for (int64_t cols = widest; cols >= (pair ? 128 : 64); cols /= 2) {
+            const double stage = pair ? 0.36 : 0.30, exchange = !pair ? 5.5 : cols == 256 ? 11.0 : 6.5;
+            const int64_t tiles = q.batch * (k == 2 ? q.tm * (q.bn * kBox / cols) : q.tm * (q.tm + 1) / 2 * (rows / cols));
+            const int64_t most = k == 2 || tiles >= units ? 1 : units / tiles;
+            for (int64_t s = 1; s <= most && s <= stages && s <= 32; ++s) {
+                const int64_t per = (stages + s - 1) / s;
+                const double t = double((tiles * s + units - 1) / units * per) * stage + (s > 1 ? exchange : double(cols) / 64.0);
+                if (best >= 0.0 && t >= best) continue;
+                best = t;
+                q.cols[k] = cols;
+                q.splits[k] = (stages + per - 1) / per;
+                q.tiles[k] = tiles;
+                q.items[k] = tiles * q.splits[k];
+            }
         }
         all += best;
     }
-    q.half = half;
     return all;
 }
 
@@ -1430,10 +1435,12 @@ Plan plan_of(int64_t batch, int64_t rows, int64_t cols) {
         return here;
     };
     const int64_t x = batch * q.bm * q.bn * kBoxBytes, sq = batch * q.bm * q.bm * kBoxBytes, diag = batch * q.bm * kBox * 4;
-    const int64_t tile = q.pair ? TileOf<true>::kRows * TileOf<true>::kCols : TileOf<false>::kRows * TileOf<false>::kCols;
-    int64_t most = 0;
-    for (int k = 0; k < 2; ++k)
-        if (q.splits[k] > 1 && q.splits[k] > most) most = q.splits[k];
+    int64_t part = 0;
+    for (int k = 0; k < 2; ++k) {
+        const int64_t sums = q.splits[k] > 1 ? q.items[k] * q.ctas * kCtaRows * q.cols[k] : 0;
+        part = sums > part ? sums : part;
+    }
+    q.half = q.tiles[0] > q.tiles[1] ? q.tiles[0] : q.tiles[1];
     q.counters = take((1 + 2 * q.half * q.ctas) * 4);
     q.norm = take(batch * q.parts * 8);
     q.d = take(diag);
@@ -1444,7 +1451,7 @@ Plan plan_of(int64_t batch, int64_t rows, int64_t cols) {
     q.af = take(2 * sq);
     q.sa = take(sq);
     q.sb = take(sq);
-    q.part = take(q.half * most * tile * 4);
+    q.part = take(part * 4);
     q.bytes = at;
     return q;
 }
@@ -1765,7 +1772,10 @@ extern "C" lc_status lc_orthogonalize(int device, void* cuda_stream, const lc_ma
     p.bn = int32_t(q.bn);
     p.steps = steps;
     p.tiles = int32_t(q.half);
-    for (int k = 0; k < 3; ++k) p.splits[k] = int32_t(q.splits[k]);
+    for (int k = 0; k < 3; ++k) {
+        p.splits[k] = int32_t(q.splits[k]);
+        p.cols[k] = int32_t(q.cols[k]);
+    }
     p.turned = q.turned;
     p.wide = rows_wide(p.out, rows > 1 ? p.out_pitch : 0, batch > 1 ? p.out_batch : 0);
     p.stall = ops_stall();
