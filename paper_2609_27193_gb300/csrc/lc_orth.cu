@@ -240,6 +240,25 @@ __device__ __forceinline__ bool grid_wait(const uint32_t* count, uint32_t want, 
         else if (t - t0 > limit_ns || it > (uint64_t(1) << 40)) return false;
     }
 }
+// One lane of a warp.
+__device__ __forceinline__ bool elected() {
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r != 0;
+}
+// mbar_wait_warp with a limit of its own.
+__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, uint64_t limit_ns) {
+    if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+    uint64_t t0 = 0;
+    for (uint64_t it = 1; it < (uint64_t(1) << 40); ++it) {
+        if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+        if (it % kPollsPerTime) continue;
+        const uint64_t t = __shfl_sync(0xffffffffu, global_ns(), 0);
+        if (t0 == 0) t0 = t;
+        else if (t - t0 > limit_ns) return false;
+    }
+    return false;
+}
 // A wait for the grid, in shared memory: as long as the grid may take.
 __device__ __forceinline__ bool wait_long(uint32_t bar, uint32_t parity, uint64_t limit_ns) {
     uint64_t t0 = 0;
@@ -462,19 +481,26 @@ __global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_
     const int phases = 3 * p.steps;
     const int64_t x_bytes = int64_t(p.bm) * p.bn * kBoxBytes, s_bytes = int64_t(p.bm) * p.bm * kBoxBytes;
 
-    if (warp == 0 && lane == 0) {
+    // Both of the next warps go through their loops as one, and one lane issues: what the copies and the products
+    // are given is then computed once for the warp, in its uniform registers.  (One lane by itself took 0.30 us a stage whatever
+    // the stage held; three stages in flight were as fast as eight.)
+    if (warp == 0) {
         // --- the operands ---
         Ring<kStages> st;
+        const bool one = elected();
         int it = 0;
         bool ok = true;
         for (int ph = 0; ph < phases && ok; ++ph) {
             const int phase = ph % 3;
-            if (ph) ok = grid_wait(p.count, uint32_t(ph) * gridDim.x, p.limit_ns);
+            if (ph) ok = __all_sync(0xffffffffu, lane != 0 || grid_wait(p.count, uint32_t(ph) * gridDim.x, p.limit_ns));
             if (!ok) break;
-            asm volatile("fence.proxy.async.global;" ::: "memory");   // what they wrote is read by copies
-            mbar_arrive(go);
+            if (one) {
+                asm volatile("fence.proxy.async.global;" ::: "memory");   // what they wrote is read by copies
+                mbar_arrive(go);
+            }
             const uint8_t* x = p.x[ph / 3 & 1];
             const int items = items_of<PAIR>(p, phase), boxes = cols_of<PAIR>(p, phase) / kCtas / kBox;   // of the right operand
+            const uint32_t bytes = Tile::kLeft + boxes * kBoxBytes;
             for (int i = unit; i < items && ok; i += units) {
                 const Item w = item_of<PAIR>(p, phase, i);
                 // first box row or column of this CTA's part of either operand
@@ -482,43 +508,48 @@ __global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_
                 const uint8_t* xm = x + w.mat * x_bytes;
                 const uint8_t* sm = (phase == 1 ? p.sa : p.sb) + w.mat * s_bytes;
                 for (int s = 0; s < w.stages; ++s, ++it, st.next()) {
-                    ok = it < kStages || mbar_wait_bounded(empty + 8 * st.at, st.round ^ 1, kWaitNs);
+                    ok = it < kStages || mbar_wait_warp(empty + 8 * st.at, st.round ^ 1);
                     if (!ok) break;
                     const int k = w.s0 + s, kt = k / kSide;
                     const uint32_t to = ring + st.at * kStageBytes, bar = full + 8 * st.at;
-                    mbar_expect_tx(bar, Tile::kLeft + boxes * kBoxBytes + (it == 0 && rank == kCtas - 1 && p.stall ? 16 : 0));
-                    // boxes one above the other, or side by side
-                    auto above = [&](uint32_t at, const uint8_t* base, int width, int r, int c, int n) {
-                        for (int m = 0; m < n; ++m)
-                            bulk_g2s(at + m * kBoxBytes, base + (int64_t(r + m) * width + c) * kBoxBytes, kBoxBytes, bar);
-                    };
-                    auto beside = [&](uint32_t at, const uint8_t* base, int width, int r, int c, int n) {
-                        bulk_g2s(at, base + (int64_t(r) * width + c) * kBoxBytes, n * kBoxBytes, bar);
-                    };
-                    if (phase == 0) {
-                        above(to, xm, p.bn, left, k, 2);
-                        above(to + Tile::kLeft, xm, p.bn, right, k, boxes);
-                    } else {
-                        if (w.i <= kt) above(to, sm, p.bm, left, k, 2);
-                        else beside(to, sm, p.bm, k, left, 2);
-                        if (phase == 2) beside(to + Tile::kLeft, xm, p.bn, k, right, boxes);
-                        else if (w.jb <= kt) above(to + Tile::kLeft, sm, p.bm, right, k, boxes);
-                        else beside(to + Tile::kLeft, sm, p.bm, k, right, boxes);
+                    if (one) {
+                        mbar_expect_tx(bar, bytes + (it == 0 && rank == kCtas - 1 && p.stall ? 16 : 0));
+                        // boxes one above the other, or side by side
+                        auto above = [&](uint32_t at, const uint8_t* base, int width, int r, int c, int n) {
+                            const uint8_t* from = base + (int64_t(r) * width + c) * kBoxBytes;
+                            bulk_g2s(at, from, kBoxBytes, bar);
+                            if (n > 1) bulk_g2s(at + kBoxBytes, from + int64_t(width) * kBoxBytes, kBoxBytes, bar);
+                        };
+                        auto beside = [&](uint32_t at, const uint8_t* base, int width, int r, int c, int n) {
+                            bulk_g2s(at, base + (int64_t(r) * width + c) * kBoxBytes, n * kBoxBytes, bar);
+                        };
+                        if (phase == 0) {
+                            above(to, xm, p.bn, left, k, 2);
+                            above(to + Tile::kLeft, xm, p.bn, right, k, boxes);
+                        } else {
+                            if (w.i <= kt) above(to, sm, p.bm, left, k, 2);
+                            else beside(to, sm, p.bm, k, left, 2);
+                            if (phase == 2) beside(to + Tile::kLeft, xm, p.bn, k, right, boxes);
+                            else if (w.jb <= kt) above(to + Tile::kLeft, sm, p.bm, right, k, boxes);
+                            else beside(to + Tile::kLeft, sm, p.bm, k, right, boxes);
+                        }
                     }
+                    __syncwarp();
                 }
             }
         }
         // every copy lands, and every arrival that ends a stage's products, before the CTA's memory is given back
         for (int i = it > kStages ? it - kStages : 0; i < it; ++i)
-            if (!mbar_wait_bounded(full + 8 * (i % kStages), (i / kStages) & 1, kWaitNs)) ok = false;
+            if (!mbar_wait_warp(full + 8 * (i % kStages), (i / kStages) & 1)) ok = false;
         bool ended = true;
         for (int i = it > kStages ? it - kStages : 0; i < it && ended; ++i)
-            ended = mbar_wait_bounded(empty + 8 * (i % kStages), (i / kStages) & 1, kWaitNs);
+            ended = mbar_wait_warp(empty + 8 * (i % kStages), (i / kStages) & 1);
         if (!ok || !ended) failed = 1;
-    } else if (warp == 1 && lane == 0) {
+    } else if (warp == 1) {
         // --- the products; in the second CTA of a pair: word of its copies for the first ---
         Ring<kStages> st;
         Ring<2> acc;
+        const bool one = elected();
         const uint32_t first_peer = PAIR ? cluster_addr(peer, 0) : 0;
         int chunk = 0;
         bool ok = true;
@@ -531,29 +562,33 @@ __global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_
                 // (a first stage comes once the grid has come here)
                 if (rank) {
                     for (int s = 0; s < w.stages && ok; ++s, st.next()) {
-                        ok = wait_long(full + 8 * st.at, st.round, s ? kWaitNs : p.limit_ns);
-                        if (ok) arrive_at(first_peer + 8 * st.at);
+                        ok = wait_warp(full + 8 * st.at, st.round, s ? kWaitNs : p.limit_ns);
+                        if (ok && one) arrive_at(first_peer + 8 * st.at);
                     }
                     continue;
                 }
-                if (chunk >= 2) ok = mbar_wait_bounded(taken + 8 * acc.at, acc.round ^ 1, kWaitNs);
+                if (chunk >= 2) ok = mbar_wait_warp(taken + 8 * acc.at, acc.round ^ 1);
                 for (int s = 0; s < w.stages && ok; ++s, st.next()) {
-                    ok = wait_long(full + 8 * st.at, st.round, s ? kWaitNs : p.limit_ns);
-                    if (PAIR && ok) ok = wait_long(peer + 8 * st.at, st.round, s ? kWaitNs : p.limit_ns);
+                    ok = wait_warp(full + 8 * st.at, st.round, s ? kWaitNs : p.limit_ns);
+                    if (PAIR && ok) ok = wait_warp(peer + 8 * st.at, st.round, s ? kWaitNs : p.limit_ns);
                     if (!ok) break;
-                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     const int kt = (w.s0 + s) / kSide;
                     // rows along the reduction: 16 of them are 2048 bytes further; across it 16 columns are 32 bytes
                     const bool ta = phase && w.i > kt, tb = phase == 2 || (phase == 1 && w.jb > kt);
                     const uint64_t l = operand_desc(ring + st.at * kStageBytes), r = l + (Tile::kLeft >> 4);
                     const uint32_t idesc = format | (ta ? 1u << 15 : 0u) | (tb ? 1u << 16 : 0u);
                     const int la = ta ? 2048 >> 4 : 2, lb = tb ? 2048 >> 4 : 2;
+                    if (one) {
+                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                        mma<PAIR>(tmem + acc.at * kCols, l, r, idesc, s > 0);
 #pragma unroll
-                    for (int k = 0; k < kBox / 16; ++k)
-                        mma<PAIR>(tmem + acc.at * kCols, l + k * la, r + k * lb, idesc, s > 0 || k > 0);
-                    commit<PAIR>(empty + 8 * st.at);
+                        for (int k = 1; k < kBox / 16; ++k) mma<PAIR>(tmem + acc.at * kCols, l + k * la, r + k * lb, idesc, 1);
+                        commit<PAIR>(empty + 8 * st.at);
+                    }
+                    __syncwarp();
                 }
-                if (ok) commit<PAIR>(summed + 8 * acc.at);
+                if (ok && one) commit<PAIR>(summed + 8 * acc.at);
+                __syncwarp();
                 acc.next();
                 ++chunk;
             }
