@@ -215,6 +215,15 @@ __device__ __forceinline__ int items_of(const OrthParams& p, int phase) {
     return p.batch * (phase == 2 ? tm * tn : tm * (tm + 1) / 2 * (TileOf<PAIR>::kRows / cols)) * p.splits[phase];
 }
 
+// From which block of the reduction on an operand's boxes are read as its rows (before it, as its columns: a symmetric
+// matrix has the boxes on and above the diagonal).
+__device__ __forceinline__ int left_block(int phase, const Item& w) { return phase == 0 ? 0 : w.i; }
+__device__ __forceinline__ int right_block(int phase, const Item& w) { return phase == 0 ? 0 : phase == 1 ? w.jb : 1 << 30; }
+
+template <int N>
+struct Step {
+    static constexpr int value = N;
+};
 template <int N>
 struct Ring {
     int at = 0;
@@ -482,8 +491,8 @@ __global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_
     const int64_t x_bytes = int64_t(p.bm) * p.bn * kBoxBytes, s_bytes = int64_t(p.bm) * p.bm * kBoxBytes;
 
     // Both of the next warps go through their loops as one, and one lane issues: what the copies and the products
-    // are given is then computed once for the warp, in its uniform registers.  (One lane by itself took 0.30 us a stage whatever
-    // the stage held; three stages in flight were as fast as eight.)
+    // are given is then computed once for the warp, in its uniform registers.  (One lane by itself took 0.30 us a stage of a
+    // single CTA's tile, whatever the stage held; three stages in flight were as fast as eight.)
     if (warp == 0) {
         // --- the operands ---
         Ring<kStages> st;
@@ -503,35 +512,36 @@ __global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_
             const uint32_t bytes = Tile::kLeft + boxes * kBoxBytes;
             for (int i = unit; i < items && ok; i += units) {
                 const Item w = item_of<PAIR>(p, phase, i);
-                // first box row or column of this CTA's part of either operand
+                // the boxes of this CTA's part of either operand at the first stage, as rows of it against columns k and as
+                // rows k of its columns
                 const int left = w.i * kSide + rank * 2, right = (w.j * kCtas + rank) * boxes;
-                const uint8_t* xm = x + w.mat * x_bytes;
-                const uint8_t* sm = (phase == 1 ? p.sa : p.sb) + w.mat * s_bytes;
-                for (int s = 0; s < w.stages; ++s, ++it, st.next()) {
+                const uint8_t* const xm = x + w.mat * x_bytes;
+                const uint8_t* const sm = (phase == 1 ? p.sa : p.sb) + w.mat * s_bytes;
+                const int64_t lw = int64_t(phase == 0 ? p.bn : p.bm) * kBoxBytes, rw = int64_t(phase == 1 ? p.bm : p.bn) * kBoxBytes;
+                const uint8_t *l0 = (phase == 0 ? xm : sm) + left * lw + w.s0 * kBoxBytes, *l1 = sm + w.s0 * lw + left * kBoxBytes;
+                const uint8_t *r0 = (phase == 1 ? sm : xm) + right * rw + w.s0 * kBoxBytes, *r1 = (phase == 1 ? sm : xm) + w.s0 * rw + right * kBoxBytes;
+                const int lb = left_block(phase, w), rb = right_block(phase, w);
+                for (int s = 0; s < w.stages; ++s, ++it, st.next(), l0 += kBoxBytes, l1 += lw, r0 += kBoxBytes, r1 += rw) {
                     ok = it < kStages || mbar_wait_warp(empty + 8 * st.at, st.round ^ 1);
                     if (!ok) break;
-                    const int k = w.s0 + s, kt = k / kSide;
+                    const int kt = (w.s0 + s) / kSide;
                     const uint32_t to = ring + st.at * kStageBytes, bar = full + 8 * st.at;
                     if (one) {
                         mbar_expect_tx(bar, bytes + (it == 0 && rank == kCtas - 1 && p.stall ? 16 : 0));
                         // boxes one above the other, or side by side
-                        auto above = [&](uint32_t at, const uint8_t* base, int width, int r, int c, int n) {
-                            const uint8_t* from = base + (int64_t(r) * width + c) * kBoxBytes;
-                            bulk_g2s(at, from, kBoxBytes, bar);
-                            if (n > 1) bulk_g2s(at + kBoxBytes, from + int64_t(width) * kBoxBytes, kBoxBytes, bar);
-                        };
-                        auto beside = [&](uint32_t at, const uint8_t* base, int width, int r, int c, int n) {
-                            bulk_g2s(at, base + (int64_t(r) * width + c) * kBoxBytes, n * kBoxBytes, bar);
-                        };
-                        if (phase == 0) {
-                            above(to, xm, p.bn, left, k, 2);
-                            above(to + Tile::kLeft, xm, p.bn, right, k, boxes);
+                        if (lb <= kt) {
+                            bulk_g2s(to, l0, kBoxBytes, bar);
+                            bulk_g2s(to + kBoxBytes, l0 + lw, kBoxBytes, bar);
                         } else {
-                            if (w.i <= kt) above(to, sm, p.bm, left, k, 2);
-                            else beside(to, sm, p.bm, k, left, 2);
-                            if (phase == 2) beside(to + Tile::kLeft, xm, p.bn, k, right, boxes);
-                            else if (w.jb <= kt) above(to + Tile::kLeft, sm, p.bm, right, k, boxes);
-                            else beside(to + Tile::kLeft, sm, p.bm, k, right, boxes);
+                            bulk_g2s(to, l1, 2 * kBoxBytes, bar);
+                        }
+                        if (boxes == 1) {
+                            bulk_g2s(to + Tile::kLeft, rb <= kt ? r0 : r1, kBoxBytes, bar);
+                        } else if (rb <= kt) {
+                            bulk_g2s(to + Tile::kLeft, r0, kBoxBytes, bar);
+                            bulk_g2s(to + Tile::kLeft + kBoxBytes, r0 + rw, kBoxBytes, bar);
+                        } else {
+                            bulk_g2s(to + Tile::kLeft, r1, 2 * kBoxBytes, bar);
                         }
                     }
                     __syncwarp();
@@ -567,22 +577,28 @@ __global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_
                     }
                     continue;
                 }
+                const int lb = left_block(phase, w), rb = right_block(phase, w);
                 if (chunk >= 2) ok = mbar_wait_warp(taken + 8 * acc.at, acc.round ^ 1);
                 for (int s = 0; s < w.stages && ok; ++s, st.next()) {
                     ok = wait_warp(full + 8 * st.at, st.round, s ? kWaitNs : p.limit_ns);
                     if (PAIR && ok) ok = wait_warp(peer + 8 * st.at, st.round, s ? kWaitNs : p.limit_ns);
                     if (!ok) break;
                     const int kt = (w.s0 + s) / kSide;
-                    // rows along the reduction: 16 of them are 2048 bytes further; across it 16 columns are 32 bytes
-                    const bool ta = phase && w.i > kt, tb = phase == 2 || (phase == 1 && w.jb > kt);
-                    const uint64_t l = operand_desc(ring + st.at * kStageBytes), r = l + (Tile::kLeft >> 4);
+                    const bool ta = lb > kt, tb = rb > kt;
                     const uint32_t idesc = format | (ta ? 1u << 15 : 0u) | (tb ? 1u << 16 : 0u);
-                    const int la = ta ? 2048 >> 4 : 2, lb = tb ? 2048 >> 4 : 2;
                     if (one) {
                         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                        mma<PAIR>(tmem + acc.at * kCols, l, r, idesc, s > 0);
+                        const uint64_t l = operand_desc(ring + st.at * kStageBytes), r = l + (Tile::kLeft >> 4);
+                        // rows along the reduction: 16 of them are 2048 bytes further; across it 16 columns are 32 bytes
+                        auto issue = [&](auto la, auto lb) {
 #pragma unroll
-                        for (int k = 1; k < kBox / 16; ++k) mma<PAIR>(tmem + acc.at * kCols, l + k * la, r + k * lb, idesc, 1);
+                            for (int k = 0; k < kBox / 16; ++k)
+                                mma<PAIR>(tmem + acc.at * kCols, l + k * la.value, r + k * lb.value, idesc, k > 0 || s > 0);
+                        };
+                        constexpr Step<2> across;
+                        constexpr Step<(2048 >> 4)> along;
+                        if (ta) tb ? issue(along, along) : issue(along, across);
+                        else tb ? issue(across, along) : issue(across, across);
                         commit<PAIR>(empty + 8 * st.at);
                     }
                     __syncwarp();
@@ -1417,10 +1433,10 @@ struct Plan {
 constexpr int kPairs = 76;    // pairs of CTAs that the device holds
 
 // One way of cutting, and what it takes: a product's stages one after the other, as often as its pieces go round the
-// device, and what becomes of the last accumulator.  A stage takes 0.36 us on a pair's tile, of 128 columns as of 256 (0.31
-// with a quarter of the products: the copies' 64 bytes a cycle and multiprocessor), and 0.30 on a single CTA's, a quarter or
-// half of that.  An accumulator takes 4, 2 and 1 us, and its splits' exchange 11, 6.5 and 5.5.  What comes on top of each
-// product (3.5 us: the copies' latency, the barrier) is the same for all.
+// device, and what becomes of the last accumulator.  A stage takes 0.36 us on a pair's tile of 256 columns, 0.27 on one of
+// 128 and 0.21 on a single CTA's, a quarter of that (the copies alone 0.30 and 0.21: some 60 bytes a cycle and
+// multiprocessor).  An accumulator takes 4, 2 and 1 us, and its splits' exchange 11, 6.5 and 5.5.  What comes on top of each
+// product (3 us: the copies' latency, the barrier) is the same for all.
 double cut(Plan& q, bool pair) {
     q.pair = pair;
     q.ctas = pair ? TileOf<true>::kCtas : TileOf<false>::kCtas;
@@ -1434,7 +1450,7 @@ double cut(Plan& q, bool pair) {
         const int64_t stages = k == 0 ? q.bn : q.bm;
         double best = -1.0;
         for (int64_t cols = widest; cols >= (pair ? 128 : 64); cols /= 2) {
-            const double stage = pair ? 0.36 : 0.30, exchange = !pair ? 5.5 : cols == 256 ? 11.0 : 6.5;
+            const double stage = !pair ? 0.21 : cols == 256 ? 0.36 : 0.27, exchange = !pair ? 5.5 : cols == 256 ? 11.0 : 6.5;
             const int64_t tiles = q.batch * (k == 2 ? q.tm * (q.bn * kBox / cols) : q.tm * (q.tm + 1) / 2 * (rows / cols));
             const int64_t most = k == 2 || tiles >= units ? 1 : units / tiles;
             for (int64_t s = 1; s <= most && s <= stages && s <= 32; ++s) {
