@@ -681,11 +681,14 @@ cudaError_t grad_ring(const AddNormGradParams& p, int sms, cudaStream_t s, int* 
     return launch_grad_ring<T, R, 512, 4 * M, KEPT>(p, sms, s, ctas);
 }
 
-// Whether the rings pay.
-bool forward_ring(int64_t ntok, int64_t row_bytes) { return row_bytes >= 1024 || ntok >= 4096; }
-bool backward_ring(int64_t ntok, int64_t row_bytes, int sms) {
-    return row_bytes >= 8192 || ntok >= (row_bytes >= 1024 ? 2 * sms : 1024);
-}
+// Whether the rings pay (microseconds through them and directly):
+//   forward    bf16: 64 rows of 768 2.4, 2.6; 2432 of 4096 10.1, 21.5; 4096 of 256 3.1, 3.2.  With a 32-bit stream only
+//              where the arrays no longer stay in L2: 1024 of 4096 columns 9.8, 8.5; 608 of 8192 11.3, 13.2; 4096 of 2048
+//              16.5, 22.4; fp32 2432 of 1024 6.5, 5.8; 4096 of 2048 16.0, 22.7
+//   backward   bf16 152 of 2048 5.4, 5.0; 304 of 2048 5.6, 6.0; 16 of 4096 4.9, 6.1; with a 32-bit stream 608 of 1024 5.9,
+//              6.5; 304 of 2048 6.1, 5.7; fp32 304 of 768 5.1, 4.9; 608 of 768 5.5, 6.3; 152 of 4096 5.8, 6.6
+bool forward_ring(int64_t ntok, int64_t dim, bool stream32) { return !stream32 || ntok * dim >= 4900000; }
+bool backward_ring(int64_t ntok, int64_t dim, bool stream32, int sms) { return dim >= 4096 || ntok >= (stream32 ? 4 : 2) * sms; }
 constexpr int64_t kMaxRows = int64_t(1) << 40;
 
 // The types that go together: 0 both bf16, 1 a 32-bit stream around bf16 branches, 2 both fp32, -1 none.
@@ -795,7 +798,7 @@ extern "C" lc_status lc_add_norm(int device, void* cuda_stream, const lc_rows* x
     using B = __nv_bfloat16;
     cudaError_t err = cudaSuccess;
     bool done = false;
-    if (vec && forward_ring(ntok, dim * te))
+    if (vec && forward_ring(ntok, dim, types > 0))
         err = types == 0 ? ring<B, B>(p, sms, s, &done) : types == 1 ? ring<B, float>(p, sms, s, &done) : ring<float, float>(p, sms, s, &done);
     if (done || err != cudaSuccess) return ops_launched(call, err);
     err = types == 0 ? direct<B, B>(p, sms, s) : types == 1 ? direct<B, float>(p, sms, s) : direct<float, float>(p, sms, s);
@@ -890,7 +893,7 @@ extern "C" lc_status lc_add_norm_grad(int device, void* cuda_stream, const lc_ro
     int ctas = 0;
     cudaError_t err = cudaSuccess;
     auto go = [&](auto f) { err = f(p, sms, s, &ctas); };
-    if (vec && backward_ring(ntok, dim * te, sms)) {
+    if (vec && backward_ring(ntok, dim, types > 0, sms)) {
         if (types == 0) go(sum ? grad_ring<B, B, false> : grad_ring<B, B, true>);
         else if (types == 1) go(sum ? grad_ring<B, float, false> : grad_ring<B, float, true>);
         else go(sum ? grad_ring<float, float, false> : grad_ring<float, float, true>);
