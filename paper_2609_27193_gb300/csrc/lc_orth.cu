@@ -31,6 +31,7 @@
 //
 // Waits are bounded: where one runs out the CTA's outputs are NaN, and with the next
 // barrier everybody's.
+#include <cuda.h>
 #include <cuda_fp16.h>
 
 #include <cmath>
@@ -71,6 +72,14 @@ struct TileOf {
 struct OrthStep {
     float a, b, c, scale;    // scale: of B's operand
 };
+// Maps of a matrix of boxes, as [box row][box column][64][64]: copies of two boxes one above the other, of two
+// side by side, of one.
+struct BoxMaps {
+    CUtensorMap down, beside, one;
+};
+struct OrthMaps {
+    BoxMaps x[2], sa, sb;    // the operands
+};
 struct OrthParams {
     uint32_t* count;         // arrivals at the grid's barriers
     uint32_t* arrived;       // [A, A^2][tiles][CTAs of a tile]: splits of a product that are done
@@ -97,6 +106,20 @@ struct OrthParams {
     OrthStep step[kMaxSteps];
 };
 
+// Boxes from column c and row r on into this CTA's shared memory; word of them goes to a barrier of the pair's first CTA.
+template <bool PAIR>
+__device__ __forceinline__ void bring(uint32_t dst, const CUtensorMap* map, int c, int r, uint32_t bar) {
+    if constexpr (PAIR)
+        asm volatile(
+            "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %2, %3, %4}], [%5];" ::"r"(
+                dst),
+            "l"(map), "r"(0), "r"(c), "r"(r), "r"(bar)
+            : "memory");
+    else
+        asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %2, %3, %4}], [%5];" ::"r"(dst),
+                     "l"(map), "r"(0), "r"(c), "r"(r), "r"(bar)
+                     : "memory");
+}
 __device__ __forceinline__ uint32_t cluster_addr(uint32_t bar, int rank) {
     uint32_t r;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(bar), "r"(rank));
@@ -443,27 +466,26 @@ struct Finish {
 };
 
 template <bool PAIR>
-__global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_constant__ OrthParams p) {
+__global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_constant__ OrthMaps maps, const __grid_constant__ OrthParams p) {
     using Tile = TileOf<PAIR>;
     constexpr int kCtas = Tile::kCtas, kStages = Tile::kStages, kStageBytes = Tile::kStageBytes;
     constexpr int kCols = Tile::kCols, kTmemCols = Tile::kTmemCols, kSide = Tile::kSide;
     extern __shared__ uint8_t raw[];
-    // full and empty: a stage's copies have landed / its products are done (each CTA's own).  peer: the other CTA's copies
-    // have landed (the first CTA's).  summed: an accumulator is complete; taken: it has been read (the first CTA's).
-    // go: the grid has come to the next product.
-    __shared__ __align__(8) uint64_t bars[3 * kStages + 5];
+    // full: both CTAs' copies of a stage have landed (the first CTA's).  empty: its products are done (each CTA's own).
+    // summed: an accumulator is complete; taken: it has been read (the first CTA's).  go: the grid has come to the next
+    // product.
+    __shared__ __align__(8) uint64_t bars[2 * kStages + 5];
     __shared__ uint32_t tmem_base;
     __shared__ volatile uint32_t failed;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = PAIR ? int(blockIdx.x & 1) : 0, unit = int(blockIdx.x) / kCtas, units = int(gridDim.x) / kCtas;
     const uint32_t ring = (smem_addr(raw) + 1023) & ~1023u;
-    const uint32_t full = smem_addr(bars), empty = full + 8 * kStages, peer = empty + 8 * kStages;
-    const uint32_t summed = peer + 8 * kStages, taken = summed + 16, go = taken + 16;
+    const uint32_t full = smem_addr(bars), empty = full + 8 * kStages;
+    const uint32_t summed = empty + 8 * kStages, taken = summed + 16, go = taken + 16;
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; ++i) {
             mbar_init(full + 8 * i, 1);
             mbar_init(empty + 8 * i, 1);
-            mbar_init(peer + 8 * i, 1);
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(summed + 8 * i, 1);
@@ -488,7 +510,6 @@ __global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = tmem_base;
     const int phases = 3 * p.steps;
-    const int64_t x_bytes = int64_t(p.bm) * p.bn * kBoxBytes, s_bytes = int64_t(p.bm) * p.bm * kBoxBytes;
 
     // Both of the next warps go through their loops as one, and one lane issues: what the copies and the products
     // are given is then computed once for the warp, in its uniform registers.  (One lane by itself took 0.30 us a stage of a
@@ -497,6 +518,7 @@ __global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_
         // --- the operands ---
         Ring<kStages> st;
         const bool one = elected();
+        const uint32_t first_full = PAIR ? cluster_addr(full, 0) : full;
         int it = 0;
         bool ok = true;
         for (int ph = 0; ph < phases && ok; ++ph) {
@@ -507,60 +529,45 @@ __global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_
                 asm volatile("fence.proxy.async.global;" ::: "memory");   // what they wrote is read by copies
                 mbar_arrive(go);
             }
-            const uint8_t* x = p.x[ph / 3 & 1];
+            const BoxMaps &xm = maps.x[ph / 3 & 1], &sm = phase == 1 ? maps.sa : maps.sb;
             const int items = items_of<PAIR>(p, phase), boxes = cols_of<PAIR>(p, phase) / kCtas / kBox;   // of the right operand
-            const uint32_t bytes = Tile::kLeft + boxes * kBoxBytes;
+            const uint32_t bytes = kCtas * (Tile::kLeft + boxes * kBoxBytes);
+            const BoxMaps &lm = phase == 0 ? xm : sm, &rm = phase == 1 ? sm : xm;
+            const CUtensorMap *const r_down = boxes == 1 ? &rm.one : &rm.down, *const r_beside = boxes == 1 ? &rm.one : &rm.beside;
             for (int i = unit; i < items && ok; i += units) {
                 const Item w = item_of<PAIR>(p, phase, i);
-                // the boxes of this CTA's part of either operand at the first stage, as rows of it against columns k and as
-                // rows k of its columns
-                const int left = w.i * kSide + rank * 2, right = (w.j * kCtas + rank) * boxes;
-                const uint8_t* const xm = x + w.mat * x_bytes;
-                const uint8_t* const sm = (phase == 1 ? p.sa : p.sb) + w.mat * s_bytes;
-                const int64_t lw = int64_t(phase == 0 ? p.bn : p.bm) * kBoxBytes, rw = int64_t(phase == 1 ? p.bm : p.bn) * kBoxBytes;
-                const uint8_t *l0 = (phase == 0 ? xm : sm) + left * lw + w.s0 * kBoxBytes, *l1 = sm + w.s0 * lw + left * kBoxBytes;
-                const uint8_t *r0 = (phase == 1 ? sm : xm) + right * rw + w.s0 * kBoxBytes, *r1 = (phase == 1 ? sm : xm) + w.s0 * rw + right * kBoxBytes;
+                // first box row or column of this CTA's part of either operand
+                const int left = w.i * kSide + rank * 2, right = (w.j * kCtas + rank) * boxes, r0 = w.mat * p.bm;
                 const int lb = left_block(phase, w), rb = right_block(phase, w);
-                for (int s = 0; s < w.stages; ++s, ++it, st.next(), l0 += kBoxBytes, l1 += lw, r0 += kBoxBytes, r1 += rw) {
+                for (int s = 0; s < w.stages; ++s, ++it, st.next()) {
                     ok = it < kStages || mbar_wait_warp(empty + 8 * st.at, st.round ^ 1);
                     if (!ok) break;
-                    const int kt = (w.s0 + s) / kSide;
-                    const uint32_t to = ring + st.at * kStageBytes, bar = full + 8 * st.at;
+                    const int k = w.s0 + s, kt = k / kSide;
+                    const uint32_t to = ring + st.at * kStageBytes, bar = first_full + 8 * st.at;
                     if (one) {
-                        mbar_expect_tx(bar, bytes + (it == 0 && rank == kCtas - 1 && p.stall ? 16 : 0));
-                        // boxes one above the other, or side by side
-                        if (lb <= kt) {
-                            bulk_g2s(to, l0, kBoxBytes, bar);
-                            bulk_g2s(to + kBoxBytes, l0 + lw, kBoxBytes, bar);
-                        } else {
-                            bulk_g2s(to, l1, 2 * kBoxBytes, bar);
-                        }
-                        if (boxes == 1) {
-                            bulk_g2s(to + Tile::kLeft, rb <= kt ? r0 : r1, kBoxBytes, bar);
-                        } else if (rb <= kt) {
-                            bulk_g2s(to + Tile::kLeft, r0, kBoxBytes, bar);
-                            bulk_g2s(to + Tile::kLeft + kBoxBytes, r0 + rw, kBoxBytes, bar);
-                        } else {
-                            bulk_g2s(to + Tile::kLeft, r1, 2 * kBoxBytes, bar);
-                        }
+                        if (rank == 0) mbar_expect_tx(full + 8 * st.at, bytes + (it == 0 && p.stall ? 16 : 0));
+                        if (lb <= kt) bring<PAIR>(to, &lm.down, k, r0 + left, bar);
+                        else bring<PAIR>(to, &lm.beside, left, r0 + k, bar);
+                        if (rb <= kt) bring<PAIR>(to + Tile::kLeft, r_down, k, r0 + right, bar);
+                        else bring<PAIR>(to + Tile::kLeft, r_beside, right, r0 + k, bar);
                     }
                     __syncwarp();
                 }
             }
         }
         // every copy lands, and every arrival that ends a stage's products, before the CTA's memory is given back
-        for (int i = it > kStages ? it - kStages : 0; i < it; ++i)
+        // (word of the second CTA's goes to the first; they have landed when their products are done, or long after)
+        for (int i = it > kStages ? it - kStages : 0; i < it && rank == 0; ++i)
             if (!mbar_wait_warp(full + 8 * (i % kStages), (i / kStages) & 1)) ok = false;
         bool ended = true;
         for (int i = it > kStages ? it - kStages : 0; i < it && ended; ++i)
             ended = mbar_wait_warp(empty + 8 * (i % kStages), (i / kStages) & 1);
         if (!ok || !ended) failed = 1;
-    } else if (warp == 1) {
-        // --- the products; in the second CTA of a pair: word of its copies for the first ---
+    } else if (warp == 1 && rank == 0) {
+        // --- the products ---
         Ring<kStages> st;
         Ring<2> acc;
         const bool one = elected();
-        const uint32_t first_peer = PAIR ? cluster_addr(peer, 0) : 0;
         int chunk = 0;
         bool ok = true;
         for (int ph = 0; ph < phases && ok; ++ph) {
@@ -569,19 +576,11 @@ __global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_
             const uint32_t format = Tile::kIdesc | uint32_t(cols_of<PAIR>(p, phase) / 8) << 17;
             for (int i = unit; i < items && ok; i += units) {
                 const Item w = item_of<PAIR>(p, phase, i);
-                // (a first stage comes once the grid has come here)
-                if (rank) {
-                    for (int s = 0; s < w.stages && ok; ++s, st.next()) {
-                        ok = wait_warp(full + 8 * st.at, st.round, s ? kWaitNs : p.limit_ns);
-                        if (ok && one) arrive_at(first_peer + 8 * st.at);
-                    }
-                    continue;
-                }
                 const int lb = left_block(phase, w), rb = right_block(phase, w);
                 if (chunk >= 2) ok = mbar_wait_warp(taken + 8 * acc.at, acc.round ^ 1);
                 for (int s = 0; s < w.stages && ok; ++s, st.next()) {
+                    // (a first stage comes once the grid has come here)
                     ok = wait_warp(full + 8 * st.at, st.round, s ? kWaitNs : p.limit_ns);
-                    if (PAIR && ok) ok = wait_warp(peer + 8 * st.at, st.round, s ? kWaitNs : p.limit_ns);
                     if (!ok) break;
                     const int kt = (w.s0 + s) / kSide;
                     const bool ta = lb > kt, tb = rb > kt;
@@ -1533,6 +1532,37 @@ float room_for(double most) {
     return float(std::ldexp(1.0, k - 1 > 15 ? 15 : k - 1));
 }
 
+using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                              const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                              CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeFn encode_fn() {
+    static EncodeFn fn = [] {
+        void* f = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+            found != cudaDriverEntryPointSuccess) {
+            cudaGetLastError();
+            f = nullptr;
+        }
+        return reinterpret_cast<EncodeFn>(f);
+    }();
+    return fn;
+}
+// Maps of `rows` x `cols` boxes (with two each way, where there are two).
+bool encode(BoxMaps* maps, void* p, int64_t rows, int64_t cols) {
+    const EncodeFn fn = encode_fn();
+    if (!fn || rows > INT32_MAX || cols > INT32_MAX) return false;
+    const cuuint64_t dims[4] = {kBox, kBox, cuuint64_t(cols), cuuint64_t(rows)};
+    const cuuint64_t strides[3] = {kBox * 2, kBoxBytes, cuuint64_t(cols) * kBoxBytes};
+    const cuuint32_t ones[4] = {1, 1, 1, 1};
+    auto one = [&](CUtensorMap* map, cuuint32_t across, cuuint32_t down) {
+        const cuuint32_t box[4] = {kBox, kBox, across, down};
+        return fn(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, p, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
+                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    };
+    return one(&maps->down, 1, 2) && one(&maps->beside, 2, 1) && one(&maps->one, 1, 1);
+}
+
 template <bool PAIR>
 cudaError_t resident(int device, int* n) {
     static int held[kOpsMaxDevices];
@@ -1593,8 +1623,13 @@ cudaError_t launch_products(int device, OrthParams& p, const Plan& q, cudaStream
     c.stream = s;
     c.attrs = attr;
     c.numAttrs = PAIR ? 2 : 1;
+    OrthMaps maps;
+    const int64_t boxes = q.batch * q.bm;
+    if (!encode(&maps.x[0], p.x[0], boxes, q.bn) || !encode(&maps.x[1], p.x[1], boxes, q.bn) || !encode(&maps.sa, p.sa, boxes, q.bm) ||
+        !encode(&maps.sb, p.sb, boxes, q.bm))
+        return cudaErrorInvalidValue;
     cudaGetLastError();
-    return cudaLaunchKernelEx(&c, orth_product_kernel<PAIR>, p);
+    return cudaLaunchKernelEx(&c, orth_product_kernel<PAIR>, maps, p);
 }
 
 // CTAs and columns over 64 of each that a small matrix takes (0: it is not one).
