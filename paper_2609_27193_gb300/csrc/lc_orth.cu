@@ -58,9 +58,11 @@ struct TileOf {
     static constexpr int kCtas = PAIR ? 2 : 1;
     static constexpr int kRows = kCtaRows * kCtas, kCols = PAIR ? 256 : 64;
     static constexpr int kSide = kRows / kBox;                 // boxes of a block on the diagonal
-    static constexpr int kLeft = 2 * kBoxBytes;                // of a stage: the left operand, and the CTA's part of the right one
-    static constexpr int kStageBytes = kLeft + kCols / kCtas / kBox * kBoxBytes;
-    static constexpr int kStages = PAIR ? 5 : 8;
+    // A stage is kDepth boxes of the reduction: of each the left operand, and the CTA's part of the right one.
+    static constexpr int kDepth = PAIR ? 1 : 2;
+    static constexpr int kLeft = 2 * kBoxBytes, kRight = kCols / kCtas / kBox * kBoxBytes;
+    static constexpr int kStageBytes = kDepth * (kLeft + kRight);
+    static constexpr int kStages = PAIR ? 5 : 4;
     // a warp has 32 rows of a quarter of the columns; half a box of staging for as many warps as fill 64 columns
     static constexpr int kStaging = kSumWarps * (kCols / 4) / kBox * (kBoxBytes / 2);
     static constexpr int kSmem = kStages * kStageBytes + kStaging + 1024;   // and room to align them to 1024 bytes
@@ -202,7 +204,7 @@ template <bool PAIR>
 __device__ __forceinline__ Item item_of(const OrthParams& p, int phase, int at) {
     const int cols = cols_of<PAIR>(p, phase), in = TileOf<PAIR>::kRows / cols;   // tiles beside one another in such a block
     const int tm = p.bm / TileOf<PAIR>::kSide, tn = p.bn * kBox / cols;
-    const int all = phase == 0 ? p.bn : p.bm, splits = p.splits[phase];
+    const int all = (phase == 0 ? p.bn : p.bm) / TileOf<PAIR>::kDepth, splits = p.splits[phase];
     Item w;
     const int t = at / splits;
     w.split = at - t * splits;
@@ -512,8 +514,9 @@ __global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_
     const int phases = 3 * p.steps;
 
     // Both of the next warps go through their loops as one, and one lane issues: what the copies and the products
-    // are given is then computed once for the warp, in its uniform registers.  (One lane by itself took 0.30 us a stage of a
-    // single CTA's tile, whatever the stage held; three stages in flight were as fast as eight.)
+    // are given is then computed once for the warp, in its uniform registers.  (One lane by itself took 0.30 us for
+    // 64 of the reduction on a single CTA's tile, whatever came with them; three stages in flight were as fast as eight.  So 0.21, and
+    // 0.17 with 128 a stage.)
     if (warp == 0) {
         // --- the operands ---
         Ring<kStages> st;
@@ -531,7 +534,7 @@ __global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_
             }
             const BoxMaps &xm = maps.x[ph / 3 & 1], &sm = phase == 1 ? maps.sa : maps.sb;
             const int items = items_of<PAIR>(p, phase), boxes = cols_of<PAIR>(p, phase) / kCtas / kBox;   // of the right operand
-            const uint32_t bytes = kCtas * (Tile::kLeft + boxes * kBoxBytes);
+            const uint32_t bytes = kCtas * Tile::kDepth * (Tile::kLeft + boxes * kBoxBytes);
             const BoxMaps &lm = phase == 0 ? xm : sm, &rm = phase == 1 ? sm : xm;
             const CUtensorMap *const r_down = boxes == 1 ? &rm.one : &rm.down, *const r_beside = boxes == 1 ? &rm.one : &rm.beside;
             for (int i = unit; i < items && ok; i += units) {
@@ -542,14 +545,19 @@ __global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_
                 for (int s = 0; s < w.stages; ++s, ++it, st.next()) {
                     ok = it < kStages || mbar_wait_warp(empty + 8 * st.at, st.round ^ 1);
                     if (!ok) break;
-                    const int k = w.s0 + s, kt = k / kSide;
+                    const int k0 = (w.s0 + s) * Tile::kDepth, kt = k0 / kSide;
                     const uint32_t to = ring + st.at * kStageBytes, bar = first_full + 8 * st.at;
                     if (one) {
                         if (rank == 0) mbar_expect_tx(full + 8 * st.at, bytes + (it == 0 && p.stall ? 16 : 0));
-                        if (lb <= kt) bring<PAIR>(to, &lm.down, k, r0 + left, bar);
-                        else bring<PAIR>(to, &lm.beside, left, r0 + k, bar);
-                        if (rb <= kt) bring<PAIR>(to + Tile::kLeft, r_down, k, r0 + right, bar);
-                        else bring<PAIR>(to + Tile::kLeft, r_beside, right, r0 + k, bar);
+#pragma unroll
+                        for (int d = 0; d < Tile::kDepth; ++d) {
+                            const int k = k0 + d;
+                            const uint32_t lt = to + d * Tile::kLeft, rt = to + Tile::kDepth * Tile::kLeft + d * Tile::kRight;
+                            if (lb <= kt) bring<PAIR>(lt, &lm.down, k, r0 + left, bar);
+                            else bring<PAIR>(lt, &lm.beside, left, r0 + k, bar);
+                            if (rb <= kt) bring<PAIR>(rt, r_down, k, r0 + right, bar);
+                            else bring<PAIR>(rt, r_beside, right, r0 + k, bar);
+                        }
                     }
                     __syncwarp();
                 }
@@ -582,17 +590,20 @@ __global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_
                     // (a first stage comes once the grid has come here)
                     ok = wait_warp(full + 8 * st.at, st.round, s ? kWaitNs : p.limit_ns);
                     if (!ok) break;
-                    const int kt = (w.s0 + s) / kSide;
+                    const int kt = (w.s0 + s) * Tile::kDepth / kSide;
                     const bool ta = lb > kt, tb = rb > kt;
                     const uint32_t idesc = format | (ta ? 1u << 15 : 0u) | (tb ? 1u << 16 : 0u);
                     if (one) {
                         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                        const uint64_t l = operand_desc(ring + st.at * kStageBytes), r = l + (Tile::kLeft >> 4);
+                        const uint64_t l = operand_desc(ring + st.at * kStageBytes), r = l + (Tile::kDepth * Tile::kLeft >> 4);
                         // rows along the reduction: 16 of them are 2048 bytes further; across it 16 columns are 32 bytes
                         auto issue = [&](auto la, auto lb) {
 #pragma unroll
-                            for (int k = 0; k < kBox / 16; ++k)
-                                mma<PAIR>(tmem + acc.at * kCols, l + k * la.value, r + k * lb.value, idesc, k > 0 || s > 0);
+                            for (int d = 0; d < Tile::kDepth; ++d)
+#pragma unroll
+                                for (int k = 0; k < kBox / 16; ++k)
+                                    mma<PAIR>(tmem + acc.at * kCols, l + (d * Tile::kLeft >> 4) + k * la.value, r + (d * Tile::kRight >> 4) + k * lb.value,
+                                              idesc, d > 0 || k > 0 || s > 0);
                         };
                         constexpr Step<2> across;
                         constexpr Step<(2048 >> 4)> along;
@@ -1433,9 +1444,9 @@ constexpr int kPairs = 76;    // pairs of CTAs that the device holds
 
 // One way of cutting, and what it takes: a product's stages one after the other, as often as its pieces go round the
 // device, and what becomes of the last accumulator.  A stage takes 0.36 us on a pair's tile of 256 columns, 0.27 on one of
-// 128 and 0.21 on a single CTA's, a quarter of that (the copies alone 0.30 and 0.21: some 60 bytes a cycle and
-// multiprocessor).  An accumulator takes 4, 2 and 1 us, and its splits' exchange 11, 6.5 and 5.5.  What comes on top of each
-// product (3 us: the copies' latency, the barrier) is the same for all.
+// 128, and 0.36 on a single CTA's, which is half of that work (the copies alone 0.30, 0.21 and 0.28).  An accumulator takes 4, 2
+// and 1 us, and its splits' exchange 10.5, 6 and 5 and a quarter more for each split.  What comes on top of each product (3 us: the copies' latency, the
+// barrier) is the same for all.
 double cut(Plan& q, bool pair) {
     q.pair = pair;
     q.ctas = pair ? TileOf<true>::kCtas : TileOf<false>::kCtas;
@@ -1443,18 +1454,18 @@ double cut(Plan& q, bool pair) {
     const int64_t units = pair ? kPairs : 2 * kPairs;
     q.tm = al(q.m, rows) / rows;
     q.bm = q.tm * rows / kBox;
-    q.bn = al(q.n, widest) / kBox;
+    q.bn = al(q.n, pair ? widest : 2 * kBox) / kBox;
     double all = 0.0;
     for (int k = 0; k < 3; ++k) {
-        const int64_t stages = k == 0 ? q.bn : q.bm;
+        const int64_t depth = pair ? TileOf<true>::kDepth : TileOf<false>::kDepth, stages = (k == 0 ? q.bn : q.bm) / depth;
         double best = -1.0;
         for (int64_t cols = widest; cols >= (pair ? 128 : 64); cols /= 2) {
-            const double stage = !pair ? 0.21 : cols == 256 ? 0.36 : 0.27, exchange = !pair ? 5.5 : cols == 256 ? 11.0 : 6.5;
+            const double stage = !pair ? 0.36 : cols == 256 ? 0.36 : 0.27, exchange = !pair ? 5.0 : cols == 256 ? 10.5 : 6.0;
             const int64_t tiles = q.batch * (k == 2 ? q.tm * (q.bn * kBox / cols) : q.tm * (q.tm + 1) / 2 * (rows / cols));
             const int64_t most = k == 2 || tiles >= units ? 1 : units / tiles;
             for (int64_t s = 1; s <= most && s <= stages && s <= 32; ++s) {
                 const int64_t per = (stages + s - 1) / s;
-                const double t = double((tiles * s + units - 1) / units * per) * stage + (s > 1 ? exchange : double(cols) / 64.0);
+                const double t = double((tiles * s + units - 1) / units * per) * stage + (s > 1 ? exchange + 0.25 * double(s) : double(cols) / 64.0);
                 if (best >= 0.0 && t >= best) continue;
                 best = t;
                 q.cols[k] = cols;
