@@ -668,6 +668,13 @@ lc_status lc_measure_noalloc_debug(int device, void* cuda_stream, const lc_segme
 #define LC_DEBUG_OPS_STALL 4
 lc_status lc_ops_debug(int32_t debug_flags);
 
+/* For a caller that knows of every array it passes that it is device memory of the
+ * call's device (an allocator's own records: torch's CUDA tensors): while on is not 0,
+ * the operators that the calling host thread calls do not ask the driver about
+ * each (0.1 us an array, 0.7 to 1.2 of the 5 to 14 us that a small call takes on
+ * the host).  All other checks stay. */
+void lc_ops_known_memory(int32_t on);
+
 /* Rows of `dim` elements of type dtype (lc_dtype); row r starts `stride`
  * elements behind row r-1.  Inputs may repeat a row (stride 0), outputs need
  * stride >= dim. */

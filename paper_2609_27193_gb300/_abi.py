@@ -159,6 +159,7 @@ SIGNATURES = {
     "lc_manifest_read": (C.c_int, [C.c_char_p, C.c_int32, P(lc_manifest_record), C.c_int64,
                                    P(C.c_int64), P(C.c_int32), P(C.c_uint32), P(C.c_int32)]),
     "lc_ops_debug": (C.c_int, [C.c_int32]),
+    "lc_ops_known_memory": (None, [C.c_int32]),
     "lc_embed": (C.c_int, [C.c_int, C.c_void_p, P(lc_rows), C.c_int64, C.c_int64, C.c_void_p, C.c_int32,
                            C.c_int64, C.c_float, P(lc_rows)]),
     "lc_embed_grad": (C.c_int, [C.c_int, C.c_void_p, P(lc_rows), C.c_void_p, C.c_int32, C.c_int64, C.c_float,

@@ -367,18 +367,28 @@ PyObject* norm_grad(PyObject* const* args, Py_ssize_t nargs) {
     return tuple(dx, dweight, dbias);
 }
 
+// A new checkpoint for rows like x's.
+void new_act_of(const at::Tensor& x, at::Tensor& q, at::Tensor& e) {
+    const int64_t blocks = (x.size(1) + LC_ACT_BLOCK - 1) / LC_ACT_BLOCK;
+    q = make({x.size(0), blocks * LC_ACT_BLOCK}, at::kChar, x);
+    e = make({x.size(0), blocks}, at::kChar, x);
+}
+
 PyObject* add_norm(PyObject* const* args, Py_ssize_t nargs) {
-    Args a(args, nargs, 11);
+    Args a(args, nargs, 13);
     const at::Tensor x = a.tensor(), residual = a.tensor(), weight = a.tensor();
     const double eps = a.number();
     at::Tensor out = a.tensor();
     const bool want = a.truth();
     at::Tensor sum = a.tensor();
-    const at::Tensor q = a.tensor(), e = a.tensor(), yq = a.tensor(), ye = a.tensor();
+    at::Tensor q = a.tensor(), e = a.tensor(), yq = a.tensor(), ye = a.tensor();
+    const bool keep_new = a.truth(), y8_new = a.truth();
     const int index = cuda_index(x);
     cuda_index(residual);
     cuda_index(weight);
-    for (const at::Tensor* t : {&residual, &weight, static_cast<const at::Tensor*>(&out), static_cast<const at::Tensor*>(&sum), &q, &e, &yq, &ye})
+    for (const at::Tensor* t : {&residual, &weight, static_cast<const at::Tensor*>(&out), static_cast<const at::Tensor*>(&sum),
+                                static_cast<const at::Tensor*>(&q), static_cast<const at::Tensor*>(&e), static_cast<const at::Tensor*>(&yq),
+                                static_cast<const at::Tensor*>(&ye)})
         same_device(index, *t);
     unrecorded("add_norm", {&x, &residual, &weight, &out, &sum});
     const lc_rows rx = rows_of(x, "x"), rr = rows_of(residual, "residual");
@@ -394,11 +404,25 @@ PyObject* add_norm(PyObject* const* args, Py_ssize_t nargs) {
     if (out.defined()) ro = rows_of(out, "out");
     const at::Tensor rstd = make({n}, at::kFloat, x);
     lc_act keep{}, y8{};
+    if (dim < 1) throw ValueError("x must have columns");
+    if (keep_new) new_act_of(x, q, e);
+    if (y8_new) new_act_of(x, yq, ye);
     if (q.defined()) keep = act_of(q, e, n, dim);
     if (yq.defined()) y8 = act_of(yq, ye, n, dim);
     check(lc_add_norm(index, stream_of(index), &rx, &rr, n, dim, w, code_of(weight, "weight"), eps, &rs, out.defined() ? &ro : nullptr,
                       stat_of(rstd, n), q.defined() ? &keep : nullptr, yq.defined() ? &y8 : nullptr));
-    for (const at::Tensor* t : {static_cast<const at::Tensor*>(&sum), static_cast<const at::Tensor*>(&out), &q, &e, &yq, &ye}) written(*t);
+    for (const at::Tensor* t : {static_cast<const at::Tensor*>(&sum), static_cast<const at::Tensor*>(&out)}) written(*t);
+    if (!keep_new) {
+        written(q);
+        written(e);
+    }
+    if (!y8_new) {
+        written(yq);
+        written(ye);
+    }
+    if (keep_new && y8_new) return tuple(sum, out, rstd, q, e, yq, ye);
+    if (keep_new) return tuple(sum, out, rstd, q, e);
+    if (y8_new) return tuple(sum, out, rstd, yq, ye);
     return tuple(sum, out, rstd);
 }
 
@@ -537,10 +561,17 @@ PyObject* set_errors(PyObject* const* args, Py_ssize_t nargs) {
     Py_RETURN_NONE;
 }
 
+// What the operators get are torch's CUDA tensors, whose device was compared: the driver need not be asked.
+struct KnownMemory {
+    KnownMemory() { lc_ops_known_memory(1); }
+    ~KnownMemory() { lc_ops_known_memory(0); }
+};
+
 // No C++ exception leaves a call.
 template <PyObject* (*F)(PyObject* const*, Py_ssize_t)>
 PyObject* guarded(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     try {
+        const KnownMemory known;
         return F(args, nargs);
     } catch (const StatusError& e) {
         PyObject* err = g_error ? PyObject_CallFunction(g_error, "is", int(e.status), lc_last_error()) : nullptr;

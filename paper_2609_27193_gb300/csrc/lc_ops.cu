@@ -19,6 +19,7 @@ bool meet(const Span2& a, const Span2& b) {
 }
 
 thread_local int32_t debug_flags = 0;
+thread_local bool known_memory = false;
 
 }  // namespace
 
@@ -43,13 +44,15 @@ lc_status ops_check(const char* call, int device, const Span2* a, int n) {
     for (int i = 0; i < n; ++i) {
         if (a[i].rows <= 0 || a[i].bytes <= 0) continue;
         if (!a[i].p) return fail_status(LC_ERR_INVALID_ARG, "%s: %s is NULL", call, a[i].name);
-        cudaPointerAttributes at;
-        if (cudaPointerGetAttributes(&at, a[i].p) != cudaSuccess) {
-            cudaGetLastError();
-            return fail_status(LC_ERR_INVALID_ARG, "%s: %s is not device memory", call, a[i].name);
+        if (!known_memory) {
+            cudaPointerAttributes at;
+            if (cudaPointerGetAttributes(&at, a[i].p) != cudaSuccess) {
+                cudaGetLastError();
+                return fail_status(LC_ERR_INVALID_ARG, "%s: %s is not device memory", call, a[i].name);
+            }
+            if (at.type != cudaMemoryTypeDevice || at.device != device)
+                return fail_status(LC_ERR_INVALID_ARG, "%s: %s is not device memory of device %d", call, a[i].name, device);
         }
-        if (at.type != cudaMemoryTypeDevice || at.device != device)
-            return fail_status(LC_ERR_INVALID_ARG, "%s: %s is not device memory of device %d", call, a[i].name, device);
         if (!a[i].out) continue;
         for (int j = 0; j < n; ++j)
             if (j != i && (j < i || !a[j].out) && meet(a[i], a[j]))
@@ -90,6 +93,8 @@ lc_status ops_launched(const char* call, cudaError_t e) {
 }
 
 }  // namespace lc
+
+extern "C" void lc_ops_known_memory(int32_t on) { lc::known_memory = on != 0; }
 
 extern "C" lc_status lc_ops_debug(int32_t flags) {
     using namespace lc;

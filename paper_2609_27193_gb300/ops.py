@@ -162,14 +162,17 @@ def add_norm(x, residual, weight, eps=1e-5, out=None, sum=None, keep=None, out8=
     is written.  sum: where the sum goes, the residual itself if wanted.  out=False: y is wanted in 8 bits only (and
     returned as None).  The sum has the residual's type and y has x's: both the same, or a float32 residual around
     bfloat16 branches."""
-    kept = None if keep is None or keep is False else _for(keep, x)
-    y8 = None if out8 is None or out8 is False else _for(out8, x)
+    if not keep and not out8:
+        return _ops.add_norm(x, residual, weight, eps, None if out is False else out, out is not False, sum,
+                             None, None, None, None, False, False)
+    kept, y8 = (_for(a, x) if isinstance(a, Act) else None for a in (keep, out8))
     result = _ops.add_norm(x, residual, weight, eps, None if out is False else out, out is not False, sum,
                            *((None, None) if kept is None else (kept.q, kept.e)),
-                           *((None, None) if y8 is None else (y8.q, y8.e)))
-    if keep is True:
-        result = (*result, kept)
-    return (*result, y8) if out8 is True else result
+                           *((None, None) if y8 is None else (y8.q, y8.e)), keep is True, out8 is True)
+    if len(result) == 3:
+        return result
+    made = tuple(Act._of(result[k], result[k + 1], x.shape[1]) for k in range(3, len(result), 2))
+    return (*result[:3], *made)
 
 
 def add_norm_grad(dy, dsum, total, weight, rstd, dx=None, dweight=None, dtype=torch.float32, accumulate=False):

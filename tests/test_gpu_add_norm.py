@@ -253,3 +253,28 @@ def test_refusals(ops):
                             ((x, r[:3], r, w, rstd), {}, ValueError)):
         with pytest.raises(error):
             ops.add_norm_grad(*args, **kw)
+
+
+def test_the_c_abi_asks_about_memory(ops):
+    """The binding vouches for torch's tensors during its own calls only, whether they succeed or not."""
+    from paper_2609_27193_gb300 import _abi
+    lib = _abi.load()
+    x, w = torch.zeros(4, 64, device="cuda"), torch.ones(64, device="cuda")
+    host = torch.zeros(4, 64).pin_memory()
+    rstd, out = torch.zeros(4, device="cuda"), torch.zeros(4, 64, device="cuda")
+
+    def rows(t):
+        return _abi.lc_rows(t.data_ptr(), 64, _abi.LC_F32, 0)
+
+    def refused():
+        st = lib.lc_add_norm(0, None, rows(x), rows(host), 4, 64, w.data_ptr(), _abi.LC_F32, 1e-5, rows(out), rows(torch.zeros_like(x)),
+                             rstd.data_ptr(), None, None)
+        assert st == _abi.LC_ERR_INVALID_ARG and b"device memory" in lib.lc_last_error()
+    refused()
+    ops.add_norm(x, x, w)
+    refused()
+    with pytest.raises(_abi.LCError):
+        ops.add_norm(x, x, w, eps=-1.0)
+    refused()
+    with pytest.raises(ValueError):
+        ops.add_norm(x, host, w)
