@@ -6,28 +6,33 @@
 // over the shorter side (a matrix with more rows than columns is worked on
 // transposed).  Each step takes a singular value s to a s + b s^3 + c s^5.
 //
-// Three kernels: one moves the momentum and leaves sums of squares, one writes X
-// in the products' layout, one does all products.  The products are on the 5th-generation
-// tensor cores, fp16 operands and fp32 sums:
+// The products are on the 5th-generation tensor cores, fp16 operands and fp32 sums:
 //
 //   * The state X is kept in fp32 beside its operand.  (With the fp16 number as state a matrix
 //     of 8 directions over noise of 1e-4 came out 4e-2 off, so 6e-4; with bf16 3e-1.)
 //   * The diagonals of A and of B = b A + c A^2 are far larger than the rest and stay in fp32, beside
 //     the operands: A^2 = A0^2 + (d_i + d_j) A0 + d^2, and X's row i is multiplied by a + e_i.  That
-//     halves the error (512 x 1024: 1.7e-3 to 5e-4 off before the output's rounding of 1.7e-3).
+//     takes the error from 1.7e-3 to 5e-4 (256 x 1024), below the output's rounding of 1.7e-3.
 //   * Operands are scaled by powers of two.  No element of X, A or B is larger than the matrix's
 //     largest singular value, which the coefficients bound, so nothing overflows fp16.
 //   * A and B are symmetric: the tiles on and above the diagonal are computed, and a product reads the
 //     others as transposes of those, which the tensor core takes either way.
 //
+// Matrices of up to 128 rows (of the shorter side) and 4096 columns stay in the memory of one cluster, one
+// launch (orth_small_kernel).  Others take three: one moves the momentum and leaves sums of squares, one
+// writes X in the products' layout, one does all products.  (256 x 256: 4, 5 and 63 us, 76 among others.)
+//
 // Matrices lie in the workspace in boxes of 64 x 64, rows of 128 bytes swizzled as the operands are
-// in shared memory, so that a box is one contiguous bulk copy and the same box serves with its rows along the
-// reduction or across it.
+// in shared memory: one bulk tensor copy brings two boxes, above or beside one another, and the same box
+// serves with its rows along the reduction or across it.
 //
 // The product kernel is one cooperative launch: its CTAs go through the 3 * steps
-// products together, with a barrier of the whole grid between them.  Two CTAs of a cluster share
-// tiles of 256 x 256 (PAIR), or a CTA has one of 128 x 64.  Warp 0 brings the operands, warp 1 issues
-// the products into two accumulators in turn, warps 4-19 turn the finished one into the next operand.
+// products together, with a barrier of the whole grid between them (1.5 us; 15 launches would keep
+// the host busy for 40).  Two CTAs of a cluster share tiles of 256 x 256 or 256 x 128 (PAIR), or a CTA has
+// one of 128 x 64.  Warp 0 brings the operands, warp 1 issues the products into two accumulators in turn,
+// warps 4-19 turn the finished one into the next operand.  Large products run at the tensor cores' power
+// limit (4096 x 14336: 0.31 to 0.36 us for 256 x 256 x 64 on a pair, where a cuBLAS product of 8192 takes 0.32 to
+// 0.36); small ones are 15 times the latency of copies (0.8 us), accumulator (1) and barrier (1.5).
 //
 // Waits are bounded: where one runs out the CTA's outputs are NaN, and with the next
 // barrier everybody's.
