@@ -727,7 +727,7 @@ __global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_
                 if (t == 0) asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(arrived) : "memory");
                 // (the counters only grow: this product's splits come on top of the earlier steps')
                 bool came = true;
-                if (lane == 0) came = grid_wait(arrived, uint32_t(splits) * uint32_t(step + 1), kWaitNs);
+                if (lane == 0) came = grid_wait(arrived, uint32_t(splits) * uint32_t(step + 1), p.limit_ns);
                 ok = sum_warps_agree(__all_sync(0xffffffffu, came));
                 if (!ok) break;
 #pragma unroll 1
@@ -1865,8 +1865,9 @@ extern "C" lc_status lc_orthogonalize(int device, void* cuda_stream, const lc_ma
     p.out = static_cast<uint8_t*>(out->data);
     p.out_pitch = out->stride * 2;
     p.out_batch = out->batch_stride * 2;
-    // the grid may be a second ahead of a CTA, and as much longer as a product takes at a twentieth of the tensor cores' rate
-    p.limit_ns = kWaitNs + uint64_t(2.0 * double(batch) * double(q.m) * double(q.m) * double(q.n) * 1e-5);
+    // the last CTAs start once other streams' kernels make room for them, and a product takes its time (at a twentieth of the
+    // tensor cores' rate)
+    p.limit_ns = (ops_stall() ? kWaitNs : 20 * kWaitNs) + uint64_t(2.0 * double(batch) * double(q.m) * double(q.m) * double(q.n) * 1e-5);
     p.batch = int32_t(batch);
     p.m = int32_t(q.m);
     p.n = int32_t(q.n);
