@@ -824,7 +824,9 @@ typedef struct {
  * and U = g + beta (momentum - g) with nesterov != 0, else U = momentum.
  * A matrix with a NaN or an infinity comes out as NaN, one of zeros as zeros
  * (with eps = 0 as NaN); the others of the batch are not affected.
- * A wait that runs out leaves NaN in out; the momentum has moved.
+ * A wait that runs out leaves NaN in out (its CTAs wait for one another for 20 s
+ * and more, since other streams' kernels may keep some from starting); the
+ * momentum has moved.
  * The product kernel is one cooperative launch: calls on two streams at once
  * follow one another where they do not fit the device together. */
 #define LC_ORTH_MAX_DIM 65536

@@ -43,9 +43,10 @@ struct AddNormGradParams {
     const float* rstd;
     uint8_t* dx;
     float* part;          // [CTAs][2][dim], the first of the two
+    uint8_t* dw;          // where the only CTA's sums go straight (null: to part)
     int64_t ntok, dy_pitch, dr_pitch, s_pitch, q_pitch, e_pitch, dx_pitch;
     float inv_dim;
-    int32_t dim, w_bf16, wide;
+    int32_t dim, w_bf16, wide, g_bf16, accumulate;
     int32_t stall;
 };
 
@@ -228,8 +229,18 @@ __global__ void __launch_bounds__(direct_threads(W)) add_norm_grad_kernel(AddNor
     for (int i = 0; i < B; ++i) {
         const int c = (warp + i * W) * LC_ACT_BLOCK + lane * 4;
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-            if (c + k < p.dim) out[c + k] = dw[i][k];
+        for (int k = 0; k < 4; ++k) {
+            if (c + k >= p.dim) continue;
+            if (!p.dw) {
+                out[c + k] = dw[i][k];
+            } else if (p.g_bf16) {
+                __nv_bfloat16* o = reinterpret_cast<__nv_bfloat16*>(p.dw) + c + k;
+                *o = __float2bfloat16_rn(p.accumulate ? __bfloat162float(*o) + dw[i][k] : dw[i][k]);
+            } else {
+                float* o = reinterpret_cast<float*>(p.dw) + c + k;
+                *o = p.accumulate ? *o + dw[i][k] : dw[i][k];
+            }
+        }
     }
 }
 
@@ -600,6 +611,7 @@ cudaError_t launch_direct_grad(const AddNormGradParams& p, int sms, cudaStream_t
     int64_t grid = int64_t(sms) * (512 / NT < 4 ? 512 / NT : 4);
     grid = grid < kGradCtas ? grid : kGradCtas;
     grid = grid < want ? grid : want;
+    if (p.dw) grid = 1;
     *ctas = int(grid);
     cudaGetLastError();
     add_norm_grad_kernel<T, R, W, B, KEPT><<<unsigned(grid), NT, 0, s>>>(p);
@@ -689,6 +701,8 @@ cudaError_t grad_ring(const AddNormGradParams& p, int sms, cudaStream_t s, int* 
 //              6.5; 304 of 2048 6.1, 5.7; fp32 304 of 768 5.1, 4.9; 608 of 768 5.5, 6.3; 152 of 4096 5.8, 6.6
 bool forward_ring(int64_t ntok, int64_t dim, bool stream32) { return !stream32 || ntok * dim >= 4900000; }
 bool backward_ring(int64_t ntok, int64_t dim, bool stream32, int sms) { return dim >= 4096 || ntok >= (stream32 ? 4 : 2) * sms; }
+// Tokens of a backward that one CTA takes: four rounds of the rows that it has at a time.
+int64_t few(int64_t dim) { return dim <= 256 ? 16 : dim <= 512 ? 8 : 4; }
 constexpr int64_t kMaxRows = int64_t(1) << 40;
 
 // The types that go together: 0 both bf16, 1 a 32-bit stream around bf16 branches, 2 both fp32, -1 none.
@@ -886,7 +900,13 @@ extern "C" lc_status lc_add_norm_grad(int device, void* cuda_stream, const lc_ro
     const int64_t many = ntok > 1;
     p.wide = wide_rows(p.dy, many * p.dy_pitch, 4 * te) && wide_rows(p.dr, many * p.dr_pitch, 4 * re) && wide_rows(p.s, many * p.s_pitch, 4 * re) &&
              wide_rows(p.dx, many * p.dx_pitch, 4 * re) && wide_rows(p.w, 0, 4 * elem_size(w_dtype));
-    const bool vec = wide_rows(p.dy, many * p.dy_pitch, 16) && wide_rows(p.dr, many * p.dr_pitch, 16) && wide_rows(p.s, many * p.s_pitch, 16) &&
+    // a few tokens: one CTA for all of them, whose sums need no second kernel (4 tokens of 256: 7.2 us on the host to 4.7)
+    if (ntok <= few(dim)) {
+        p.dw = static_cast<uint8_t*>(dweight);
+        p.g_bf16 = g_dtype == LC_BF16;
+        p.accumulate = accumulate != 0;
+    }
+    const bool vec = !p.dw && wide_rows(p.dy, many * p.dy_pitch, 16) && wide_rows(p.dr, many * p.dr_pitch, 16) && wide_rows(p.s, many * p.s_pitch, 16) &&
                      wide_rows(p.dx, many * p.dx_pitch, 16) && dim * te % 16 == 0;
     const int sms = ops_sm_count(device);
     using B = __nv_bfloat16;
@@ -903,6 +923,6 @@ extern "C" lc_status lc_add_norm_grad(int device, void* cuda_stream, const lc_ro
         else if (types == 1) go(sum ? direct_grad<B, float, false> : direct_grad<B, float, true>);
         else go(sum ? direct_grad<float, float, false> : direct_grad<float, float, true>);
     }
-    if (err == cudaSuccess) err = norm_fold(p.part, ctas, p.dim, dweight, nullptr, g_dtype == LC_BF16, accumulate != 0, s);
+    if (err == cudaSuccess && !p.dw) err = norm_fold(p.part, ctas, p.dim, dweight, nullptr, g_dtype == LC_BF16, accumulate != 0, s);
     return ops_launched(call, err);
 }
