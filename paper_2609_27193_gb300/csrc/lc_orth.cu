@@ -189,6 +189,26 @@ __device__ __forceinline__ void tmem_ld16(uint32_t addr, float (&f)[16]) {
     for (int i = 0; i < 16; ++i) f[i] = __uint_as_float(r[i]);
 }
 
+// Sixteen columns from each of two places.
+__device__ __forceinline__ void tmem_ld16(uint32_t addr, float (&f)[16], uint32_t addr2, float (&g)[16]) {
+    uint32_t r[16], q[16];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%32];\n\t"
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%33];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(q[0]), "=r"(q[1]), "=r"(q[2]), "=r"(q[3]),
+          "=r"(q[4]), "=r"(q[5]), "=r"(q[6]), "=r"(q[7]), "=r"(q[8]), "=r"(q[9]), "=r"(q[10]), "=r"(q[11]), "=r"(q[12]), "=r"(q[13]),
+          "=r"(q[14]), "=r"(q[15])
+        : "r"(addr), "r"(addr2)
+        : "memory");
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        f[i] = __uint_as_float(r[i]);
+        g[i] = __uint_as_float(q[i]);
+    }
+}
+
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
     const __half2 h = __floats2half2_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&h);
@@ -1235,7 +1255,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) orth_small_kernel(const __gr
             }
             __syncwarp();
         }
-        ok = mbar_wait_bounded(done, round, kWaitNs) && ok;
+        ok = ok && mbar_wait_bounded(done, round, kWaitNs);
         round ^= 1;
         __syncwarp();
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -1259,12 +1279,14 @@ __global__ void __launch_bounds__(kSmallThreads, 1) orth_small_kernel(const __gr
         const bool diagonal = group == quad;
         const float to_a = p.a_scale / (p.x_scale * p.x_scale), nan = __uint_as_float(0x7fffffffu);
         float f[32];
+        {
+            float g[16], h[16];
+            tmem_ld16(from, g, from + 16, h);
 #pragma unroll
-        for (int c = 0; c < 32; c += 16) {
-            float g[16];
-            tmem_ld16(from + c, g);
-#pragma unroll
-            for (int k = 0; k < 16; ++k) f[c + k] = g[k];
+            for (int k = 0; k < 16; ++k) {
+                f[k] = g[k];
+                f[16 + k] = h[k];
+            }
         }
         if (!ok) {
 #pragma unroll
@@ -1291,6 +1313,8 @@ __global__ void __launch_bounds__(kSmallThreads, 1) orth_small_kernel(const __gr
                 sts128(as + small_at(row, group * 32 + k), make_uint4(w[0], w[1], w[2], w[3]));
             }
         } else {
+            // (plain stores and the cluster's barrier: stores that a barrier of the receiver counts, without waiting for all,
+            // took 46 us a call for 43 with two CTAs, 54 for 57 with sixteen)
             // a CTA adds up 128 / C rows, in the CTAs' order; four columns of these rows are one piece (and 16 bytes more,
             // so that pieces of a row lie in different banks)
             const int each = kSmallRows / C, pitch = each * 16 + 16;
@@ -1337,10 +1361,11 @@ __global__ void __launch_bounds__(kSmallThreads, 1) orth_small_kernel(const __gr
             // b A0 + c (A0^2 + (d_i + d_j) A0), times B's scale; here A0, d and A0^2 are times a_scale (A0^2 twice)
             const float back = 1.0f / p.a_scale, dr = d[row], to_b = co.c * back * back * co.scale;
             const float2 cs = both(to_b), bc = both(fmaf(to_b, dr, co.b * back * co.scale));
+            float g2[2][16];
+            tmem_ld16(from, g2[0], from + 16, g2[1]);
 #pragma unroll
             for (int c = 0; c < 32; c += 16) {
-                float g[16];
-                tmem_ld16(from + c, g);
+                float(&g)[16] = g2[c / 16];
                 if (diagonal) {
                     // (A0 is zero there)
                     float on = 0.0f;
@@ -1382,8 +1407,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) orth_small_kernel(const __gr
 #pragma unroll
         for (int c = 0; c < kMine; c += 16) {
             float g[16], h[16];
-            tmem_ld16(tmem + mine + group * kMine + c, g);
-            tmem_ld16(state + c, h);
+            tmem_ld16(tmem + mine + group * kMine + c, g, state + c, h);
 #pragma unroll
             for (int k = 0; k < 16; k += 2) {
                 const float2 v = fma2(both(keep), make_float2(h[k], h[k + 1]), mul2(make_float2(g[k], g[k + 1]), both(back)));
