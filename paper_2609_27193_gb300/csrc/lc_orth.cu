@@ -1676,10 +1676,13 @@ cudaError_t launch_products(int device, OrthParams& p, const Plan& q, cudaStream
 struct Small {
     int ctas, blocks;
 };
-Small small_of(int64_t m, int64_t n) {
+// As few as hold it; twice as many, with half of the columns each, where the device has room for all matrices' clusters at once (128 x
+// 512: 39 us with four, 43 with two; 128 x 1024 42 with eight, 47 with four, but sixteen of them 84 and 49).
+Small small_of(int64_t batch, int64_t m, int64_t n) {
     if (m > kSmallRows || n > kSmallCols * kSmallCtas) return {0, 0};
     int c = 1;
     while (int64_t(c) * kSmallCols < n) c *= 2;
+    if (c > 1 && c < kSmallCtas && batch * 2 * c <= (c > 2 ? 64 : 128)) c *= 2;
     return {c, int((n + c * 64 - 1) / (c * 64))};
 }
 template <int K>
@@ -1744,7 +1747,7 @@ using namespace lc;
 
 extern "C" uint64_t lc_orthogonalize_workspace(int64_t batch, int64_t rows, int64_t cols) {
     if (!orth_sizes(batch, rows, cols) || batch == 0) return 0;
-    if (small_of(rows < cols ? rows : cols, rows < cols ? cols : rows).ctas) return 0;
+    if (small_of(batch, rows < cols ? rows : cols, rows < cols ? cols : rows).ctas) return 0;
     return uint64_t(plan_of(batch, rows, cols).bytes);
 }
 
@@ -1789,7 +1792,7 @@ extern "C" lc_status lc_orthogonalize(int device, void* cuda_stream, const lc_ma
     // elements of about 1 where the matrix has no structure: sqrt(m n) times those of X
     const float middle = float(std::ldexp(1.0, std::ilogb(std::sqrt(double(q.m) * double(q.n)))));
     if (middle < p.x_scale) p.x_scale = middle;
-    const Small small = small_of(q.m, q.n);
+    const Small small = small_of(batch, q.m, q.n);
     const uint64_t need = lc_orthogonalize_workspace(batch, rows, cols);
     if (workspace_bytes < need)
         return fail_status(LC_ERR_CAPACITY, "%s: %llu bytes of workspace, %llu needed", call, (unsigned long long)workspace_bytes,
