@@ -858,37 +858,48 @@ __global__ void __launch_bounds__(256) orth_norm_kernel(PrepParams p) {
         for (int i = int(blockIdx.x) * 256 + int(threadIdx.x); i < p.nzero; i += p.parts * 256) p.zero[i] = 0;
     const uint8_t* u = p.u + int64_t(mat) * p.u_batch;
     uint8_t* m = p.m ? p.m + int64_t(mat) * p.m_batch : nullptr;
-    const int64_t width = (p.cols + 7) / 8, all = p.rows * width;
+    const int64_t width = (p.cols + 7) / 8, all = p.rows * width, step = int64_t(p.parts) * 256;
     float s1 = 0.0f, s2 = 0.0f;
-    for (int64_t at = int64_t(blockIdx.x) * 256 + threadIdx.x; at < all; at += int64_t(p.parts) * 256) {
-        int64_t r, c;
-        split_item(at, width, r, c);
-        c *= 8;
-        float f[8];
-        load8(u + r * p.u_pitch, p.u_bf16, p.wide, c, p.cols, f);
+    // two eights at a time, all of them asked for before the first is worked on
+    for (int64_t at = int64_t(blockIdx.x) * 256 + threadIdx.x; at < all; at += 2 * step) {
+        float f[2][8], v[2][8];
+        int64_t r[2], c[2];
+        const bool two = at + step < all;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            split_item(h && two ? at + step : at, width, r[h], c[h]);
+            c[h] *= 8;
+            load8(u + r[h] * p.u_pitch, p.u_bf16, p.wide, c[h], p.cols, f[h]);
+        }
         if (m) {
-            float v[8];
-            float* row = reinterpret_cast<float*>(m + r * p.m_pitch);
-            load8(reinterpret_cast<const uint8_t*>(row), false, p.wide, c, p.cols, v);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                v[k] = moved(p, v[k], f[k]);
-                f[k] = update_of(p, v[k], f[k]);
-            }
-            if (p.wide && c + 8 <= p.cols) {
-                *reinterpret_cast<float4*>(row + c) = make_float4(v[0], v[1], v[2], v[3]);
-                *reinterpret_cast<float4*>(row + c + 4) = make_float4(v[4], v[5], v[6], v[7]);
-            } else {
-#pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    if (c + k < p.cols) row[c + k] = v[k];
-            }
+            for (int h = 0; h < 2; ++h) load8(m + r[h] * p.m_pitch, false, p.wide, c[h], p.cols, v[h]);
         }
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            s1 = fmaf(f[k], f[k], s1);
-            const float small = f[k] * 0x1p-80f;
-            s2 = fmaf(small, small, s2);
+        for (int h = 0; h < 2; ++h) {
+            if (h && !two) break;
+            if (m) {
+                float* row = reinterpret_cast<float*>(m + r[h] * p.m_pitch) + c[h];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    v[h][k] = moved(p, v[h][k], f[h][k]);
+                    f[h][k] = update_of(p, v[h][k], f[h][k]);
+                }
+                if (p.wide && c[h] + 8 <= p.cols) {
+                    *reinterpret_cast<float4*>(row) = make_float4(v[h][0], v[h][1], v[h][2], v[h][3]);
+                    *reinterpret_cast<float4*>(row + 4) = make_float4(v[h][4], v[h][5], v[h][6], v[h][7]);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        if (c[h] + k < p.cols) row[k] = v[h][k];
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                s1 = fmaf(f[h][k], f[h][k], s1);
+                const float small = f[h][k] * 0x1p-80f;
+                s2 = fmaf(small, small, s2);
+            }
         }
     }
 #pragma unroll
