@@ -196,8 +196,8 @@ def _packed(steps, coefficients):
     """The coefficients of every step as the library takes them: three doubles each."""
     if not 1 <= steps <= 16:
         raise ValueError("1 to 16 steps, not %d" % steps)
-    every = coefficients if isinstance(coefficients[0], tuple) else (coefficients,) * steps
-    if len(every) != steps or any(len(c) != 3 for c in every):
+    every = coefficients if coefficients and isinstance(coefficients[0], tuple) else (coefficients,) * steps
+    if len(every) != steps or any(not isinstance(c, tuple) or len(c) != 3 for c in every):
         raise ValueError("three coefficients for every step, or for each of %d" % steps)
     return struct.pack("%dd" % (3 * steps), *(x for c in every for x in c))
 

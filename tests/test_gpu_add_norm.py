@@ -13,7 +13,7 @@ from tests.test_gpu_ops import BF, F32, SUMS, U, gen, norm_grad_ref, quantize, r
 TYPES = [(BF, BF), (BF, F32), (F32, F32)]
 # the forms: a warp or several a row, through rings or not, widths off 4 and off 128, the widest
 SHAPES = [(1, 1), (1, 256), (3, 5), (4, 9000), (8, 300), (9, 300), (16, 250), (17, 250), (64, 256), (5, 127), (6, 129), (17, 520), (9, 915), (33, 1024), (300, 768), (4, 4100),
-          (7, 8191), (2, 12296), (3, 16384), (4200, 96), (5000, 256), (700, 1000), (613, 2048), (620, 4096), (305, 8192), (310, 16384)]
+          (7, 8191), (2, 12296), (3, 16384), (4200, 96), (5000, 256), (700, 1000), (613, 2048), (620, 4096), (305, 8192), (310, 16384), (2500, 2052)]
 
 
 @pytest.fixture(scope="module")

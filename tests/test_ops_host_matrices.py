@@ -88,5 +88,7 @@ def test_without_a_device():
     from paper_2609_27193_gb300 import ops
     with pytest.raises(ValueError):
         ops.orthogonalize(torch.zeros(4, 4))
-    with pytest.raises(ValueError):
-        ops.orthogonalize(torch.zeros(4, 4), steps=0)
+    for kw in (dict(steps=0), dict(steps=17), dict(coefficients=()), dict(coefficients=(1.0,)), dict(coefficients=[[1.0, 2.0]]),
+               dict(steps=2, coefficients=((1.0, 2.0, 3.0), 4.0)), dict(steps=3, coefficients=((1.0, 2.0, 3.0),) * 2)):
+        with pytest.raises(ValueError):
+            ops.orthogonalize(torch.zeros(4, 4), **kw)
