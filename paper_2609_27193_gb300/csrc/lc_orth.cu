@@ -67,9 +67,9 @@ struct TileOf {
     static constexpr int kDepth = PAIR ? 1 : 2;
     static constexpr int kLeft = 2 * kBoxBytes, kRight = kCols / kCtas / kBox * kBoxBytes;
     static constexpr int kStageBytes = kDepth * (kLeft + kRight);
-    static constexpr int kStages = PAIR ? 5 : 4;
-    // a warp has 32 rows of a quarter of the columns; half a box of staging for as many warps as fill 64 columns
-    static constexpr int kStaging = kSumWarps * (kCols / 4) / kBox * (kBoxBytes / 2);
+    static constexpr int kStages = PAIR ? 6 : 4;
+    // half a box of staging for each group of 32 rows, two of them where there is more than one box
+    static constexpr int kStaging = (kCols > kBox ? 2 : 1) * 4 * (kBoxBytes / 2);
     static constexpr int kSmem = kStages * kStageBytes + kStaging + 1024;   // and room to align them to 1024 bytes
     static constexpr int kTmemCols = 2 * kCols;
     // fp32 accumulator, fp16 operands; columns, and which way their rows lie, are added for each product
@@ -342,6 +342,9 @@ __device__ __forceinline__ bool sum_warps_agree(bool ok) {
     return r != 0;
 }
 
+// The four warps with the same rows meet.
+__device__ __forceinline__ void rows_meet(int quad) { asm volatile("bar.sync %0, 128;" ::"r"(2 + quad) : "memory"); }
+
 __device__ __forceinline__ void sts128(uint32_t addr, const uint4& v) {
     asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
@@ -357,21 +360,21 @@ __device__ __forceinline__ uint32_t lds16(uint32_t addr) {
 }
 
 // 32 rows of 64 columns of the output, from 4 KB of staging in shared memory (rows of 128 bytes,
-// swizzled), by `share` warps of which this is the `part`th.  r0, c0: the first row and column.
-__device__ __forceinline__ void store_rows(const OrthParams& p, int mat, int r0, int c0, uint32_t stage, int share, int part, int lane) {
+// swizzled), by four warps of which this is the `part`th.  r0, c0: the first row and column.
+__device__ __forceinline__ void store_rows(const OrthParams& p, int mat, int r0, int c0, uint32_t stage, int part, int lane) {
     uint8_t* base = p.out + int64_t(mat) * p.out_batch;
     if (p.wide && c0 + kBox <= p.n) {
         const int piece = lane % 8;
-#pragma unroll 2
-        for (int k = part; k < 8; k += share) {
-            const int r = k * 4 + lane / 8;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int r = (k * 4 + part) * 4 + lane / 8;
             const uint4 v = lds128(stage + piece_at(r, piece));
             if (r0 + r < p.m) *reinterpret_cast<uint4*>(base + int64_t(r0 + r) * p.out_pitch + c0 * 2 + piece * 16) = v;
         }
         return;
     }
 #pragma unroll 4
-    for (int k = part; k < 64; k += share) {
+    for (int k = part; k < 64; k += 4) {
         const int r = k / 2, c = k % 2 * 32 + lane;
         const uint32_t v = lds16(stage + piece_at(r, c / 8) + c % 8 * 2);
         if (r0 + r < p.m && c0 + c < p.n) *reinterpret_cast<uint16_t*>(base + int64_t(r0 + r) * p.out_pitch + (c0 + c) * 2) = uint16_t(v);
@@ -651,6 +654,9 @@ __global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_
         const int row = quad * 32 + lane;                 // of this CTA's 128
         const uint32_t first_taken = PAIR ? cluster_addr(taken, 0) : taken;
         const uint32_t from = tmem + (uint32_t(quad * 32) << 16);
+        const uint32_t staging = ring + kStages * kStageBytes + quad * (kBoxBytes / 2);
+        constexpr bool kTwo = kCols > kBox;
+        int turn = 0;
         Ring<2> acc;
         bool ok = true;
         for (int ph = 0; ph < phases; ++ph) {
@@ -659,38 +665,28 @@ __global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_
             ok = sum_warps_agree(wait_long(go, ph & 1, p.limit_ns));
             if (!ok) break;
             const int splits = p.splits[phase], items = items_of<PAIR>(p, phase);
-            const int cols = cols_of<PAIR>(p, phase), warp_cols = cols / 4;
-            // half a box of staging, filled by `share` warps with the same rows; the first of them stores it
-            const int share = kBox / warp_cols, part = group % share, place = group / share * 4 + quad;
-            const uint32_t stage = ring + kStages * kStageBytes + place * (kBoxBytes / 2);
-            auto stage_meet = [&]() {
-                if (share == 1) __syncwarp();
-                else asm volatile("bar.sync %0, %1;" ::"r"(2 + place), "r"(share * 32) : "memory");
-            };
+            const int cols = cols_of<PAIR>(p, phase);
             for (int i = unit; i < items; i += units, acc.next()) {
                 const Item w = item_of<PAIR>(p, phase, i);
                 Finish fin(p, phase, step, final, w.mat, w.i * Tile::kRows + rank * kCtaRows + row);
-                const int c0 = w.j * cols + group * warp_cols;
+                const int c0 = w.j * cols + group * kChunk;   // the four groups of warps share every box's columns
                 if (splits == 1) {
                     // what is read beside the accumulator is on its way before that is complete, and then a chunk ahead
                     fin.ask<2>(c0, lane);
                     ok = sum_warps_agree(mbar_wait_warp(summed + 8 * acc.at, acc.round));
                     if (!ok) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    // the staging's last rows have been read
-                    if (part == 0 && lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-                    stage_meet();
 #pragma unroll 1
-                    for (int c = 0; c < warp_cols; c += kChunk) {
+                    for (int c = 0; c < cols; c += kBox) {
                         float f[kChunk];
-                        tmem_ld16(from + acc.at * kCols + group * warp_cols + c, f);
-                        if (c + kChunk == warp_cols) {
+                        tmem_ld16(from + acc.at * kCols + group * kChunk + c, f);
+                        if (c + kBox == cols) {
                             asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                             __syncwarp();
                             if (lane == 0) arrive_at(first_taken + 8 * acc.at);
                         }
                         fin.take<2>();
-                        if (c + kChunk < warp_cols) fin.ask<2>(c0 + c + kChunk, lane);
+                        if (c + kBox < cols) fin.ask<2>(c0 + c + kBox, lane);
                         uint4 v[2];
 #pragma unroll
                         for (int k = 0; k < 2; ++k) v[k] = fin.piece(c0 + c + 8 * k, k, f + 8 * k);
@@ -707,20 +703,26 @@ __global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_
                                 v[k] = make_uint4(pack_bf16(f[8 * k], f[8 * k + 1]), pack_bf16(f[8 * k + 2], f[8 * k + 3]),
                                                   pack_bf16(f[8 * k + 4], f[8 * k + 5]), pack_bf16(f[8 * k + 6], f[8 * k + 7]));
                         }
+                        // 32 rows of a box are one piece of memory.  Two halves of staging take turns: the one before this has
+                        // been read when its store's thread comes to this one's meeting.
+                        const uint32_t stage = staging + (kTwo ? turn : 0) * 4 * (kBoxBytes / 2);
+                        if constexpr (!kTwo) {
+                            if (group == 0 && lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                            rows_meet(quad);
+                        }
 #pragma unroll
-                        for (int k = 0; k < 2; ++k) sts128(stage + piece_at(lane, (c0 + c) % kBox / 8 + k), v[k]);
-                    }
-                    // 32 rows of a box are one piece of memory
-                    const int col = c0 - c0 % kBox;
-                    if (!final) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    stage_meet();
-                    if (!final) {
-                        if (part == 0 && lane == 0) {
+                        for (int k = 0; k < 2; ++k) sts128(stage + piece_at(lane, group * 2 + k), v[k]);
+                        if (!final) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                        if (kTwo && group == 0 && lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                        rows_meet(quad);
+                        const int col = w.j * cols + c;
+                        if (final) {
+                            store_rows(p, w.mat, fin.gr - lane, col, stage, group, lane);
+                        } else if (group == 0 && lane == 0) {
                             bulk_s2g(fin.out + int64_t(col / kBox) * kBoxBytes + quad % 2 * (kBoxBytes / 2), stage, kBoxBytes / 2);
                             asm volatile("cp.async.bulk.commit_group;" ::: "memory");
                         }
-                    } else if (!p.turned) {
-                        store_rows(p, w.mat, fin.gr - lane, col, stage, share, part, lane);
+                        turn ^= 1;
                     }
                     continue;
                 }
