@@ -31,7 +31,7 @@
 // the host busy for 40).  Two CTAs of a cluster share tiles of 256 x 256 or 256 x 128 (PAIR), or a CTA has
 // one of 128 x 64.  Warp 0 brings the operands, warp 1 issues the products into two accumulators in turn,
 // warps 4-19 turn the finished one into the next operand.  Large products run at the tensor cores' power
-// limit (4096 x 14336: 0.31 to 0.36 us for 256 x 256 x 64 on a pair, where a cuBLAS product of 8192 takes 0.32 to
+// limit (4096 x 14336: 0.30 to 0.36 us for 256 x 256 x 64 on a pair, where a cuBLAS product of 8192 takes 0.32 to
 // 0.36); small ones are 15 times the latency of copies (0.8 us), accumulator (1) and barrier (1.5).
 //
 // Waits are bounded: where one runs out the CTA's outputs are NaN, and with the next
