@@ -669,10 +669,13 @@ lc_status lc_measure_noalloc_debug(int device, void* cuda_stream, const lc_segme
 lc_status lc_ops_debug(int32_t debug_flags);
 
 /* For a caller that knows of every array it passes that it is device memory of the
- * call's device (an allocator's own records: torch's CUDA tensors): while on is not 0,
- * the operators that the calling host thread calls do not ask the driver about
- * each (0.1 us an array, 0.7 to 1.2 of the 5 to 14 us that a small call takes on
- * the host).  All other checks stay. */
+ * call's device, as long as the array: while on is not 0, the operators that the
+ * calling host thread calls do not ask the driver about each (0.1 us an array,
+ * 0.7 to 1.2 of the 5 to 14 us that a small call takes on the host).  All other
+ * checks stay.  The binding over torch tensors knows it of those whose storage is
+ * from torch's own CUDA allocators (one of their pools may be filled by an allocator
+ * of the program's: what that hands out counts as theirs) and reaches as far as the
+ * tensor does; one tensor of another origin in a call, and the driver is asked. */
 void lc_ops_known_memory(int32_t on);
 
 /* Rows of `dim` elements of type dtype (lc_dtype); row r starts `stride`

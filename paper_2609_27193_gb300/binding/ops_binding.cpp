@@ -9,6 +9,7 @@
 #include <ATen/core/Tensor.h>
 #include <ATen/cuda/EmptyTensor.h>
 #include <c10/core/GradMode.h>
+#include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAStream.h>
 #include <cuda_runtime_api.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -35,6 +36,9 @@ struct ValueError : std::runtime_error {
 struct StatusError {
     lc_status status;
 };
+struct Refused : std::runtime_error {   // as LC_ERR_INVALID_ARG
+    using std::runtime_error::runtime_error;
+};
 struct Raised {};              // a Python error is set already
 
 void check(lc_status st) {
@@ -42,6 +46,35 @@ void check(lc_status st) {
 }
 
 // --- arguments ----------------------------------------------------------------
+
+// Whether a tensor's memory came from torch's own CUDA allocators, which hand out device memory of the device that
+// the tensor names.  (An allocator that the program put in their place, another process's memory, what came by
+// DLPack or as an address can be anything.)
+bool from_torch(const c10::Storage& storage) {
+    // which allocator there is does not change any more once there is a CUDA tensor
+    static const c10::DeleterFnPtr own = [] {
+        c10::cuda::CUDACachingAllocator::CUDAAllocator* a = c10::cuda::CUDACachingAllocator::get();
+        const std::string name = a ? a->name() : "";
+        return name == "native" || name == "cudaMallocAsync" ? a->raw_deleter() : nullptr;
+    }();
+    return own && storage.data_ptr().get_deleter() == own;
+}
+
+// A tensor keeps its device, shape and offset when its storage is released or cut (resize_ of it): the address is then
+// an offset from nothing, or its rows lie beyond the end.  Where the memory is not torch's the library asks the driver
+// about every array of the call.
+void look_behind(const at::Tensor& t) {
+    if (t.layout() != at::kStrided || !t.has_storage() || t.numel() == 0) return;
+    int64_t last = t.storage_offset();
+    const at::IntArrayRef sizes = t.sizes(), strides = t.strides();
+    for (size_t k = 0; k < sizes.size(); ++k) last += (sizes[k] - 1) * strides[k];
+    const uint64_t reach = uint64_t(last + 1) * t.element_size();
+    const c10::Storage& storage = t.storage();
+    if (storage.nbytes() < reach || (t.is_cuda() && !storage.data()))
+        throw Refused("a tensor reaches " + std::to_string(reach) + " bytes of a storage that has " +
+                      std::to_string(storage.data() || !t.is_cuda() ? storage.nbytes() : 0));
+    if (t.is_cuda() && !from_torch(storage)) lc_ops_known_memory(0);
+}
 
 struct Args {
     PyObject* const* a;
@@ -54,7 +87,9 @@ struct Args {
         PyObject* o = a[at++];
         if (o == Py_None) return at::Tensor();
         if (!THPVariable_Check(o)) throw TypeError("a tensor is needed");
-        return THPVariable_Unpack(o);
+        const at::Tensor& t = THPVariable_Unpack(o);
+        look_behind(t);
+        return t;
     }
     int64_t integer() {
         const long long v = PyLong_AsLongLong(a[at++]);
@@ -561,11 +596,22 @@ PyObject* set_errors(PyObject* const* args, Py_ssize_t nargs) {
     Py_RETURN_NONE;
 }
 
-// What the operators get are torch's CUDA tensors, whose device was compared: the driver need not be asked.
+// What the operators get are torch's CUDA tensors, whose device and storage are looked at: the driver need not be asked,
+// unless one of them has memory of another origin (look_behind takes the word back).
 struct KnownMemory {
     KnownMemory() { lc_ops_known_memory(1); }
     ~KnownMemory() { lc_ops_known_memory(0); }
 };
+
+void raise_status(lc_status status, const char* what) {
+    PyObject* err = g_error ? PyObject_CallFunction(g_error, "is", int(status), what) : nullptr;
+    if (err) {
+        PyErr_SetObject(g_error, err);
+        Py_DECREF(err);
+    } else if (!PyErr_Occurred()) {
+        PyErr_SetString(PyExc_RuntimeError, what);
+    }
+}
 
 // No C++ exception leaves a call.
 template <PyObject* (*F)(PyObject* const*, Py_ssize_t)>
@@ -574,13 +620,9 @@ PyObject* guarded(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
         const KnownMemory known;
         return F(args, nargs);
     } catch (const StatusError& e) {
-        PyObject* err = g_error ? PyObject_CallFunction(g_error, "is", int(e.status), lc_last_error()) : nullptr;
-        if (err) {
-            PyErr_SetObject(g_error, err);
-            Py_DECREF(err);
-        } else if (!PyErr_Occurred()) {
-            PyErr_SetString(PyExc_RuntimeError, lc_last_error());
-        }
+        raise_status(e.status, lc_last_error());
+    } catch (const Refused& e) {
+        raise_status(LC_ERR_INVALID_ARG, e.what());
     } catch (const TypeError& e) {
         PyErr_SetString(PyExc_TypeError, e.what());
     } catch (const ValueError& e) {
