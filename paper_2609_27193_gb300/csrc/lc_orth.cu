@@ -819,7 +819,7 @@ __global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_
 struct PrepParams {
     const uint8_t* u;
     uint8_t* m;              // momentum (null: none)
-    float2* part;            // [batch][parts]
+    float4* part;            // [batch][parts]: Squares
     uint32_t* zero;          // counters of the product kernel
     uint8_t* hi;
     uint8_t* xf;
@@ -851,17 +851,67 @@ __device__ __forceinline__ void load8(const uint8_t* row, bool bf16, bool wide, 
 __device__ __forceinline__ float moved(const PrepParams& p, float m, float g) { return fmaf(1.0f - p.beta, g - m, m); }
 __device__ __forceinline__ float update_of(const PrepParams& p, float m, float g) { return p.nesterov ? fmaf(p.beta, m - g, g) : m; }
 
-// Moves the momentum and leaves sums of the update's squares, one pair a CTA: as they are, and of values
-// times 2^-80 for a matrix whose squares leave fp32's range.
+// Sums of an update's squares: as they are, and of values times 2^-80 and 2^100 for a matrix whose squares leave fp32's
+// range on either side.  A sum of plain squares from 2^-80 on has lost nothing that counts: what a square below 2^-126 loses is
+// at most 2^-150, and 2^32 of them 2^-118.  Below it no value is above 2^-40, so the scaled squares stay below 2^120, and
+// the smallest value of all, 2^-149, has one of 2^-98.  The scaled sums are added to where a thread's plain one
+// says that they may be needed: below 2^-80, as all threads' are where the matrix's is, or above 2^60 (what it left out
+// until then is nothing beside a sum beyond 2^128).
+struct Squares {
+    float plain = 0.0f, down = 0.0f, up = 0.0f;
+    template <int N>
+    __device__ __forceinline__ void count(const float (&f)[N]) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) plain = fmaf(f[k], f[k], plain);
+        if (plain < 0x1p-80f) {
+#pragma unroll
+            for (int k = 0; k < N; ++k) up = fmaf(f[k] * 0x1p100f, f[k] * 0x1p100f, up);
+        } else if (plain > 0x1p60f) {
+#pragma unroll
+            for (int k = 0; k < N; ++k) down = fmaf(f[k] * 0x1p-80f, f[k] * 0x1p-80f, down);
+        }
+    }
+    __device__ __forceinline__ void add(const float4& v) {
+        plain += v.x;
+        down += v.y;
+        up += v.z;
+    }
+    __device__ __forceinline__ float4 all() const { return make_float4(plain, down, up, 0.0f); }
+    // over a warp's lanes
+    __device__ __forceinline__ void join() {
+#pragma unroll
+        for (int o = 16; o; o >>= 1) {
+            plain += __shfl_xor_sync(0xffffffffu, plain, o);
+            down += __shfl_xor_sync(0xffffffffu, down, o);
+            up += __shfl_xor_sync(0xffffffffu, up, o);
+        }
+    }
+    // What an update is multiplied by, one factor after the other, to be X times x_scale: a power of two that brings very
+    // large and very small values near 1, and the rest.
+    __device__ __forceinline__ void factors(float x_scale, double eps, float (&f)[2]) const {
+        const bool large = plain > 3.402823466e38f;
+        const double norm = large ? sqrt(double(down)) * 0x1p80 : plain < 0x1p-80f ? sqrt(double(up)) * 0x1p-100 : sqrt(double(plain));
+        const double to = double(x_scale) / (norm + eps);
+        f[0] = large ? 0x1p-64f : 1.0f;
+        f[1] = float(to * (large ? 0x1p64 : 1.0));
+        if (to > 0x1p100) {
+            // (zeros over an eps of next to nothing are zeros, over none NaN)
+            f[0] = 0x1p100f;
+            f[1] = norm + eps > 0.0 ? float(fmin(to * 0x1p-100, 3.4e38)) : __uint_as_float(0x7f800000u);
+        }
+    }
+};
+
+// Moves the momentum and leaves sums of the update's squares, one set a CTA.
 __global__ void __launch_bounds__(256) orth_norm_kernel(PrepParams p) {
-    __shared__ float2 sums[8];
+    __shared__ float4 sums[8];
     const int mat = blockIdx.y;
     if (mat == 0)
         for (int i = int(blockIdx.x) * 256 + int(threadIdx.x); i < p.nzero; i += p.parts * 256) p.zero[i] = 0;
     const uint8_t* u = p.u + int64_t(mat) * p.u_batch;
     uint8_t* m = p.m ? p.m + int64_t(mat) * p.m_batch : nullptr;
     const int64_t width = (p.cols + 7) / 8, all = p.rows * width, step = int64_t(p.parts) * 256;
-    float s1 = 0.0f, s2 = 0.0f;
+    Squares s;
     // two eights at a time, all of them asked for before the first is worked on
     for (int64_t at = int64_t(blockIdx.x) * 256 + threadIdx.x; at < all; at += 2 * step) {
         float f[2][8], v[2][8];
@@ -896,58 +946,31 @@ __global__ void __launch_bounds__(256) orth_norm_kernel(PrepParams p) {
                         if (c[h] + k < p.cols) row[k] = v[h][k];
                 }
             }
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                s1 = fmaf(f[h][k], f[h][k], s1);
-                const float small = f[h][k] * 0x1p-80f;
-                s2 = fmaf(small, small, s2);
-            }
+            s.count(f[h]);
         }
     }
-#pragma unroll
-    for (int o = 16; o; o >>= 1) {
-        s1 += __shfl_xor_sync(0xffffffffu, s1, o);
-        s2 += __shfl_xor_sync(0xffffffffu, s2, o);
-    }
-    if (threadIdx.x % 32 == 0) sums[threadIdx.x / 32] = make_float2(s1, s2);
+    s.join();
+    if (threadIdx.x % 32 == 0) sums[threadIdx.x / 32] = s.all();
     __syncthreads();
     if (threadIdx.x) return;
-    for (int w = 1; w < 8; ++w) {
-        s1 += sums[w].x;
-        s2 += sums[w].y;
-    }
-    p.part[int64_t(mat) * p.parts + blockIdx.x] = make_float2(s1, s2);
+    for (int w = 1; w < 8; ++w) s.add(sums[w]);
+    p.part[int64_t(mat) * p.parts + blockIdx.x] = s.all();
 }
 
 // The update over its norm as X: operand and fp32, box by box.
 __global__ void __launch_bounds__(256) orth_split_kernel(PrepParams p) {
-    __shared__ float2 sums[8];
+    __shared__ float4 sums[8];
     __shared__ float factor[2];
     __shared__ float tile[kBox][kBox + 1];
     const int mat = blockIdx.y, t = threadIdx.x;
-    float s1 = 0.0f, s2 = 0.0f;
-    for (int i = t; i < p.parts; i += 256) {
-        const float2 v = p.part[int64_t(mat) * p.parts + i];
-        s1 += v.x;
-        s2 += v.y;
-    }
-#pragma unroll
-    for (int o = 16; o; o >>= 1) {
-        s1 += __shfl_xor_sync(0xffffffffu, s1, o);
-        s2 += __shfl_xor_sync(0xffffffffu, s2, o);
-    }
-    if (t % 32 == 0) sums[t / 32] = make_float2(s1, s2);
+    Squares s;
+    for (int i = t; i < p.parts; i += 256) s.add(p.part[int64_t(mat) * p.parts + i]);
+    s.join();
+    if (t % 32 == 0) sums[t / 32] = s.all();
     __syncthreads();
     if (t == 0) {
-        for (int w = 1; w < 8; ++w) {
-            s1 += sums[w].x;
-            s2 += sums[w].y;
-        }
-        // squares beyond the range: values and norm times 2^-64
-        const bool large = s1 > 3.402823466e38f;
-        const double norm = large ? sqrt(double(s2)) * 0x1p80 : sqrt(double(s1));
-        factor[0] = large ? 0x1p-64f : 1.0f;
-        factor[1] = float(double(p.x_scale) / (norm + p.eps) * (large ? 0x1p64 : 1.0));
+        for (int w = 1; w < 8; ++w) s.add(sums[w]);
+        s.factors(p.x_scale, p.eps, factor);
     }
     __syncthreads();
     const float f0 = factor[0], f1 = factor[1];
@@ -1040,9 +1063,6 @@ __device__ __forceinline__ float4 lds_quad(uint32_t addr) {
 __device__ __forceinline__ void st_cluster(uint32_t addr, const float4& v) {
     asm volatile("st.shared::cluster.v4.f32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
 }
-__device__ __forceinline__ void st_cluster(uint32_t addr, const float2& v) {
-    asm volatile("st.shared::cluster.v2.f32 [%0], {%1,%2};" ::"r"(addr), "f"(v.x), "f"(v.y) : "memory");
-}
 __device__ __forceinline__ void st_cluster(uint32_t addr, const uint4& v) {
     asm volatile("st.shared::cluster.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
@@ -1104,7 +1124,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) orth_small_kernel(const __gr
     __shared__ __align__(8) uint64_t done_bar;
     __shared__ uint32_t tmem_base;
     __shared__ __align__(16) float d[kSmallRows], e[kSmallRows];
-    __shared__ float2 sums[kSmallThreads / 32], all[kSmallCtas];
+    __shared__ __align__(16) float4 sums[kSmallThreads / 32], all[kSmallCtas];
     __shared__ float factor[2];
     const int t = threadIdx.x, warp = t >> 5, lane = t & 31, quad = warp & 3, group = warp >> 2, row = quad * 32 + lane;
     const int C = p.ctas, rank = int(blockIdx.x) % C, mat = int(blockIdx.x) / C;
@@ -1127,13 +1147,10 @@ __global__ void __launch_bounds__(kSmallThreads, 1) orth_small_kernel(const __gr
     const int64_t first = int64_t(rank) * kN;    // X's first column here
     const int64_t n = p.turned ? p.rows : p.cols;
     const int rows = int(p.turned ? p.cols : p.rows);
-    float s1 = 0.0f, s2 = 0.0f;
-    auto count = [&](const float4& f) {
-        for (float v : {f.x, f.y, f.z, f.w}) {
-            s1 = fmaf(v, v, s1);
-            v *= 0x1p-80f;
-            s2 = fmaf(v, v, s2);
-        }
+    Squares s;
+    auto count = [&](const float4& v) {
+        const float f[4] = {v.x, v.y, v.z, v.w};
+        s.count(f);
     };
     // values c .. c + 3 of a row of `cols` move its momentum and become what comes of it
     auto move = [&](float* at, int64_t c, int64_t cols, float4& v) {
@@ -1193,12 +1210,8 @@ __global__ void __launch_bounds__(kSmallThreads, 1) orth_small_kernel(const __gr
             sts_quad(xs + q * kQuadPitch + r * 16, v);
         }
     }
-#pragma unroll
-    for (int o = 16; o; o >>= 1) {
-        s1 += __shfl_xor_sync(0xffffffffu, s1, o);
-        s2 += __shfl_xor_sync(0xffffffffu, s2, o);
-    }
-    if (lane == 0) sums[warp] = make_float2(s1, s2);
+    s.join();
+    if (lane == 0) sums[warp] = s.all();
     __syncthreads();
     float x[kMine];
 #pragma unroll
@@ -1212,24 +1225,15 @@ __global__ void __launch_bounds__(kSmallThreads, 1) orth_small_kernel(const __gr
     __syncwarp();
     asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
     if (t < C) {
-        s1 = s2 = 0.0f;
-        for (int w = 0; w < kSmallThreads / 32; ++w) {
-            s1 += sums[w].x;
-            s2 += sums[w].y;
-        }
-        st_cluster(cluster_addr(smem_addr(&all[rank]), t), make_float2(s1, s2));
+        s = Squares();
+        for (int w = 0; w < kSmallThreads / 32; ++w) s.add(sums[w]);
+        st_cluster(cluster_addr(smem_addr(&all[rank]), t), s.all());
     }
     cluster_meet();
     if (t == 0) {
-        s1 = s2 = 0.0f;
-        for (int k = 0; k < C; ++k) {
-            s1 += all[k].x;
-            s2 += all[k].y;
-        }
-        const bool large = s1 > 3.402823466e38f;
-        const double norm = large ? sqrt(double(s2)) * 0x1p80 : sqrt(double(s1));
-        factor[0] = large ? 0x1p-64f : 1.0f;
-        factor[1] = float(double(p.x_scale) / (norm + p.eps) * (large ? 0x1p64 : 1.0));
+        s = Squares();
+        for (int k = 0; k < C; ++k) s.add(all[k]);
+        s.factors(p.x_scale, p.eps, factor);
     }
     __syncthreads();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -1545,7 +1549,7 @@ Plan plan_of(int64_t batch, int64_t rows, int64_t cols) {
     }
     q.half = q.tiles[0] > q.tiles[1] ? q.tiles[0] : q.tiles[1];
     q.counters = take((1 + 2 * q.half * q.ctas) * 4);
-    q.norm = take(batch * q.parts * 8);
+    q.norm = take(batch * q.parts * 16);
     q.d = take(diag);
     q.e = take(diag);
     q.x0 = take(x);
@@ -1832,7 +1836,7 @@ extern "C" lc_status lc_orthogonalize(int device, void* cuda_stream, const lc_ma
         a.m_batch = momentum->batch_stride * 4;
         a.wide = a.wide && rows_wide(a.m, rows > 1 ? a.m_pitch : 0, batch > 1 ? a.m_batch : 0);
     }
-    a.part = reinterpret_cast<float2*>(w + q.norm);
+    a.part = reinterpret_cast<float4*>(w + q.norm);
     a.zero = reinterpret_cast<uint32_t*>(w + q.counters);
     a.nzero = int32_t((q.norm - q.counters) / 4);
     a.parts = int32_t(q.parts);
