@@ -1525,6 +1525,7 @@ double cut(Plan& q, bool pair) {
     return all;
 }
 
+// (of one matrix at least)
 Plan plan_of(int64_t batch, int64_t rows, int64_t cols) {
     Plan q{}, single{};
     q.batch = batch;
@@ -1789,7 +1790,7 @@ extern "C" lc_status lc_orthogonalize(int device, void* cuda_stream, const lc_ma
     if (st != LC_OK) return st;
     if (momentum && momentum->dtype != LC_F32) return fail_status(LC_ERR_INVALID_ARG, "%s: the momentum is kept in fp32", call);
     if (out->dtype != LC_BF16) return fail_status(LC_ERR_INVALID_ARG, "%s: out is bf16", call);
-    const Plan q = plan_of(batch, rows, cols);
+    const int64_t m = rows < cols ? rows : cols, long_side = rows < cols ? cols : rows;
     // what no singular value exceeds at any step, from which the operands' scales follow
     OrthParams p{};
     double r = 1.0, most = 1.0;
@@ -1807,9 +1808,8 @@ extern "C" lc_status lc_orthogonalize(int device, void* cuda_stream, const lc_ma
     p.a_scale = room_for(most * most);
     p.x_scale = room_for(most);
     // elements of about 1 where the matrix has no structure: sqrt(m n) times those of X
-    const float middle = float(std::ldexp(1.0, std::ilogb(std::sqrt(double(q.m) * double(q.n)))));
+    const float middle = float(std::ldexp(1.0, std::ilogb(std::sqrt(double(m) * double(long_side)))));
     if (middle < p.x_scale) p.x_scale = middle;
-    const Small small = small_of(batch, q.m, q.n);
     const uint64_t need = lc_orthogonalize_workspace(batch, rows, cols);
     if (workspace_bytes < need)
         return fail_status(LC_ERR_CAPACITY, "%s: %llu bytes of workspace, %llu needed", call, (unsigned long long)workspace_bytes,
@@ -1822,6 +1822,8 @@ extern "C" lc_status lc_orthogonalize(int device, void* cuda_stream, const lc_ma
     if (st != LC_OK) return st;
     if (!cur.ok) return fail_status(LC_ERR_CUDA, "%s: cannot make device %d current", call, device);
     if (!batch) return LC_OK;
+    const Plan q = plan_of(batch, rows, cols);
+    const Small small = small_of(batch, m, long_side);
     uint8_t* const w = static_cast<uint8_t*>(workspace);
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
     PrepParams a{};
