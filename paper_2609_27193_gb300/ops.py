@@ -107,6 +107,15 @@ def _for(act, x):
     return act
 
 
+def _given(name, act, x):
+    """The checkpoint that was given to be written; None for a new one (True) and for none."""
+    if isinstance(act, Act):
+        return _for(act, x)
+    if act is not True and (isinstance(act, torch.Tensor) or act):
+        raise TypeError("%s must be True or an Act, not %s" % (name, type(act).__name__))
+    return None
+
+
 def embed(table, ids, scale=1.0, out=None):
     """scale * table[ids]: [tokens, dim] in the table's type.  A negative id
     gives a zero row, an id beyond the table a row of NaN."""
@@ -162,10 +171,10 @@ def add_norm(x, residual, weight, eps=1e-5, out=None, sum=None, keep=None, out8=
     is written.  sum: where the sum goes, the residual itself if wanted.  out=False: y is wanted in 8 bits only (and
     returned as None).  The sum has the residual's type and y has x's: both the same, or a float32 residual around
     bfloat16 branches."""
-    if not keep and not out8:
+    if (keep is None or keep is False) and (out8 is None or out8 is False):
         return _ops.add_norm(x, residual, weight, eps, None if out is False else out, out is not False, sum,
                              None, None, None, None, False, False)
-    kept, y8 = (_for(a, x) if isinstance(a, Act) else None for a in (keep, out8))
+    kept, y8 = _given("keep", keep, x), _given("out8", out8, x)
     result = _ops.add_norm(x, residual, weight, eps, None if out is False else out, out is not False, sum,
                            *((None, None) if kept is None else (kept.q, kept.e)),
                            *((None, None) if y8 is None else (y8.q, y8.e)), keep is True, out8 is True)
