@@ -662,8 +662,9 @@ lc_status lc_measure_noalloc_debug(int device, void* cuda_stream, const lc_segme
  * from here on: 0, or LC_DEBUG_OPS_STALL, with which the first copy into
  * every ring of the norms' rows (forward and backward), and into the ring of
  * the last CTA of every tile of the weight gradient's and of
- * lc_orthogonalize's products (of more than 128 rows and columns), announces
- * 16 bytes that never come.
+ * lc_orthogonalize's products, announces 16 bytes that never come; where
+ * lc_orthogonalize keeps a matrix in one cluster (up to 128 rows or columns),
+ * nobody hears of the first product.
  * Errors: INVALID_ARG (other flags). */
 #define LC_DEBUG_OPS_STALL 4
 lc_status lc_ops_debug(int32_t debug_flags);

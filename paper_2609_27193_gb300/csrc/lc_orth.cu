@@ -1043,6 +1043,7 @@ struct SmallParams {
     double eps;
     float beta, x_scale, a_scale;
     int32_t ctas, u_bf16, nesterov, turned, steps;
+    int32_t stall;           // test switch: nobody hears of the first product
     int32_t wide, out_wide;  // rows on 16-byte boundaries
     OrthStep step[kMaxSteps];
 };
@@ -1259,21 +1260,22 @@ __global__ void __launch_bounds__(kSmallThreads, 1) orth_small_kernel(const __gr
     const float x_back = 1.0f / p.x_scale;
     uint32_t round = 0;
     bool ok = true;
-    // everybody's writes are in place, one thread issues the products, and everybody waits for them
+    // everybody's writes are in place, one thread issues the products, and everybody waits for them.  After a wait of its own
+    // that ran out it issues no more (the others' next wait runs out too), so that one product at most is unaccounted for.
     auto products = [&](auto issue) {
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
         __syncthreads();
         if (warp == 0) {
-            if (lane == 0) {
+            if (lane == 0 && ok) {
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 issue();
-                commit<false>(done);
+                if (!p.stall) commit<false>(done);
             }
             __syncwarp();
         }
         ok = ok && mbar_wait_bounded(done, round, kWaitNs);
-        round ^= 1;
+        if (ok) round ^= 1;
         __syncwarp();
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     };
@@ -1466,6 +1468,8 @@ __global__ void __launch_bounds__(kSmallThreads, 1) orth_small_kernel(const __gr
             if (r < rows) store_quad(out + r * p.out_pitch, p.out_wide, first + q * 4, n, lds_quad(xs + q * kQuadPitch + r * 16));
         }
     }
+    // (the product that was given up on uses the CTA's memory until it is done)
+    if (!ok && t == 0) mbar_wait_bounded(done, round, kDrainNs);
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
     if (warp == 0) {
@@ -1876,6 +1880,7 @@ extern "C" lc_status lc_orthogonalize(int device, void* cuda_stream, const lc_ma
         o.nesterov = a.nesterov;
         o.turned = a.turned;
         o.steps = steps;
+        o.stall = ops_stall();
         o.wide = a.wide;
         o.out_wide = rows_wide(o.out, rows > 1 ? o.out_pitch : 0, batch > 1 ? o.out_batch : 0);
         for (int k = 0; k < steps; ++k) o.step[k] = p.step[k];
