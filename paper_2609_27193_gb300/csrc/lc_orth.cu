@@ -34,8 +34,8 @@
 // limit (4096 x 14336: 0.30 to 0.36 us for 256 x 256 x 64 on a pair, where a cuBLAS product of 8192 takes 0.32 to
 // 0.36); small ones are 15 times the latency of copies (0.8 us), accumulator (1) and barrier (1.5).
 //
-// Waits are bounded: where one runs out the CTA's outputs are NaN, and with the next
-// barrier everybody's.
+// Waits are bounded.  A copying or issuing warp whose wait ran out stops, so the accumulator that the summing warps wait
+// for does not come: their own wait runs out, the CTA's outputs are NaN, and with the next barrier everybody's.
 #include <cuda.h>
 #include <cuda_fp16.h>
 
@@ -506,7 +506,6 @@ __global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_
     // product.
     __shared__ __align__(8) uint64_t bars[2 * kStages + 5];
     __shared__ uint32_t tmem_base;
-    __shared__ volatile uint32_t failed;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = PAIR ? int(blockIdx.x & 1) : 0, unit = int(blockIdx.x) / kCtas, units = int(gridDim.x) / kCtas;
     const uint32_t ring = (smem_addr(raw) + 1023) & ~1023u;
@@ -522,7 +521,6 @@ __global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_
             mbar_init(taken + 8 * i, kCtas * kSumWarps);
         }
         mbar_init(go, 1);
-        failed = 0;
         mbar_init_fence();
     }
     if (warp == 1) {
@@ -592,13 +590,13 @@ __global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_
             }
         }
         // every copy lands, and every arrival that ends a stage's products, before the CTA's memory is given back
-        // (word of the second CTA's goes to the first; they have landed when their products are done, or long after)
+        // (word of the second CTA's goes to the first; they have landed when their products are done, or long after).  Limited
+        // waits, for that alone.
         for (int i = it > kStages ? it - kStages : 0; i < it && rank == 0; ++i)
-            if (!mbar_wait_warp(full + 8 * (i % kStages), (i / kStages) & 1)) ok = false;
+            mbar_wait_warp(full + 8 * (i % kStages), (i / kStages) & 1);
         bool ended = true;
         for (int i = it > kStages ? it - kStages : 0; i < it && ended; ++i)
             ended = mbar_wait_warp(empty + 8 * (i % kStages), (i / kStages) & 1);
-        if (!ok || !ended) failed = 1;
     } else if (warp == 1 && rank == 0) {
         // --- the products ---
         Ring<kStages> st;
@@ -647,7 +645,6 @@ __global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_
                 ++chunk;
             }
         }
-        if (!ok) failed = 1;
     } else if (warp >= kSumWarp) {
         // --- what comes of an accumulator ---
         const int quad = warp & 3, group = (warp - kSumWarp) >> 2, t = threadIdx.x - kSumWarp * 32;
@@ -789,7 +786,6 @@ __global__ void __launch_bounds__(kThreads, 1) orth_product_kernel(const __grid_
             }
         }
         if (!ok) {
-            failed = 1;
             // what is on its way out of shared memory ends first
             if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
             // NaN where this CTA's outputs would be
