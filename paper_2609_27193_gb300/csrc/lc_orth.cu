@@ -954,7 +954,7 @@ __global__ void __launch_bounds__(256) orth_norm_kernel(PrepParams p) {
 }
 
 // The update over its norm as X: operand and fp32, box by box.
-__global__ void __launch_bounds__(256) orth_split_kernel(PrepParams p) {
+__global__ void __launch_bounds__(256, 6) orth_split_kernel(PrepParams p) {
     __shared__ float4 sums[8];
     __shared__ float factor[2];
     __shared__ float tile[kBox][kBox + 1];
