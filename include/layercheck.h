@@ -820,9 +820,11 @@ typedef struct {
  *   out = X rounded to bf16,
  * over the shorter side (X^T X where rows > cols).  coefficients: host array of
  * steps times a, b, c; what they let singular values in [0, 1] grow to is
- * bounded (16), and refused above.  update: bf16 or fp32.  out: bf16; it is off
- * by about 1e-3 of its size before that rounding (operands are fp16; X itself,
- * sums, diagonals and the norm are held in 32 bits).
+ * bounded (16), and refused above.  update: bf16 or fp32.  out: bf16; before that
+ * rounding it is off by 2e-4 to 1e-3 of its norm, 2.4e-3 for a matrix of rank one
+ * (operands are fp16; X itself, sums, diagonals and the norm are held in 32 bits).
+ * The arrays' extents, each from its first to its last element, must not meet:
+ * an output between the update's rows is refused.
  * momentum (fp32; NULL: U = update): with g the update given it moves first,
  *   momentum += (1 - beta) (g - momentum),
  * and U = g + beta (momentum - g) with nesterov != 0, else U = momentum.

@@ -696,7 +696,8 @@ cudaError_t grad_ring(const AddNormGradParams& p, int sms, cudaStream_t s, int* 
 // Whether the rings pay (microseconds through them and directly):
 //   forward    bf16: 64 rows of 768 2.4, 2.6; 2432 of 4096 10.1, 21.5; 4096 of 256 3.1, 3.2.  With a 32-bit stream only
 //              where the arrays no longer stay in L2: 1024 of 4096 columns 9.8, 8.5; 608 of 8192 11.3, 13.2; 4096 of 2048
-//              16.5, 22.4; fp32 2432 of 1024 6.5, 5.8; 4096 of 2048 16.0, 22.7
+//              16.5, 22.4; fp32 2432 of 1024 6.5, 5.8; 4096 of 2048 16.0, 22.7 (the border is a round one: just above it, at
+//              2432 of 2048 around bf16, the rings take 10.8 and the direct form would 9.9)
 //   backward   bf16 152 of 2048 5.4, 5.0; 304 of 2048 5.6, 6.0; 16 of 4096 4.9, 6.1; with a 32-bit stream 608 of 1024 5.9,
 //              6.5; 304 of 2048 6.1, 5.7; fp32 304 of 768 5.1, 4.9; 608 of 768 5.5, 6.3; 152 of 4096 5.8, 6.6
 bool forward_ring(int64_t ntok, int64_t dim, bool stream32) { return !stream32 || ntok * dim >= 4900000; }

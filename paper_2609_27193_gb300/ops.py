@@ -15,7 +15,8 @@ calls and one another.  There is no CPU fallback.
 Autograd records none of this: the gradients are calls too, for training loops
 that write their backward pass themselves and for torch.autograd.Function.
 embed, norm, add_norm and orthogonalize refuse inputs that require a gradient while
-grad mode is on.
+grad mode is on.  A tensor whose storage was released, or holds less than the tensor
+reaches, is refused by every call, and so is memory that is not device memory.
 
 Tensors are rows of their last dimension: [tokens, dim] with any row stride
 (an expanded row, stride 0, may be an input) and bfloat16 or float32 elements;
@@ -214,10 +215,13 @@ def _packed(steps, coefficients):
 def orthogonalize(update, momentum=None, beta=0.95, nesterov=True, steps=5, coefficients=(3.4445, -4.7750, 2.0315),
                   eps=1e-7, out=None):
     """The update of a weight matrix, [rows, cols], or of a batch of them, [batch, rows, cols], made nearly orthogonal:
-    X = U / (|U| + eps), then `steps` times A = X X^T, X = a X + (b A + c A^2) X, in bfloat16.  coefficients: (a, b, c),
-    or a sequence of one triple a step.  U is the update, or with `momentum` (float32, written) what comes of it:
+    X = U / (|U| + eps), then `steps` times A = X X^T, X = a X + (b A + c A^2) X, returned as bfloat16.  The products take
+    fp16 operands; X itself, sums, the diagonals of A and of b A + c A^2 and the norm are held in 32 bits, which leaves the result
+    off by some 1e-3 of its norm before its rounding (2.4e-3 for a matrix of rank one).  coefficients: (a, b, c), or a
+    sequence of one triple a step.  U is the update, or with `momentum` (float32, written) what comes of it:
     momentum += (1 - beta) (update - momentum), and U = update + beta (momentum - update), without nesterov the
-    momentum itself."""
+    momentum itself.  update, momentum and out may have any row and batch strides, but none may lie between another's
+    first and last element."""
     if not isinstance(coefficients, tuple) or not all(isinstance(c, (int, float, tuple)) for c in coefficients):
         coefficients = tuple(tuple(c) if hasattr(c, "__len__") else c for c in coefficients)
     return _ops.orthogonalize(update, momentum, beta, nesterov, _packed(steps, coefficients), eps, out)
